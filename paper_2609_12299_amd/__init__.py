@@ -5,7 +5,9 @@ Cross-Layer GPU Performance Measurements around Semantic Regions"
 (arxiv 2609.12299): marker records become region instances with nesting,
 per-region duration statistics, class overlap and ambiguity counts, and PC
 samples are attributed to those instances, computed by hand-written HIP
-kernels for gfx950 behind a C ABI (include/argus_attr.h).
+kernels for gfx950 behind a C ABI (include/argus_attr.h).  The operators of a
+decode step, whose kernels write marker records of their own regions, stand
+beside it (include/argus_decode.h).
 """
 from .attr import (ABI_VERSION, COUNTER_NAMES, FORCE_EVENT_SORT, FORCE_FULL_SORT,
                    FORCE_RECORD_RADIX, INSTANCE_DTYPE, NOALLOC_SCRATCH_BYTES, NUM_COUNTERS,
@@ -22,6 +24,13 @@ from .attr import (ABI_VERSION, COUNTER_NAMES, FORCE_EVENT_SORT, FORCE_FULL_SORT
                    join_probes, argus_attr_handoffs, argus_attr_handoffs_workspace_bytes,
                    argus_handoffs_config, argus_handoffs_io, phase_handoffs,
                    argus_attr_chrome_trace, argus_trace_options)
+from .decode import (COMPACT_COUNTER_NAMES, NUM_REGIONS, REGION_NAMES, STEP_COUNTER_NAMES,
+                     MarkerBuffer, append_tokens, argus_decode_append, argus_decode_attend,
+                     argus_decode_attend_workspace_bytes, argus_decode_compact,
+                     argus_decode_compact_workspace_bytes, argus_decode_last_error,
+                     argus_decode_select, argus_decode_select_workspace_bytes, argus_decode_step,
+                     argus_decode_step_workspace_bytes, attend_pages, compact_pages, select_beams,
+                     step_pages)
 
 __all__ = [
     "ABI_VERSION", "COUNTER_NAMES", "FORCE_EVENT_SORT", "FORCE_FULL_SORT", "FORCE_RECORD_RADIX",
@@ -37,4 +46,10 @@ __all__ = [
     "argus_probes_config", "argus_probes_io", "join_probes", "argus_attr_handoffs",
     "argus_attr_handoffs_workspace_bytes", "argus_handoffs_config", "argus_handoffs_io",
     "phase_handoffs", "argus_attr_chrome_trace", "argus_trace_options",
+    "COMPACT_COUNTER_NAMES", "NUM_REGIONS", "REGION_NAMES", "STEP_COUNTER_NAMES", "MarkerBuffer",
+    "append_tokens", "argus_decode_append", "argus_decode_attend",
+    "argus_decode_attend_workspace_bytes", "argus_decode_compact",
+    "argus_decode_compact_workspace_bytes", "argus_decode_last_error", "argus_decode_select",
+    "argus_decode_select_workspace_bytes", "argus_decode_step", "argus_decode_step_workspace_bytes",
+    "attend_pages", "compact_pages", "select_beams", "step_pages",
 ]

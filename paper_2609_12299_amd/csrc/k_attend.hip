@@ -1,0 +1,157 @@
+// k_attend.hip -- host side of the attention of one new token over a paged
+// cache (k_attend.h), and the error text and device check of all operators.
+#include <atomic>
+
+#include "k_attend.h"
+
+namespace argus {
+namespace decode {
+
+namespace {
+thread_local char g_why[256];
+std::atomic<unsigned char> g_dev_ok[64];
+}  // namespace
+
+int refuse(int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_why, sizeof(g_why), fmt, ap);
+  va_end(ap);
+  return code;
+}
+void accepted() { g_why[0] = 0; }
+
+int device_ok() {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return refuse(ARGUS_E_HIP, "no device");
+  if (dev < 0 || dev >= 64) return refuse(ARGUS_E_DEVICE, "device %d", dev);
+  if (!g_dev_ok[dev].load(std::memory_order_relaxed)) {
+    hipDeviceProp_t prop;
+    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return refuse(ARGUS_E_HIP, "no device properties");
+    if (strncmp(prop.gcnArchName, "gfx950", 6) != 0) return refuse(ARGUS_E_DEVICE, "the device is no gfx950");
+    g_dev_ok[dev].store(1, std::memory_order_relaxed);
+  }
+  return ARGUS_OK;
+}
+
+namespace {
+
+// Blocks that share a batch: two per compute unit, all resident at once.
+constexpr uint32_t kShareBlocks = 512;
+// Segments of at most this many tiles are not shared: a block each.
+constexpr uint32_t kWholeTiles = 16;
+
+struct Plan {
+  uint32_t dp, nq, row_tiles, hs, blocks, grid;
+  size_t o_at, desc_at, bytes;
+};
+
+int make_plan(const argus_attend_config* c, Plan* p) {
+  if (!c) return refuse(ARGUS_E_INVAL, "no configuration");
+  if (c->abi_version != ARGUS_ATTR_ABI_VERSION) return refuse(ARGUS_E_ABI, "abi_version %u", c->abi_version);
+  if (c->q_type > ARGUS_FP16) return refuse(ARGUS_E_INVAL, "q is bf16 or fp16");
+  if (c->cache_type != c->q_type && c->cache_type != ARGUS_FP8)
+    return refuse(ARGUS_E_INVAL, "the cache is of q's type or fp8 (e4m3)");
+  if (c->seqs > (1u << 20)) return refuse(ARGUS_E_CAPACITY, "seqs %u", c->seqs);
+  if (c->kv_heads < 1 || c->kv_heads > 1024 || c->group < 1 || c->group > 256)
+    return refuse(ARGUS_E_INVAL, "kv_heads %u (1..1024), group %u (1..256)", c->kv_heads, c->group);
+  const uint32_t unit = c->head_dim > 128 || c->cache_type == ARGUS_FP8 ? 16u : 8u;
+  if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % unit)
+    return refuse(ARGUS_E_INVAL, "head_dim %u: a multiple of %u up to 256", c->head_dim, unit);
+  if (!power_of_two(c->page_size) || c->page_size < 8 || c->page_size > 65536)
+    return refuse(ARGUS_E_INVAL, "page_size %u: a power of two, 8..65536", c->page_size);
+  if (c->num_pages < 1 || c->num_pages > 0x7FFFFFFFu || c->columns < 1 ||
+      (uint64_t)c->columns * c->page_size > 0x7FFFFFFFull || c->window > 0x7FFFFFFFu || c->sinks > 0x7FFFFFFFu)
+    return refuse(ARGUS_E_CAPACITY, "pages, columns, window or sinks out of range");
+  p->dp = c->head_dim <= 64 ? 64u : c->head_dim <= 128 ? 128u : 256u;
+  p->nq = p->dp < 256 && c->group > 16 ? 2u : 1u;
+  p->row_tiles = (c->group + 16 * p->nq - 1) / (16 * p->nq);
+  p->hs = c->kv_heads * p->row_tiles;
+  const uint64_t segs = (uint64_t)c->seqs * p->hs;
+  if (segs > (1u << 30)) return refuse(ARGUS_E_CAPACITY, "seqs x heads");
+  // tiles of the longest sequence that the table (or the window) allows
+  uint64_t tiles = ((uint64_t)c->columns * c->page_size + kTile - 1) / kTile;
+  if (c->window) {
+    const uint64_t w = (c->window + kTile - 1) / kTile + 1 + (uint64_t)(c->sinks + kTile - 1) / kTile;
+    tiles = w < tiles ? w : tiles;
+  }
+  p->blocks = tiles <= kWholeTiles ? 0 : kShareBlocks;
+  p->grid = p->blocks ? p->blocks : (uint32_t)segs;
+  const size_t rows = (size_t)p->blocks * 2 * 16 * p->nq;
+  p->o_at = up256(rows * 2 * sizeof(float));
+  p->desc_at = p->o_at + up256(rows * p->dp * sizeof(float));
+  p->bytes = p->blocks ? p->desc_at + up256((size_t)p->blocks * 16) : 0;
+  return ARGUS_OK;
+}
+
+}  // namespace
+}  // namespace decode
+}  // namespace argus
+
+using namespace argus;
+using namespace argus::decode;
+
+extern "C" const char* argus_decode_last_error(void) { return g_why; }
+
+extern "C" size_t argus_decode_attend_workspace_bytes(const argus_attend_config* cfg) {
+  accepted();
+  Plan p;
+  return make_plan(cfg, &p) == ARGUS_OK ? p.bytes : (size_t)-1;
+}
+
+extern "C" int argus_decode_attend(const argus_attend_config* cfg, const argus_attend_io* io, void* d_workspace,
+                                   size_t workspace_bytes, argus_markers* markers, void* stream_v) {
+  accepted();
+  Plan p;
+  int rc = make_plan(cfg, &p);
+  if (rc != ARGUS_OK) return rc;
+  if (!io || (cfg->seqs && (!io->d_table || !io->d_q || !io->d_lens || !io->d_out)))
+    return refuse(ARGUS_E_INVAL, "a required pointer is NULL");
+  if ((rc = check_view(io->k, cfg->cache_type, "k")) != ARGUS_OK || (rc = check_view(io->v, cfg->cache_type, "v")) != ARGUS_OK)
+    return rc;
+  if (!aligned_to(io->d_q, 16) || io->q_seq_stride % 8 || io->q_head_stride % 8 || !aligned_to(io->d_out, 16) ||
+      !aligned_to(io->d_table, 4) || !aligned_to(io->d_lens, 4) || !aligned_to(io->d_k_scale, 4) ||
+      !aligned_to(io->d_v_scale, 4) || !aligned_to(io->d_lse, 4))
+    return refuse(ARGUS_E_ALIGN, "rows of q and out lie on 16 bytes");
+  if (io->table_stride < (int64_t)cfg->columns && cfg->seqs > 1)
+    return refuse(ARGUS_E_INVAL, "table_stride %lld below columns", (long long)io->table_stride);
+  if (marks_bad(markers)) return refuse(ARGUS_E_INVAL, "markers: alignment or region_base");
+  if (p.bytes && !d_workspace) return refuse(ARGUS_E_INVAL, "no workspace");
+  if (p.bytes && !aligned_to(d_workspace, 256)) return refuse(ARGUS_E_ALIGN, "the workspace lies on 256 bytes");
+  if (workspace_bytes < p.bytes)
+    return refuse(ARGUS_E_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
+  const uint32_t join_rows = cfg->group < 16 * p.nq ? cfg->group : 16 * p.nq;
+  const uint32_t per_wave = 6;  // its own region, and in it the place and the tokens
+  const uint64_t records = ((uint64_t)p.grid * per_wave + (p.blocks ? (uint64_t)p.blocks * join_rows * 2 : 0)) * kWaves;
+  if (!marks_fit(markers, records)) return refuse(ARGUS_E_CAPACITY, "%llu marker records do not fit", (unsigned long long)records);
+  if (cfg->seqs == 0) return ARGUS_OK;
+  if ((rc = device_ok()) != ARGUS_OK) return rc;
+
+  AttendArgs a{};
+  const int64_t e = type_bytes(cfg->cache_type);
+  a.q = (const uint16_t*)io->d_q;
+  a.q_seq = io->q_seq_stride, a.q_head = io->q_head_stride;
+  a.k = (const uint8_t*)io->k.base, a.v = (const uint8_t*)io->v.base;
+  a.k_page = io->k.page_stride * e, a.k_head = io->k.head_stride * e, a.k_tok = io->k.token_stride * e;
+  a.v_page = io->v.page_stride * e, a.v_head = io->v.head_stride * e, a.v_tok = io->v.token_stride * e;
+  a.table = io->d_table, a.table_stride = io->table_stride, a.lens = io->d_lens;
+  a.k_scale = io->d_k_scale, a.v_scale = io->d_v_scale;
+  a.out = (uint16_t*)io->d_out, a.lse = io->d_lse;
+  a.part_ml = (float*)d_workspace;
+  a.part_o = (float*)((char*)d_workspace + p.o_at);
+  a.desc = (uint32_t*)((char*)d_workspace + p.desc_at);
+  a.S = cfg->seqs, a.H = cfg->kv_heads, a.G = cfg->group, a.D = cfg->head_dim;
+  a.HS = p.hs, a.row_tiles = p.row_tiles;
+  a.shift = log2_of(cfg->page_size), a.num_pages = cfg->num_pages, a.columns = cfg->columns;
+  a.window = cfg->window, a.sinks = cfg->sinks;
+  a.blocks = p.blocks, a.scale = cfg->scale;
+  a.marks = take_marks(markers, p.grid, per_wave);
+  hipStream_t st = (hipStream_t)stream_v;
+  const bool f8 = cfg->cache_type == ARGUS_FP8, bf = cfg->q_type == ARGUS_BF16;
+  (f8 ? (bf ? launch_attend_bf16_f8 : launch_attend_fp16_f8) : (bf ? launch_attend_bf16 : launch_attend_fp16))(a, p.grid, st);
+  if (p.blocks) {
+    a.marks = take_marks(markers, (uint64_t)p.blocks * join_rows, 2);
+    (bf ? launch_join_type<0> : launch_join_type<1>)(a, dim3(p.blocks, join_rows), st);
+  }
+  return hipGetLastError() == hipSuccess ? ARGUS_OK : refuse(ARGUS_E_HIP, "launch failed");
+}

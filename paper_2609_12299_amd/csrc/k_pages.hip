@@ -1,0 +1,801 @@
+// k_pages.hip -- the paged cache of a decode step: new tokens written into their
+// pages, page tables moved from one step to the next, pools compacted.
+#include "decode.h"
+
+#include "chain.h"
+
+namespace argus {
+namespace decode {
+namespace {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------- append
+
+struct AppendArgs {
+  const uint8_t *new_k, *new_v;  // strides in bytes
+  int64_t k_row, k_hd, v_row, v_hd;
+  uint8_t *k, *v;
+  int64_t k_page, k_head, k_tok, v_page, v_head, v_tok;
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t *starts, *offsets;
+  const float *k_scale, *v_scale;
+  uint32_t S, rows, shift, num_pages, columns, tokens;  // tokens of a block
+  FastDiv per_token, per_side, per_head;                // chunks of a token, of its keys, of a head
+  Marks marks;
+};
+
+constexpr uint32_t kMaxTokens = 16;
+
+// x / s rounded to nearest, limited to the range of e4m3.  y = 1 / s correctly
+// rounded; then fma(x - q s, y, q) with q = x y is the correctly rounded
+// quotient (Markstein), save where q overflows, which the limit settles.
+ARGUS_DEV float quotient(float x, float s, float y) {
+  const float q = x * y;
+  float r = fmaf(fmaf(-q, s, x), y, q);
+  r = fabsf(q) > 1000.0f ? q : r;  // beyond the range; infinities have no remainder
+  r = r > 448.0f ? 448.0f : r;     // NaN stays
+  return r < -448.0f ? -448.0f : r;
+}
+
+template <int T>  // 0: bf16, 1: fp16
+ARGUS_DEV f32x2 pair(uint32_t w) {
+  if constexpr (T == 0) {
+    return (f32x2){__builtin_bit_cast(float, w << 16), __builtin_bit_cast(float, w & 0xFFFF0000u)};
+  } else {
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_convertvector(__builtin_bit_cast(f16x2, w), f32x2);
+  }
+}
+
+// A chunk is 16 bytes of the cache: 8 elements copied, or 16 in 8 bits.  A block
+// finds the places of its tokens once, then its threads go over their chunks,
+// which lie one after the other in the input.
+// MODE 0: copy; 1: bf16 to e4m3; 2: fp16 to e4m3.
+template <int MODE>
+__global__ __launch_bounds__(kThreads) void k_append(AppendArgs a) {
+  __shared__ int64_t s_page[kMaxTokens];   // -1: left out
+  __shared__ uint32_t s_place[kMaxTokens];
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_APPEND);
+  const uint32_t tid = threadIdx.x;
+  const uint32_t row0 = blockIdx.x * a.tokens;
+  const uint32_t tokens = a.rows - row0 < a.tokens ? a.rows - row0 : a.tokens;
+  if (tid < tokens) {
+    const int32_t row = (int32_t)(row0 + tid);
+    uint32_t s = row0 + tid;
+    int64_t pos;
+    bool in = true;
+    if (a.offsets) {
+      uint32_t lo = 0, hi = a.S;  // the first sequence that ends behind the row
+      while (lo < hi) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (a.offsets[mid + 1] > row) hi = mid; else lo = mid + 1;
+      }
+      in = lo < a.S && a.offsets[0] <= row;
+      s = in ? lo : 0;
+      pos = in ? (int64_t)a.starts[s] + row - a.offsets[s] : -1;
+    } else {
+      pos = a.starts[s];
+    }
+    in = pos >= 0 && (uint64_t)pos >> a.shift < a.columns;
+    const int32_t page = in ? a.table[(int64_t)s * a.table_stride + (pos >> a.shift)] : -1;
+    s_page[tid] = (uint32_t)page < a.num_pages ? page : -1;
+    s_place[tid] = (uint32_t)pos & ((1u << a.shift) - 1);
+  }
+  __syncthreads();
+  const uint32_t n = tokens * a.per_token.d;
+  for (uint32_t e = tid; e < n; e += kThreads) {
+    const uint32_t t = divide(e, a.per_token);
+    uint32_t x = e - t * a.per_token.d;
+    const bool values = x >= a.per_side.d;
+    if (values) x -= a.per_side.d;
+    const uint32_t h = divide(x, a.per_head), at = (x - h * a.per_head.d) * 16;
+    const int64_t page = s_page[t];
+    if (page < 0) continue;
+    const uint8_t* src = values ? a.new_v + (int64_t)(row0 + t) * a.v_row + (int64_t)h * a.v_hd
+                                : a.new_k + (int64_t)(row0 + t) * a.k_row + (int64_t)h * a.k_hd;
+    uint8_t* dst = values ? a.v + page * a.v_page + (int64_t)h * a.v_head + (int64_t)s_place[t] * a.v_tok
+                          : a.k + page * a.k_page + (int64_t)h * a.k_head + (int64_t)s_place[t] * a.k_tok;
+    u32x4 out;
+    if constexpr (MODE == 0) {
+      out = *reinterpret_cast<const u32x4*>(src + at);
+    } else {
+      const u32x4 lo = *reinterpret_cast<const u32x4*>(src + 2 * at);
+      const u32x4 hi = *reinterpret_cast<const u32x4*>(src + 2 * at + 16);
+      const float* scale = values ? a.v_scale : a.k_scale;
+      const float sc = scale ? scale[h] : 1.0f, inv = 1.0f / sc;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x2 p = pair<MODE - 1>(i < 2 ? lo[2 * i] : hi[2 * i - 4]);
+        const f32x2 q = pair<MODE - 1>(i < 2 ? lo[2 * i + 1] : hi[2 * i - 3]);
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(p.x, sc, inv), quotient(p.y, sc, inv), 0, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(q.x, sc, inv), quotient(q.y, sc, inv), w, true);
+        out[i] = (uint32_t)w;
+      }
+    }
+    *reinterpret_cast<u32x4*>(dst + at) = out;
+  }
+  mk.end(ARGUS_REGION_APPEND);
+}
+
+// ------------------------------------------------------------ page copies
+
+struct Planes {
+  uint8_t* base;
+  int64_t plane_stride, page_stride;
+  uint32_t planes, units;  // 16-byte units of a page
+};
+struct Caches {
+  Planes c[ARGUS_MAX_CACHES];
+  uint32_t n;
+};
+
+// Copies pages src(i) to dst(i), i < n, in every plane of every cache, by the
+// waves first, first + step, ...: 4 KiB at a time, four loads in flight per lane.
+template <class Pair>
+ARGUS_DEV void copy_pages(const Caches& all, uint32_t n, uint32_t first, uint32_t step, Pair pair_of) {
+  const uint32_t lane = lane_id();
+  for (uint32_t ci = 0; ci < all.n; ++ci) {
+    const Planes c = all.c[ci];
+    const uint32_t parts = (c.units + 255) / 256;
+    const uint64_t total = (uint64_t)n * c.planes * parts;
+    for (uint64_t w = first; w < total; w += step) {
+      const uint32_t part = (uint32_t)(w % parts);
+      const uint64_t r = w / parts;
+      const uint32_t plane = (uint32_t)(r % c.planes), i = (uint32_t)(r / c.planes);
+      uint32_t src, dst;
+      if (!pair_of(i, &src, &dst)) continue;
+      uint8_t* base = c.base + (int64_t)plane * c.plane_stride;
+      const u32x4* from = reinterpret_cast<const u32x4*>(base + (int64_t)src * c.page_stride) + part * 256 + lane;
+      u32x4* to = reinterpret_cast<u32x4*>(base + (int64_t)dst * c.page_stride) + part * 256 + lane;
+      const uint32_t left = c.units - part * 256;
+      u32x4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (lane + 64 * j < left) v[j] = from[64 * j];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (lane + 64 * j < left) to[64 * j] = v[j];
+    }
+  }
+}
+
+constexpr uint32_t kCopyBlocks = 2048;
+
+// ------------------------------------------------------------------ step
+
+struct StepArgs {
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t *lens, *parents, *grow, *held;
+  int32_t *new_table, *new_lens, *refs, *counters;
+  uint64_t* best;      // [pages] of the sequences that have the page last: (length + 1) << 32 | ~sequence
+  uint32_t* lasts;     // [pages] how many they are
+  uint32_t* base;      // [S] fresh pages before the sequence's
+  uint2* copies;       // [S] page, rank of the fresh page
+  uint32_t* free_list; // [pages]
+  uint64_t* words;     // look-back over the tiles of pages
+  uint32_t* state;     // 0: ticket, 1: free pages, 2: needed pages, 3: copies
+  uint32_t S0, S, P, N, shift, window, sinks;
+  uint32_t row_lanes;  // claim, place: threads of a row (a power of two)
+  uint32_t rows_blocks;
+  Caches caches;
+  Marks marks;
+};
+
+constexpr uint32_t kPageTile = 4096;
+
+struct Row {
+  uint32_t src, len, grown, used, need;  // old sequence, old and new length, old pages, new pages
+  bool kept, bad, cut;
+};
+
+ARGUS_DEV Row row_of(const StepArgs& a, uint32_t s) {
+  Row r;
+  const int32_t parent = a.parents ? a.parents[s] : (int32_t)s;
+  r.bad = parent < -1 || parent >= (int64_t)a.S0;
+  r.kept = parent >= 0 && !r.bad;
+  r.src = r.kept ? (uint32_t)parent : 0u;
+  const uint32_t most = a.P << a.shift, mask = (1u << a.shift) - 1;
+  const int32_t n = r.kept ? a.lens[r.src] : 0;
+  r.len = n < 0 ? 0u : ((uint32_t)n < most ? (uint32_t)n : most);
+  const int32_t g = a.grow ? a.grow[s] : 0;
+  const uint32_t more = g < 0 ? 0u : (uint32_t)g;
+  r.cut = more > most - r.len;
+  r.grown = r.cut ? most : r.len + more;
+  r.used = (r.len >> a.shift) + ((r.len & mask) != 0);
+  r.need = (r.grown >> a.shift) + ((r.grown & mask) != 0);
+  return r;
+}
+
+// The entry that the row takes over in a column (-1: none).
+ARGUS_DEV int32_t entry_of(const StepArgs& a, const Row& r, uint32_t col) {
+  if (!r.kept || col >= r.used) return -1;
+  const int32_t e = a.table[(int64_t)r.src * a.table_stride + col];
+  if ((uint32_t)e >= a.N) return -1;
+  if (a.window) {
+    const int64_t first = (int64_t)r.len + (r.grown > r.len ? 1 : 0) - (int64_t)a.window;
+    if ((((int64_t)col + 1) << a.shift) <= first && ((uint64_t)col << a.shift) >= a.sinks) return -1;
+  }
+  return e;
+}
+
+ARGUS_DEV bool ends_inside(const StepArgs& a, const Row& r) { return (r.len & ((1u << a.shift) - 1)) != 0; }
+
+__global__ __launch_bounds__(kThreads) void k_step_clear(StepArgs a) {
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_STEP_CLEAR);
+  const uint32_t i0 = blockIdx.x * kThreads + threadIdx.x, step = gridDim.x * kThreads;
+  for (uint32_t p = i0; p < a.N; p += step) {
+    const int32_t h = a.held ? a.held[p] : 0;
+    a.refs[p] = h < 0 ? 0 : h;
+    a.best[p] = 0;
+    a.lasts[p] = 0;
+  }
+  for (uint32_t p = i0; p < (a.N + kPageTile - 1) / kPageTile; p += step) a.words[p] = 0;
+  if (i0 < 8) {
+    a.state[i0] = 0;
+    a.counters[i0] = 0;
+  }
+  mk.end(ARGUS_REGION_STEP_CLEAR);
+}
+
+// The entries that the new sequences take over, and who has which page.
+__global__ __launch_bounds__(kThreads) void k_step_claim(StepArgs a) {
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_STEP_CLAIM);
+  const uint32_t rows = kThreads / a.row_lanes;
+  const uint32_t s = blockIdx.x * rows + threadIdx.x / a.row_lanes, c0 = threadIdx.x % a.row_lanes;
+  if (s < a.S) {
+    const Row r = row_of(a, s);
+    for (uint32_t c = c0; c < a.P; c += a.row_lanes) {
+      const int32_t e = entry_of(a, r, c);
+      a.new_table[(int64_t)s * a.P + c] = e;
+      if (e < 0) continue;
+      atomicAdd(&a.refs[e], 1);
+      if (c + 1 == r.used && ends_inside(a, r)) {
+        atomicMax((unsigned long long*)&a.best[e], (unsigned long long)(r.len + 1) << 32 | (0xFFFFFFFFu - s));
+        atomicAdd(&a.lasts[e], 1u);
+      }
+    }
+    if (c0 == 0) {
+      a.new_lens[s] = (int32_t)r.grown;
+      if (r.bad) atomicAdd(&a.counters[ARGUS_ST_BAD_PARENT], 1);
+      if (r.cut) atomicAdd(&a.counters[ARGUS_ST_CUT], 1);
+    }
+  }
+  mk.end(ARGUS_REGION_STEP_CLAIM);
+}
+
+// The page that the row has to copy before it grows (-1: none).
+ARGUS_DEV int32_t page_to_copy(const StepArgs& a, const Row& r, uint32_t s) {
+  if (!r.kept || r.grown == r.len || !ends_inside(a, r)) return -1;
+  const int32_t e = a.new_table[(int64_t)s * a.P + r.used - 1];
+  if (e < 0) return -1;
+  const bool mine = (a.held == nullptr || a.held[e] <= 0) && a.lasts[e] == (uint32_t)a.refs[e] &&
+                    (uint32_t)a.best[e] == 0xFFFFFFFFu - s;
+  return mine ? -1 : e;
+}
+
+// Block 0: fresh pages that the sequences before each one take, in order.
+// The others: the free pages in order, one tile of the pool after the other.
+__global__ __launch_bounds__(kThreads) void k_step_plan(StepArgs a) {
+  constexpr uint32_t kItems = kPageTile / kThreads;
+  __shared__ uint32_t s_tile;
+  __shared__ uint2 s_wave[kWaves];
+  __shared__ uint32_t s_before;
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_STEP_PLAN);
+  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+  if (blockIdx.x == 0) {
+    uint2 before = make_uint2(0, 0);  // pages, copies
+    for (uint32_t s0 = 0; s0 < a.S; s0 += kThreads) {
+      const uint32_t s = s0 + tid;
+      int32_t page = -1;
+      uint2 v = make_uint2(0, 0);
+      if (s < a.S) {
+        const Row r = row_of(a, s);
+        page = page_to_copy(a, r, s);
+        v = make_uint2(r.need - r.used + (page >= 0), page >= 0);
+      }
+      uint2 incl = v;
+      for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t x = __shfl_up(incl.x, d), y = __shfl_up(incl.y, d);
+        if (lane >= (uint32_t)d) incl.x += x, incl.y += y;
+      }
+      if (lane == 63) s_wave[wave] = incl;
+      __syncthreads();
+      uint2 at = before;
+      for (uint32_t w = 0; w < (uint32_t)kWaves; ++w) {
+        if (w < wave) at.x += s_wave[w].x, at.y += s_wave[w].y;
+        before.x += s_wave[w].x, before.y += s_wave[w].y;
+      }
+      __syncthreads();
+      if (s < a.S) {
+        const uint32_t base = at.x + incl.x - v.x;
+        a.base[s] = base | (page >= 0 ? 0x80000000u : 0u);
+        if (page >= 0) a.copies[at.y + incl.y - 1] = make_uint2((uint32_t)page, base);
+      }
+    }
+    if (tid == 0) {
+      a.state[2] = before.x;
+      a.state[3] = before.y;
+    }
+  } else {
+    // Tiles are taken in order, so a block waits for running blocks alone.
+    if (tid == 0) s_tile = atomicAdd(&a.state[0], 1u);
+    __syncthreads();
+    const uint32_t tile = s_tile, p0 = tile * kPageTile + tid * kItems;
+    uint32_t free = 0;
+    for (uint32_t i = 0; i < kItems; ++i)
+      if (p0 + i < a.N && a.refs[p0 + i] == 0) free |= 1u << i;
+    const uint32_t n = (uint32_t)__popc(free);
+    uint32_t incl = n;
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t x = __shfl_up(incl, d);
+      if (lane >= (uint32_t)d) incl += x;
+    }
+    if (lane == 63) s_wave[wave].x = incl;
+    __syncthreads();
+    uint32_t at = incl - n, total = 0;
+    for (uint32_t w = 0; w < (uint32_t)kWaves; ++w) {
+      if (w < wave) at += s_wave[w].x;
+      total += s_wave[w].x;
+    }
+    if (wave == 0) {
+      uint64_t error = 0;
+      const uint32_t before = (uint32_t)scan_lookback(a.words, tile, total, &error, 1);
+      if (lane == 0) {
+        if (error) a.counters[ARGUS_ST_INTERNAL] = 1;
+        s_before = before;
+        if ((uint64_t)(tile + 1) * kPageTile >= a.N) a.state[1] = before + total;
+      }
+    }
+    __syncthreads();
+    at += s_before;
+    for (uint32_t i = 0; i < kItems; ++i)
+      if (free >> i & 1u) a.free_list[at++] = p0 + i;
+  }
+  mk.end(ARGUS_REGION_STEP_PLAN);
+}
+
+// Fresh pages into the tables (the first rows_blocks blocks), pages copied (the others).
+__global__ __launch_bounds__(kThreads) void k_step_place(StepArgs a) {
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_STEP_PLACE);
+  const uint32_t n_free = a.state[1], needed = a.state[2];
+  if (blockIdx.x < a.rows_blocks) {
+    const uint32_t rows = kThreads / a.row_lanes;
+    const uint32_t s = blockIdx.x * rows + threadIdx.x / a.row_lanes, c0 = threadIdx.x % a.row_lanes;
+    if (s < a.S) {
+      const Row r = row_of(a, s);
+      const uint32_t word = a.base[s], base = word & 0x7FFFFFFFu, copy = word >> 31;
+      for (uint32_t c = r.used + c0; c < r.need; c += a.row_lanes) {
+        const uint32_t rank = base + copy + c - r.used;
+        const int32_t page = rank < n_free ? (int32_t)a.free_list[rank] : -1;
+        a.new_table[(int64_t)s * a.P + c] = page;
+        if (page >= 0) a.refs[page] = 1;
+      }
+      if (copy && c0 == 0) {
+        int32_t* at = &a.new_table[(int64_t)s * a.P + r.used - 1];
+        const int32_t page = base < n_free ? (int32_t)a.free_list[base] : -1;
+        const int32_t old = *at;
+        *at = page;
+        if (page >= 0) {
+          a.refs[page] = 1;
+          atomicAdd(&a.counters[ARGUS_ST_COPIED], 1);
+        }
+        if (atomicSub(&a.refs[old], 1) == 1) atomicSub(&a.counters[ARGUS_ST_LIVE], 1);
+      }
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+      a.counters[ARGUS_ST_NEEDED] = (int32_t)needed;
+      a.counters[ARGUS_ST_SHORT] = (int32_t)(needed > n_free ? needed - n_free : 0u);
+      atomicAdd(&a.counters[ARGUS_ST_LIVE], (int32_t)(a.N - n_free + (needed < n_free ? needed : n_free)));
+    }
+  } else {
+    const uint32_t wave = (blockIdx.x - a.rows_blocks) * kWaves + threadIdx.x / 64;
+    copy_pages(a.caches, a.state[3], __builtin_amdgcn_readfirstlane(wave), (gridDim.x - a.rows_blocks) * kWaves,
+               [&](uint32_t i, uint32_t* src, uint32_t* dst) {
+                 const uint2 c = a.copies[i];
+                 if (c.y >= n_free) return false;
+                 *src = c.x;
+                 *dst = a.free_list[c.y];
+                 return true;
+               });
+  }
+  mk.end(ARGUS_REGION_STEP_PLACE);
+}
+
+// --------------------------------------------------------------- compact
+
+struct CompactArgs {
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t* refs;
+  int32_t *new_table, *new_refs, *map, *counters;
+  uint32_t* tile_live;  // [tiles] live pages of each
+  uint32_t* rank;       // [pages] live pages below
+  uint32_t* holes;      // [pages] free pages below n, in order
+  uint32_t* movers;     // [pages] the r-th live page, for those from n on
+  uint32_t* state;      // 0: n, 1: live pages below n
+  uint32_t S, P, N, tiles;
+  uint32_t page_blocks, row_blocks;
+  Caches caches;
+  Marks marks;
+};
+
+__global__ __launch_bounds__(kThreads) void k_compact_count(CompactArgs a) {
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_COMPACT_COUNT);
+  __shared__ uint32_t s_wave[kWaves];
+  uint32_t n = 0;
+  for (uint32_t i = 0; i < kPageTile; i += kThreads) {
+    const uint32_t p = blockIdx.x * kPageTile + i + threadIdx.x;
+    n += p < a.N && a.refs[p] > 0;
+  }
+  for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
+  if ((threadIdx.x & 63u) == 0) s_wave[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) a.tile_live[blockIdx.x] = s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
+  mk.end(ARGUS_REGION_COMPACT_COUNT);
+}
+
+__global__ __launch_bounds__(kThreads) void k_compact_plan(CompactArgs a) {
+  constexpr uint32_t kItems = kPageTile / kThreads;
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_COMPACT_PLAN);
+  __shared__ uint2 s_wave[kWaves];
+  __shared__ uint32_t s_scan[kWaves];
+  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+  uint32_t before = 0, n = 0;
+  for (uint32_t t = tid; t < a.tiles; t += kThreads) {
+    const uint32_t v = a.tile_live[t];
+    n += v;
+    before += t < blockIdx.x ? v : 0u;
+  }
+  for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d), before += __shfl_xor(before, d);
+  if (lane == 0) s_wave[wave] = make_uint2(n, before);
+  const uint32_t p0 = blockIdx.x * kPageTile + tid * kItems;
+  uint32_t live = 0;
+  for (uint32_t i = 0; i < kItems; ++i)
+    if (p0 + i < a.N && a.refs[p0 + i] > 0) live |= 1u << i;
+  uint32_t incl = (uint32_t)__popc(live);
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t x = __shfl_up(incl, d);
+    if (lane >= (uint32_t)d) incl += x;
+  }
+  if (lane == 63) s_scan[wave] = incl;
+  __syncthreads();
+  n = s_wave[0].x + s_wave[1].x + s_wave[2].x + s_wave[3].x;
+  uint32_t rank = s_wave[0].y + s_wave[1].y + s_wave[2].y + s_wave[3].y + incl - (uint32_t)__popc(live);
+  for (uint32_t w = 0; w < wave; ++w) rank += s_scan[w];
+  for (uint32_t i = 0; i < kItems; ++i) {
+    const uint32_t p = p0 + i;
+    if (p >= a.N) break;
+    if (p == n) a.state[1] = rank;
+    a.rank[p] = rank;
+    if (live >> i & 1u) {
+      if (p >= n) a.movers[rank] = p;
+      ++rank;
+    } else if (p < n) {
+      a.holes[p - rank] = p;
+    }
+  }
+  if (blockIdx.x == 0 && tid == 0) {
+    a.state[0] = n;
+    if (n == a.N) a.state[1] = n;
+  }
+  mk.end(ARGUS_REGION_COMPACT_PLAN);
+}
+
+__global__ __launch_bounds__(kThreads) void k_compact_move(CompactArgs a) {
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_COMPACT_MOVE);
+  const uint32_t n = a.state[0], stay = a.state[1];
+  uint32_t b = blockIdx.x;
+  if (b < a.page_blocks) {
+    const uint32_t p = b * kThreads + threadIdx.x;
+    if (p < a.N) {
+      const int32_t refs = a.refs[p];
+      const uint32_t rank = a.rank[p];
+      a.map[p] = refs <= 0 ? -1 : p < n ? (int32_t)p : (int32_t)a.holes[rank - stay];
+      a.new_refs[p] = p >= n ? 0 : refs > 0 ? refs : a.refs[a.movers[stay + p - rank]];
+    }
+    if (b == 0 && threadIdx.x < ARGUS_CO_NUM_COUNTERS)
+      a.counters[threadIdx.x] = threadIdx.x == ARGUS_CO_LIVE ? (int32_t)n : threadIdx.x == ARGUS_CO_MOVED ? (int32_t)(n - stay) : 0;
+  } else if ((b -= a.page_blocks) < a.row_blocks) {
+    const uint64_t total = (uint64_t)a.S * a.P;
+    for (uint64_t e = (uint64_t)b * kThreads + threadIdx.x; e < total; e += (uint64_t)a.row_blocks * kThreads) {
+      const uint32_t s = (uint32_t)(e / a.P), c = (uint32_t)(e % a.P);
+      const int32_t p = a.table[(int64_t)s * a.table_stride + c];
+      int32_t to = -1;
+      if ((uint32_t)p < a.N && a.refs[p] > 0) to = (uint32_t)p < n ? p : (int32_t)a.holes[a.rank[p] - stay];
+      a.new_table[e] = to;
+    }
+  } else {
+    b -= a.row_blocks;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(b * kWaves + threadIdx.x / 64);
+    copy_pages(a.caches, n - stay, wave, (gridDim.x - a.page_blocks - a.row_blocks) * kWaves,
+               [&](uint32_t i, uint32_t* src, uint32_t* dst) {
+                 *src = a.movers[stay + i];
+                 *dst = a.holes[i];
+                 return true;
+               });
+  }
+  mk.end(ARGUS_REGION_COMPACT_MOVE);
+}
+
+// ------------------------------------------------------------------ host
+
+int take_caches(const argus_page_planes* in, uint32_t n, Caches* out) {
+  if (n > ARGUS_MAX_CACHES) return refuse(ARGUS_E_INVAL, "num_caches %u (0..%d)", n, ARGUS_MAX_CACHES);
+  out->n = n;
+  for (uint32_t i = 0; i < n; ++i) {
+    if (!in[i].base || in[i].planes < 1 || in[i].page_bytes < 16)
+      return refuse(ARGUS_E_INVAL, "cache %u: no base, planes or page_bytes", i);
+    if (!aligned_to(in[i].base, 16) || in[i].plane_stride % 16 || in[i].page_stride % 16 || in[i].page_bytes % 16)
+      return refuse(ARGUS_E_ALIGN, "cache %u: base, strides and page_bytes are multiples of 16", i);
+    out->c[i] = Planes{(uint8_t*)in[i].base, in[i].plane_stride, in[i].page_stride, in[i].planes, in[i].page_bytes / 16};
+  }
+  return ARGUS_OK;
+}
+
+struct StepLayout {
+  size_t best, lasts, base, copies, free_list, words, state, bytes;
+};
+StepLayout step_layout(uint32_t S, uint32_t N) {
+  StepLayout l{};
+  size_t o = 0;
+  auto take = [&](size_t b) {
+    const size_t at = o;
+    o += up256(b ? b : 1);
+    return at;
+  };
+  l.best = take(8ull * N);
+  l.lasts = take(4ull * N);
+  l.free_list = take(4ull * N);
+  l.base = take(4ull * S);
+  l.copies = take(8ull * S);
+  l.words = take(8ull * ((N + kPageTile - 1) / kPageTile));
+  l.state = take(64);
+  l.bytes = o;
+  return l;
+}
+
+uint32_t row_lanes_for(uint32_t columns) {
+  uint32_t l = 1;
+  while (l < columns && l < (uint32_t)kThreads) l <<= 1;
+  return l;
+}
+
+}  // namespace
+}  // namespace decode
+}  // namespace argus
+
+using namespace argus;
+using namespace argus::decode;
+
+extern "C" int argus_decode_append(const argus_append_config* cfg, const argus_append_io* io, argus_markers* markers,
+                                   void* stream_v) {
+  accepted();
+  if (!cfg || !io) return refuse(ARGUS_E_INVAL, "no configuration");
+  if (cfg->abi_version != ARGUS_ATTR_ABI_VERSION) return refuse(ARGUS_E_ABI, "abi_version %u", cfg->abi_version);
+  if (cfg->source_type > ARGUS_FP16) return refuse(ARGUS_E_INVAL, "new rows are bf16 or fp16");
+  if (cfg->cache_type != cfg->source_type && cfg->cache_type != ARGUS_FP8)
+    return refuse(ARGUS_E_INVAL, "the cache is of the rows' type or fp8 (e4m3)");
+  const bool f8 = cfg->cache_type == ARGUS_FP8;
+  const uint32_t unit = f8 ? 16u : 8u;
+  if (cfg->seqs > (1u << 20)) return refuse(ARGUS_E_CAPACITY, "seqs %u", cfg->seqs);
+  if (cfg->kv_heads < 1 || cfg->kv_heads > 1024) return refuse(ARGUS_E_INVAL, "kv_heads %u (1..1024)", cfg->kv_heads);
+  if (cfg->head_dim < 8 || cfg->head_dim > 256 || cfg->head_dim % unit)
+    return refuse(ARGUS_E_INVAL, "head_dim %u: a multiple of %u up to 256", cfg->head_dim, unit);
+  if (!power_of_two(cfg->page_size) || cfg->page_size < 8 || cfg->page_size > 65536)
+    return refuse(ARGUS_E_INVAL, "page_size %u: a power of two, 8..65536", cfg->page_size);
+  if (cfg->num_pages < 1 || cfg->num_pages > 0x7FFFFFFFu || cfg->columns < 1 ||
+      (uint64_t)cfg->columns * cfg->page_size > 0x7FFFFFFFull || cfg->rows > 0x7FFFFFFFu)
+    return refuse(ARGUS_E_CAPACITY, "pages, columns or rows out of range");
+  if (!io->d_offsets && cfg->rows && cfg->rows != cfg->seqs)
+    return refuse(ARGUS_E_INVAL, "without offsets there is one row per sequence: %u rows, %u sequences", cfg->rows, cfg->seqs);
+  if (cfg->rows && cfg->seqs && (!io->d_new_k || !io->d_new_v || !io->d_table || !io->d_starts))
+    return refuse(ARGUS_E_INVAL, "a required pointer is NULL");
+  int rc;
+  if ((rc = check_view(io->k, cfg->cache_type, "k")) != ARGUS_OK || (rc = check_view(io->v, cfg->cache_type, "v")) != ARGUS_OK)
+    return rc;
+  if (!aligned_to(io->d_new_k, 16) || !aligned_to(io->d_new_v, 16) || io->k_row_stride % 8 || io->k_head_stride % 8 ||
+      io->v_row_stride % 8 || io->v_head_stride % 8 || !aligned_to(io->d_table, 4) || !aligned_to(io->d_starts, 4) ||
+      !aligned_to(io->d_offsets, 4) || !aligned_to(io->d_k_scale, 4) || !aligned_to(io->d_v_scale, 4))
+    return refuse(ARGUS_E_ALIGN, "rows of the new keys and values lie on 16 bytes");
+  if (io->table_stride < (int64_t)cfg->columns && cfg->seqs > 1)
+    return refuse(ARGUS_E_INVAL, "table_stride %lld below columns", (long long)io->table_stride);
+  if (marks_bad(markers)) return refuse(ARGUS_E_INVAL, "markers: alignment or region_base");
+  AppendArgs a{};
+  const uint32_t per_head = cfg->head_dim / unit, per_token = 2 * cfg->kv_heads * per_head;
+  // Blocks of 1024 chunks where there are enough of them, else a token each.
+  a.tokens = cfg->rows >= 4096 ? 1024 / per_token : 1;
+  a.tokens = a.tokens < 1 ? 1 : a.tokens > kMaxTokens ? kMaxTokens : a.tokens;
+  const uint32_t blocks = (cfg->rows + a.tokens - 1) / a.tokens;
+  if (!marks_fit(markers, (uint64_t)blocks * kWaves * 2)) return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
+  if (cfg->rows == 0 || cfg->seqs == 0) return ARGUS_OK;
+  if ((rc = device_ok()) != ARGUS_OK) return rc;
+  const int64_t e = type_bytes(cfg->cache_type);
+  a.new_k = (const uint8_t*)io->d_new_k, a.new_v = (const uint8_t*)io->d_new_v;
+  a.k_row = io->k_row_stride * 2, a.k_hd = io->k_head_stride * 2;
+  a.v_row = io->v_row_stride * 2, a.v_hd = io->v_head_stride * 2;
+  a.k = (uint8_t*)io->k.base, a.v = (uint8_t*)io->v.base;
+  a.k_page = io->k.page_stride * e, a.k_head = io->k.head_stride * e, a.k_tok = io->k.token_stride * e;
+  a.v_page = io->v.page_stride * e, a.v_head = io->v.head_stride * e, a.v_tok = io->v.token_stride * e;
+  a.table = io->d_table, a.table_stride = io->table_stride;
+  a.starts = io->d_starts, a.offsets = io->d_offsets;
+  a.k_scale = io->d_k_scale, a.v_scale = io->d_v_scale;
+  a.S = cfg->seqs, a.rows = cfg->rows, a.shift = log2_of(cfg->page_size);
+  a.num_pages = cfg->num_pages, a.columns = cfg->columns;
+  a.per_token = fast_div(per_token);
+  a.per_side = fast_div(per_token / 2);
+  a.per_head = fast_div(per_head);
+  a.marks = take_marks(markers, blocks, 2);
+  hipStream_t st = (hipStream_t)stream_v;
+  if (!f8) hipLaunchKernelGGL(k_append<0>, dim3(blocks), dim3(kThreads), 0, st, a);
+  else if (cfg->source_type == ARGUS_BF16) hipLaunchKernelGGL(k_append<1>, dim3(blocks), dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL(k_append<2>, dim3(blocks), dim3(kThreads), 0, st, a);
+  return hipGetLastError() == hipSuccess ? ARGUS_OK : refuse(ARGUS_E_HIP, "launch failed");
+}
+
+extern "C" size_t argus_decode_step_workspace_bytes(uint32_t new_seqs, uint32_t num_pages) {
+  accepted();
+  if (new_seqs > (1u << 20) || num_pages < 1 || num_pages > (1u << 28)) {
+    refuse(ARGUS_E_CAPACITY, "new_seqs %u, num_pages %u", new_seqs, num_pages);
+    return (size_t)-1;
+  }
+  return step_layout(new_seqs, num_pages).bytes;
+}
+
+extern "C" int argus_decode_step(const argus_step_config* cfg, const argus_step_io* io, void* d_workspace,
+                                 size_t workspace_bytes, argus_markers* markers, void* stream_v) {
+  accepted();
+  if (!cfg || !io) return refuse(ARGUS_E_INVAL, "no configuration");
+  if (cfg->abi_version != ARGUS_ATTR_ABI_VERSION) return refuse(ARGUS_E_ABI, "abi_version %u", cfg->abi_version);
+  if (cfg->old_seqs > (1u << 20) || cfg->new_seqs > (1u << 20) || cfg->num_pages < 1 || cfg->num_pages > (1u << 28))
+    return refuse(ARGUS_E_CAPACITY, "sequences or pages out of range");
+  if (!power_of_two(cfg->page_size) || cfg->page_size > 65536)
+    return refuse(ARGUS_E_INVAL, "page_size %u: a power of two up to 65536", cfg->page_size);
+  if (cfg->columns < 1 || (uint64_t)cfg->columns * cfg->page_size > 0x7FFFFFFFull ||
+      (uint64_t)cfg->columns * cfg->new_seqs > 0x7FFF0000ull || cfg->window > 0x7FFFFFFFu || cfg->sinks > 0x7FFFFFFFu)
+    return refuse(ARGUS_E_CAPACITY, "columns, window or sinks out of range");
+  if (!io->d_parents && cfg->new_seqs && cfg->old_seqs != cfg->new_seqs)
+    return refuse(ARGUS_E_INVAL, "without parents the sequences stay: %u old, %u new", cfg->old_seqs, cfg->new_seqs);
+  if ((cfg->old_seqs && (!io->d_table || !io->d_lens)) || (cfg->new_seqs && (!io->d_new_table || !io->d_new_lens)) ||
+      !io->d_refs || !io->d_counters)
+    return refuse(ARGUS_E_INVAL, "a required pointer is NULL");
+  if (io->d_new_table == io->d_table || (io->d_new_lens && io->d_new_lens == io->d_lens) || io->d_refs == io->d_held)
+    return refuse(ARGUS_E_INVAL, "the new table, lens and refs are other buffers than the old");
+  if (!aligned_to(io->d_table, 4) || !aligned_to(io->d_lens, 4) || !aligned_to(io->d_parents, 4) || !aligned_to(io->d_grow, 4) ||
+      !aligned_to(io->d_held, 4) || !aligned_to(io->d_new_table, 4) || !aligned_to(io->d_new_lens, 4) ||
+      !aligned_to(io->d_refs, 4) || !aligned_to(io->d_counters, 4))
+    return refuse(ARGUS_E_ALIGN, "tables lie on 4 bytes");
+  if (cfg->old_seqs > 1 && io->table_stride < (int64_t)cfg->columns)
+    return refuse(ARGUS_E_INVAL, "table_stride %lld below columns", (long long)io->table_stride);
+  StepArgs a{};
+  int rc = take_caches(io->caches, cfg->num_caches, &a.caches);
+  if (rc != ARGUS_OK) return rc;
+  if (marks_bad(markers)) return refuse(ARGUS_E_INVAL, "markers: alignment or region_base");
+  const StepLayout l = step_layout(cfg->new_seqs, cfg->num_pages);
+  if (!d_workspace) return refuse(ARGUS_E_INVAL, "no workspace");
+  if (!aligned_to(d_workspace, 256)) return refuse(ARGUS_E_ALIGN, "the workspace lies on 256 bytes");
+  if (workspace_bytes < l.bytes) return refuse(ARGUS_E_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, l.bytes);
+  char* ws = (char*)d_workspace;
+  a.table = io->d_table, a.table_stride = io->table_stride, a.lens = io->d_lens, a.parents = io->d_parents;
+  a.grow = io->d_grow, a.held = io->d_held, a.new_table = io->d_new_table, a.new_lens = io->d_new_lens;
+  a.refs = io->d_refs, a.counters = io->d_counters;
+  a.best = (uint64_t*)(ws + l.best), a.lasts = (uint32_t*)(ws + l.lasts), a.base = (uint32_t*)(ws + l.base);
+  a.copies = (uint2*)(ws + l.copies), a.free_list = (uint32_t*)(ws + l.free_list), a.words = (uint64_t*)(ws + l.words);
+  a.state = (uint32_t*)(ws + l.state);
+  a.S0 = cfg->old_seqs, a.S = cfg->new_seqs, a.P = cfg->columns, a.N = cfg->num_pages;
+  a.shift = log2_of(cfg->page_size), a.window = cfg->window, a.sinks = cfg->sinks;
+  a.row_lanes = row_lanes_for(a.P);
+  const uint32_t rows = kThreads / a.row_lanes;
+  a.rows_blocks = (a.S + rows - 1) / rows;
+  if (a.rows_blocks == 0) a.rows_blocks = 1;
+  const uint32_t tiles = (a.N + kPageTile - 1) / kPageTile;
+  uint32_t clear = (a.N + kThreads - 1) / kThreads;
+  clear = clear > 1024 ? 1024 : clear;
+  const uint32_t copy_blocks = a.caches.n && a.S ? kCopyBlocks : 0;
+  const uint32_t grid[4] = {clear, a.rows_blocks, tiles + 1, a.rows_blocks + copy_blocks};
+  if (!marks_fit(markers, ((uint64_t)grid[0] + grid[1] + grid[2] + grid[3]) * kWaves * 2))
+    return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
+  if ((rc = device_ok()) != ARGUS_OK) return rc;
+  hipStream_t st = (hipStream_t)stream_v;
+  a.marks = take_marks(markers, grid[0], 2);
+  hipLaunchKernelGGL(k_step_clear, dim3(grid[0]), dim3(kThreads), 0, st, a);
+  a.marks = take_marks(markers, grid[1], 2);
+  hipLaunchKernelGGL(k_step_claim, dim3(grid[1]), dim3(kThreads), 0, st, a);
+  a.marks = take_marks(markers, grid[2], 2);
+  hipLaunchKernelGGL(k_step_plan, dim3(grid[2]), dim3(kThreads), 0, st, a);
+  a.marks = take_marks(markers, grid[3], 2);
+  hipLaunchKernelGGL(k_step_place, dim3(grid[3]), dim3(kThreads), 0, st, a);
+  return hipGetLastError() == hipSuccess ? ARGUS_OK : refuse(ARGUS_E_HIP, "launch failed");
+}
+
+namespace {
+struct CompactLayout {
+  size_t tile_live, rank, holes, movers, state, bytes;
+};
+CompactLayout compact_layout(uint32_t N) {
+  CompactLayout l{};
+  size_t o = 0;
+  auto take = [&](size_t b) {
+    const size_t at = o;
+    o += up256(b);
+    return at;
+  };
+  l.tile_live = take(4ull * ((N + kPageTile - 1) / kPageTile));
+  l.rank = take(4ull * N);
+  l.holes = take(4ull * N);
+  l.movers = take(4ull * N);
+  l.state = take(64);
+  l.bytes = o;
+  return l;
+}
+}  // namespace
+
+extern "C" size_t argus_decode_compact_workspace_bytes(uint32_t num_pages) {
+  accepted();
+  if (num_pages < 1 || num_pages > (1u << 28)) {
+    refuse(ARGUS_E_CAPACITY, "num_pages %u", num_pages);
+    return (size_t)-1;
+  }
+  return compact_layout(num_pages).bytes;
+}
+
+extern "C" int argus_decode_compact(const argus_compact_config* cfg, const argus_compact_io* io, void* d_workspace,
+                                    size_t workspace_bytes, argus_markers* markers, void* stream_v) {
+  accepted();
+  if (!cfg || !io) return refuse(ARGUS_E_INVAL, "no configuration");
+  if (cfg->abi_version != ARGUS_ATTR_ABI_VERSION) return refuse(ARGUS_E_ABI, "abi_version %u", cfg->abi_version);
+  if (cfg->seqs > (1u << 20) || cfg->columns < 1 || (uint64_t)cfg->columns * cfg->seqs > 0x7FFF0000ull ||
+      cfg->num_pages < 1 || cfg->num_pages > (1u << 28))
+    return refuse(ARGUS_E_CAPACITY, "sequences, columns or pages out of range");
+  if ((cfg->seqs && (!io->d_table || !io->d_new_table)) || !io->d_refs || !io->d_new_refs || !io->d_map || !io->d_counters)
+    return refuse(ARGUS_E_INVAL, "a required pointer is NULL");
+  if ((cfg->seqs && io->d_new_table == io->d_table) || io->d_new_refs == io->d_refs)
+    return refuse(ARGUS_E_INVAL, "the new table and refs are other buffers than the old");
+  if (!aligned_to(io->d_table, 4) || !aligned_to(io->d_refs, 4) || !aligned_to(io->d_new_table, 4) ||
+      !aligned_to(io->d_new_refs, 4) || !aligned_to(io->d_map, 4) || !aligned_to(io->d_counters, 4))
+    return refuse(ARGUS_E_ALIGN, "tables lie on 4 bytes");
+  if (cfg->seqs > 1 && io->table_stride < (int64_t)cfg->columns)
+    return refuse(ARGUS_E_INVAL, "table_stride %lld below columns", (long long)io->table_stride);
+  CompactArgs a{};
+  int rc = take_caches(io->caches, cfg->num_caches, &a.caches);
+  if (rc != ARGUS_OK) return rc;
+  if (marks_bad(markers)) return refuse(ARGUS_E_INVAL, "markers: alignment or region_base");
+  const CompactLayout l = compact_layout(cfg->num_pages);
+  if (!d_workspace) return refuse(ARGUS_E_INVAL, "no workspace");
+  if (!aligned_to(d_workspace, 256)) return refuse(ARGUS_E_ALIGN, "the workspace lies on 256 bytes");
+  if (workspace_bytes < l.bytes) return refuse(ARGUS_E_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, l.bytes);
+  char* ws = (char*)d_workspace;
+  a.table = io->d_table, a.table_stride = io->table_stride, a.refs = io->d_refs;
+  a.new_table = io->d_new_table, a.new_refs = io->d_new_refs, a.map = io->d_map, a.counters = io->d_counters;
+  a.tile_live = (uint32_t*)(ws + l.tile_live), a.rank = (uint32_t*)(ws + l.rank), a.holes = (uint32_t*)(ws + l.holes);
+  a.movers = (uint32_t*)(ws + l.movers), a.state = (uint32_t*)(ws + l.state);
+  a.S = cfg->seqs, a.P = cfg->columns, a.N = cfg->num_pages;
+  a.tiles = (a.N + kPageTile - 1) / kPageTile;
+  a.page_blocks = (a.N + kThreads - 1) / kThreads;
+  const uint64_t entries = (uint64_t)a.S * a.P;
+  a.row_blocks = (uint32_t)((entries + 4 * kThreads - 1) / (4 * kThreads));
+  const uint32_t copy_blocks = a.caches.n ? kCopyBlocks : 0;
+  const uint32_t grid[3] = {a.tiles, a.tiles, a.page_blocks + a.row_blocks + copy_blocks};
+  if (!marks_fit(markers, ((uint64_t)grid[0] + grid[1] + grid[2]) * kWaves * 2))
+    return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
+  if ((rc = device_ok()) != ARGUS_OK) return rc;
+  hipStream_t st = (hipStream_t)stream_v;
+  a.marks = take_marks(markers, grid[0], 2);
+  hipLaunchKernelGGL(k_compact_count, dim3(grid[0]), dim3(kThreads), 0, st, a);
+  a.marks = take_marks(markers, grid[1], 2);
+  hipLaunchKernelGGL(k_compact_plan, dim3(grid[1]), dim3(kThreads), 0, st, a);
+  a.marks = take_marks(markers, grid[2], 2);
+  hipLaunchKernelGGL(k_compact_move, dim3(grid[2]), dim3(kThreads), 0, st, a);
+  return hipGetLastError() == hipSuccess ? ARGUS_OK : refuse(ARGUS_E_HIP, "launch failed");
+}
