@@ -22,12 +22,14 @@
 // the result).
 //
 // Shares: the units of work are the tiles of all (sequence, head) segments one
-// after the other, at least one each.  Block b takes units [b * per, (b + 1) *
-// per) whatever the lengths are (they are known on the device alone), so a batch
-// of one long and many short sequences loads all compute units alike.  A
-// segment that lies in one block is finished there; of the others each block
-// leaves its piece (m, l, O in 32 bits), and k_attend_join joins them in the
-// order of the blocks: results do not depend on timing.
+// after the other, kPieceCost more for each segment, and wave w takes units
+// [w * per, (w + 1) * per) whatever the lengths are (they are known on the
+// device alone): a batch of one long and many short sequences loads all compute
+// units alike, and the short ones' latencies lie side by side.  A segment that lies
+// in one share is finished there; of the others each wave leaves its piece (m, l,
+// O in 32 bits), and k_attend_join joins them in the order of the shares: results
+// do not depend on timing.  Where the table allows short sequences only, a block
+// takes a segment and joins its four waves through LDS: one launch.
 #pragma once
 
 #include "decode.h"
@@ -36,7 +38,8 @@ namespace argus {
 namespace decode {
 
 constexpr uint32_t kTile = 32;        // tokens per step of a wave
-constexpr uint32_t kMaxBlocks = 1024;  // that share a batch
+constexpr uint64_t kMinShare = 4;     // units of a share, at least
+constexpr uint32_t kPieceCost = 3;    // what a segment costs beside its tiles, in tiles
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -58,12 +61,13 @@ struct AttendArgs {
   const float *k_scale, *v_scale;
   uint16_t* out;
   float* lse;
-  float* part_o;    // [blocks][2][16 NQ][DP]
-  float* part_ml;   // [blocks][2][16 NQ][2]
-  uint32_t* desc;   // [blocks][4]: segment left open by the block, its last block
+  float* part_o;    // [shares][2][16 NQ][DP]
+  float* part_ml;   // [shares][2][16 NQ][2]
+  uint4* open;      // [min(shares, segments)] segment in pieces, its first and last share; y > z: none
   uint32_t S, H, G, D, HS, row_tiles;
   uint32_t shift, num_pages, columns, window, sinks;
-  uint32_t blocks;  // 0: one block per segment
+  uint32_t shares;  // waves that share the batch
+  uint32_t by_seg;  // `open` goes by segment, else by share
   float scale;
   Marks marks;
 };
@@ -153,408 +157,450 @@ constexpr float kSlack = 5.5f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 ARGUS_DEV float exp_of(float x) { return exp2f(x * kLog2e); }
 
-// T: type of q, out and the products; F8: the cache holds e4m3; DP: head size
-// rounded up to 64, 128 or 256; NQ: 16-wide column tiles; EXACT: head size = DP.
+// One wave's part of a segment: O, maxima and sums of tiles t0, t0 + dt, ... < t1
+// for the 16 NQ query rows from q0 on.  T: type of q, out and the products; F8:
+// the cache holds e4m3; DP: head size rounded up to 64, 128 or 256; NQ: 16-wide
+// column tiles; EXACT: head size = DP.
 template <int T, bool F8, int DP, int NQ, bool EXACT>
-__global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a) {
+ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint32_t h, uint32_t q0, uint32_t rows,
+                            uint32_t t0, uint32_t t1, uint32_t dt, f32x4 (&acc)[NQ][DP / 16], float (&m)[NQ],
+                            float (&l)[NQ]) {
   constexpr int KF = DP / 32;               // fragments of a key row
   constexpr int KL = F8 ? DP / 64 : DP / 32;  // 16-byte loads of a key row by the 4 lanes that share it
   constexpr int VW = DP / 16;               // elements of a value row per lane
   constexpr int VD = VW * (F8 ? 1 : 2) / 4;   // in 32-bit words
   constexpr int VH = VW / 2;                // 16-bit pairs per lane
-  constexpr int QP = DP + 4;                // pitch of a row of O in LDS
   using Hf = Half<T>;
-  __shared__ uint64_t s_base[kThreads + 1];
-  __shared__ uint64_t s_wave[kWaves];
+  const uint32_t lane = threadIdx.x & 63u, c = lane & 15u, g = lane >> 4;
+  // the query rows as operands: lane (q, g) holds 8 elements of its row per fragment
+  u32x4 qf[NQ][KF];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const uint32_t row = 16 * i + c;
+    const uint16_t* qr = a.q + (int64_t)s * a.q_seq + (int64_t)(h * a.G + q0 + (row < rows ? row : 0)) * a.q_head;
+#pragma unroll
+    for (int f = 0; f < KF; ++f) {
+      const uint32_t d = F8 ? 64 * (f / 2) + 16 * g + 8 * (f % 2) : 32 * f + 8 * g;
+      qf[i][f] = row < rows && d < a.D ? *reinterpret_cast<const u32x4*>(qr + d) : (u32x4)(0u);
+    }
+  }
+  const float kc = a.scale * (a.k_scale ? a.k_scale[h] : 1.0f);
+  const int32_t* tab = a.table + (int64_t)s * a.table_stride;
+  const uint8_t* kb = a.k + (int64_t)h * a.k_head;
+  const uint8_t* vb = a.v + (int64_t)h * a.v_head;
+  const uint32_t in_page = (1u << a.shift) - 1;
+
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    m[i] = -INFINITY;
+    l[i] = 0.0f;
+#pragma unroll
+    for (int f = 0; f < VW; ++f) acc[i][f] = (f32x4)(0.0f);
+  }
+
+  for (uint32_t t = t0; t < t1; t += dt) {
+    const uint32_t tok = (t < p.sink_tiles ? t : t - p.sink_tiles + p.first) * kTile;
+    // the pages of the lane's two key rows, and of its two runs of four value rows
+    int32_t kp[2], vp[2];
+    bool seen[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t kcol = (tok + 16 * i + c) >> a.shift, vcol = (tok + 16 * i + 4 * g) >> a.shift;
+      kp[i] = kcol < a.columns ? tab[kcol] : -1;
+      vp[i] = vcol < a.columns ? tab[vcol] : -1;
+      if ((uint32_t)kp[i] >= a.num_pages) kp[i] = 0;  // any row: its scores are not taken
+      seen[i] = (uint32_t)vp[i] < a.num_pages;
+      if (!seen[i]) vp[i] = 0;
+    }
+    u32x4 kr[2][KL];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint8_t* r = kb + (int64_t)kp[i] * a.k_page + (int64_t)((tok + 16 * i + c) & in_page) * a.k_tok;
+#pragma unroll
+      for (int f = 0; f < KL; ++f) {
+        const uint32_t d = 64 * f + 16 * g;  // byte of the row
+        const bool in = EXACT || d < a.D * (F8 ? 1u : 2u);
+        kr[i][f] = *reinterpret_cast<const u32x4*>(r + (in ? d : 0u));
+        if (!EXACT && !in) kr[i][f] = (u32x4)(0u);
+      }
+    }
+    uint32_t vr[8][VD];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t at = tok + 16 * (i / 4) + 4 * g + i % 4;
+      uint32_t b = c * (VD * 4);
+      if (!EXACT && b >= a.D * (F8 ? 1u : 2u)) b = 0;  // rows of O beyond the head size: not written
+      const uint8_t* r = vb + (int64_t)vp[i / 4] * a.v_page + (int64_t)(at & in_page) * a.v_tok + b;
+      if constexpr (VD == 1) {
+        vr[i][0] = *reinterpret_cast<const uint32_t*>(r);
+      } else if constexpr (VD == 2) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(r);
+        vr[i][0] = x.x, vr[i][1] = x.y;
+      } else {
+#pragma unroll
+        for (int j = 0; j < VD / 4; ++j) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(r + 16 * j);
+          vr[i][4 * j] = x.x, vr[i][4 * j + 1] = x.y, vr[i][4 * j + 2] = x.z, vr[i][4 * j + 3] = x.w;
+        }
+      }
+    }
+    // which of the lane's eight tokens are visible
+    uint32_t vis = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t at = tok + 16 * (i / 4) + 4 * g + i % 4;
+      const bool in = at < p.len && (at >= p.lo || at < p.sinks) && seen[i / 4];
+      vis |= in ? 1u << i : 0u;
+    }
+    const bool whole = __all(vis == 0xFFu);
+    if (!whole) {  // what is not visible may hold anything
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < VD; ++j) vr[i][j] = vis >> i & 1u ? vr[i][j] : 0u;
+    }
+
+    // scores
+    f32x4 sc[NQ][2];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) sc[i][0] = sc[i][1] = (f32x4)(0.0f);
+#pragma unroll
+    for (int f = 0; f < KF; ++f) {
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        u32x4 kf;
+        if constexpr (F8) {
+          const uint32_t w0 = kr[hh][f / 2][2 * (f % 2)], w1 = kr[hh][f / 2][2 * (f % 2) + 1];
+          kf = (u32x4){widen<T>(w0, false), widen<T>(w0, true), widen<T>(w1, false), widen<T>(w1, true)};
+        } else {
+          kf = kr[hh][f];
+        }
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) sc[i][hh] = Hf::mfma(kf, qf[i][f], sc[i][hh]);
+      }
+    }
+
+    // weights
+    u32x4 p_hi[NQ], p_lo[NQ];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = sc[i][j / 4][j % 4] * kc;
+      if (!whole) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = vis >> j & 1u ? x[j] : -INFINITY;
+      }
+      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      if (__any(top > m[i] + kSlack)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float mn = fmaxf(m[i], top);
+        const float scale = m[i] == -INFINITY ? 0.0f : exp_of(m[i] - mn);
+        l[i] *= scale;
+#pragma unroll
+        for (int f = 0; f < VW; ++f) acc[i][f] *= scale;
+        m[i] = mn;
+      }
+      const float ms = m[i] == -INFINITY ? 0.0f : m[i];
+      float w[8], sum = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        w[j] = __builtin_amdgcn_exp2f(fmaf(x[j] - ms, kLog2e, Hf::kRaise));
+        sum += w[j];
+      }
+      l[i] += sum;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t hi, lo;
+        Hf::split(w[2 * j], w[2 * j + 1], &hi, &lo);
+        p_hi[i][j] = hi;
+        p_lo[i][j] = lo;
+      }
+    }
+
+    // values
+#pragma unroll
+    for (int f = 0; f < VH; ++f) {  // elements 2 f and 2 f + 1 of the lane's piece of a row
+      u32x4 even, odd;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {  // tokens 2 j and 2 j + 1
+        uint32_t x, y;
+        if constexpr (F8) {
+          x = widen<T>(vr[2 * j][f / 2], f % 2), y = widen<T>(vr[2 * j + 1][f / 2], f % 2);
+        } else {
+          x = vr[2 * j][f], y = vr[2 * j + 1][f];
+        }
+        even[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+        odd[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+      }
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        acc[i][2 * f] = Hf::mfma(even, p_hi[i], acc[i][2 * f]);
+        acc[i][2 * f + 1] = Hf::mfma(odd, p_hi[i], acc[i][2 * f + 1]);
+        acc[i][2 * f] = Hf::mfma(even, p_lo[i], acc[i][2 * f]);
+        acc[i][2 * f + 1] = Hf::mfma(odd, p_lo[i], acc[i][2 * f + 1]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    l[i] += __shfl_xor(l[i], 16);
+    l[i] += __shfl_xor(l[i], 32);
+  }
+}
+
+// A segment per block, the tiles dealt out to its waves.
+template <int T, bool F8, int DP, int NQ, bool EXACT>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend_whole(AttendArgs a) {
+  constexpr int VW = DP / 16, QP = DP + 4;  // QP: pitch of a row of O in LDS
+  using Hf = Half<T>;
   __shared__ float s_ml[kWaves][16 * NQ][2];
   __shared__ __align__(16) float s_o[kWaves][16 * NQ][QP];
-
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_ATTEND);
   mk.begin(ARGUS_REGION_ATTEND_PLACE);
-  const uint32_t tid = threadIdx.x, lane = tid & 63u;
+  const uint32_t tid = threadIdx.x, c = tid & 15u, g = (tid & 63u) >> 4;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint32_t c = lane & 15u, g = lane >> 4;
-
-  // ---- this block's units [u, end), and the segment that they start in
-  uint64_t u, end, off;
-  uint32_t s;
-  if (a.blocks == 0) {
-    s = blockIdx.x / a.HS;
-    const Span p = span_of(a, s);
-    u = 0;
-    end = p.tiles;
-    off = (uint64_t)(blockIdx.x % a.HS) * p.tiles;
-  } else {
-    const uint32_t run = (a.S + kThreads - 1) / kThreads;
-    uint64_t mine = 0;
-    for (uint32_t i = 0; i < run; ++i) {
-      const uint32_t x = tid * run + i;
-      if (x < a.S) mine += span_of(a, x).tiles;
-    }
-    uint64_t incl = mine;
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint64_t o = __shfl_up(incl, d);
-      if (lane >= (uint32_t)d) incl += o;
-    }
-    if (lane == 63) s_wave[wave] = incl;
-    __syncthreads();
-    uint64_t before = 0, total = 0;
-    for (uint32_t w = 0; w < (uint32_t)kWaves; ++w) {
-      if (w < wave) before += s_wave[w];
-      total += s_wave[w];
-    }
-    s_base[tid] = (before + incl - mine) * a.HS;
-    total *= a.HS;
-    if (tid == 0) s_base[kThreads] = total;
-    __syncthreads();
-    uint64_t per = (total + a.blocks - 1) / a.blocks;
-    per = per < (uint64_t)kWaves ? (uint64_t)kWaves : per;
-    u = blockIdx.x * per;
-    end = u + per < total ? u + per : total;
-    s = 0;
-    off = 0;
-    if (u < end) {
-      uint32_t lo = 0, hi = kThreads;  // last thread whose sequences start at or before u
-      while (hi - lo > 1) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (s_base[mid] <= u) lo = mid; else hi = mid;
-      }
-      s = lo * run;
-      off = u - s_base[lo];
-      for (;;) {
-        const uint64_t w = (uint64_t)span_of(a, s).tiles * a.HS;
-        if (off < w) break;
-        off -= w;
-        ++s;
-      }
-    }
-  }
-  s = __builtin_amdgcn_readfirstlane(s);
-  u = uniform64(u), end = uniform64(end), off = uniform64(off);
+  const uint32_t s = blockIdx.x / a.HS, hs = blockIdx.x % a.HS;
+  const uint32_t h = hs / a.row_tiles, q0 = (hs % a.row_tiles) * 16 * NQ;
+  const uint32_t rows = a.G - q0 < 16u * NQ ? a.G - q0 : 16u * NQ;
+  const Span p = span_of(a, s);
   mk.end(ARGUS_REGION_ATTEND_PLACE);
   mk.begin(ARGUS_REGION_ATTEND_TOKENS);
-
-  bool open = false;  // a segment starts here and does not end
-  uint32_t open_seg = 0;
-  uint64_t open_end = 0;
-  while (u < end) {
-    const Span p = span_of(a, s);
-    const uint32_t hs = (uint32_t)(off / p.tiles), t0 = (uint32_t)(off % p.tiles);
-    const uint32_t n = end - u < p.tiles - t0 ? (uint32_t)(end - u) : p.tiles - t0;
-    const uint32_t h = hs / a.row_tiles, q0 = (hs % a.row_tiles) * 16 * NQ;
-    const uint32_t rows = a.G - q0 < 16u * NQ ? a.G - q0 : 16u * NQ;
-
-    // the query rows as operands: lane (q, g) holds 8 elements of its row per fragment
-    u32x4 qf[NQ][KF];
+  f32x4 acc[NQ][VW];
+  float m[NQ], l[NQ];
+  attend_tiles<T, F8, DP, NQ, EXACT>(a, p, s, h, q0, rows, wave, p.tiles, kWaves, acc, m, l);
+  // Lane (q, g) holds of its column the elements d = (4 g + r) VW + f.
 #pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-      const uint32_t row = 16 * i + c;
-      const uint16_t* qr = a.q + (int64_t)s * a.q_seq + (int64_t)(h * a.G + q0 + (row < rows ? row : 0)) * a.q_head;
-#pragma unroll
-      for (int f = 0; f < KF; ++f) {
-        const uint32_t d = F8 ? 64 * (f / 2) + 16 * g + 8 * (f % 2) : 32 * f + 8 * g;
-        qf[i][f] = row < rows && d < a.D ? *reinterpret_cast<const u32x4*>(qr + d) : (u32x4)(0u);
-      }
+  for (int i = 0; i < NQ; ++i) {
+    const uint32_t row = 16 * i + c;
+    if (g == 0) {
+      s_ml[wave][row][0] = m[i];
+      s_ml[wave][row][1] = l[i];
     }
-    const float kc = a.scale * (a.k_scale ? a.k_scale[h] : 1.0f);
-    const int32_t* tab = a.table + (int64_t)s * a.table_stride;
-    const uint8_t* kb = a.k + (int64_t)h * a.k_head;
-    const uint8_t* vb = a.v + (int64_t)h * a.v_head;
-    const uint32_t in_page = (1u << a.shift) - 1;
-
-    f32x4 acc[NQ][VW];
-    float m[NQ], l[NQ];
+    if (row < rows) {
 #pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-      m[i] = -INFINITY;
-      l[i] = 0.0f;
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int f = 0; f < VW; ++f) acc[i][f] = (f32x4)(0.0f);
-    }
-
-    for (uint32_t t = t0 + wave; t < t0 + n; t += kWaves) {
-      const uint32_t tok = (t < p.sink_tiles ? t : t - p.sink_tiles + p.first) * kTile;
-      // the pages of the lane's two key rows, and of its two runs of four value rows
-      int32_t kp[2], vp[2];
-      bool seen[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint32_t kcol = (tok + 16 * i + c) >> a.shift, vcol = (tok + 16 * i + 4 * g) >> a.shift;
-        kp[i] = kcol < a.columns ? tab[kcol] : -1;
-        vp[i] = vcol < a.columns ? tab[vcol] : -1;
-        if ((uint32_t)kp[i] >= a.num_pages) kp[i] = 0;  // any row: its scores are not taken
-        seen[i] = (uint32_t)vp[i] < a.num_pages;
-        if (!seen[i]) vp[i] = 0;
-      }
-      u32x4 kr[2][KL];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint8_t* r = kb + (int64_t)kp[i] * a.k_page + (int64_t)((tok + 16 * i + c) & in_page) * a.k_tok;
-#pragma unroll
-        for (int f = 0; f < KL; ++f) {
-          const uint32_t d = 64 * f + 16 * g;  // byte of the row
-          const bool in = EXACT || d < a.D * (F8 ? 1u : 2u);
-          kr[i][f] = *reinterpret_cast<const u32x4*>(r + (in ? d : 0u));
-          if (!EXACT && !in) kr[i][f] = (u32x4)(0u);
-        }
-      }
-      uint32_t vr[8][VD];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t at = tok + 16 * (i / 4) + 4 * g + i % 4;
-        uint32_t b = c * (VD * 4);
-        if (!EXACT && b >= a.D * (F8 ? 1u : 2u)) b = 0;  // rows of O beyond the head size: not written
-        const uint8_t* r = vb + (int64_t)vp[i / 4] * a.v_page + (int64_t)(at & in_page) * a.v_tok + b;
-        if constexpr (VD == 1) {
-          vr[i][0] = *reinterpret_cast<const uint32_t*>(r);
-        } else if constexpr (VD == 2) {
-          const u32x2 x = *reinterpret_cast<const u32x2*>(r);
-          vr[i][0] = x.x, vr[i][1] = x.y;
-        } else {
-#pragma unroll
-          for (int j = 0; j < VD / 4; ++j) {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(r + 16 * j);
-            vr[i][4 * j] = x.x, vr[i][4 * j + 1] = x.y, vr[i][4 * j + 2] = x.z, vr[i][4 * j + 3] = x.w;
-          }
-        }
-      }
-      // which of the lane's eight tokens are visible
-      uint32_t vis = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t at = tok + 16 * (i / 4) + 4 * g + i % 4;
-        const bool in = at < p.len && (at >= p.lo || at < p.sinks) && seen[i / 4];
-        vis |= in ? 1u << i : 0u;
-      }
-      const bool whole = __all(vis == 0xFFu);
-      if (!whole) {  // what is not visible may hold anything
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int j = 0; j < VD; ++j) vr[i][j] = vis >> i & 1u ? vr[i][j] : 0u;
-      }
-
-      // scores
-      f32x4 sc[NQ][2];
-#pragma unroll
-      for (int i = 0; i < NQ; ++i) sc[i][0] = sc[i][1] = (f32x4)(0.0f);
-#pragma unroll
-      for (int f = 0; f < KF; ++f) {
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          u32x4 kf;
-          if constexpr (F8) {
-            const uint32_t w0 = kr[hh][f / 2][2 * (f % 2)], w1 = kr[hh][f / 2][2 * (f % 2) + 1];
-            kf = (u32x4){widen<T>(w0, false), widen<T>(w0, true), widen<T>(w1, false), widen<T>(w1, true)};
-          } else {
-            kf = kr[hh][f];
-          }
-#pragma unroll
-          for (int i = 0; i < NQ; ++i) sc[i][hh] = Hf::mfma(kf, qf[i][f], sc[i][hh]);
-        }
-      }
-
-      // weights
-      u32x4 p_hi[NQ], p_lo[NQ];
-#pragma unroll
-      for (int i = 0; i < NQ; ++i) {
-        float x[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = sc[i][j / 4][j % 4] * kc;
-        if (!whole) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = vis >> j & 1u ? x[j] : -INFINITY;
-        }
-        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        if (__any(top > m[i] + kSlack)) {
-          top = fmaxf(top, __shfl_xor(top, 16));
-          top = fmaxf(top, __shfl_xor(top, 32));
-          const float mn = fmaxf(m[i], top);
-          const float scale = m[i] == -INFINITY ? 0.0f : exp_of(m[i] - mn);
-          l[i] *= scale;
-#pragma unroll
-          for (int f = 0; f < VW; ++f) acc[i][f] *= scale;
-          m[i] = mn;
-        }
-        const float ms = m[i] == -INFINITY ? 0.0f : m[i];
-        float w[8], sum = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          w[j] = __builtin_amdgcn_exp2f(fmaf(x[j] - ms, kLog2e, Hf::kRaise));
-          sum += w[j];
-        }
-        l[i] += sum;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          uint32_t hi, lo;
-          Hf::split(w[2 * j], w[2 * j + 1], &hi, &lo);
-          p_hi[i][j] = hi;
-          p_lo[i][j] = lo;
-        }
-      }
-
-      // values
-#pragma unroll
-      for (int f = 0; f < VH; ++f) {  // elements 2 f and 2 f + 1 of the lane's piece of a row
-        u32x4 even, odd;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {  // tokens 2 j and 2 j + 1
-          uint32_t x, y;
-          if constexpr (F8) {
-            x = widen<T>(vr[2 * j][f / 2], f % 2), y = widen<T>(vr[2 * j + 1][f / 2], f % 2);
-          } else {
-            x = vr[2 * j][f], y = vr[2 * j + 1][f];
-          }
-          even[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-          odd[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-        }
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-          acc[i][2 * f] = Hf::mfma(even, p_hi[i], acc[i][2 * f]);
-          acc[i][2 * f + 1] = Hf::mfma(odd, p_hi[i], acc[i][2 * f + 1]);
-          acc[i][2 * f] = Hf::mfma(even, p_lo[i], acc[i][2 * f]);
-          acc[i][2 * f + 1] = Hf::mfma(odd, p_lo[i], acc[i][2 * f + 1]);
-        }
-      }
-    }
-
-    // ---- the block's waves joined.  Lane (q, g) holds of its column the
-    // elements d = (4 g + r) VW + f.
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-      l[i] += __shfl_xor(l[i], 16);
-      l[i] += __shfl_xor(l[i], 32);
-      const uint32_t row = 16 * i + c;
-      if (g == 0) {
-        s_ml[wave][row][0] = m[i];
-        s_ml[wave][row][1] = l[i];
-      }
-      if (row < rows) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int f = 0; f < VW; f += 4)
-            *reinterpret_cast<f32x4*>(&s_o[wave][row][(4 * g + r) * VW + f]) =
-                (f32x4){acc[i][f][r], acc[i][f + 1][r], acc[i][f + 2][r], acc[i][f + 3][r]};
-      }
-    }
-    __syncthreads();
-    const bool done = n == p.tiles;
-    const uint64_t seg_row = (uint64_t)s * a.H * a.G + (uint64_t)h * a.G + q0;
-    const uint64_t slot = 2ull * blockIdx.x + (t0 == 0 ? 1u : 0u);
-    const float vs = a.v_scale ? a.v_scale[h] : 1.0f;
-    const uint32_t quads = a.D / 4;
-    for (uint32_t e = tid; e < rows * quads; e += kThreads) {
-      const uint32_t row = e / quads, d = (e % quads) * 4;
-      float mw[kWaves], top = -INFINITY, sum = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        mw[w] = s_ml[w][row][0];
-        top = fmaxf(top, mw[w]);
-      }
-      f32x4 o = (f32x4)(0.0f);
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float x = mw[w] == -INFINITY ? (s_ml[w][row][1] != 0.0f ? 1.0f : 0.0f) : exp_of(mw[w] - top);
-        sum += s_ml[w][row][1] * x;
-        o += *reinterpret_cast<const f32x4*>(&s_o[w][row][d]) * x;
-      }
-      if (done) {
-        const float inv = sum == 0.0f ? 0.0f : vs / sum;
-        const uint32_t lo = Hf::pack(o.x * inv, o.y * inv), hi = Hf::pack(o.z * inv, o.w * inv);
-        *reinterpret_cast<u32x2*>(a.out + (seg_row + row) * a.D + d) = (u32x2){lo, hi};
-        if (d == 0 && a.lse)
-          a.lse[seg_row + row] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top - Hf::kRaise * kLn2) + logf(sum);
-      } else {
-        *reinterpret_cast<f32x4*>(a.part_o + (slot * 16 * NQ + row) * DP + d) = o;
-        if (d == 0) {
-          a.part_ml[(slot * 16 * NQ + row) * 2] = top;
-          a.part_ml[(slot * 16 * NQ + row) * 2 + 1] = sum;
-        }
-      }
-    }
-    __syncthreads();
-    if (!done && t0 == 0) {
-      open = true;
-      open_seg = s * a.HS + hs;
-      open_end = u + p.tiles;
-    }
-    u += n;
-    off += n;
-    if (off == (uint64_t)p.tiles * a.HS) {
-      off = 0;
-      ++s;
+        for (int f = 0; f < VW; f += 4)
+          *reinterpret_cast<f32x4*>(&s_o[wave][row][(4 * g + r) * VW + f]) =
+              (f32x4){acc[i][f][r], acc[i][f + 1][r], acc[i][f + 2][r], acc[i][f + 3][r]};
     }
   }
-  if (a.blocks && tid == 0) {
-    const uint64_t total = s_base[kThreads];
-    uint64_t per = (total + a.blocks - 1) / a.blocks;
-    per = per < (uint64_t)kWaves ? (uint64_t)kWaves : per;
-    a.desc[4 * blockIdx.x] = open ? 1u : 0u;
-    a.desc[4 * blockIdx.x + 1] = open_seg;
-    a.desc[4 * blockIdx.x + 2] = open ? (uint32_t)((open_end - 1) / per) : 0u;
+  __syncthreads();
+  const uint64_t seg_row = (uint64_t)s * a.H * a.G + (uint64_t)h * a.G + q0;
+  const float vs = a.v_scale ? a.v_scale[h] : 1.0f;
+  const uint32_t quads = a.D / 4;
+  for (uint32_t e = tid; e < rows * quads; e += kThreads) {
+    const uint32_t row = e / quads, d = (e % quads) * 4;
+    float mw[kWaves], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      mw[w] = s_ml[w][row][0];
+      top = fmaxf(top, mw[w]);
+    }
+    f32x4 o = (f32x4)(0.0f);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float x = mw[w] == -INFINITY ? (s_ml[w][row][1] != 0.0f ? 1.0f : 0.0f) : exp_of(mw[w] - top);
+      sum += s_ml[w][row][1] * x;
+      o += *reinterpret_cast<const f32x4*>(&s_o[w][row][d]) * x;
+    }
+    const float inv = sum == 0.0f ? 0.0f : vs / sum;
+    *reinterpret_cast<u32x2*>(a.out + (seg_row + row) * a.D + d) = (u32x2){Hf::pack(o.x * inv, o.y * inv), Hf::pack(o.z * inv, o.w * inv)};
+    if (d == 0 && a.lse)
+      a.lse[seg_row + row] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top - Hf::kRaise * kLn2) + logf(sum);
   }
   mk.end(ARGUS_REGION_ATTEND_TOKENS);
   mk.end(ARGUS_REGION_ATTEND);
 }
 
-// One row of a segment that k_attend left in pieces: block x of the grid looks
-// after the segment that attend's block x left open, if it did.
+// The batch shared among the grid's waves.
+template <int T, bool F8, int DP, int NQ, bool EXACT>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend_shared(AttendArgs a) {
+  constexpr int VW = DP / 16;
+  using Hf = Half<T>;
+  __shared__ uint64_t s_base[kThreads + 1];
+  __shared__ uint64_t s_wave[kWaves];
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_ATTEND);
+  mk.begin(ARGUS_REGION_ATTEND_PLACE);
+  const uint32_t tid = threadIdx.x, lane = tid & 63u, c = lane & 15u, g = lane >> 4;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t run = (a.S + kThreads - 1) / kThreads;
+  uint64_t mine = 0;
+  for (uint32_t i = 0; i < run; ++i) {
+    const uint32_t x = tid * run + i;
+    if (x < a.S) mine += span_of(a, x).tiles + kPieceCost;
+  }
+  uint64_t incl = mine;
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint64_t o = __shfl_up(incl, d);
+    if (lane >= (uint32_t)d) incl += o;
+  }
+  if (lane == 63) s_wave[wave] = incl;
+  __syncthreads();
+  uint64_t before = 0, total = 0;
+  for (uint32_t w = 0; w < (uint32_t)kWaves; ++w) {
+    if (w < wave) before += s_wave[w];
+    total += s_wave[w];
+  }
+  s_base[tid] = (before + incl - mine) * a.HS;
+  total *= a.HS;
+  __syncthreads();
+  // this wave's units [u, end), and the sequence that they start in
+  const uint32_t share = blockIdx.x * kWaves + wave;
+  uint64_t per = (total + a.shares - 1) / a.shares;
+  per = per < kMinShare ? kMinShare : per;
+  uint64_t u = share * per, end = u + per < total ? u + per : total, off = 0;
+  uint32_t s = 0;
+  if (u < end) {
+    uint32_t lo = 0, hi = kThreads;  // last thread whose sequences start at or before u
+    while (hi - lo > 1) {
+      const uint32_t mid = (lo + hi) / 2;
+      if (s_base[mid] <= u) lo = mid; else hi = mid;
+    }
+    s = lo * run;
+    off = u - s_base[lo];
+    for (;;) {
+      const uint64_t w = (uint64_t)(span_of(a, s).tiles + kPieceCost) * a.HS;
+      if (off < w) break;
+      off -= w;
+      ++s;
+    }
+  }
+  s = __builtin_amdgcn_readfirstlane(s);
+  u = uniform64(u), end = uniform64(end), off = uniform64(off), per = uniform64(per);
+  mk.end(ARGUS_REGION_ATTEND_PLACE);
+  mk.begin(ARGUS_REGION_ATTEND_TOKENS);
+
+  bool open = false;  // a segment starts here and does not end
+  while (u < end) {
+    const Span p = span_of(a, s);
+    const uint32_t units = p.tiles + kPieceCost;
+    const uint32_t hs = (uint32_t)(off / units), o0 = (uint32_t)(off % units);
+    const uint32_t n = end - u < units - o0 ? (uint32_t)(end - u) : units - o0;
+    // its cost comes before its tiles
+    const uint32_t t0 = o0 < kPieceCost ? 0 : o0 - kPieceCost, t1 = o0 + n < kPieceCost ? 0 : o0 + n - kPieceCost;
+    if (t0 < t1) {
+      const uint32_t h = hs / a.row_tiles, q0 = (hs % a.row_tiles) * 16 * NQ;
+      const uint32_t rows = a.G - q0 < 16u * NQ ? a.G - q0 : 16u * NQ;
+      f32x4 acc[NQ][VW];
+      float m[NQ], l[NQ];
+      attend_tiles<T, F8, DP, NQ, EXACT>(a, p, s, h, q0, rows, t0, t1, 1, acc, m, l);
+      const bool done = t0 == 0 && t1 == p.tiles;
+      const uint32_t seg = s * a.HS + hs;
+      if (t0 == 0) {
+        const uint64_t last = (u - o0 + units - 1) / per;
+        if (lane == 0 && (a.by_seg || !done))
+          a.open[a.by_seg ? seg : share] = make_uint4(seg, done ? 1u : share, done ? 0u : (uint32_t)last, 0u);
+        open = !done;
+      }
+      const uint64_t seg_row = (uint64_t)s * a.H * a.G + (uint64_t)h * a.G + q0;
+      const uint64_t slot = 2ull * share + (t0 == 0 ? 1u : 0u);
+      const float vs = a.v_scale ? a.v_scale[h] : 1.0f;
+      // Lane (q, g) holds of its column the elements d = (4 g + r) VW + f.
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        const uint32_t row = 16 * i + c;
+        if (row < rows) {
+          const float inv = l[i] == 0.0f ? 0.0f : vs / l[i];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+#pragma unroll
+            for (int f = 0; f < VW; f += 4) {
+              const uint32_t d = (4 * g + r) * VW + f;
+              const f32x4 o = (f32x4){acc[i][f][r], acc[i][f + 1][r], acc[i][f + 2][r], acc[i][f + 3][r]};
+              if (!done)
+                *reinterpret_cast<f32x4*>(a.part_o + (slot * 16 * NQ + row) * DP + d) = o;
+              else if (EXACT || d < a.D)
+                *reinterpret_cast<u32x2*>(a.out + (seg_row + row) * a.D + d) =
+                    (u32x2){Hf::pack(o.x * inv, o.y * inv), Hf::pack(o.z * inv, o.w * inv)};
+            }
+          }
+          if (g == 0) {
+            if (!done)
+              *reinterpret_cast<f32x2*>(a.part_ml + (slot * 16 * NQ + row) * 2) = (f32x2){m[i], l[i]};
+            else if (a.lse)
+              a.lse[seg_row + row] = l[i] == 0.0f ? -INFINITY : (m[i] == -INFINITY ? 0.0f : m[i] - Hf::kRaise * kLn2) + logf(l[i]);
+          }
+        }
+      }
+    }
+    u += n;
+    off += n;
+    if (off == (uint64_t)units * a.HS) {
+      off = 0;
+      ++s;
+    }
+  }
+  if (!a.by_seg && !open && lane == 0) a.open[share] = make_uint4(0u, 1u, 0u, 0u);
+  mk.end(ARGUS_REGION_ATTEND_TOKENS);
+  mk.end(ARGUS_REGION_ATTEND);
+}
+
+// Four rows of a segment that was left in pieces: piece 0 is the second of its
+// first share, piece i the first of share i further on.
 template <int T, int DP, int NQ>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
-  constexpr uint32_t kQuads = DP / 4, kParts = kThreads / kQuads;
+  constexpr uint32_t kRows = 4, kQuads = DP / 4, kParts = kThreads / (kQuads * kRows);
   using Hf = Half<T>;
-  __shared__ float s_w[kMaxBlocks];
-  __shared__ float s_red[2 * kWaves];
-  __shared__ __align__(16) float s_o[kParts][DP];
+  __shared__ float s_m[kRows][kParts], s_l[kRows][kParts];
+  __shared__ __align__(16) float s_o[kRows][kParts][DP];
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_ATTEND_JOIN);
-  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-  const uint32_t b = blockIdx.x, row = blockIdx.y;
-  const uint32_t seg = a.desc[4 * b + 1];
-  const uint32_t s = seg / a.HS, hs = seg % a.HS;
-  const uint32_t h = hs / a.row_tiles, q0 = (hs % a.row_tiles) * 16 * NQ;
-  if (a.desc[4 * b] != 0 && q0 + row < a.G) {  // (the same in every thread)
-    const uint32_t n = a.desc[4 * b + 2] - b + 1;
-    // piece i > 0 is the first of block b + i, piece 0 the last of block b
-    float top = -INFINITY;
-    for (uint32_t i = tid; i < n; i += kThreads) {
-      const uint64_t r = (2ull * (b + i) + (i == 0 ? 1u : 0u)) * 16 * NQ + row;
-      const float m = a.part_ml[2 * r], l = a.part_ml[2 * r + 1];
-      s_w[i] = m == -INFINITY && !(l != 0.0f) ? -INFINITY : (m == -INFINITY ? 0.0f : m);
-      top = fmaxf(top, s_w[i]);
-    }
-    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if (lane == 0) s_red[wave] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-    float sum = 0.0f;
-    for (uint32_t i = tid; i < n; i += kThreads) {
-      const uint64_t r = (2ull * (b + i) + (i == 0 ? 1u : 0u)) * 16 * NQ + row;
-      const float w = s_w[i] == -INFINITY ? 0.0f : exp_of(s_w[i] - top);
-      s_w[i] = w;
-      sum += w == 0.0f ? 0.0f : w * a.part_ml[2 * r + 1];
-    }
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    if (lane == 0) s_red[kWaves + wave] = sum;
-    __syncthreads();
-    sum = s_red[kWaves] + s_red[kWaves + 1] + s_red[kWaves + 2] + s_red[kWaves + 3];
-    const uint32_t part = tid / kQuads, d = (tid % kQuads) * 4;
+  const uint4 open = a.open[blockIdx.x];
+  if (open.y <= open.z) {
+    const uint32_t s = open.x / a.HS, hs = open.x % a.HS, n = open.z - open.y + 1;
+    const uint32_t h = hs / a.row_tiles, q0 = (hs % a.row_tiles) * 16 * NQ;
+    const uint32_t rows = a.G - q0 < 16u * NQ ? a.G - q0 : 16u * NQ;
+    const uint32_t tid = threadIdx.x, r4 = tid / (kQuads * kParts), part = tid / kQuads % kParts, d = (tid % kQuads) * 4;
+    const uint32_t row = blockIdx.y * kRows + r4, at = row < rows ? row : 0;
+    float m = -INFINITY, l = 0.0f;
     f32x4 o = (f32x4)(0.0f);
-#pragma unroll 8
-    for (uint32_t i = part; i < n; i += kParts) {
-      const uint64_t r = (2ull * (b + i) + (i == 0 ? 1u : 0u)) * 16 * NQ + row;
-      if (d < a.D) o += *reinterpret_cast<const f32x4*>(a.part_o + r * DP + d) * s_w[i];
+    constexpr uint32_t kDeep = 8;
+    for (uint32_t i0 = part; i0 < n; i0 += kParts * kDeep) {
+      f32x2 ml[kDeep];
+      f32x4 v[kDeep];
+      float top = m;
+#pragma unroll
+      for (uint32_t j = 0; j < kDeep; ++j) {
+        const uint32_t i = i0 + j * kParts;
+        const uint64_t x = (2ull * (open.y + (i < n ? i : 0)) + (i == 0 || i >= n ? 1u : 0u)) * 16 * NQ + at;
+        ml[j] = *reinterpret_cast<const f32x2*>(a.part_ml + 2 * x);
+        v[j] = *reinterpret_cast<const f32x4*>(a.part_o + x * DP + d);
+        if (i >= n) ml[j] = (f32x2){-INFINITY, 0.0f}, v[j] = (f32x4)(0.0f);
+        top = fmaxf(top, ml[j].x);
+      }
+      const float keep = m == -INFINITY ? 1.0f : exp_of(m - top);  // (nothing yet, or NaN)
+      l *= keep;
+      o *= keep;
+#pragma unroll
+      for (uint32_t j = 0; j < kDeep; ++j) {
+        const float w = ml[j].x == -INFINITY ? 1.0f : exp_of(ml[j].x - top);  // a maximum of -inf: zeros, or NaN
+        l += ml[j].y * w;
+        o += v[j] * w;
+      }
+      m = top;
     }
-    *reinterpret_cast<f32x4*>(&s_o[part][d]) = o;
+    if (d == 0) s_m[r4][part] = m, s_l[r4][part] = l;
+    *reinterpret_cast<f32x4*>(&s_o[r4][part][d]) = o;
     __syncthreads();
-    if (part == 0 && d < a.D) {
-      for (uint32_t i = 1; i < kParts; ++i) o += *reinterpret_cast<const f32x4*>(&s_o[i][d]);
-      const uint64_t at = (uint64_t)s * a.H * a.G + (uint64_t)h * a.G + q0 + row;
+    if (part == 0 && row < rows && d < a.D) {
+      float top = m, sum = 0.0f;
+      for (uint32_t i = 1; i < kParts; ++i) top = fmaxf(top, s_m[r4][i]);
+      o = (f32x4)(0.0f);
+      for (uint32_t i = 0; i < kParts; ++i) {
+        const float w = s_m[r4][i] == -INFINITY ? 1.0f : exp_of(s_m[r4][i] - top);
+        sum += s_l[r4][i] * w;
+        o += *reinterpret_cast<const f32x4*>(&s_o[r4][i][d]) * w;
+      }
+      const uint64_t out = (uint64_t)s * a.H * a.G + (uint64_t)h * a.G + q0 + row;
       const float inv = sum == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[h] : 1.0f) / sum;
-      *reinterpret_cast<u32x2*>(a.out + at * a.D + d) = (u32x2){Hf::pack(o.x * inv, o.y * inv), Hf::pack(o.z * inv, o.w * inv)};
-      if (d == 0 && a.lse) a.lse[at] = sum == 0.0f ? -INFINITY : top - Hf::kRaise * kLn2 + logf(sum);
+      *reinterpret_cast<u32x2*>(a.out + out * a.D + d) = (u32x2){Hf::pack(o.x * inv, o.y * inv), Hf::pack(o.z * inv, o.w * inv)};
+      if (d == 0 && a.lse)
+        a.lse[out] = sum == 0.0f ? -INFINITY : (top == -INFINITY ? 0.0f : top - Hf::kRaise * kLn2) + logf(sum);
     }
   }
   mk.end(ARGUS_REGION_ATTEND_JOIN);
@@ -562,10 +608,14 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
 
 template <int T, bool F8, int DP, int NQ>
 void launch_attend_as(const AttendArgs& a, uint32_t grid, hipStream_t st) {
-  if (a.D == DP)
-    hipLaunchKernelGGL((k_attend<T, F8, DP, NQ, true>), dim3(grid), dim3(kThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL((k_attend<T, F8, DP, NQ, false>), dim3(grid), dim3(kThreads), 0, st, a);
+  const dim3 g(grid), b(kThreads);
+  if (a.shares) {
+    if (a.D == DP) hipLaunchKernelGGL((k_attend_shared<T, F8, DP, NQ, true>), g, b, 0, st, a);
+    else hipLaunchKernelGGL((k_attend_shared<T, F8, DP, NQ, false>), g, b, 0, st, a);
+  } else {
+    if (a.D == DP) hipLaunchKernelGGL((k_attend_whole<T, F8, DP, NQ, true>), g, b, 0, st, a);
+    else hipLaunchKernelGGL((k_attend_whole<T, F8, DP, NQ, false>), g, b, 0, st, a);
+  }
 }
 
 // The head size rounded up, and as many column tiles as the group needs: two

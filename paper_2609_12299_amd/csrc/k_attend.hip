@@ -36,14 +36,16 @@ int device_ok() {
 
 namespace {
 
-// Blocks that share a batch: two per compute unit, all resident at once.
-constexpr uint32_t kShareBlocks = 512;
+// Waves that share a batch: three blocks of four for each of the 256 compute
+// units, all resident at once (head sizes beyond 128: one), and not so many that
+// joining the pieces of few segments takes longer than they save.
+constexpr uint32_t kShares = 256 * 3 * kWaves, kSharesWide = 256 * kWaves, kSharesOfSegment = 256;
 // Segments of at most this many tiles are not shared: a block each.
 constexpr uint32_t kWholeTiles = 16;
 
 struct Plan {
-  uint32_t dp, nq, row_tiles, hs, blocks, grid;
-  size_t o_at, desc_at, bytes;
+  uint32_t dp, nq, row_tiles, hs, shares, segs, grid, opens, join_rows;
+  size_t o_at, open_at, bytes;
 };
 
 int make_plan(const argus_attend_config* c, Plan* p) {
@@ -75,12 +77,23 @@ int make_plan(const argus_attend_config* c, Plan* p) {
     const uint64_t w = (c->window + kTile - 1) / kTile + 1 + (uint64_t)(c->sinks + kTile - 1) / kTile;
     tiles = w < tiles ? w : tiles;
   }
-  p->blocks = tiles <= kWholeTiles ? 0 : kShareBlocks;
-  p->grid = p->blocks ? p->blocks : (uint32_t)segs;
-  const size_t rows = (size_t)p->blocks * 2 * 16 * p->nq;
+  p->segs = (uint32_t)segs;
+  uint64_t shares = 0;
+  if (tiles > kWholeTiles && segs) {
+    shares = p->dp == 256 ? kSharesWide : kShares;
+    shares = segs * kSharesOfSegment < shares ? segs * kSharesOfSegment : shares;
+    const uint64_t useful = segs * (tiles + kPieceCost) / kMinShare + 1;
+    shares = useful < shares ? useful : shares;
+    shares = (shares + kWaves - 1) / kWaves * kWaves;
+  }
+  p->shares = (uint32_t)shares;
+  p->grid = shares ? p->shares / kWaves : p->segs;
+  p->opens = p->shares < p->segs ? p->shares : p->segs;
+  p->join_rows = c->group < 16 * p->nq ? c->group : 16 * p->nq;
+  const size_t rows = (size_t)shares * 2 * 16 * p->nq;
   p->o_at = up256(rows * 2 * sizeof(float));
-  p->desc_at = p->o_at + up256(rows * p->dp * sizeof(float));
-  p->bytes = p->blocks ? p->desc_at + up256((size_t)p->blocks * 16) : 0;
+  p->open_at = p->o_at + up256(rows * p->dp * sizeof(float));
+  p->bytes = shares ? p->open_at + up256((size_t)p->opens * 16) : 0;
   return ARGUS_OK;
 }
 
@@ -120,9 +133,9 @@ extern "C" int argus_decode_attend(const argus_attend_config* cfg, const argus_a
   if (p.bytes && !aligned_to(d_workspace, 256)) return refuse(ARGUS_E_ALIGN, "the workspace lies on 256 bytes");
   if (workspace_bytes < p.bytes)
     return refuse(ARGUS_E_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
-  const uint32_t join_rows = cfg->group < 16 * p.nq ? cfg->group : 16 * p.nq;
+  const uint64_t joins = p.shares ? (uint64_t)p.opens * ((p.join_rows + 3) / 4) : 0;
   const uint32_t per_wave = 6;  // its own region, and in it the place and the tokens
-  const uint64_t records = ((uint64_t)p.grid * per_wave + (p.blocks ? (uint64_t)p.blocks * join_rows * 2 : 0)) * kWaves;
+  const uint64_t records = ((uint64_t)p.grid * per_wave + joins * 2) * kWaves;
   if (!marks_fit(markers, records)) return refuse(ARGUS_E_CAPACITY, "%llu marker records do not fit", (unsigned long long)records);
   if (cfg->seqs == 0) return ARGUS_OK;
   if ((rc = device_ok()) != ARGUS_OK) return rc;
@@ -139,19 +152,19 @@ extern "C" int argus_decode_attend(const argus_attend_config* cfg, const argus_a
   a.out = (uint16_t*)io->d_out, a.lse = io->d_lse;
   a.part_ml = (float*)d_workspace;
   a.part_o = (float*)((char*)d_workspace + p.o_at);
-  a.desc = (uint32_t*)((char*)d_workspace + p.desc_at);
+  a.open = (uint4*)((char*)d_workspace + p.open_at);
   a.S = cfg->seqs, a.H = cfg->kv_heads, a.G = cfg->group, a.D = cfg->head_dim;
   a.HS = p.hs, a.row_tiles = p.row_tiles;
   a.shift = log2_of(cfg->page_size), a.num_pages = cfg->num_pages, a.columns = cfg->columns;
   a.window = cfg->window, a.sinks = cfg->sinks;
-  a.blocks = p.blocks, a.scale = cfg->scale;
+  a.shares = p.shares, a.by_seg = p.segs <= p.shares, a.scale = cfg->scale;
   a.marks = take_marks(markers, p.grid, per_wave);
   hipStream_t st = (hipStream_t)stream_v;
   const bool f8 = cfg->cache_type == ARGUS_FP8, bf = cfg->q_type == ARGUS_BF16;
   (f8 ? (bf ? launch_attend_bf16_f8 : launch_attend_fp16_f8) : (bf ? launch_attend_bf16 : launch_attend_fp16))(a, p.grid, st);
-  if (p.blocks) {
-    a.marks = take_marks(markers, (uint64_t)p.blocks * join_rows, 2);
-    (bf ? launch_join_type<0> : launch_join_type<1>)(a, dim3(p.blocks, join_rows), st);
+  if (p.shares) {
+    a.marks = take_marks(markers, joins, 2);
+    (bf ? launch_join_type<0> : launch_join_type<1>)(a, dim3(p.opens, (p.join_rows + 3) / 4), st);
   }
   return hipGetLastError() == hipSuccess ? ARGUS_OK : refuse(ARGUS_E_HIP, "launch failed");
 }
