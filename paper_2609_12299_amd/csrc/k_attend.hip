@@ -36,10 +36,10 @@ int device_ok() {
 
 namespace {
 
-// Waves that share a batch: three blocks of four for each of the 256 compute
+// Waves that share a batch: two blocks of four for each of the 256 compute
 // units, all resident at once (head sizes beyond 128: one), and not so many that
 // joining the pieces of few segments takes longer than they save.
-constexpr uint32_t kShares = 256 * 3 * kWaves, kSharesWide = 256 * kWaves, kSharesOfSegment = 256;
+constexpr uint32_t kShares = 256 * 2 * kWaves, kSharesWide = 256 * kWaves, kSharesOfSegment = 256;
 // Segments of at most this many tiles are not shared: a block each.
 constexpr uint32_t kWholeTiles = 16;
 

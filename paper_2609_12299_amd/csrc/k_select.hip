@@ -1,15 +1,18 @@
 // k_select.hip -- beam search's selection over beams and vocabulary.
 //
-// k_select_rows reads the logits once: a block takes a chunk of one row into
-// registers, and gives the sum of its exponentials relative to the largest and
-// its k first candidates.  The bound below which nothing has to be looked at comes
-// from the threads' own maxima: in `lists` >= k disjoint sets of threads, the
-// least of the sets' maxima has at least k elements at or above it, and few more
-// (about lists * ln(lists)).  Those are ranked by counting.  Where equal values
-// make them too many, the block picks its k one after the other.
+// k_select_rows reads the logits once.  A wave takes a part of one row, 64 lanes
+// of 32 elements at a time, the next ones under way while it looks at them, and
+// keeps the sum of their exponentials and a list of candidates in LDS.  The
+// least that a candidate needs is known after the first step: of `lists` >= k
+// disjoint sets of lanes, the least of the sets' maxima has k elements at or
+// above it, and few more (about lists * ln(lists)).  From then on a step costs a
+// comparison of each lane's largest value, and the few lanes above it look closer.
+// When the list is half full, it is cut to its first k, and what the k-th has
+// becomes the least: the list never overflows, however many values are equal.
 //
-// k_select_beams, one block per group of beams, joins the chunks' sums to the
-// rows' logarithms and picks among the rows' candidates in the same way.
+// k_select_beams, one block per group of beams, joins the parts' sums to the
+// rows' logarithms and picks among the rows' candidates by the same sets of
+// maxima, ranking those above by counting.
 //
 // What bounds it: the reading of the logits, and the exponential of each.
 #include "decode.h"
@@ -21,9 +24,10 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr uint32_t kItems = 32;                   // elements of a thread
-constexpr uint32_t kChunkElems = kItems * kThreads;
-constexpr uint32_t kCands = 512;                  // candidates that are ranked by counting
+constexpr uint32_t kItems = 32;               // elements of a lane per step
+constexpr uint32_t kStep = kItems * 64;
+constexpr uint32_t kList = 128;               // candidates of a wave
+constexpr uint32_t kCands = 512;              // candidates of a group that are ranked by counting
 constexpr uint32_t kMaxK = 64, kMaxBeams = 64;
 
 struct SelectArgs {
@@ -34,9 +38,11 @@ struct SelectArgs {
   float* new_scores;
   int32_t *parents, *tokens;
   uint8_t* new_finished;
-  float2* sums;     // [rows][chunks] largest value m, sum of exp(x - m)
-  uint64_t* cands;  // [rows][chunks][k] (value, token) as a key, 0: none
-  uint32_t W, V, K, chunks, lists;
+  float2* sums;     // [rows][parts] m about the largest value, sum of exp(x - m)
+  uint64_t* cands;  // [rows][parts][k] (value, token) as a key, 0: none; no order
+  uint32_t W, V, K, parts, lists;
+  uint32_t steps;   // of a part
+  uint32_t rows;
   int32_t eos;
   Marks marks;
 };
@@ -49,13 +55,6 @@ ARGUS_DEV uint32_t order_of(float x) {
 ARGUS_DEV float value_of(uint32_t o) { return __builtin_bit_cast(float, o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
 ARGUS_DEV uint64_t key_of(float x, uint32_t token) { return join64(~token, order_of(x)); }
 
-template <int TYPE>
-ARGUS_DEV float element(const uint8_t* p) {
-  if constexpr (TYPE == ARGUS_FP32) return *reinterpret_cast<const float*>(p);
-  const uint32_t w = *reinterpret_cast<const uint16_t*>(p);
-  if constexpr (TYPE == ARGUS_BF16) return __builtin_bit_cast(float, w << 16);
-  return (float)__builtin_bit_cast(_Float16, (uint16_t)w);
-}
 template <int TYPE>
 ARGUS_DEV float of_word(uint32_t w, int half) {
   if constexpr (TYPE == ARGUS_FP32) return __builtin_bit_cast(float, w);
@@ -72,107 +71,134 @@ ARGUS_DEV float wave_sum(float v) {
   return v;
 }
 
+// How far a value may rise above the reference of the exponentials.
+constexpr float kSlack = 8.0f;
+
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
   constexpr uint32_t kBytes = TYPE == ARGUS_FP32 ? 4 : 2, kPer = 16 / kBytes, kVecs = kItems / kPer;
-  __shared__ uint32_t s_list[kMaxK];
-  __shared__ float s_red[2 * kWaves];
-  __shared__ uint64_t s_cand[kCands];
-  __shared__ uint32_t s_n;
-  __shared__ uint64_t s_best[kWaves];
+  __shared__ uint64_t s_list[kWaves][kList];
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_SELECT_ROWS);
-  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-  const uint32_t row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
-  if (a.finished && a.finished[row]) {  // stands for itself: nothing of the row is looked at
-    mk.end(ARGUS_REGION_SELECT_ROWS);
-    return;
-  }
-  const uint8_t* base = a.logits + (int64_t)(row / a.W) * a.group_stride + (int64_t)(row % a.W) * a.beam_stride;
-  // Vectors lie on 16 bytes: element j of the row is at place j + lead.
-  const uint32_t lead = (uint32_t)((uintptr_t)base & 15u) / kBytes;
-  float x[kItems];
+  const uint32_t lane = threadIdx.x & 63u;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t job = blockIdx.x * kWaves + wave, row = job / a.parts, part = job % a.parts;
+  // (a finished beam stands for itself: nothing of its row is looked at)
+  if (row < a.rows && !(a.finished && a.finished[row])) {
+    uint64_t* list = s_list[wave];
+    const uint8_t* base = a.logits + (int64_t)(row / a.W) * a.group_stride + (int64_t)(row % a.W) * a.beam_stride;
+    // Vectors lie on 16 bytes: element j of the row is at place j + lead.
+    const uint32_t lead = (uint32_t)((uintptr_t)base & 15u) / kBytes;
+    const uint32_t first = part * a.steps * kStep, places = a.V + lead;
+    const uint32_t left = first < places ? (places - first + kStep - 1) / kStep : 0;
+    const uint32_t steps = left < a.steps ? left : a.steps;
+    auto load = [&](uint32_t step, u32x4 (&w)[kVecs]) {
 #pragma unroll
-  for (uint32_t v = 0; v < kVecs; ++v) {
-    const int64_t j = (int64_t)chunk * kChunkElems + (v * kThreads + tid) * kPer - lead;
-    if (j >= 0 && j + kPer <= a.V) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(base + j * kBytes);
+      for (uint32_t v = 0; v < kVecs; ++v) {
+        const int64_t j = (int64_t)first + step * kStep + (v * 64 + lane) * kPer - lead;
+        if (j >= 0 && j + kPer <= a.V) {
+          w[v] = *reinterpret_cast<const u32x4*>(base + j * kBytes);
+        } else {
 #pragma unroll
-      for (uint32_t i = 0; i < kPer; ++i) x[v * kPer + i] = of_word<TYPE>(w[i * kBytes / 4], i % (4 / kBytes));
-    } else {
-#pragma unroll
-      for (uint32_t i = 0; i < kPer; ++i)
-        x[v * kPer + i] = j + i >= 0 && j + i < a.V ? element<TYPE>(base + (j + i) * kBytes) : -INFINITY;
-    }
-  }
-  if (tid < a.lists) s_list[tid] = 0;
-  if (tid == 0) s_n = 0;
-  float top = x[0];
-#pragma unroll
-  for (uint32_t i = 1; i < kItems; ++i) top = fmaxf(top, x[i]);
-  const float wtop = wave_max(top);
-  if (lane == 0) s_red[wave] = wtop;
-  __syncthreads();
-  atomicMax(&s_list[tid & (a.lists - 1)], order_of(top));
-  const float all = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-  const float shift = all == -INFINITY ? 0.0f : all;  // (values times log2 e could overflow: the difference first)
-  float sum = 0.0f;
-#pragma unroll
-  for (uint32_t i = 0; i < kItems; ++i) sum += __builtin_amdgcn_exp2f((x[i] - shift) * kLog2e);
-  sum = wave_sum(sum);
-  if (lane == 0) s_red[kWaves + wave] = sum;
-  __syncthreads();
-  if (tid == 0)
-    a.sums[blockIdx.x] = make_float2(all, s_red[kWaves] + s_red[kWaves + 1] + s_red[kWaves + 2] + s_red[kWaves + 3]);
-  uint32_t lo = s_list[lane & (a.lists - 1)];
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t o = __shfl_xor(lo, d);
-    lo = o < lo ? o : lo;
-  }
-  const float bound = value_of(lo);
-  // (a list without a value leaves 0: the order of a NaN, which nothing is below)
-  const bool any = lo != 0;
-#pragma unroll
-  for (uint32_t i = 0; i < kItems; ++i) {
-    if ((any ? x[i] >= bound : x[i] == x[i]) && x[i] > -INFINITY) {
-      const uint32_t at = atomicAdd(&s_n, 1u);
-      const uint32_t token = chunk * kChunkElems + ((i / kPer) * kThreads + tid) * kPer + i % kPer - lead;
-      if (at < kCands) s_cand[at] = key_of(x[i], token);
-    }
-  }
-  __syncthreads();
-  const uint32_t n = s_n;
-  uint64_t* out = a.cands + (uint64_t)blockIdx.x * a.K;
-  if (n <= kCands) {
-    for (uint32_t c = tid; c < n; c += kThreads) {
-      const uint64_t k = s_cand[c];
-      uint32_t rank = 0;
-      for (uint32_t o = 0; o < n; ++o) rank += s_cand[o] > k;
-      if (rank < a.K) out[rank] = k;
-    }
-    for (uint32_t r = n + tid; r < a.K; r += kThreads) out[r] = 0;
-  } else {
-    uint64_t last = ~0ull;  // the key picked before
-    for (uint32_t r = 0; r < a.K; ++r) {
-      uint64_t best = 0;
-#pragma unroll
-      for (uint32_t i = 0; i < kItems; ++i) {
-        const uint32_t token = chunk * kChunkElems + ((i / kPer) * kThreads + tid) * kPer + i % kPer - lead;
-        const uint64_t k = x[i] > -INFINITY ? key_of(x[i], token) : 0ull;
-        best = k < last && k > best ? k : best;
+          for (uint32_t i = 0; i < kPer; ++i) {
+            // outside the row: minus infinity
+            uint32_t e = TYPE == ARGUS_FP32 ? 0xFF800000u : TYPE == ARGUS_BF16 ? 0xFF80u : 0xFC00u;
+            if (j + i >= 0 && j + i < a.V) {
+              if constexpr (TYPE == ARGUS_FP32) e = *reinterpret_cast<const uint32_t*>(base + (j + i) * kBytes);
+              else e = *reinterpret_cast<const uint16_t*>(base + (j + i) * kBytes);
+            }
+            if constexpr (TYPE == ARGUS_FP32) w[v][i] = e;
+            else w[v][i / 2] = i % 2 ? w[v][i / 2] | e << 16 : e;
+          }
+        }
       }
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = __shfl_xor(best, d);
-        best = o > best ? o : best;
+    };
+    uint32_t n = 0;          // candidates in the list
+    uint64_t least = 0;      // keys have to be above it
+    float least_value = -INFINITY;
+    // The list cut to its first k.
+    auto cut = [&]() {
+      __builtin_amdgcn_wave_barrier();
+      const uint64_t k0 = lane < n ? list[lane] : 0, k1 = lane + 64 < n ? list[lane + 64] : 0;
+      uint32_t r0 = 0, r1 = 0;
+      for (uint32_t i = 0; i < n; ++i) {
+        const uint64_t o = list[i];
+        r0 += o > k0;
+        r1 += o > k1;
       }
-      if (lane == 0) s_best[wave] = best;
-      __syncthreads();
-      best = s_best[0];
-      for (uint32_t w = 1; w < (uint32_t)kWaves; ++w) best = s_best[w] > best ? s_best[w] : best;
-      if (tid == 0) out[r] = best;
-      last = best;
-      __syncthreads();
+      __builtin_amdgcn_wave_barrier();
+      if (lane < n && r0 < a.K) list[r0] = k0;
+      if (lane + 64 < n && r1 < a.K) list[r1] = k1;
+      __builtin_amdgcn_wave_barrier();
+      n = n < a.K ? n : a.K;
+      if (n == a.K) {
+        least = list[a.K - 1];
+        least_value = value_of((uint32_t)(least >> 32));
+      }
+    };
+    float ref = -INFINITY, sum = 0.0f;
+    auto look = [&](uint32_t step, const u32x4 (&w)[kVecs]) {
+      float x[kItems];
+#pragma unroll
+      for (uint32_t i = 0; i < kItems; ++i) x[i] = of_word<TYPE>(w[i / kPer][(i % kPer) * kBytes / 4], i % (4 / kBytes));
+      float top = x[0];
+#pragma unroll
+      for (uint32_t i = 1; i < kItems; ++i) top = fmaxf(top, x[i]);
+      if (__any(top > ref + kSlack)) {
+        const float was = ref;
+        ref = fmaxf(ref, wave_max(top));
+        sum *= was == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((was - ref) * kLog2e);
+      }
+      const float shift = ref == -INFINITY ? 0.0f : ref;  // (values times log2 e could overflow: the difference first)
+      float part_sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (uint32_t i = 0; i < kItems; ++i) part_sum[i % 4] += __builtin_amdgcn_exp2f((x[i] - shift) * kLog2e);
+      sum += (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
+      if (step == 0) {
+        uint32_t lo = order_of(top);
+        for (uint32_t d = a.lists; d < 64; d <<= 1) {
+          const uint32_t o = __shfl_xor(lo, d);
+          lo = o > lo ? o : lo;
+        }
+        for (uint32_t d = 1; d < a.lists; d <<= 1) {
+          const uint32_t o = __shfl_xor(lo, d);
+          lo = o < lo ? o : lo;
+        }
+        least_value = value_of(lo);
+        least = join64(0u, lo);  // below every key of this value
+      }
+      if (__any(top >= least_value && top > -INFINITY)) {
+        const uint32_t token0 = first + step * kStep + lane * kPer - lead;
+#pragma unroll
+        for (uint32_t i = 0; i < kItems; ++i) {
+          if (__any(x[i] >= least_value)) {
+            const uint64_t key = key_of(x[i], token0 + (i / kPer) * 64 * kPer + i % kPer);
+            uint64_t take = __ballot(x[i] >= least_value && key > least && x[i] > -INFINITY);
+            if (n + (uint32_t)__popcll(take) > kList) {
+              cut();
+              take = __ballot(x[i] >= least_value && key > least && x[i] > -INFINITY);
+            }
+            if (take >> lane & 1u) list[n + (uint32_t)__popcll(take & lanemask_lt())] = key;
+            n += (uint32_t)__popcll(take);
+          }
+        }
+        if (n > kList / 2) cut();
+      }
+    };
+    u32x4 w0[kVecs], w1[kVecs];
+    if (steps) load(0, w0);
+    for (uint32_t step = 0; step < steps; step += 2) {
+      if (step + 1 < steps) load(step + 1, w1);
+      look(step, w0);
+      if (step + 1 < steps) {
+        if (step + 2 < steps) load(step + 2, w0);
+        look(step + 1, w1);
+      }
     }
+    cut();
+    sum = wave_sum(sum);
+    if (lane == 0) a.sums[job] = make_float2(ref, sum);
+    if (lane < a.K) a.cands[(uint64_t)job * a.K + lane] = lane < n ? list[lane] : 0;
   }
   mk.end(ARGUS_REGION_SELECT_ROWS);
 }
@@ -201,10 +227,10 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
     const bool done = a.finished && a.finished[row];
     float top = -INFINITY, sum = 0.0f;
     if (!done) {
-      for (uint32_t c = lane; c < a.chunks; c += 64) top = fmaxf(top, a.sums[(uint64_t)row * a.chunks + c].x);
+      for (uint32_t c = lane; c < a.parts; c += 64) top = fmaxf(top, a.sums[(uint64_t)row * a.parts + c].x);
       top = wave_max(top);
-      for (uint32_t c = lane; c < a.chunks; c += 64) {
-        const float2 v = a.sums[(uint64_t)row * a.chunks + c];
+      for (uint32_t c = lane; c < a.parts; c += 64) {
+        const float2 v = a.sums[(uint64_t)row * a.parts + c];
         sum += v.x == -INFINITY ? v.y : v.y * exp2f((v.x - top) * kLog2e);
       }
       sum = wave_sum(sum);
@@ -218,18 +244,19 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
   if (tid < a.lists) s_list[tid] = 0;
   if (tid == 0) s_n = 0;
   __syncthreads();
-  const uint32_t per_row = a.chunks * a.K, total = a.W * per_row;
+  // Candidate i: the i / parts-th of the list of part i % parts (of the whole
+  // group), so that each set of threads has candidates of all ranks.
+  const uint32_t parts = a.W * a.parts, total = parts * a.K;
   const uint64_t* cands = a.cands + (uint64_t)group * total;
-  // Candidate i of the group; false: none.
-  auto pick_of = [&](uint32_t i, Pick* p) {
-    const uint32_t w = i / per_row, r = i % per_row;
+  auto pick_of = [&](uint32_t i, Pick* p) {  // false: none
+    const uint32_t r = i / parts, j = i - r * parts, w = j / a.parts;
     float score;
     if (s_done[w]) {
-      if (r != 0) return false;
+      if (r != 0 || j != w * a.parts) return false;
       p->key = 0;
       score = s_score[w];
     } else {
-      p->key = cands[i];
+      p->key = cands[(uint64_t)j * a.K + r];
       if (p->key == 0) return false;
       score = s_score[w] + (value_of((uint32_t)(p->key >> 32)) - s_lse[w]);
     }
@@ -313,9 +340,12 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
 }
 
 struct Plan {
-  uint32_t chunks;
+  uint32_t parts, steps;
   size_t cands_at, bytes;
 };
+
+// Waves that read the logits, all resident at once where there are so many steps.
+constexpr uint32_t kRowWaves = 256 * 4 * 6;
 
 int make_plan(const argus_select_config* c, Plan* p) {
   if (!c) return refuse(ARGUS_E_INVAL, "no configuration");
@@ -324,14 +354,18 @@ int make_plan(const argus_select_config* c, Plan* p) {
   if (c->beams < 1 || c->beams > kMaxBeams || c->k < 1 || c->k > kMaxK)
     return refuse(ARGUS_E_INVAL, "beams %u, k %u (1..64)", c->beams, c->k);
   if (c->vocab < 1 || c->vocab > (1u << 24)) return refuse(ARGUS_E_INVAL, "vocab %u (1..2^24)", c->vocab);
-  // a row may start anywhere on 16 bytes: up to 15 bytes before its chunks
+  if (c->groups > (1u << 20)) return refuse(ARGUS_E_CAPACITY, "groups %u", c->groups);
+  // a row may start anywhere on 16 bytes: up to 15 bytes before its steps
   const uint32_t lead = c->type == ARGUS_FP32 ? 3u : 7u;
-  p->chunks = (c->vocab + lead + kChunkElems - 1) / kChunkElems;
-  const uint64_t parts = (uint64_t)c->groups * c->beams * p->chunks;
-  if (c->groups > (1u << 20) || parts > 0x7FFFFFFFull || (uint64_t)c->beams * p->chunks * c->k > 0x7FFFFFFFull)
-    return refuse(ARGUS_E_CAPACITY, "groups x beams x vocab");
-  p->cands_at = up256(parts * sizeof(float2));
-  p->bytes = p->cands_at + up256(parts * c->k * sizeof(uint64_t));
+  const uint64_t rows = (uint64_t)c->groups * c->beams;
+  const uint32_t steps = (c->vocab + lead + kStep - 1) / kStep;
+  const uint64_t parts = rows ? kRowWaves / rows : 1;
+  p->parts = parts < 1 ? 1u : parts < steps ? (uint32_t)parts : steps;
+  p->steps = (steps + p->parts - 1) / p->parts;
+  p->parts = (steps + p->steps - 1) / p->steps;
+  const uint64_t jobs = rows * p->parts;
+  p->cands_at = up256(jobs * sizeof(float2));
+  p->bytes = p->cands_at + up256(jobs * c->k * sizeof(uint64_t));
   return ARGUS_OK;
 }
 
@@ -369,7 +403,7 @@ extern "C" int argus_decode_select(const argus_select_config* cfg, const argus_s
   if (!d_workspace && cfg->groups) return refuse(ARGUS_E_INVAL, "no workspace");
   if (!aligned_to(d_workspace, 256)) return refuse(ARGUS_E_ALIGN, "the workspace lies on 256 bytes");
   if (workspace_bytes < p.bytes) return refuse(ARGUS_E_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
-  const uint32_t grid = cfg->groups * cfg->beams * p.chunks;
+  const uint32_t grid = (cfg->groups * cfg->beams * p.parts + kWaves - 1) / kWaves;
   if (!marks_fit(markers, ((uint64_t)grid + cfg->groups) * kWaves * 2))
     return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
   if (cfg->groups == 0) return ARGUS_OK;
@@ -381,7 +415,8 @@ extern "C" int argus_decode_select(const argus_select_config* cfg, const argus_s
   a.new_scores = io->d_new_scores, a.parents = io->d_parents, a.tokens = io->d_tokens, a.new_finished = io->d_new_finished;
   a.sums = (float2*)d_workspace;
   a.cands = (uint64_t*)((char*)d_workspace + p.cands_at);
-  a.W = cfg->beams, a.V = cfg->vocab, a.K = cfg->k, a.chunks = p.chunks, a.eos = cfg->eos;
+  a.W = cfg->beams, a.V = cfg->vocab, a.K = cfg->k, a.parts = p.parts, a.eos = cfg->eos;
+  a.steps = p.steps, a.rows = cfg->groups * cfg->beams;
   a.lists = 1;
   while (a.lists < a.K) a.lists <<= 1;
   hipStream_t st = (hipStream_t)stream_v;
