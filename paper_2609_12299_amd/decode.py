@@ -14,7 +14,6 @@ from .attr import ABI_VERSION, ArgusError, load_library
 
 BF16, FP16, FP32, FP8 = 0, 1, 2, 3
 MAX_CACHES = 4
-NUM_COUNTERS_STEP = 8
 STEP_COUNTER_NAMES = ["needed", "short", "copied", "live", "bad_parents", "cut"]
 COMPACT_COUNTER_NAMES = ["live", "moved"]
 REGION_NAMES = ["attend", "attend.place", "attend.tokens", "attend.join", "append", "step.clear",
@@ -164,77 +163,83 @@ def argus_decode_select(cfg, io, d_workspace, workspace_bytes, markers, stream) 
 
 
 # ------------------------------------------------------------ torch wrappers
+#
+# A decode step's calls are short: the checks below cost one comparison each, and
+# messages are put together only where one fails.
 
 _torch = None
 _types = {}
+_raw_stream = None
 
 
 def _t():
-    global _torch
+    global _torch, _raw_stream
     if _torch is None:
         import torch
         _types.update({torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32,
                        torch.float8_e4m3fn: FP8})
+        # (the handle alone: a tenth of the time of a stream object)
+        _raw_stream = torch._C._cuda_getCurrentRawStream
         _torch = torch
     return _torch
 
 
-def _need(ok: bool, why: str) -> None:
-    if not ok:
-        raise ArgusError(-1, why)
+def _bad(why: str):
+    raise ArgusError(-1, why)
 
 
 def _type(x, allowed, name: str) -> int:
     got = _types.get(x.dtype)
-    _need(got in allowed, f"{name}: type {x.dtype}")
+    if got not in allowed:
+        _bad(f"{name}: type {x.dtype}")
     return got
 
 
 def _ints(x, shape, name: str, dev) -> int:
     """Address of a dense int32 tensor of this shape on this device."""
-    t = _torch
-    _need(x.dtype == t.int32 and x.shape == shape and x.device == dev and x.is_contiguous(),
-          f"{name}: int32 {tuple(shape)}, dense, on {dev}; got {x.dtype} {tuple(x.shape)} on {x.device}")
+    if not (x.dtype == _torch.int32 and x.shape == shape and x.device == dev and x.is_contiguous()):
+        _bad(f"{name}: int32 {tuple(shape)}, dense, on {dev}; got {x.dtype} {tuple(x.shape)} on {x.device}")
     return x.data_ptr()
 
 
 def _table(x, name: str, dev):
-    _need(x.dtype == _torch.int32 and x.dim() == 2 and x.device == dev and (x.stride(1) == 1 or x.shape[1] == 1),
-          f"{name}: int32 [sequences, columns] with contiguous rows on {dev}")
+    if not (x.dtype == _torch.int32 and x.dim() == 2 and x.device == dev and (x.stride(1) == 1 or x.shape[1] == 1)):
+        _bad(f"{name}: int32 [sequences, columns] with contiguous rows on {dev}")
     return x.data_ptr(), x.stride(0)
 
 
 def _scales(x, heads: int, name: str, dev):
     if x is None:
         return None
-    _need(x.dtype == _torch.float32 and x.shape == (heads,) and x.device == dev and x.is_contiguous(),
-          f"{name}: float32 [{heads}], dense, on {dev}")
+    if not (x.dtype == _torch.float32 and x.shape == (heads,) and x.device == dev and x.is_contiguous()):
+        _bad(f"{name}: float32 [{heads}], dense, on {dev}")
     return x.data_ptr()
 
 
 def _view(c, name: str, dev) -> argus_page_view:
-    _need(c.dim() == 4 and c.device == dev and (c.stride(3) == 1 or c.shape[3] == 1),
-          f"{name}: [pages, kv_heads, page_size, head_dim] with contiguous rows on {dev}")
     st = c.stride()
+    if not (len(st) == 4 and c.device == dev and (st[3] == 1 or c.shape[3] == 1)):
+        _bad(f"{name}: [pages, kv_heads, page_size, head_dim] with contiguous rows on {dev}")
     return argus_page_view(c.data_ptr(), st[0], st[1], st[2])
 
 
-def _planes(caches, num_pages: int, dev):
-    _need(len(caches) <= MAX_CACHES, f"at most {MAX_CACHES} caches")
-    out = (argus_page_planes * MAX_CACHES)()
+def _planes(caches, num_pages: int, dev, out) -> None:
+    if len(caches) > MAX_CACHES:
+        _bad(f"at most {MAX_CACHES} caches")
     for i, c in enumerate(caches):
-        _need(c.device == dev and c.dim() >= 3 and c.shape[1] == num_pages,
-              f"caches[{i}]: [layers, {num_pages} pages, ...] on {dev}")
-        e = c.element_size()
-        one = c[0, 0] if c.shape[0] else c
+        st, shape, e = c.stride(), c.shape, c.element_size()
+        if not (c.device == dev and len(shape) >= 3 and shape[1] == num_pages):
+            _bad(f"caches[{i}]: [layers, {num_pages} pages, ...] on {dev}")
         # a page is one run of memory, in whatever order its dimensions lie
         run = 1
-        for st, n in sorted(zip(one.stride(), one.shape)):
+        for step, n in sorted(zip(st[2:], shape[2:])):
             if n != 1:
-                _need(st == run, f"caches[{i}]: a page's elements do not lie in one run of memory")
+                if step != run:
+                    _bad(f"caches[{i}]: a page's elements do not lie in one run of memory")
                 run *= n
-        out[i] = argus_page_planes(c.data_ptr(), c.stride(0) * e, c.stride(1) * e, c.shape[0], run * e)
-    return out
+        p = out[i]
+        p.base, p.plane_stride, p.page_stride = c.data_ptr(), st[0] * e, st[1] * e
+        p.planes, p.page_bytes = shape[0], run * e
 
 
 class MarkerBuffer:
@@ -260,37 +265,36 @@ class MarkerBuffer:
 
 
 class _on:
-    """The stream of a call: allocations belong to it, so that the allocator hands their memory on in
-    its order."""
+    """A call on another stream than the current one, or on another device: allocations belong to
+    that stream, so that the allocator hands their memory on in its order."""
 
     def __init__(self, stream, dev):
-        self.dev, self.stream, self.ctx = dev, stream, None
+        t = _torch
+        self.ctx = t.cuda.stream(stream) if stream is not None else t.cuda.device(dev)
 
     def __enter__(self):
-        t = _torch
-        cur = t.cuda.current_stream(self.dev)
-        if self.stream is not None and self.stream != cur:
-            self.ctx = t.cuda.stream(self.stream)
-            self.ctx.__enter__()
-            cur = self.stream
-        elif self.dev.index is not None and self.dev.index != t.cuda.current_device():
-            self.ctx = t.cuda.device(self.dev)
-            self.ctx.__enter__()
-        return cur.cuda_stream
+        return self.ctx.__enter__()
 
     def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
+        return self.ctx.__exit__(*exc)
+
+
+def _elsewhere(stream, dev) -> bool:
+    """Whether the call leaves the current stream or device."""
+    return stream is not None or dev.index != _torch.cuda.current_device()
 
 
 def _workspace(need: int, dev):
-    """(tensor, address): 256-byte aligned, as the allocator's blocks are."""
-    if need == (1 << 64) - 1:
+    """(tensor, address on 256 bytes)"""
+    if need == _NO_SIZE:
         raise ArgusError(-1, argus_decode_last_error())
     if need == 0:
         return None, None
     ws = _torch.empty(need + 256, dtype=_torch.uint8, device=dev)
     return ws, (ws.data_ptr() + 255) & ~255
+
+
+_NO_SIZE = (1 << 64) - 1
 
 
 def _done(rc: int, call: str) -> None:
@@ -317,36 +321,45 @@ def attend_pages(q, k_cache, v_cache, table, lens, scale: float | None = None, w
     nothing answers zeros and -inf."""
     t = _t()
     dev = q.device
-    _need(q.dim() == 3 and (q.stride(2) == 1 or q.shape[2] == 1), "q: [seqs, heads, head_dim], contiguous rows")
+    if _elsewhere(stream, dev):
+        with _on(stream, dev):
+            return attend_pages(q, k_cache, v_cache, table, lens, scale, window, sinks, k_scale, v_scale, lse,
+                                out, markers)
+    qs = q.stride()
+    if not (len(qs) == 3 and (qs[2] == 1 or q.shape[2] == 1)):
+        _bad("q: [seqs, heads, head_dim], contiguous rows")
     S, heads, D = q.shape
     qt = _type(q, (BF16, FP16), "q")
     ct = _type(k_cache, (qt, FP8), "k_cache")
     k, v = _view(k_cache, "k_cache", dev), _view(v_cache, "v_cache", dev)
-    N, H, ps, _ = k_cache.shape
-    _need(v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype and k_cache.shape[3] == D,
-          f"k_cache {tuple(k_cache.shape)} {k_cache.dtype}, v_cache {tuple(v_cache.shape)} {v_cache.dtype}, head_dim {D}")
-    _need(H > 0 and heads % H == 0, f"{heads} heads over {H} of the cache")
+    N, H, ps, kd = k_cache.shape
+    if not (v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype and kd == D):
+        _bad(f"k_cache {tuple(k_cache.shape)} {k_cache.dtype}, v_cache {tuple(v_cache.shape)} {v_cache.dtype}, head_dim {D}")
+    if H == 0 or heads % H:
+        _bad(f"{heads} heads over {H} of the cache")
     tab, tab_stride = _table(table, "table", dev)
-    _need(table.shape[0] == S, f"table of {table.shape[0]} sequences, q of {S}")
-    _need(0 <= window < 2 ** 31 and 0 <= sinks < 2 ** 31, f"window {window}, sinks {sinks}")
-    cfg = argus_attend_config(ABI_VERSION, qt, ct, S, H, heads // H if heads else 1, D, ps, N, table.shape[1],
-                              int(window), int(sinks), D ** -0.5 if scale is None else float(scale), 0)
-    with _on(stream, dev) as s:
-        if out is None:
-            out = t.empty((S, heads, D), dtype=q.dtype, device=dev)
-        else:
-            _need(out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.is_contiguous(),
-                  "out: like q, dense")
-        res = dict(out=out)
-        if lse:
-            res["lse"] = t.empty((S, heads), dtype=t.float32, device=dev)
-        need = argus_decode_attend_workspace_bytes(cfg)
-        ws, ws_ptr = _workspace(need, dev)
-        io = argus_attend_io(q.data_ptr(), q.stride(0), q.stride(1), k, v, tab, tab_stride,
-                             _ints(lens, (S,), "lens", dev), _scales(k_scale, H, "k_scale", dev),
-                             _scales(v_scale, H, "v_scale", dev), out.data_ptr(),
-                             res["lse"].data_ptr() if lse else None)
-        _done(argus_decode_attend(cfg, io, ws_ptr, need, _marks(markers), s), "argus_decode_attend")
+    tS, P = table.shape
+    if tS != S:
+        _bad(f"table of {tS} sequences, q of {S}")
+    if not (0 <= window < 2 ** 31 and 0 <= sinks < 2 ** 31):
+        _bad(f"window {window}, sinks {sinks}")
+    cfg = argus_attend_config(ABI_VERSION, qt, ct, S, H, heads // H if heads else 1, D, ps, N, P, window, sinks,
+                              D ** -0.5 if scale is None else scale, 0)
+    if out is None:
+        out = t.empty((S, heads, D), dtype=q.dtype, device=dev)
+    elif not (out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.is_contiguous()):
+        _bad("out: like q, dense")
+    res = dict(out=out)
+    l_ptr = None
+    if lse:
+        res["lse"] = t.empty((S, heads), dtype=t.float32, device=dev)
+        l_ptr = res["lse"].data_ptr()
+    need = argus_decode_attend_workspace_bytes(cfg)
+    ws, ws_ptr = _workspace(need, dev)
+    io = argus_attend_io(q.data_ptr(), qs[0], qs[1], k, v, tab, tab_stride, _ints(lens, (S,), "lens", dev),
+                         _scales(k_scale, H, "k_scale", dev), _scales(v_scale, H, "v_scale", dev),
+                         out.data_ptr(), l_ptr)
+    _done(argus_decode_attend(cfg, io, ws_ptr, need, _marks(markers), _raw_stream(dev.index)), "argus_decode_attend")
     return res
 
 
@@ -360,29 +373,31 @@ def append_tokens(new_k, new_v, k_cache, v_cache, table, starts, offsets=None, k
     +-448.  Row r of sequence s (offsets[s] <= r < offsets[s + 1]; without offsets one
     row per sequence) goes to position starts[s] + r - offsets[s]; rows without a held
     page are left out."""
-    t = _t()
+    _t()
     dev = k_cache.device
-    for x, name in ((new_k, "new_k"), (new_v, "new_v")):
-        _need(x.dim() == 3 and x.device == dev and (x.stride(2) == 1 or x.shape[2] == 1),
-              f"{name}: [rows, kv_heads, head_dim] with contiguous rows on {dev}")
-    st = _type(new_k, (BF16, FP16), "new_k")
-    ct = _type(k_cache, (st, FP8), "k_cache")
+    if _elsewhere(stream, dev):
+        with _on(stream, dev):
+            return append_tokens(new_k, new_v, k_cache, v_cache, table, starts, offsets, k_scale, v_scale, markers)
+    ks, vs = new_k.stride(), new_v.stride()
     k, v = _view(k_cache, "k_cache", dev), _view(v_cache, "v_cache", dev)
     N, H, ps, D = k_cache.shape
     rows = new_k.shape[0]
-    _need(v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype, "k_cache and v_cache differ")
-    _need(new_k.shape == (rows, H, D) and new_v.shape == (rows, H, D) and new_v.dtype == new_k.dtype,
-          f"new_k {tuple(new_k.shape)}, new_v {tuple(new_v.shape)} for a cache of {H} heads of {D}")
+    if not (len(ks) == len(vs) == 3 and (ks[2] == vs[2] == 1 or D == 1) and new_k.device == dev and new_v.device == dev):
+        _bad(f"new_k, new_v: [rows, kv_heads, head_dim] with contiguous rows on {dev}")
+    st = _type(new_k, (BF16, FP16), "new_k")
+    ct = _type(k_cache, (st, FP8), "k_cache")
+    if not (v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype):
+        _bad("k_cache and v_cache differ")
+    if not (new_k.shape == (rows, H, D) and new_v.shape == (rows, H, D) and new_v.dtype == new_k.dtype):
+        _bad(f"new_k {tuple(new_k.shape)}, new_v {tuple(new_v.shape)} for a cache of {H} heads of {D}")
     tab, tab_stride = _table(table, "table", dev)
-    S = table.shape[0]
-    cfg = argus_append_config(ABI_VERSION, st, ct, S, H, D, ps, N, table.shape[1], rows)
-    ks, vs = new_k.stride(), new_v.stride()
+    S, P = table.shape
+    cfg = argus_append_config(ABI_VERSION, st, ct, S, H, D, ps, N, P, rows)
     io = argus_append_io(new_k.data_ptr(), new_v.data_ptr(), ks[0], ks[1], vs[0], vs[1], k, v, tab,
                          tab_stride, _ints(starts, (S,), "starts", dev),
                          None if offsets is None else _ints(offsets, (S + 1,), "offsets", dev),
                          _scales(k_scale, H, "k_scale", dev), _scales(v_scale, H, "v_scale", dev))
-    with _on(stream, dev) as s:
-        _done(argus_decode_append(cfg, io, _marks(markers), s), "argus_decode_append")
+    _done(argus_decode_append(cfg, io, _marks(markers), _raw_stream(dev.index)), "argus_decode_append")
 
 
 def step_pages(table, lens, parents, grow, page_size: int, held=None, num_pages: int | None = None,
@@ -399,29 +414,34 @@ def step_pages(table, lens, parents, grow, page_size: int, held=None, num_pages:
     counters [8] (STEP_COUNTER_NAMES), int32; an entry without a page is -1."""
     t = _t()
     dev = table.device
+    if _elsewhere(stream, dev):
+        with _on(stream, dev):
+            return step_pages(table, lens, parents, grow, page_size, held, num_pages, caches, window, sinks, markers)
     if num_pages is None:
-        _need(held is not None or len(caches) > 0, "num_pages, held or a cache gives the number of pages")
+        if held is None and len(caches) == 0:
+            _bad("num_pages, held or a cache gives the number of pages")
         num_pages = held.shape[0] if held is not None else caches[0].shape[1]
-    N = int(num_pages)
+    N = num_pages
     tab, tab_stride = _table(table, "table", dev)
     S0, P = table.shape
     S = S0 if parents is None else parents.shape[0]
-    _need(0 <= window < 2 ** 31 and 0 <= sinks < 2 ** 31, f"window {window}, sinks {sinks}")
-    _need(1 <= N <= 2 ** 28 and 0 < page_size <= 65536, f"num_pages {N}, page_size {page_size}")
-    cfg = argus_step_config(ABI_VERSION, S0, S, P, N, int(page_size), int(window), int(sinks), len(caches), 0)
-    with _on(stream, dev) as s:
-        out = dict(table=t.empty((S, P), dtype=t.int32, device=dev), lens=t.empty(S, dtype=t.int32, device=dev),
-                   refs=t.empty(N, dtype=t.int32, device=dev),
-                   counters=t.empty(NUM_COUNTERS_STEP, dtype=t.int32, device=dev))
-        io = argus_step_io(tab, tab_stride, _ints(lens, (S0,), "lens", dev),
-                           None if parents is None else _ints(parents, (S,), "parents", dev),
-                           None if grow is None else _ints(grow, (S,), "grow", dev),
-                           None if held is None else _ints(held, (N,), "held", dev),
-                           out["table"].data_ptr(), out["lens"].data_ptr(), out["refs"].data_ptr(),
-                           out["counters"].data_ptr(), _planes(caches, N, dev))
-        need = argus_decode_step_workspace_bytes(S, N)
-        ws, ws_ptr = _workspace(need, dev)
-        _done(argus_decode_step(cfg, io, ws_ptr, need, _marks(markers), s), "argus_decode_step")
+    if not (0 <= window < 2 ** 31 and 0 <= sinks < 2 ** 31 and 1 <= N <= 2 ** 28 and 0 < page_size <= 65536):
+        _bad(f"window {window}, sinks {sinks}, num_pages {N}, page_size {page_size}")
+    cfg = argus_step_config(ABI_VERSION, S0, S, P, N, page_size, window, sinks, len(caches), 0)
+    i32 = t.int32
+    out = dict(table=t.empty((S, P), dtype=i32, device=dev), lens=t.empty(S, dtype=i32, device=dev),
+               refs=t.empty(N, dtype=i32, device=dev), counters=t.empty(8, dtype=i32, device=dev))
+    io = argus_step_io(tab, tab_stride, _ints(lens, (S0,), "lens", dev),
+                       None if parents is None else _ints(parents, (S,), "parents", dev),
+                       None if grow is None else _ints(grow, (S,), "grow", dev),
+                       None if held is None else _ints(held, (N,), "held", dev),
+                       out["table"].data_ptr(), out["lens"].data_ptr(), out["refs"].data_ptr(),
+                       out["counters"].data_ptr())
+    if caches:
+        _planes(caches, N, dev, io.caches)
+    need = argus_decode_step_workspace_bytes(S, N)
+    ws, ws_ptr = _workspace(need, dev)
+    _done(argus_decode_step(cfg, io, ws_ptr, need, _marks(markers), _raw_stream(dev.index)), "argus_decode_step")
     return out
 
 
@@ -431,20 +451,25 @@ def compact_pages(table, refs, caches=(), markers=None, stream=None) -> dict:
     -1 for a free one) and counters (COMPACT_COUNTER_NAMES)."""
     t = _t()
     dev = table.device
+    if _elsewhere(stream, dev):
+        with _on(stream, dev):
+            return compact_pages(table, refs, caches, markers)
     tab, tab_stride = _table(table, "table", dev)
     S, P = table.shape
     N = refs.shape[0]
-    _need(1 <= N <= 2 ** 28, f"{N} pages")
+    if not 1 <= N <= 2 ** 28:
+        _bad(f"{N} pages")
     cfg = argus_compact_config(ABI_VERSION, S, P, N, len(caches), 0)
-    with _on(stream, dev) as s:
-        out = dict(table=t.empty((S, P), dtype=t.int32, device=dev), refs=t.empty(N, dtype=t.int32, device=dev),
-                   map=t.empty(N, dtype=t.int32, device=dev), counters=t.empty(8, dtype=t.int32, device=dev))
-        io = argus_compact_io(tab, tab_stride, _ints(refs, (N,), "refs", dev), out["table"].data_ptr(),
-                              out["refs"].data_ptr(), out["map"].data_ptr(), out["counters"].data_ptr(),
-                              _planes(caches, N, dev))
-        need = argus_decode_compact_workspace_bytes(N)
-        ws, ws_ptr = _workspace(need, dev)
-        _done(argus_decode_compact(cfg, io, ws_ptr, need, _marks(markers), s), "argus_decode_compact")
+    i32 = t.int32
+    out = dict(table=t.empty((S, P), dtype=i32, device=dev), refs=t.empty(N, dtype=i32, device=dev),
+               map=t.empty(N, dtype=i32, device=dev), counters=t.empty(8, dtype=i32, device=dev))
+    io = argus_compact_io(tab, tab_stride, _ints(refs, (N,), "refs", dev), out["table"].data_ptr(),
+                          out["refs"].data_ptr(), out["map"].data_ptr(), out["counters"].data_ptr())
+    if caches:
+        _planes(caches, N, dev, io.caches)
+    need = argus_decode_compact_workspace_bytes(N)
+    ws, ws_ptr = _workspace(need, dev)
+    _done(argus_decode_compact(cfg, io, ws_ptr, need, _marks(markers), _raw_stream(dev.index)), "argus_decode_compact")
     return out
 
 
@@ -459,25 +484,31 @@ def select_beams(logits, scores, k: int, finished=None, eos: int = -1, markers=N
     -1, False."""
     t = _t()
     dev = logits.device
+    if _elsewhere(stream, dev):
+        with _on(stream, dev):
+            return select_beams(logits, scores, k, finished, eos, markers)
     lt = _type(logits, (BF16, FP16, FP32), "logits")
-    _need(logits.dim() == 3 and (logits.stride(2) == 1 or logits.shape[2] == 1),
-          "logits: [groups, beams, vocab], contiguous rows")
+    ls = logits.stride()
+    if not (len(ls) == 3 and (ls[2] == 1 or logits.shape[2] == 1)):
+        _bad("logits: [groups, beams, vocab], contiguous rows")
     G, W, V = logits.shape
-    _need(scores.dtype == t.float32 and scores.shape == (G, W) and scores.device == dev and scores.is_contiguous(),
-          f"scores: float32 {(G, W)}, dense, on {dev}")
+    if not (scores.dtype == t.float32 and scores.shape == (G, W) and scores.device == dev and scores.is_contiguous()):
+        _bad(f"scores: float32 {(G, W)}, dense, on {dev}")
+    done = None
     if finished is not None:
-        _need(finished.dtype in (t.bool, t.uint8) and finished.shape == (G, W) and finished.device == dev
-              and finished.is_contiguous(), f"finished: bool {(G, W)}, dense, on {dev}")
-    _need(0 < k <= 64, f"k {k} (1..64)")
-    _need(-2 ** 31 <= eos < 2 ** 31, f"eos {eos}")
-    cfg = argus_select_config(ABI_VERSION, lt, G, W, V, int(k), int(eos), 0)
-    with _on(stream, dev) as s:
-        out = dict(scores=t.empty((G, k), dtype=t.float32, device=dev), parents=t.empty((G, k), dtype=t.int32, device=dev),
-                   tokens=t.empty((G, k), dtype=t.int32, device=dev), finished=t.empty((G, k), dtype=t.bool, device=dev))
-        io = argus_select_io(logits.data_ptr(), logits.stride(0), logits.stride(1), scores.data_ptr(),
-                             None if finished is None else finished.data_ptr(), out["scores"].data_ptr(),
-                             out["parents"].data_ptr(), out["tokens"].data_ptr(), out["finished"].data_ptr())
-        need = argus_decode_select_workspace_bytes(cfg)
-        ws, ws_ptr = _workspace(need, dev)
-        _done(argus_decode_select(cfg, io, ws_ptr, need, _marks(markers), s), "argus_decode_select")
+        if not (finished.dtype in (t.bool, t.uint8) and finished.shape == (G, W) and finished.device == dev
+                and finished.is_contiguous()):
+            _bad(f"finished: bool {(G, W)}, dense, on {dev}")
+        done = finished.data_ptr()
+    if not (0 < k <= 64 and -2 ** 31 <= eos < 2 ** 31):
+        _bad(f"k {k} (1..64), eos {eos}")
+    cfg = argus_select_config(ABI_VERSION, lt, G, W, V, k, eos, 0)
+    shape = (G, k)
+    out = dict(scores=t.empty(shape, dtype=t.float32, device=dev), parents=t.empty(shape, dtype=t.int32, device=dev),
+               tokens=t.empty(shape, dtype=t.int32, device=dev), finished=t.empty(shape, dtype=t.bool, device=dev))
+    io = argus_select_io(logits.data_ptr(), ls[0], ls[1], scores.data_ptr(), done, out["scores"].data_ptr(),
+                         out["parents"].data_ptr(), out["tokens"].data_ptr(), out["finished"].data_ptr())
+    need = argus_decode_select_workspace_bytes(cfg)
+    ws, ws_ptr = _workspace(need, dev)
+    _done(argus_decode_select(cfg, io, ws_ptr, need, _marks(markers), _raw_stream(dev.index)), "argus_decode_select")
     return out
