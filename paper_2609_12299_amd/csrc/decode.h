@@ -12,7 +12,7 @@
 namespace argus {
 namespace decode {
 
-constexpr int kThreads = 256;  // of every kernel of these operators
+constexpr int kThreads = 256;  // of a block, where nothing else is said
 constexpr int kWaves = kThreads / 64;
 
 // ---------------------------------------------------------------- markers
@@ -29,7 +29,7 @@ struct WaveMarks {
   uint32_t ctx = 0, region = 0;
   ARGUS_DEV WaveMarks(const Marks& m) {
     if (m.rec) {
-      const uint32_t wave = __builtin_amdgcn_readfirstlane((blockIdx.y * gridDim.x + blockIdx.x) * kWaves + threadIdx.x / 64);
+      const uint32_t wave = __builtin_amdgcn_readfirstlane((blockIdx.y * gridDim.x + blockIdx.x) * (blockDim.x / 64) + threadIdx.x / 64);
       at = m.rec + (uint64_t)wave * m.per_wave;
       ctx = m.ctx + wave;
       region = m.region;

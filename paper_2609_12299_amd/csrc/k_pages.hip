@@ -174,6 +174,7 @@ struct StepArgs {
   int32_t *new_table, *new_lens, *refs, *counters;
   uint64_t* best;      // [pages] of the sequences that have the page last: (length + 1) << 32 | ~sequence
   uint32_t* lasts;     // [pages] how many they are
+  int2* ends;          // [S] page that the sequence would write on (-1: none), pages that it grows by
   uint32_t* base;      // [S] fresh pages before the sequence's
   uint2* copies;       // [S] page, rank of the fresh page
   uint32_t* free_list; // [pages]
@@ -187,6 +188,59 @@ struct StepArgs {
 };
 
 constexpr uint32_t kPageTile = 4096;
+constexpr uint32_t kPageItems = 16;  // pages of a thread
+static_assert(kPageItems * kThreads == kPageTile, "a tile per block");
+// Calls of at most so many table entries and pages are planned by one block of
+// kSmallThreads: two launches instead of four (16 beams of 64 columns over 1024
+// pages: 21 us a call against 28; 512 x 256 entries over 16384 pages by one block:
+// 95 us against 31).
+constexpr uint32_t kSmallEntries = 16384, kSmallPages = 16384;
+constexpr uint32_t kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
+
+// Bit i: page p0 + i is in the pool and has (LIVE) or has not any reference.
+// AGENT: the counts were changed by atomics of this kernel, which do not pass the L1.
+template <bool LIVE, bool AGENT>
+ARGUS_DEV uint32_t page_flags(const int32_t* refs, uint32_t p0, uint32_t N) {
+  int32_t v[kPageItems];
+  if (!AGENT && p0 + kPageItems <= N && ((uintptr_t)refs & 15u) == 0) {
+#pragma unroll
+    for (uint32_t i = 0; i < kPageItems; i += 4) {
+      const int4 q = *reinterpret_cast<const int4*>(refs + p0 + i);
+      v[i] = q.x, v[i + 1] = q.y, v[i + 2] = q.z, v[i + 3] = q.w;
+    }
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < kPageItems; ++i) {
+      const bool in = p0 + i < N;
+      const uint32_t* at = (const uint32_t*)refs + (in ? p0 + i : 0);
+      const int32_t x = AGENT ? (int32_t)ld_agent(at) : (int32_t)*at;
+      v[i] = in ? x : (LIVE ? 0 : 1);
+    }
+  }
+  uint32_t flags = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < kPageItems; ++i) flags |= (LIVE ? v[i] > 0 : v[i] == 0) ? 1u << i : 0u;
+  return flags;
+}
+
+// Exclusive prefix of v over the block and, in *total, the block's sum.
+template <uint32_t WAVES>
+ARGUS_DEV uint32_t block_scan(uint32_t v, uint32_t* s_wave, uint32_t* total) {
+  const uint32_t lane = lane_id(), wave = threadIdx.x >> 6;
+  const uint32_t incl = (uint32_t)wave_incl_scan32((int32_t)v);
+  __syncthreads();
+  if (lane == 63) s_wave[wave] = incl;
+  __syncthreads();
+  uint32_t at = incl - v, all = 0;
+#pragma unroll
+  for (uint32_t w = 0; w < WAVES; ++w) {
+    const uint32_t x = s_wave[w];
+    at += w < wave ? x : 0u;
+    all += x;
+  }
+  *total = all;
+  return at;
+}
 
 struct Row {
   uint32_t src, len, grown, used, need;  // old sequence, old and new length, old pages, new pages
@@ -225,18 +279,132 @@ ARGUS_DEV int32_t entry_of(const StepArgs& a, const Row& r, uint32_t col) {
 
 ARGUS_DEV bool ends_inside(const StepArgs& a, const Row& r) { return (r.len & ((1u << a.shift) - 1)) != 0; }
 
+ARGUS_DEV void clear_page(const StepArgs& a, uint32_t p) {
+  const int32_t h = a.held ? a.held[p] : 0;
+  a.refs[p] = h < 0 ? 0 : h;
+  a.best[p] = 0;
+  a.lasts[p] = 0;
+}
+
+// The entries that sequence s takes over, by `lanes` threads from c0 on.
+ARGUS_DEV void claim_row(const StepArgs& a, uint32_t s, uint32_t c0, uint32_t lanes) {
+  const Row r = row_of(a, s);
+  const bool inside = ends_inside(a, r);
+  int32_t end = -1;
+  for (uint32_t c = c0; c < a.P; c += lanes) {
+    const int32_t e = entry_of(a, r, c);
+    a.new_table[(int64_t)s * a.P + c] = e;
+    const bool last = c + 1 == r.used && inside;
+    if (e >= 0) {
+      atomicAdd(&a.refs[e], 1);
+      if (last) {
+        atomicMax((unsigned long long*)&a.best[e], (unsigned long long)(r.len + 1) << 32 | (0xFFFFFFFFu - s));
+        atomicAdd(&a.lasts[e], 1u);
+      }
+    }
+    if (c + 1 == r.used) end = last && r.grown > r.len ? e : -1;
+    if (c + 1 == r.used || (r.used == 0 && c == 0)) a.ends[s] = make_int2(end, (int32_t)(r.need - r.used));
+  }
+  if (c0 == 0) {
+    a.new_lens[s] = (int32_t)r.grown;
+    if (r.bad) atomicAdd(&a.counters[ARGUS_ST_BAD_PARENT], 1);
+    if (r.cut) atomicAdd(&a.counters[ARGUS_ST_CUT], 1);
+  }
+}
+
+// Whether sequence s may write on in page e, which it has last.
+ARGUS_DEV bool writes_on(const StepArgs& a, uint32_t s, int32_t e) {
+  const uint32_t refs = ld_agent((const uint32_t*)&a.refs[e]), lasts = ld_agent(&a.lasts[e]);
+  const uint64_t best = ld_agent(&a.best[e]);
+  return (a.held == nullptr || a.held[e] <= 0) && lasts == refs && (uint32_t)best == 0xFFFFFFFFu - s;
+}
+
+// Fresh pages that the sequences before each one take, by one block.
+template <uint32_t THREADS>
+ARGUS_DEV void plan_rows(const StepArgs& a, uint32_t* s_wave) {
+  constexpr uint32_t kRows = 4;  // of a thread
+  uint32_t pages = 0, copies = 0;  // before
+  for (uint32_t s0 = 0; s0 < a.S; s0 += THREADS * kRows) {
+    int2 e[kRows];
+    uint32_t need[kRows], n = 0, nc = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kRows; ++i) {
+      const uint32_t s = s0 + threadIdx.x * kRows + i;
+      e[i] = s < a.S ? a.ends[s] : make_int2(-1, 0);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kRows; ++i) {
+      if (e[i].x >= 0 && writes_on(a, s0 + threadIdx.x * kRows + i, e[i].x)) e[i].x = -1;
+      need[i] = (uint32_t)e[i].y + (e[i].x >= 0);
+      n += need[i];
+      nc += e[i].x >= 0;
+    }
+    uint32_t total, total_c;
+    uint32_t at = pages + block_scan<THREADS / 64>(n, s_wave, &total);
+    uint32_t at_c = copies + block_scan<THREADS / 64>(nc, s_wave, &total_c);
+    pages += total;
+    copies += total_c;
+#pragma unroll
+    for (uint32_t i = 0; i < kRows; ++i) {
+      const uint32_t s = s0 + threadIdx.x * kRows + i;
+      if (s < a.S) a.base[s] = at | (e[i].x >= 0 ? 0x80000000u : 0u);
+      if (e[i].x >= 0) a.copies[at_c++] = make_uint2((uint32_t)e[i].x, at);
+      at += need[i];
+    }
+  }
+  if (threadIdx.x == 0) {
+    a.state[2] = pages;
+    a.state[3] = copies;
+  }
+}
+
+// Fresh pages into the table of sequence s, by `lanes` threads from c0 on.
+ARGUS_DEV void place_row(const StepArgs& a, uint32_t s, uint32_t c0, uint32_t lanes, uint32_t n_free) {
+  const Row r = row_of(a, s);
+  const uint32_t word = a.base[s], base = word & 0x7FFFFFFFu, copy = word >> 31;
+  for (uint32_t c = r.used + c0; c < r.need; c += lanes) {
+    const uint32_t rank = base + copy + c - r.used;
+    const int32_t page = rank < n_free ? (int32_t)a.free_list[rank] : -1;
+    a.new_table[(int64_t)s * a.P + c] = page;
+    if (page >= 0) a.refs[page] = 1;
+  }
+  if (copy && c0 == 0) {
+    int32_t* at = &a.new_table[(int64_t)s * a.P + r.used - 1];
+    const int32_t page = base < n_free ? (int32_t)a.free_list[base] : -1;
+    const int32_t old = a.ends[s].x;
+    *at = page;
+    if (page >= 0) {
+      a.refs[page] = 1;
+      atomicAdd(&a.counters[ARGUS_ST_COPIED], 1);
+    }
+    if (atomicSub(&a.refs[old], 1) == 1) atomicSub(&a.counters[ARGUS_ST_LIVE], 1);
+  }
+}
+
+ARGUS_DEV void count_pages(const StepArgs& a, uint32_t n_free, uint32_t needed) {
+  a.counters[ARGUS_ST_NEEDED] = (int32_t)needed;
+  a.counters[ARGUS_ST_SHORT] = (int32_t)(needed > n_free ? needed - n_free : 0u);
+  atomicAdd(&a.counters[ARGUS_ST_LIVE], (int32_t)(a.N - n_free + (needed < n_free ? needed : n_free)));
+}
+
+ARGUS_DEV void copy_step(const StepArgs& a, uint32_t wave, uint32_t waves) {
+  const uint32_t n_free = a.state[1];
+  copy_pages(a.caches, a.state[3], wave, waves, [&](uint32_t i, uint32_t* src, uint32_t* dst) {
+    const uint2 c = a.copies[i];
+    if (c.y >= n_free) return false;
+    *src = c.x;
+    *dst = a.free_list[c.y];
+    return true;
+  });
+}
+
 __global__ __launch_bounds__(kThreads) void k_step_clear(StepArgs a) {
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_STEP_CLEAR);
   const uint32_t i0 = blockIdx.x * kThreads + threadIdx.x, step = gridDim.x * kThreads;
-  for (uint32_t p = i0; p < a.N; p += step) {
-    const int32_t h = a.held ? a.held[p] : 0;
-    a.refs[p] = h < 0 ? 0 : h;
-    a.best[p] = 0;
-    a.lasts[p] = 0;
-  }
+  for (uint32_t p = i0; p < a.N; p += step) clear_page(a, p);
   for (uint32_t p = i0; p < (a.N + kPageTile - 1) / kPageTile; p += step) a.words[p] = 0;
-  if (i0 < 8) {
+  if (i0 < ARGUS_ST_NUM_COUNTERS) {
     a.state[i0] = 0;
     a.counters[i0] = 0;
   }
@@ -248,107 +416,33 @@ __global__ __launch_bounds__(kThreads) void k_step_claim(StepArgs a) {
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_STEP_CLAIM);
   const uint32_t rows = kThreads / a.row_lanes;
-  const uint32_t s = blockIdx.x * rows + threadIdx.x / a.row_lanes, c0 = threadIdx.x % a.row_lanes;
-  if (s < a.S) {
-    const Row r = row_of(a, s);
-    for (uint32_t c = c0; c < a.P; c += a.row_lanes) {
-      const int32_t e = entry_of(a, r, c);
-      a.new_table[(int64_t)s * a.P + c] = e;
-      if (e < 0) continue;
-      atomicAdd(&a.refs[e], 1);
-      if (c + 1 == r.used && ends_inside(a, r)) {
-        atomicMax((unsigned long long*)&a.best[e], (unsigned long long)(r.len + 1) << 32 | (0xFFFFFFFFu - s));
-        atomicAdd(&a.lasts[e], 1u);
-      }
-    }
-    if (c0 == 0) {
-      a.new_lens[s] = (int32_t)r.grown;
-      if (r.bad) atomicAdd(&a.counters[ARGUS_ST_BAD_PARENT], 1);
-      if (r.cut) atomicAdd(&a.counters[ARGUS_ST_CUT], 1);
-    }
-  }
+  const uint32_t s = blockIdx.x * rows + threadIdx.x / a.row_lanes;
+  if (s < a.S) claim_row(a, s, threadIdx.x % a.row_lanes, a.row_lanes);
   mk.end(ARGUS_REGION_STEP_CLAIM);
 }
 
-// The page that the row has to copy before it grows (-1: none).
-ARGUS_DEV int32_t page_to_copy(const StepArgs& a, const Row& r, uint32_t s) {
-  if (!r.kept || r.grown == r.len || !ends_inside(a, r)) return -1;
-  const int32_t e = a.new_table[(int64_t)s * a.P + r.used - 1];
-  if (e < 0) return -1;
-  const bool mine = (a.held == nullptr || a.held[e] <= 0) && a.lasts[e] == (uint32_t)a.refs[e] &&
-                    (uint32_t)a.best[e] == 0xFFFFFFFFu - s;
-  return mine ? -1 : e;
-}
-
-// Block 0: fresh pages that the sequences before each one take, in order.
-// The others: the free pages in order, one tile of the pool after the other.
+// Block 0: the sequences' fresh pages.  The others: the free pages in order, one
+// tile of the pool after the other.
 __global__ __launch_bounds__(kThreads) void k_step_plan(StepArgs a) {
-  constexpr uint32_t kItems = kPageTile / kThreads;
-  __shared__ uint32_t s_tile;
-  __shared__ uint2 s_wave[kWaves];
-  __shared__ uint32_t s_before;
+  __shared__ uint32_t s_tile, s_before;
+  __shared__ uint32_t s_wave[kWaves];
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_STEP_PLAN);
-  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+  const uint32_t tid = threadIdx.x;
   if (blockIdx.x == 0) {
-    uint2 before = make_uint2(0, 0);  // pages, copies
-    for (uint32_t s0 = 0; s0 < a.S; s0 += kThreads) {
-      const uint32_t s = s0 + tid;
-      int32_t page = -1;
-      uint2 v = make_uint2(0, 0);
-      if (s < a.S) {
-        const Row r = row_of(a, s);
-        page = page_to_copy(a, r, s);
-        v = make_uint2(r.need - r.used + (page >= 0), page >= 0);
-      }
-      uint2 incl = v;
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t x = __shfl_up(incl.x, d), y = __shfl_up(incl.y, d);
-        if (lane >= (uint32_t)d) incl.x += x, incl.y += y;
-      }
-      if (lane == 63) s_wave[wave] = incl;
-      __syncthreads();
-      uint2 at = before;
-      for (uint32_t w = 0; w < (uint32_t)kWaves; ++w) {
-        if (w < wave) at.x += s_wave[w].x, at.y += s_wave[w].y;
-        before.x += s_wave[w].x, before.y += s_wave[w].y;
-      }
-      __syncthreads();
-      if (s < a.S) {
-        const uint32_t base = at.x + incl.x - v.x;
-        a.base[s] = base | (page >= 0 ? 0x80000000u : 0u);
-        if (page >= 0) a.copies[at.y + incl.y - 1] = make_uint2((uint32_t)page, base);
-      }
-    }
-    if (tid == 0) {
-      a.state[2] = before.x;
-      a.state[3] = before.y;
-    }
+    plan_rows<kThreads>(a, s_wave);
   } else {
     // Tiles are taken in order, so a block waits for running blocks alone.
     if (tid == 0) s_tile = atomicAdd(&a.state[0], 1u);
     __syncthreads();
-    const uint32_t tile = s_tile, p0 = tile * kPageTile + tid * kItems;
-    uint32_t free = 0;
-    for (uint32_t i = 0; i < kItems; ++i)
-      if (p0 + i < a.N && a.refs[p0 + i] == 0) free |= 1u << i;
-    const uint32_t n = (uint32_t)__popc(free);
-    uint32_t incl = n;
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t x = __shfl_up(incl, d);
-      if (lane >= (uint32_t)d) incl += x;
-    }
-    if (lane == 63) s_wave[wave].x = incl;
-    __syncthreads();
-    uint32_t at = incl - n, total = 0;
-    for (uint32_t w = 0; w < (uint32_t)kWaves; ++w) {
-      if (w < wave) at += s_wave[w].x;
-      total += s_wave[w].x;
-    }
-    if (wave == 0) {
+    const uint32_t tile = s_tile, p0 = tile * kPageTile + tid * kPageItems;
+    const uint32_t free = page_flags<false, false>(a.refs, p0, a.N);
+    uint32_t total;
+    uint32_t at = block_scan<kWaves>((uint32_t)__popc(free), s_wave, &total);
+    if (tid < 64) {
       uint64_t error = 0;
       const uint32_t before = (uint32_t)scan_lookback(a.words, tile, total, &error, 1);
-      if (lane == 0) {
+      if (tid == 0) {
         if (error) a.counters[ARGUS_ST_INTERNAL] = 1;
         s_before = before;
         if ((uint64_t)(tile + 1) * kPageTile >= a.N) a.state[1] = before + total;
@@ -356,8 +450,7 @@ __global__ __launch_bounds__(kThreads) void k_step_plan(StepArgs a) {
     }
     __syncthreads();
     at += s_before;
-    for (uint32_t i = 0; i < kItems; ++i)
-      if (free >> i & 1u) a.free_list[at++] = p0 + i;
+    for (uint32_t f = free; f; f &= f - 1) a.free_list[at++] = p0 + (uint32_t)__builtin_ctz(f);
   }
   mk.end(ARGUS_REGION_STEP_PLAN);
 }
@@ -366,47 +459,55 @@ __global__ __launch_bounds__(kThreads) void k_step_plan(StepArgs a) {
 __global__ __launch_bounds__(kThreads) void k_step_place(StepArgs a) {
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_STEP_PLACE);
-  const uint32_t n_free = a.state[1], needed = a.state[2];
   if (blockIdx.x < a.rows_blocks) {
+    const uint32_t n_free = a.state[1];
     const uint32_t rows = kThreads / a.row_lanes;
-    const uint32_t s = blockIdx.x * rows + threadIdx.x / a.row_lanes, c0 = threadIdx.x % a.row_lanes;
-    if (s < a.S) {
-      const Row r = row_of(a, s);
-      const uint32_t word = a.base[s], base = word & 0x7FFFFFFFu, copy = word >> 31;
-      for (uint32_t c = r.used + c0; c < r.need; c += a.row_lanes) {
-        const uint32_t rank = base + copy + c - r.used;
-        const int32_t page = rank < n_free ? (int32_t)a.free_list[rank] : -1;
-        a.new_table[(int64_t)s * a.P + c] = page;
-        if (page >= 0) a.refs[page] = 1;
-      }
-      if (copy && c0 == 0) {
-        int32_t* at = &a.new_table[(int64_t)s * a.P + r.used - 1];
-        const int32_t page = base < n_free ? (int32_t)a.free_list[base] : -1;
-        const int32_t old = *at;
-        *at = page;
-        if (page >= 0) {
-          a.refs[page] = 1;
-          atomicAdd(&a.counters[ARGUS_ST_COPIED], 1);
-        }
-        if (atomicSub(&a.refs[old], 1) == 1) atomicSub(&a.counters[ARGUS_ST_LIVE], 1);
-      }
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-      a.counters[ARGUS_ST_NEEDED] = (int32_t)needed;
-      a.counters[ARGUS_ST_SHORT] = (int32_t)(needed > n_free ? needed - n_free : 0u);
-      atomicAdd(&a.counters[ARGUS_ST_LIVE], (int32_t)(a.N - n_free + (needed < n_free ? needed : n_free)));
-    }
+    const uint32_t s = blockIdx.x * rows + threadIdx.x / a.row_lanes;
+    if (s < a.S) place_row(a, s, threadIdx.x % a.row_lanes, a.row_lanes, n_free);
+    if (blockIdx.x == 0 && threadIdx.x == 0) count_pages(a, n_free, a.state[2]);
   } else {
     const uint32_t wave = (blockIdx.x - a.rows_blocks) * kWaves + threadIdx.x / 64;
-    copy_pages(a.caches, a.state[3], __builtin_amdgcn_readfirstlane(wave), (gridDim.x - a.rows_blocks) * kWaves,
-               [&](uint32_t i, uint32_t* src, uint32_t* dst) {
-                 const uint2 c = a.copies[i];
-                 if (c.y >= n_free) return false;
-                 *src = c.x;
-                 *dst = a.free_list[c.y];
-                 return true;
-               });
+    copy_step(a, __builtin_amdgcn_readfirstlane(wave), (gridDim.x - a.rows_blocks) * kWaves);
   }
+  mk.end(ARGUS_REGION_STEP_PLACE);
+}
+
+// All of a small call but its copies, by one block.  What its atomics change is
+// read past the L1.
+__global__ __launch_bounds__(kSmallThreads) void k_step_small(StepArgs a) {
+  __shared__ uint32_t s_wave[kSmallWaves];
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_STEP_PLAN);
+  const uint32_t tid = threadIdx.x;
+  for (uint32_t p = tid; p < a.N; p += kSmallThreads) clear_page(a, p);
+  if (tid < ARGUS_ST_NUM_COUNTERS) a.counters[tid] = 0;
+  __syncthreads();
+  const uint32_t rows = kSmallThreads / a.row_lanes;
+  for (uint32_t s = tid / a.row_lanes; s < a.S; s += rows) claim_row(a, s, tid % a.row_lanes, a.row_lanes);
+  __syncthreads();
+  plan_rows<kSmallThreads>(a, s_wave);
+  uint32_t n_free = 0;
+  for (uint32_t p = 0; p < a.N; p += kSmallThreads * kPageItems) {
+    const uint32_t p0 = p + tid * kPageItems;
+    const uint32_t free = page_flags<false, true>(a.refs, p0, a.N);
+    uint32_t total;
+    uint32_t at = n_free + block_scan<kSmallWaves>((uint32_t)__popc(free), s_wave, &total);
+    for (uint32_t f = free; f; f &= f - 1) a.free_list[at++] = p0 + (uint32_t)__builtin_ctz(f);
+    n_free += total;
+  }
+  __syncthreads();
+  for (uint32_t s = tid / a.row_lanes; s < a.S; s += rows) place_row(a, s, tid % a.row_lanes, a.row_lanes, n_free);
+  if (tid == 0) {
+    a.state[1] = n_free;
+    count_pages(a, n_free, a.state[2]);
+  }
+  mk.end(ARGUS_REGION_STEP_PLAN);
+}
+
+__global__ __launch_bounds__(kThreads) void k_step_copy(StepArgs a) {
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_STEP_PLACE);
+  copy_step(a, __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + threadIdx.x / 64), gridDim.x * kWaves);
   mk.end(ARGUS_REGION_STEP_PLACE);
 }
 
@@ -429,51 +530,19 @@ struct CompactArgs {
 };
 
 __global__ __launch_bounds__(kThreads) void k_compact_count(CompactArgs a) {
+  __shared__ uint32_t s_wave[kWaves];
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_COMPACT_COUNT);
-  __shared__ uint32_t s_wave[kWaves];
-  uint32_t n = 0;
-  for (uint32_t i = 0; i < kPageTile; i += kThreads) {
-    const uint32_t p = blockIdx.x * kPageTile + i + threadIdx.x;
-    n += p < a.N && a.refs[p] > 0;
-  }
-  for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
-  if ((threadIdx.x & 63u) == 0) s_wave[threadIdx.x >> 6] = n;
-  __syncthreads();
-  if (threadIdx.x == 0) a.tile_live[blockIdx.x] = s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
+  uint32_t total;
+  block_scan<kWaves>((uint32_t)__popc(page_flags<true, false>(a.refs, blockIdx.x * kPageTile + threadIdx.x * kPageItems, a.N)),
+                     s_wave, &total);
+  if (threadIdx.x == 0) a.tile_live[blockIdx.x] = total;
   mk.end(ARGUS_REGION_COMPACT_COUNT);
 }
 
-__global__ __launch_bounds__(kThreads) void k_compact_plan(CompactArgs a) {
-  constexpr uint32_t kItems = kPageTile / kThreads;
-  WaveMarks mk(a.marks);
-  mk.begin(ARGUS_REGION_COMPACT_PLAN);
-  __shared__ uint2 s_wave[kWaves];
-  __shared__ uint32_t s_scan[kWaves];
-  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-  uint32_t before = 0, n = 0;
-  for (uint32_t t = tid; t < a.tiles; t += kThreads) {
-    const uint32_t v = a.tile_live[t];
-    n += v;
-    before += t < blockIdx.x ? v : 0u;
-  }
-  for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d), before += __shfl_xor(before, d);
-  if (lane == 0) s_wave[wave] = make_uint2(n, before);
-  const uint32_t p0 = blockIdx.x * kPageTile + tid * kItems;
-  uint32_t live = 0;
-  for (uint32_t i = 0; i < kItems; ++i)
-    if (p0 + i < a.N && a.refs[p0 + i] > 0) live |= 1u << i;
-  uint32_t incl = (uint32_t)__popc(live);
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t x = __shfl_up(incl, d);
-    if (lane >= (uint32_t)d) incl += x;
-  }
-  if (lane == 63) s_scan[wave] = incl;
-  __syncthreads();
-  n = s_wave[0].x + s_wave[1].x + s_wave[2].x + s_wave[3].x;
-  uint32_t rank = s_wave[0].y + s_wave[1].y + s_wave[2].y + s_wave[3].y + incl - (uint32_t)__popc(live);
-  for (uint32_t w = 0; w < wave; ++w) rank += s_scan[w];
-  for (uint32_t i = 0; i < kItems; ++i) {
+// Ranks, holes and movers of pages p0, ..., `rank` live pages before them and n in all.
+ARGUS_DEV void rank_pages(const CompactArgs& a, uint32_t p0, uint32_t live, uint32_t rank, uint32_t n) {
+  for (uint32_t i = 0; i < kPageItems; ++i) {
     const uint32_t p = p0 + i;
     if (p >= a.N) break;
     if (p == n) a.state[1] = rank;
@@ -485,12 +554,50 @@ __global__ __launch_bounds__(kThreads) void k_compact_plan(CompactArgs a) {
       a.holes[p - rank] = p;
     }
   }
+}
+
+__global__ __launch_bounds__(kThreads) void k_compact_plan(CompactArgs a) {
+  __shared__ uint32_t s_wave[kWaves];
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_COMPACT_PLAN);
+  const uint32_t tid = threadIdx.x;
+  uint32_t before = 0, n = 0;
+  for (uint32_t t = tid; t < a.tiles; t += kThreads) {
+    const uint32_t v = a.tile_live[t];
+    n += v;
+    before += t < blockIdx.x ? v : 0u;
+  }
+  const uint32_t p0 = blockIdx.x * kPageTile + tid * kPageItems;
+  const uint32_t live = page_flags<true, false>(a.refs, p0, a.N);
+  uint32_t total, all, all_before;
+  block_scan<kWaves>(n, s_wave, &all);
+  block_scan<kWaves>(before, s_wave, &all_before);
+  const uint32_t rank = all_before + block_scan<kWaves>((uint32_t)__popc(live), s_wave, &total);
+  rank_pages(a, p0, live, rank, all);
   if (blockIdx.x == 0 && tid == 0) {
+    a.state[0] = all;
+    if (all == a.N) a.state[1] = all;
+  }
+  mk.end(ARGUS_REGION_COMPACT_PLAN);
+}
+
+// Both of them for a small pool, by one block.
+__global__ __launch_bounds__(kSmallThreads) void k_compact_small(CompactArgs a) {
+  __shared__ uint32_t s_wave[kSmallWaves];
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_COMPACT_PLAN);
+  const uint32_t p0 = threadIdx.x * kPageItems;
+  const uint32_t live = page_flags<true, false>(a.refs, p0, a.N);
+  uint32_t n;
+  const uint32_t rank = block_scan<kSmallWaves>((uint32_t)__popc(live), s_wave, &n);
+  rank_pages(a, p0, live, rank, n);
+  if (threadIdx.x == 0) {
     a.state[0] = n;
     if (n == a.N) a.state[1] = n;
   }
   mk.end(ARGUS_REGION_COMPACT_PLAN);
 }
+static_assert(kSmallPages <= kSmallThreads * kPageItems, "a small pool in one round");
 
 __global__ __launch_bounds__(kThreads) void k_compact_move(CompactArgs a) {
   WaveMarks mk(a.marks);
@@ -545,7 +652,7 @@ int take_caches(const argus_page_planes* in, uint32_t n, Caches* out) {
 }
 
 struct StepLayout {
-  size_t best, lasts, base, copies, free_list, words, state, bytes;
+  size_t best, lasts, ends, base, copies, free_list, words, state, bytes;
 };
 StepLayout step_layout(uint32_t S, uint32_t N) {
   StepLayout l{};
@@ -558,6 +665,7 @@ StepLayout step_layout(uint32_t S, uint32_t N) {
   l.best = take(8ull * N);
   l.lasts = take(4ull * N);
   l.free_list = take(4ull * N);
+  l.ends = take(8ull * S);
   l.base = take(4ull * S);
   l.copies = take(8ull * S);
   l.words = take(8ull * ((N + kPageTile - 1) / kPageTile));
@@ -690,7 +798,7 @@ extern "C" int argus_decode_step(const argus_step_config* cfg, const argus_step_
   a.table = io->d_table, a.table_stride = io->table_stride, a.lens = io->d_lens, a.parents = io->d_parents;
   a.grow = io->d_grow, a.held = io->d_held, a.new_table = io->d_new_table, a.new_lens = io->d_new_lens;
   a.refs = io->d_refs, a.counters = io->d_counters;
-  a.best = (uint64_t*)(ws + l.best), a.lasts = (uint32_t*)(ws + l.lasts), a.base = (uint32_t*)(ws + l.base);
+  a.best = (uint64_t*)(ws + l.best), a.lasts = (uint32_t*)(ws + l.lasts), a.ends = (int2*)(ws + l.ends), a.base = (uint32_t*)(ws + l.base);
   a.copies = (uint2*)(ws + l.copies), a.free_list = (uint32_t*)(ws + l.free_list), a.words = (uint64_t*)(ws + l.words);
   a.state = (uint32_t*)(ws + l.state);
   a.S0 = cfg->old_seqs, a.S = cfg->new_seqs, a.P = cfg->columns, a.N = cfg->num_pages;
@@ -703,11 +811,24 @@ extern "C" int argus_decode_step(const argus_step_config* cfg, const argus_step_
   uint32_t clear = (a.N + kThreads - 1) / kThreads;
   clear = clear > 1024 ? 1024 : clear;
   const uint32_t copy_blocks = a.caches.n && a.S ? kCopyBlocks : 0;
+  hipStream_t st = (hipStream_t)stream_v;
+  if ((uint64_t)a.S * a.P <= kSmallEntries && a.N <= kSmallPages) {
+    // (the block's waves write their markers as those of four blocks)
+    if (!marks_fit(markers, ((uint64_t)kSmallWaves / kWaves + copy_blocks) * kWaves * 2))
+      return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
+    if ((rc = device_ok()) != ARGUS_OK) return rc;
+    a.marks = take_marks(markers, kSmallWaves / kWaves, 2);
+    hipLaunchKernelGGL(k_step_small, dim3(1), dim3(kSmallThreads), 0, st, a);
+    if (copy_blocks) {
+      a.marks = take_marks(markers, copy_blocks, 2);
+      hipLaunchKernelGGL(k_step_copy, dim3(copy_blocks), dim3(kThreads), 0, st, a);
+    }
+    return hipGetLastError() == hipSuccess ? ARGUS_OK : refuse(ARGUS_E_HIP, "launch failed");
+  }
   const uint32_t grid[4] = {clear, a.rows_blocks, tiles + 1, a.rows_blocks + copy_blocks};
   if (!marks_fit(markers, ((uint64_t)grid[0] + grid[1] + grid[2] + grid[3]) * kWaves * 2))
     return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
   if ((rc = device_ok()) != ARGUS_OK) return rc;
-  hipStream_t st = (hipStream_t)stream_v;
   a.marks = take_marks(markers, grid[0], 2);
   hipLaunchKernelGGL(k_step_clear, dim3(grid[0]), dim3(kThreads), 0, st, a);
   a.marks = take_marks(markers, grid[1], 2);
@@ -786,16 +907,22 @@ extern "C" int argus_decode_compact(const argus_compact_config* cfg, const argus
   const uint64_t entries = (uint64_t)a.S * a.P;
   a.row_blocks = (uint32_t)((entries + 4 * kThreads - 1) / (4 * kThreads));
   const uint32_t copy_blocks = a.caches.n ? kCopyBlocks : 0;
-  const uint32_t grid[3] = {a.tiles, a.tiles, a.page_blocks + a.row_blocks + copy_blocks};
-  if (!marks_fit(markers, ((uint64_t)grid[0] + grid[1] + grid[2]) * kWaves * 2))
-    return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
+  const uint32_t moves = a.page_blocks + a.row_blocks + copy_blocks;
+  const bool small = a.N <= kSmallPages;
+  const uint64_t blocks = small ? (uint64_t)kSmallWaves / kWaves + moves : 2ull * a.tiles + moves;
+  if (!marks_fit(markers, blocks * kWaves * 2)) return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
   if ((rc = device_ok()) != ARGUS_OK) return rc;
   hipStream_t st = (hipStream_t)stream_v;
-  a.marks = take_marks(markers, grid[0], 2);
-  hipLaunchKernelGGL(k_compact_count, dim3(grid[0]), dim3(kThreads), 0, st, a);
-  a.marks = take_marks(markers, grid[1], 2);
-  hipLaunchKernelGGL(k_compact_plan, dim3(grid[1]), dim3(kThreads), 0, st, a);
-  a.marks = take_marks(markers, grid[2], 2);
-  hipLaunchKernelGGL(k_compact_move, dim3(grid[2]), dim3(kThreads), 0, st, a);
+  if (small) {
+    a.marks = take_marks(markers, kSmallWaves / kWaves, 2);
+    hipLaunchKernelGGL(k_compact_small, dim3(1), dim3(kSmallThreads), 0, st, a);
+  } else {
+    a.marks = take_marks(markers, a.tiles, 2);
+    hipLaunchKernelGGL(k_compact_count, dim3(a.tiles), dim3(kThreads), 0, st, a);
+    a.marks = take_marks(markers, a.tiles, 2);
+    hipLaunchKernelGGL(k_compact_plan, dim3(a.tiles), dim3(kThreads), 0, st, a);
+  }
+  a.marks = take_marks(markers, moves, 2);
+  hipLaunchKernelGGL(k_compact_move, dim3(moves), dim3(kThreads), 0, st, a);
   return hipGetLastError() == hipSuccess ? ARGUS_OK : refuse(ARGUS_E_HIP, "launch failed");
 }
