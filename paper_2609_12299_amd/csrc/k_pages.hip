@@ -191,10 +191,11 @@ constexpr uint32_t kPageTile = 4096;
 constexpr uint32_t kPageItems = 16;  // pages of a thread
 static_assert(kPageItems * kThreads == kPageTile, "a tile per block");
 // Calls of at most so many table entries and pages are planned by one block of
-// kSmallThreads: two launches instead of four (16 beams of 64 columns over 1024
-// pages: 21 us a call against 28; 512 x 256 entries over 16384 pages by one block:
-// 95 us against 31).
-constexpr uint32_t kSmallEntries = 16384, kSmallPages = 16384;
+// kSmallThreads, in one launch instead of three (step) or two (compact).  16
+// beams of 64 columns over 1024 pages: 19 us a call against 27; 512 of 256 over
+// 16384 pages by one block 311 against 25.  Compacting 640 pages: 17 us against
+// 22; 16384 pages by one block 235 against 229.
+constexpr uint32_t kSmallEntries = 4096, kSmallPages = 4096;
 constexpr uint32_t kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
 
 // Bit i: page p0 + i is in the pool and has (LIVE) or has not any reference.

@@ -6,15 +6,17 @@
 // least that a candidate needs is known after the first step: of `lists` >= k
 // disjoint sets of lanes, the least of the sets' maxima has k elements at or
 // above it, and few more (about lists * ln(lists)).  From then on a step costs a
-// comparison of each lane's largest value, and the few lanes above it look closer.
-// When the list is half full, it is cut to its first k, and what the k-th has
-// becomes the least: the list never overflows, however many values are equal.
+// comparison of each lane's largest value; where some are above, the step's elements
+// go to LDS and the wave looks through those of the lanes in question.  When the
+// list is half full, it is cut to its first k, and what the k-th has becomes the
+// least: the list never overflows, however many values are equal.
 //
 // k_select_beams, one block per group of beams, joins the parts' sums to the
 // rows' logarithms and picks among the rows' candidates by the same sets of
 // maxima, ranking those above by counting.
 //
-// What bounds it: the reading of the logits, and the exponential of each.
+// What bounds it: the reading of the logits, and the exponential of each (a
+// quarter of the rate of other instructions).
 #include "decode.h"
 
 namespace argus {
@@ -22,6 +24,9 @@ namespace decode {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// for elements read from LDS that was written as vectors
+typedef float any_f32 __attribute__((may_alias));
+typedef uint16_t any_u16 __attribute__((may_alias));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint32_t kItems = 32;               // elements of a lane per step
@@ -78,6 +83,7 @@ template <int TYPE>
 __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
   constexpr uint32_t kBytes = TYPE == ARGUS_FP32 ? 4 : 2, kPer = 16 / kBytes, kVecs = kItems / kPer;
   __shared__ uint64_t s_list[kWaves][kList];
+  __shared__ u32x4 s_step[kWaves][kVecs * 64];
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_SELECT_ROWS);
   const uint32_t lane = threadIdx.x & 63u;
@@ -87,40 +93,30 @@ __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
   if (row < a.rows && !(a.finished && a.finished[row])) {
     uint64_t* list = s_list[wave];
     const uint8_t* base = a.logits + (int64_t)(row / a.W) * a.group_stride + (int64_t)(row % a.W) * a.beam_stride;
-    // Vectors lie on 16 bytes: element j of the row is at place j + lead.
-    const uint32_t lead = (uint32_t)((uintptr_t)base & 15u) / kBytes;
-    const uint32_t first = part * a.steps * kStep, places = a.V + lead;
-    const uint32_t left = first < places ? (places - first + kStep - 1) / kStep : 0;
+    // Vectors lie on 16 bytes: `head` elements come before the first of `vecs`
+    // vectors, less than a vector behind the last.
+    uint32_t head = (uint32_t)(0 - (uintptr_t)base & 15u) / kBytes;
+    head = head < a.V ? head : a.V;
+    const uint32_t vecs = (a.V - head) / kPer, tail = head + vecs * kPer;
+    const u32x4* body = reinterpret_cast<const u32x4*>(base + head * kBytes);
+    const uint32_t first = part * a.steps * kVecs * 64;  // vector
+    const uint32_t left = first < vecs ? (vecs - first + kVecs * 64 - 1) / (kVecs * 64) : 0;
     const uint32_t steps = left < a.steps ? left : a.steps;
+    constexpr uint32_t kNone = TYPE == ARGUS_FP32 ? 0xFF800000u : TYPE == ARGUS_BF16 ? 0xFF80FF80u : 0xFC00FC00u;  // -inf
     auto load = [&](uint32_t step, u32x4 (&w)[kVecs]) {
+      const uint32_t v0 = first + step * kVecs * 64 + lane;
 #pragma unroll
-      for (uint32_t v = 0; v < kVecs; ++v) {
-        const int64_t j = (int64_t)first + step * kStep + (v * 64 + lane) * kPer - lead;
-        if (j >= 0 && j + kPer <= a.V) {
-          w[v] = *reinterpret_cast<const u32x4*>(base + j * kBytes);
-        } else {
-#pragma unroll
-          for (uint32_t i = 0; i < kPer; ++i) {
-            // outside the row: minus infinity
-            uint32_t e = TYPE == ARGUS_FP32 ? 0xFF800000u : TYPE == ARGUS_BF16 ? 0xFF80u : 0xFC00u;
-            if (j + i >= 0 && j + i < a.V) {
-              if constexpr (TYPE == ARGUS_FP32) e = *reinterpret_cast<const uint32_t*>(base + (j + i) * kBytes);
-              else e = *reinterpret_cast<const uint16_t*>(base + (j + i) * kBytes);
-            }
-            if constexpr (TYPE == ARGUS_FP32) w[v][i] = e;
-            else w[v][i / 2] = i % 2 ? w[v][i / 2] | e << 16 : e;
-          }
-        }
-      }
+      for (uint32_t v = 0; v < kVecs; ++v) w[v] = v0 + v * 64 < vecs ? body[v0 + v * 64] : (u32x4)(kNone);
     };
-    uint32_t n = 0;          // candidates in the list
-    uint64_t least = 0;      // keys have to be above it
+    uint32_t n = 0;           // candidates in the list
+    uint64_t least = 0;       // their keys are above it
     float least_value = -INFINITY;
-    // The list cut to its first k.
+    // The list cut to its first k, in order.
     auto cut = [&]() {
       __builtin_amdgcn_wave_barrier();
       const uint64_t k0 = lane < n ? list[lane] : 0, k1 = lane + 64 < n ? list[lane + 64] : 0;
       uint32_t r0 = 0, r1 = 0;
+#pragma unroll 4
       for (uint32_t i = 0; i < n; ++i) {
         const uint64_t o = list[i];
         r0 += o > k0;
@@ -136,7 +132,24 @@ __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
         least_value = value_of((uint32_t)(least >> 32));
       }
     };
+    auto append = [&](bool want, uint64_t key) {  // at most 64 at a time
+      const uint64_t take = __ballot(want);
+      if (want) list[n + (uint32_t)__popcll(take & lanemask_lt())] = key;
+      n += (uint32_t)__popcll(take);
+    };
     float ref = -INFINITY, sum = 0.0f;
+    if (part == 0) {  // what lies before and behind the vectors: at most 2 * (kPer - 1) elements
+      const uint32_t j = lane < kPer ? lane : tail + lane - kPer;
+      const bool in = lane < kPer ? j < head : lane < 2 * kPer && j < a.V;
+      float x = -INFINITY;
+      if (in) {
+        if constexpr (TYPE == ARGUS_FP32) x = *reinterpret_cast<const float*>(base + (uint64_t)j * kBytes);
+        else x = of_word<TYPE>(*reinterpret_cast<const uint16_t*>(base + (uint64_t)j * kBytes), 0);
+      }
+      ref = wave_max(x);
+      sum = __builtin_amdgcn_exp2f((x - (ref == -INFINITY ? 0.0f : ref)) * kLog2e);
+      append(x > -INFINITY, key_of(x, j));
+    }
     auto look = [&](uint32_t step, const u32x4 (&w)[kVecs]) {
       float x[kItems];
 #pragma unroll
@@ -167,22 +180,28 @@ __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
         least_value = value_of(lo);
         least = join64(0u, lo);  // below every key of this value
       }
-      if (__any(top >= least_value && top > -INFINITY)) {
-        const uint32_t token0 = first + step * kStep + lane * kPer - lead;
+      uint64_t hot = __ballot(top >= least_value && top > -INFINITY);
+      if (hot) {
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (uint32_t i = 0; i < kItems; ++i) {
-          if (__any(x[i] >= least_value)) {
-            const uint64_t key = key_of(x[i], token0 + (i / kPer) * 64 * kPer + i % kPer);
-            uint64_t take = __ballot(x[i] >= least_value && key > least && x[i] > -INFINITY);
-            if (n + (uint32_t)__popcll(take) > kList) {
-              cut();
-              take = __ballot(x[i] >= least_value && key > least && x[i] > -INFINITY);
-            }
-            if (take >> lane & 1u) list[n + (uint32_t)__popcll(take & lanemask_lt())] = key;
-            n += (uint32_t)__popcll(take);
-          }
+        for (uint32_t v = 0; v < kVecs; ++v) s_step[wave][v * 64 + lane] = w[v];
+        __builtin_amdgcn_wave_barrier();
+        // two lanes' 32 elements at a time
+        while (hot) {
+          if (n > kList / 2) cut();
+          const uint32_t l0 = (uint32_t)__builtin_ctzll(hot);
+          hot &= hot - 1;
+          const uint32_t l1 = hot ? (uint32_t)__builtin_ctzll(hot) : l0;
+          const bool in = lane < kItems || l1 != l0;
+          hot &= hot - 1;
+          const uint32_t i = lane % kItems, at = (i / kPer) * 64 + (lane < kItems ? l0 : l1);
+          float y;
+          if constexpr (TYPE == ARGUS_FP32) y = reinterpret_cast<const any_f32*>(&s_step[wave][at])[i % kPer];
+          else y = of_word<TYPE>(reinterpret_cast<const any_u16*>(&s_step[wave][at])[i % kPer], 0);
+          const uint32_t token = head + (first + step * kVecs * 64 + at) * kPer + i % kPer;
+          const uint64_t key = key_of(y, token);
+          append(in && y >= least_value && key > least && y > -INFINITY, key);
         }
-        if (n > kList / 2) cut();
       }
     };
     u32x4 w0[kVecs], w1[kVecs];
@@ -203,18 +222,16 @@ __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
   mk.end(ARGUS_REGION_SELECT_ROWS);
 }
 
+// A candidate's place in the order: score, then ~beam; then the logit and ~token.
 struct Pick {
-  uint32_t order, beam;  // of the score; ~beam
-  uint64_t key;
+  uint64_t first, key;
 };
-ARGUS_DEV bool before(const Pick& x, const Pick& y) {
-  const uint64_t a = join64(x.beam, x.order), b = join64(y.beam, y.order);
-  return a > b || (a == b && x.key > y.key);
-}
+ARGUS_DEV bool before(const Pick& x, const Pick& y) { return x.first > y.first || (x.first == y.first && x.key > y.key); }
 
 __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
+  constexpr uint32_t kMine = 4;  // candidates that a thread holds at a time
   __shared__ float s_lse[kMaxBeams], s_score[kMaxBeams];
-  __shared__ uint8_t s_done[kMaxBeams];
+  __shared__ uint32_t s_done[kMaxBeams];
   __shared__ uint32_t s_list[kMaxK];
   __shared__ uint32_t s_n;
   __shared__ Pick s_cand[kCands];
@@ -222,52 +239,80 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_SELECT_BEAMS);
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, group = blockIdx.x;
-  for (uint32_t w = wave; w < a.W; w += kWaves) {
+  // Candidate i: the i / parts-th of the list of part i % parts (of the whole
+  // group), so that each set of threads has candidates of all ranks.
+  const uint32_t parts = a.W * a.parts, total = parts * a.K;
+  const uint64_t* cands = a.cands + (uint64_t)group * total;
+  uint64_t key[kMine];
+  uint32_t beam[kMine];  // and, from bit 8 on, whether it is its beam's first
+  auto fetch = [&](uint32_t i0) {
+#pragma unroll
+    for (uint32_t c = 0; c < kMine; ++c) {
+      const uint32_t i = i0 + c * kThreads + tid;
+      const uint32_t r = i / parts, j = i - r * parts, w = j / a.parts;
+      key[c] = i < total ? cands[(uint64_t)j * a.K + r] : 0;
+      beam[c] = i < total ? w | (r == 0 && j == w * a.parts ? 256u : 0u) : 0xFFFFu;
+    }
+  };
+  fetch(0);  // under way while the sums are joined
+  for (uint32_t w = tid / 16; w < a.W; w += kThreads / 16) {  // 16 lanes a row
     const uint32_t row = group * a.W + w;
     const bool done = a.finished && a.finished[row];
+    const float score = a.scores[row];
     float top = -INFINITY, sum = 0.0f;
     if (!done) {
-      for (uint32_t c = lane; c < a.parts; c += 64) top = fmaxf(top, a.sums[(uint64_t)row * a.parts + c].x);
-      top = wave_max(top);
-      for (uint32_t c = lane; c < a.parts; c += 64) {
+      for (uint32_t c = tid % 16; c < a.parts; c += 16) {
         const float2 v = a.sums[(uint64_t)row * a.parts + c];
-        sum += v.x == -INFINITY ? v.y : v.y * exp2f((v.x - top) * kLog2e);
+        const float most = fmaxf(top, v.x);
+        // (a part without a value leaves 0, a NaN stays)
+        sum = sum * (top == -INFINITY ? 1.0f : exp2f((top - most) * kLog2e)) +
+              v.y * (v.x == -INFINITY ? 1.0f : exp2f((v.x - most) * kLog2e));
+        top = most;
       }
-      sum = wave_sum(sum);
     }
-    if (lane == 0) {
+    for (int d = 1; d < 16; d <<= 1) {
+      const float o = __shfl_xor(top, d), os = __shfl_xor(sum, d), most = fmaxf(top, o);
+      sum = sum * (top == -INFINITY ? 1.0f : exp2f((top - most) * kLog2e)) +
+            os * (o == -INFINITY ? 1.0f : exp2f((o - most) * kLog2e));
+      top = most;
+    }
+    if (tid % 16 == 0) {
       s_lse[w] = top + logf(sum);
-      s_score[w] = a.scores[row];
+      s_score[w] = score;
       s_done[w] = done;
     }
   }
   if (tid < a.lists) s_list[tid] = 0;
   if (tid == 0) s_n = 0;
   __syncthreads();
-  // Candidate i: the i / parts-th of the list of part i % parts (of the whole
-  // group), so that each set of threads has candidates of all ranks.
-  const uint32_t parts = a.W * a.parts, total = parts * a.K;
-  const uint64_t* cands = a.cands + (uint64_t)group * total;
-  auto pick_of = [&](uint32_t i, Pick* p) {  // false: none
-    const uint32_t r = i / parts, j = i - r * parts, w = j / a.parts;
+  // What fetch() has brought, as a place in the order; false: no candidate.
+  auto pick_of = [&](uint32_t c, Pick* p) {
+    if (beam[c] == 0xFFFFu) return false;
+    const uint32_t w = beam[c] & 255u;
     float score;
     if (s_done[w]) {
-      if (r != 0 || j != w * a.parts) return false;
+      if (beam[c] < 256u) return false;
       p->key = 0;
       score = s_score[w];
     } else {
-      p->key = cands[(uint64_t)j * a.K + r];
+      p->key = key[c];
       if (p->key == 0) return false;
       score = s_score[w] + (value_of((uint32_t)(p->key >> 32)) - s_lse[w]);
     }
-    p->order = order_of(score);
-    p->beam = ~w;
+    p->first = join64(~w, order_of(score));
     return score > -INFINITY;
   };
   uint32_t top = 0;
-  for (uint32_t i = tid; i < total; i += kThreads) {
-    Pick p;
-    if (pick_of(i, &p)) top = p.order > top ? p.order : top;
+  for (uint32_t i0 = 0; i0 < total; i0 += kMine * kThreads) {
+    if (i0) fetch(i0);
+#pragma unroll
+    for (uint32_t c = 0; c < kMine; ++c) {
+      Pick p;
+      if (pick_of(c, &p)) {
+        const uint32_t o = (uint32_t)(p.first >> 32);
+        top = o > top ? o : top;
+      }
+    }
   }
   atomicMax(&s_list[tid & (a.lists - 1)], top);
   __syncthreads();
@@ -276,20 +321,24 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
     const uint32_t o = __shfl_xor(bound, d);
     bound = o < bound ? o : bound;
   }
-  for (uint32_t i = tid; i < total; i += kThreads) {
-    Pick p;
-    if (pick_of(i, &p) && p.order >= bound) {
-      const uint32_t at = atomicAdd(&s_n, 1u);
-      if (at < kCands) s_cand[at] = p;
+  for (uint32_t i0 = 0; i0 < total; i0 += kMine * kThreads) {
+    if (total > kMine * kThreads) fetch(i0);
+#pragma unroll
+    for (uint32_t c = 0; c < kMine; ++c) {
+      Pick p;
+      if (pick_of(c, &p) && (uint32_t)(p.first >> 32) >= bound) {
+        const uint32_t at = atomicAdd(&s_n, 1u);
+        if (at < kCands) s_cand[at] = p;
+      }
     }
   }
   __syncthreads();
   const uint32_t n = s_n;
   auto put = [&](uint32_t r, const Pick& p) {
-    const uint32_t w = ~p.beam;
+    const uint32_t w = ~(uint32_t)p.first;
     const uint64_t at = (uint64_t)group * a.K + r;
     const int32_t token = s_done[w] ? a.eos : (int32_t)~(uint32_t)p.key;
-    a.new_scores[at] = value_of(p.order);
+    a.new_scores[at] = value_of((uint32_t)(p.first >> 32));
     a.parents[at] = (int32_t)(group * a.W + w);
     a.tokens[at] = token;
     a.new_finished[at] = s_done[w] || (token == a.eos && a.eos >= 0);
@@ -305,21 +354,27 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
     for (uint32_t c = tid; c < n; c += kThreads) {
       const Pick p = s_cand[c];
       uint32_t rank = 0;
+#pragma unroll 4
       for (uint32_t o = 0; o < n; ++o) rank += before(s_cand[o], p);
       if (rank < a.K) put(rank, p);
     }
     for (uint32_t r = n + tid; r < a.K; r += kThreads) put_none(r);
   } else {
-    Pick last{0xFFFFFFFFu, 0xFFFFFFFFu, ~0ull};
+    // Too many equal scores to be ranked: one after the other.
+    Pick last{~0ull, ~0ull};
     bool more = true;
     for (uint32_t r = 0; r < a.K; ++r) {
-      Pick best{0, 0, 0};
-      for (uint32_t i = tid; more && i < total; i += kThreads) {
-        Pick p;
-        if (pick_of(i, &p) && before(last, p) && before(p, best)) best = p;
+      Pick best{0, 0};
+      for (uint32_t i0 = 0; more && i0 < total; i0 += kMine * kThreads) {
+        fetch(i0);
+#pragma unroll
+        for (uint32_t c = 0; c < kMine; ++c) {
+          Pick p;
+          if (pick_of(c, &p) && before(last, p) && before(p, best)) best = p;
+        }
       }
       for (int d = 1; d < 64; d <<= 1) {
-        const Pick o{__shfl_xor(best.order, d), __shfl_xor(best.beam, d), __shfl_xor(best.key, d)};
+        const Pick o{__shfl_xor(best.first, d), __shfl_xor(best.key, d)};
         if (before(o, best)) best = o;
       }
       if (lane == 0) s_best[wave] = best;
@@ -327,7 +382,7 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
       best = s_best[0];
       for (uint32_t w = 1; w < (uint32_t)kWaves; ++w)
         if (before(s_best[w], best)) best = s_best[w];
-      more = more && best.order != 0;
+      more = more && best.first != 0;
       if (tid == 0) {
         if (more) put(r, best);
         else put_none(r);
@@ -345,7 +400,7 @@ struct Plan {
 };
 
 // Waves that read the logits, all resident at once where there are so many steps.
-constexpr uint32_t kRowWaves = 256 * 4 * 6;
+constexpr uint32_t kRowWaves = 256 * 4 * 4;
 
 int make_plan(const argus_select_config* c, Plan* p) {
   if (!c) return refuse(ARGUS_E_INVAL, "no configuration");
@@ -355,10 +410,8 @@ int make_plan(const argus_select_config* c, Plan* p) {
     return refuse(ARGUS_E_INVAL, "beams %u, k %u (1..64)", c->beams, c->k);
   if (c->vocab < 1 || c->vocab > (1u << 24)) return refuse(ARGUS_E_INVAL, "vocab %u (1..2^24)", c->vocab);
   if (c->groups > (1u << 20)) return refuse(ARGUS_E_CAPACITY, "groups %u", c->groups);
-  // a row may start anywhere on 16 bytes: up to 15 bytes before its steps
-  const uint32_t lead = c->type == ARGUS_FP32 ? 3u : 7u;
   const uint64_t rows = (uint64_t)c->groups * c->beams;
-  const uint32_t steps = (c->vocab + lead + kStep - 1) / kStep;
+  const uint32_t steps = (c->vocab + kStep - 1) / kStep;
   const uint64_t parts = rows ? kRowWaves / rows : 1;
   p->parts = parts < 1 ? 1u : parts < steps ? (uint32_t)parts : steps;
   p->steps = (steps + p->parts - 1) / p->parts;
