@@ -21,9 +21,9 @@
 // taken as the sum of two 16-bit numbers, so that its rounding is not seen in
 // the result).
 //
-// Shares: the units of work are the tiles of all (sequence, head) segments one
-// after the other, kPieceCost more for each segment, and wave w takes units
-// [w * per, (w + 1) * per) whatever the lengths are (they are known on the
+// Shares: the units of work are the tiles (groups of 2^unit_shift tiles, where
+// there could be more than 2^31) of all (sequence, head) segments one after the
+// other, kPieceCost tiles more for each segment, and wave w takes units [w * per, (w + 1) * per) whatever the lengths are (they are known on the
 // device alone): a batch of one long and many short sequences loads all compute
 // units alike, and the short ones' latencies lie side by side.  A segment that lies
 // in one share is finished there; of the others each wave leaves its piece (m, l,
@@ -38,8 +38,8 @@ namespace argus {
 namespace decode {
 
 constexpr uint32_t kTile = 32;        // tokens per step of a wave
-constexpr uint64_t kMinShare = 4;     // units of a share, at least
-constexpr uint32_t kPieceCost = 3;    // what a segment costs beside its tiles, in tiles
+constexpr uint32_t kMinShare = 4;     // units of a share, at least
+constexpr uint32_t kPieceCost = 4;    // what a segment costs beside its tiles, in tiles
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -53,8 +53,10 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 struct AttendArgs {
   const uint16_t* q;
   int64_t q_seq, q_head;
-  const uint8_t *k, *v;                 // strides in bytes
-  int64_t k_page, k_head, k_tok, v_page, v_head, v_tok;
+  const uint8_t *k, *v;
+  int64_t k_head, v_head;               // bytes
+  uint32_t k_page, v_page;              // 16 bytes
+  uint32_t k_tok, v_tok;                // bytes
   const int32_t* table;
   int64_t table_stride;
   const int32_t* lens;
@@ -67,6 +69,7 @@ struct AttendArgs {
   uint32_t S, H, G, D, HS, row_tiles;
   uint32_t shift, num_pages, columns, window, sinks;
   uint32_t shares;  // waves that share the batch
+  uint32_t unit_shift;
   uint32_t by_seg;  // `open` goes by segment, else by share
   float scale;
   Marks marks;
@@ -78,9 +81,8 @@ struct Span {
   uint32_t len, lo, sinks, sink_tiles, first, tiles;
 };
 
-ARGUS_DEV Span span_of(const AttendArgs& a, uint32_t s) {
+ARGUS_DEV Span span_of(const AttendArgs& a, int32_t n) {
   Span p;
-  const int32_t n = a.lens[s];
   const uint32_t most = a.columns << a.shift;
   p.len = n < 0 ? 0u : ((uint32_t)n < most ? (uint32_t)n : most);
   p.lo = a.window && p.len > a.window ? p.len - a.window : 0u;
@@ -138,22 +140,24 @@ struct Half<1> {
   static constexpr float kRaise = 7.0f;
 };
 
-// Two bytes of e4m3 in a 16-bit pair each (exact: every e4m3 number is one of both types).
+// Two bytes of e4m3 (every such number is one of bf16 and of fp16).
 template <int T>
 ARGUS_DEV uint32_t widen(uint32_t w, bool hi) {
-  const f32x2 f = hi ? __builtin_amdgcn_cvt_pk_f32_fp8(w, true) : __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
-  return Half<T>::pack(f.x, f.y);
-}
-
-ARGUS_DEV uint64_t uniform64(uint64_t v) {
-  return join64(__builtin_amdgcn_readfirstlane((uint32_t)v), __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32)));
+  if constexpr (T == 0)
+    return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)
+                                           : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
+  else
+    return __builtin_bit_cast(uint32_t, hi ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true)
+                                           : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
 }
 
 // How far a score may rise above the running maximum before the maximum moves:
 // weights stay below 2^8, and the sums need no rescaling at most steps.
 constexpr float kSlack = 5.5f;
-// Scores are kept as they are, and the difference to the maximum is taken to
-// base 2: a score near the largest float times log2 e would overflow.
+// A weight is 2^(x kd2 - base), one multiply-add and the exponential.  Beyond
+// kFar the product's rounding would show in that, and near the largest float it
+// would overflow: then the difference of the scores first, and that to base 2.
+constexpr float kFar = 1e6f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 ARGUS_DEV float exp_of(float x) { return exp2f(x * kLog2e); }
 
@@ -170,8 +174,13 @@ ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint
   constexpr int VW = DP / 16;               // elements of a value row per lane
   constexpr int VD = VW * (F8 ? 1 : 2) / 4;   // in 32-bit words
   constexpr int VH = VW / 2;                // 16-bit pairs per lane
+  // Small tiles leave too little under way with one at a time (64 sequences of up to
+  // 16384 tokens, head size 64: fp8 38 us against 48, bf16 56 against 58); for larger
+  // ones the rows of two would not fit the registers.
+  constexpr bool AHEAD = DP == 64;
   using Hf = Half<T>;
   const uint32_t lane = threadIdx.x & 63u, c = lane & 15u, g = lane >> 4;
+  const float kc = a.scale * (a.k_scale ? a.k_scale[h] : 1.0f), kd = fabsf(kc);
   // the query rows as operands: lane (q, g) holds 8 elements of its row per fragment
   u32x4 qf[NQ][KF];
 #pragma unroll
@@ -182,9 +191,9 @@ ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint
     for (int f = 0; f < KF; ++f) {
       const uint32_t d = F8 ? 64 * (f / 2) + 16 * g + 8 * (f % 2) : 32 * f + 8 * g;
       qf[i][f] = row < rows && d < a.D ? *reinterpret_cast<const u32x4*>(qr + d) : (u32x4)(0u);
+      if (kc < 0.0f) qf[i][f] ^= 0x80008000u;  // so that the largest product is the largest score
     }
   }
-  const float kc = a.scale * (a.k_scale ? a.k_scale[h] : 1.0f);
   const int32_t* tab = a.table + (int64_t)s * a.table_stride;
   const uint8_t* kb = a.k + (int64_t)h * a.k_head;
   const uint8_t* vb = a.v + (int64_t)h * a.v_head;
@@ -198,66 +207,88 @@ ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint
     for (int f = 0; f < VW; ++f) acc[i][f] = (f32x4)(0.0f);
   }
 
-  for (uint32_t t = t0; t < t1; t += dt) {
-    const uint32_t tok = (t < p.sink_tiles ? t : t - p.sink_tiles + p.first) * kTile;
-    // the pages of the lane's two key rows, and of its two runs of four value rows
-    int32_t kp[2], vp[2];
-    bool seen[2];
+  float base[NQ];  // the maximum to base 2, less kRaise
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) base[i] = 0.0f;
+  const float kd2 = kd * kLog2e;
+  bool far = !(kd > 1e-30f && kd < 1e30f);  // scores so large, or a scale so odd, that the differences come first
+
+  // The pages of tile t's rows: of the lane's two keys, and of its two runs of four values.
+  struct Ids {
+    int32_t k[2], v[2];
+  };
+  auto token_of = [&](uint32_t t) { return (t < p.sink_tiles ? t : t - p.sink_tiles + p.first) * kTile; };
+  auto find = [&](uint32_t t, Ids& ids) {
+    const uint32_t tok = token_of(t < t1 ? t : t1 - 1);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint32_t kcol = (tok + 16 * i + c) >> a.shift, vcol = (tok + 16 * i + 4 * g) >> a.shift;
-      kp[i] = kcol < a.columns ? tab[kcol] : -1;
-      vp[i] = vcol < a.columns ? tab[vcol] : -1;
-      if ((uint32_t)kp[i] >= a.num_pages) kp[i] = 0;  // any row: its scores are not taken
-      seen[i] = (uint32_t)vp[i] < a.num_pages;
-      if (!seen[i]) vp[i] = 0;
+      const int32_t kp = tab[kcol < a.columns ? kcol : 0], vp = tab[vcol < a.columns ? vcol : 0];
+      ids.k[i] = kcol < a.columns ? kp : -1;
+      ids.v[i] = vcol < a.columns ? vp : -1;
     }
-    u32x4 kr[2][KL];
+  };
+  // Its rows, and which of the lane's eight tokens are visible.  (A page that is not
+  // held: any row, what comes of it is not taken.)
+  struct Rows {
+    u32x4 k[2][KL];
+    uint32_t v[8][VD];
+    uint32_t vis;
+  };
+  auto load = [&](uint32_t t, const Ids& ids, Rows& w) {
+    const uint32_t tok = token_of(t);
+    bool held = true;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const uint8_t* r = kb + (int64_t)kp[i] * a.k_page + (int64_t)((tok + 16 * i + c) & in_page) * a.k_tok;
+      const uint32_t page = (uint32_t)ids.k[i] < a.num_pages ? (uint32_t)ids.k[i] : 0u;
+      const uint8_t* r = kb + ((uint64_t)page * a.k_page << 4) + ((tok + 16 * i + c) & in_page) * a.k_tok;
 #pragma unroll
       for (int f = 0; f < KL; ++f) {
         const uint32_t d = 64 * f + 16 * g;  // byte of the row
         const bool in = EXACT || d < a.D * (F8 ? 1u : 2u);
-        kr[i][f] = *reinterpret_cast<const u32x4*>(r + (in ? d : 0u));
-        if (!EXACT && !in) kr[i][f] = (u32x4)(0u);
+        w.k[i][f] = *reinterpret_cast<const u32x4*>(r + (in ? d : 0u));
+        if (!EXACT && !in) w.k[i][f] = (u32x4)(0u);
       }
     }
-    uint32_t vr[8][VD];
+    uint32_t b = c * (VD * 4);
+    if (!EXACT && b >= a.D * (F8 ? 1u : 2u)) b = 0;  // rows of O beyond the head size: not written
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t at = tok + 16 * (i / 4) + 4 * g + i % 4;
-      uint32_t b = c * (VD * 4);
-      if (!EXACT && b >= a.D * (F8 ? 1u : 2u)) b = 0;  // rows of O beyond the head size: not written
-      const uint8_t* r = vb + (int64_t)vp[i / 4] * a.v_page + (int64_t)(at & in_page) * a.v_tok + b;
+      const uint32_t page = (uint32_t)ids.v[i / 4] < a.num_pages ? (uint32_t)ids.v[i / 4] : 0u;
+      const uint8_t* r = vb + ((uint64_t)page * a.v_page << 4) + (((tok + 16 * (i / 4) + 4 * g) & in_page) * a.v_tok + b) + i % 4 * a.v_tok;
       if constexpr (VD == 1) {
-        vr[i][0] = *reinterpret_cast<const uint32_t*>(r);
+        w.v[i][0] = *reinterpret_cast<const uint32_t*>(r);
       } else if constexpr (VD == 2) {
         const u32x2 x = *reinterpret_cast<const u32x2*>(r);
-        vr[i][0] = x.x, vr[i][1] = x.y;
+        w.v[i][0] = x.x, w.v[i][1] = x.y;
       } else {
 #pragma unroll
         for (int j = 0; j < VD / 4; ++j) {
           const u32x4 x = *reinterpret_cast<const u32x4*>(r + 16 * j);
-          vr[i][4 * j] = x.x, vr[i][4 * j + 1] = x.y, vr[i][4 * j + 2] = x.z, vr[i][4 * j + 3] = x.w;
+          w.v[i][4 * j] = x.x, w.v[i][4 * j + 1] = x.y, w.v[i][4 * j + 2] = x.z, w.v[i][4 * j + 3] = x.w;
         }
       }
+      held = held && (uint32_t)ids.v[i / 4] < a.num_pages;
     }
     // which of the lane's eight tokens are visible
-    uint32_t vis = 0;
+    w.vis = 0xFFu;
+    if (!F8 || tok < p.lo || tok + kTile > p.len || !__all(held)) {
+      w.vis = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t at = tok + 16 * (i / 4) + 4 * g + i % 4;
-      const bool in = at < p.len && (at >= p.lo || at < p.sinks) && seen[i / 4];
-      vis |= in ? 1u << i : 0u;
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t at = tok + 16 * (i / 4) + 4 * g + i % 4;
+        const bool in = at < p.len && (at >= p.lo || at < p.sinks) && (uint32_t)ids.v[i / 4] < a.num_pages;
+        w.vis |= in ? 1u << i : 0u;
+      }
     }
-    const bool whole = __all(vis == 0xFFu);
+  };
+  auto take = [&](Rows& w) {
+    const bool whole = __all(w.vis == 0xFFu);
     if (!whole) {  // what is not visible may hold anything
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < VD; ++j) vr[i][j] = vis >> i & 1u ? vr[i][j] : 0u;
+        for (int j = 0; j < VD; ++j) w.v[i][j] = w.vis >> i & 1u ? w.v[i][j] : 0u;
     }
 
     // scores
@@ -270,10 +301,10 @@ ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint
       for (int hh = 0; hh < 2; ++hh) {
         u32x4 kf;
         if constexpr (F8) {
-          const uint32_t w0 = kr[hh][f / 2][2 * (f % 2)], w1 = kr[hh][f / 2][2 * (f % 2) + 1];
+          const uint32_t w0 = w.k[hh][f / 2][2 * (f % 2)], w1 = w.k[hh][f / 2][2 * (f % 2) + 1];
           kf = (u32x4){widen<T>(w0, false), widen<T>(w0, true), widen<T>(w1, false), widen<T>(w1, true)};
         } else {
-          kf = kr[hh][f];
+          kf = w.k[hh][f];
         }
 #pragma unroll
         for (int i = 0; i < NQ; ++i) sc[i][hh] = Hf::mfma(kf, qf[i][f], sc[i][hh]);
@@ -286,12 +317,13 @@ ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint
     for (int i = 0; i < NQ; ++i) {
       float x[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = sc[i][j / 4][j % 4] * kc;
+      for (int j = 0; j < 8; ++j) x[j] = sc[i][j / 4][j % 4];
       if (!whole) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = vis >> j & 1u ? x[j] : -INFINITY;
+        for (int j = 0; j < 8; ++j) x[j] = w.vis >> j & 1u ? x[j] : -INFINITY;
       }
       float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      top = top == -INFINITY ? top : top * kd;  // (kd may be 0)
       if (__any(top > m[i] + kSlack)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
@@ -301,19 +333,28 @@ ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint
 #pragma unroll
         for (int f = 0; f < VW; ++f) acc[i][f] *= scale;
         m[i] = mn;
+        base[i] = mn == -INFINITY ? 0.0f : fmaf(mn, kLog2e, -Hf::kRaise);
+        far = far || __any(fabsf(mn) > kFar && mn != -INFINITY);
       }
-      const float ms = m[i] == -INFINITY ? 0.0f : m[i];
-      float w[8], sum = 0.0f;
+      float wt[8], sum = 0.0f;
+      if (!far) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        w[j] = __builtin_amdgcn_exp2f(fmaf(x[j] - ms, kLog2e, Hf::kRaise));
-        sum += w[j];
+        for (int j = 0; j < 8; ++j) wt[j] = __builtin_amdgcn_exp2f(fmaf(x[j], kd2, -base[i]));
+      } else {
+        const float ms = m[i] == -INFINITY ? 0.0f : m[i];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float y = x[j] == -INFINITY ? x[j] : x[j] * kd;
+          wt[j] = __builtin_amdgcn_exp2f(fmaf(y - ms, kLog2e, Hf::kRaise));
+        }
       }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += wt[j];
       l[i] += sum;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         uint32_t hi, lo;
-        Hf::split(w[2 * j], w[2 * j + 1], &hi, &lo);
+        Hf::split(wt[2 * j], wt[2 * j + 1], &hi, &lo);
         p_hi[i][j] = hi;
         p_lo[i][j] = lo;
       }
@@ -327,9 +368,9 @@ ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint
       for (int j = 0; j < 4; ++j) {  // tokens 2 j and 2 j + 1
         uint32_t x, y;
         if constexpr (F8) {
-          x = widen<T>(vr[2 * j][f / 2], f % 2), y = widen<T>(vr[2 * j + 1][f / 2], f % 2);
+          x = widen<T>(w.v[2 * j][f / 2], f % 2), y = widen<T>(w.v[2 * j + 1][f / 2], f % 2);
         } else {
-          x = vr[2 * j][f], y = vr[2 * j + 1][f];
+          x = w.v[2 * j][f], y = w.v[2 * j + 1][f];
         }
         even[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
         odd[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
@@ -340,6 +381,45 @@ ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint
         acc[i][2 * f + 1] = Hf::mfma(odd, p_hi[i], acc[i][2 * f + 1]);
         acc[i][2 * f] = Hf::mfma(even, p_lo[i], acc[i][2 * f]);
         acc[i][2 * f + 1] = Hf::mfma(odd, p_lo[i], acc[i][2 * f + 1]);
+      }
+    }
+  };
+
+  if (t0 < t1) {
+    uint32_t t = t0;
+    Ids i0, i1;
+    Rows w0;
+    find(t, i0);
+    if constexpr (AHEAD) {
+      // The next tile's rows, and the pages of the one after it, are under way while a
+      // tile is taken.  (No load stands in a branch that is left again: one that may
+      // or may not have been made would be waited for at once.)
+      Rows w1;
+      find(t + dt, i1);
+      load(t, i0, w0);
+      for (;;) {
+        if (t + dt >= t1) {
+          take(w0);
+          break;
+        }
+        t += dt;
+        find(t + dt, i0);
+        load(t, i1, w1);
+        take(w0);
+        if (t + dt >= t1) {
+          take(w1);
+          break;
+        }
+        t += dt;
+        find(t + dt, i1);
+        load(t, i0, w0);
+        take(w1);
+      }
+    } else {
+      for (; t < t1; t += dt) {
+        load(t, i0, w0);
+        find(t + dt, i0);
+        take(w0);
       }
     }
   }
@@ -365,7 +445,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend_whole(At
   const uint32_t s = blockIdx.x / a.HS, hs = blockIdx.x % a.HS;
   const uint32_t h = hs / a.row_tiles, q0 = (hs % a.row_tiles) * 16 * NQ;
   const uint32_t rows = a.G - q0 < 16u * NQ ? a.G - q0 : 16u * NQ;
-  const Span p = span_of(a, s);
+  const Span p = span_of(a, a.lens[s]);
   mk.end(ARGUS_REGION_ATTEND_PLACE);
   mk.begin(ARGUS_REGION_ATTEND_TOKENS);
   f32x4 acc[NQ][VW];
@@ -421,29 +501,34 @@ template <int T, bool F8, int DP, int NQ, bool EXACT>
 __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend_shared(AttendArgs a) {
   constexpr int VW = DP / 16;
   using Hf = Half<T>;
-  __shared__ uint64_t s_base[kThreads + 1];
-  __shared__ uint64_t s_wave[kWaves];
+  __shared__ uint32_t s_base[kThreads];
+  __shared__ uint32_t s_wave[kWaves];
+  __shared__ int32_t s_len[kThreads];
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_ATTEND);
   mk.begin(ARGUS_REGION_ATTEND_PLACE);
   const uint32_t tid = threadIdx.x, lane = tid & 63u, c = lane & 15u, g = lane >> 4;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t ones = (1u << a.unit_shift) - 1;
+  auto units_of = [&](const Span& p) { return (p.tiles + kPieceCost + ones) >> a.unit_shift; };
+  // A thread looks after `run` sequences in a row.
   const uint32_t run = (a.S + kThreads - 1) / kThreads;
-  uint64_t mine = 0;
+  uint32_t mine = 0;
   for (uint32_t i = 0; i < run; ++i) {
     const uint32_t x = tid * run + i;
-    if (x < a.S) mine += span_of(a, x).tiles + kPieceCost;
+    if (x < a.S) {
+      const int32_t len = a.lens[x];
+      s_len[tid] = len;
+      mine += units_of(span_of(a, len));
+    }
   }
-  uint64_t incl = mine;
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t o = __shfl_up(incl, d);
-    if (lane >= (uint32_t)d) incl += o;
-  }
+  const uint32_t incl = (uint32_t)wave_incl_scan32((int32_t)mine);
   if (lane == 63) s_wave[wave] = incl;
   __syncthreads();
-  uint64_t before = 0, total = 0;
+  uint32_t before = 0, total = 0;
+#pragma unroll
   for (uint32_t w = 0; w < (uint32_t)kWaves; ++w) {
-    if (w < wave) before += s_wave[w];
+    before += w < wave ? s_wave[w] : 0u;
     total += s_wave[w];
   }
   s_base[tid] = (before + incl - mine) * a.HS;
@@ -451,38 +536,39 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend_shared(A
   __syncthreads();
   // this wave's units [u, end), and the sequence that they start in
   const uint32_t share = blockIdx.x * kWaves + wave;
-  uint64_t per = (total + a.shares - 1) / a.shares;
+  uint32_t per = (total + a.shares - 1) / a.shares;
   per = per < kMinShare ? kMinShare : per;
-  uint64_t u = share * per, end = u + per < total ? u + per : total, off = 0;
-  uint32_t s = 0;
+  uint32_t u = share < total / per + 1 ? share * per : total, end = total - u < per ? total : u + per, off = 0, s = 0;
   if (u < end) {
-    uint32_t lo = 0, hi = kThreads;  // last thread whose sequences start at or before u
-    while (hi - lo > 1) {
-      const uint32_t mid = (lo + hi) / 2;
-      if (s_base[mid] <= u) lo = mid; else hi = mid;
-    }
-    s = lo * run;
-    off = u - s_base[lo];
-    for (;;) {
-      const uint64_t w = (uint64_t)(span_of(a, s).tiles + kPieceCost) * a.HS;
+    uint32_t n = 0;  // threads whose sequences start at or before u
+#pragma unroll
+    for (uint32_t i = 0; i < (uint32_t)kThreads / 64; ++i) n += (uint32_t)__popcll(__ballot(s_base[64 * i + lane] <= u));
+    s = (n - 1) * run;
+    off = u - s_base[n - 1];
+    while (run > 1) {
+      const uint32_t w = units_of(span_of(a, a.lens[s])) * a.HS;
       if (off < w) break;
       off -= w;
       ++s;
     }
   }
   s = __builtin_amdgcn_readfirstlane(s);
-  u = uniform64(u), end = uniform64(end), off = uniform64(off), per = uniform64(per);
+  off = __builtin_amdgcn_readfirstlane(off);
+  u = __builtin_amdgcn_readfirstlane(u), end = __builtin_amdgcn_readfirstlane(end), per = __builtin_amdgcn_readfirstlane(per);
   mk.end(ARGUS_REGION_ATTEND_PLACE);
   mk.begin(ARGUS_REGION_ATTEND_TOKENS);
 
   bool open = false;  // a segment starts here and does not end
   while (u < end) {
-    const Span p = span_of(a, s);
-    const uint32_t units = p.tiles + kPieceCost;
-    const uint32_t hs = (uint32_t)(off / units), o0 = (uint32_t)(off % units);
-    const uint32_t n = end - u < units - o0 ? (uint32_t)(end - u) : units - o0;
+    const Span p = span_of(a, __builtin_amdgcn_readfirstlane(run == 1 ? s_len[s] : a.lens[s]));
+    const uint32_t units = units_of(p);
+    const uint32_t hs = off / units, o0 = off - hs * units;
+    const uint32_t n = end - u < units - o0 ? end - u : units - o0;
     // its cost comes before its tiles
-    const uint32_t t0 = o0 < kPieceCost ? 0 : o0 - kPieceCost, t1 = o0 + n < kPieceCost ? 0 : o0 + n - kPieceCost;
+    const uint32_t a0 = o0 << a.unit_shift, a1 = (o0 + n) << a.unit_shift;
+    const uint32_t t0 = a0 < kPieceCost ? 0 : a0 - kPieceCost;
+    uint32_t t1 = a1 < kPieceCost ? 0 : a1 - kPieceCost;
+    t1 = t1 < p.tiles ? t1 : p.tiles;
     if (t0 < t1) {
       const uint32_t h = hs / a.row_tiles, q0 = (hs % a.row_tiles) * 16 * NQ;
       const uint32_t rows = a.G - q0 < 16u * NQ ? a.G - q0 : 16u * NQ;
@@ -492,9 +578,9 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend_shared(A
       const bool done = t0 == 0 && t1 == p.tiles;
       const uint32_t seg = s * a.HS + hs;
       if (t0 == 0) {
-        const uint64_t last = (u - o0 + units - 1) / per;
+        const uint32_t last = (u - o0 + units - 1) / per;
         if (lane == 0 && (a.by_seg || !done))
-          a.open[a.by_seg ? seg : share] = make_uint4(seg, done ? 1u : share, done ? 0u : (uint32_t)last, 0u);
+          a.open[a.by_seg ? seg : share] = make_uint4(seg, done ? 1u : share, done ? 0u : last, 0u);
         open = !done;
       }
       const uint64_t seg_row = (uint64_t)s * a.H * a.G + (uint64_t)h * a.G + q0;
@@ -530,7 +616,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend_shared(A
     }
     u += n;
     off += n;
-    if (off == (uint64_t)units * a.HS) {
+    if (off == units * a.HS) {
       off = 0;
       ++s;
     }

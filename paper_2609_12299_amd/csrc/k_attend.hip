@@ -36,15 +36,16 @@ int device_ok() {
 
 namespace {
 
-// Waves that share a batch: two blocks of four for each of the 256 compute
-// units, all resident at once (head sizes beyond 128: one), and not so many that
-// joining the pieces of few segments takes longer than they save.
-constexpr uint32_t kShares = 256 * 2 * kWaves, kSharesWide = 256 * kWaves, kSharesOfSegment = 256;
+// Waves that share a batch: one block of four for each of the 256 compute
+// units (twice as many: 731 us against 716 for four sequences of 262143 tokens, 106
+// against 97 for 128 of 1000, 78.6 against 74.5 for the 8-bit batch), and no more
+// of one segment than are soon joined.
+constexpr uint32_t kShares = 256 * kWaves, kSharesOfSegment = 256;
 // Segments of at most this many tiles are not shared: a block each.
 constexpr uint32_t kWholeTiles = 16;
 
 struct Plan {
-  uint32_t dp, nq, row_tiles, hs, shares, segs, grid, opens, join_rows;
+  uint32_t dp, nq, row_tiles, hs, shares, segs, grid, opens, join_rows, unit_shift;
   size_t o_at, open_at, bytes;
 };
 
@@ -78,10 +79,11 @@ int make_plan(const argus_attend_config* c, Plan* p) {
     tiles = w < tiles ? w : tiles;
   }
   p->segs = (uint32_t)segs;
+  p->unit_shift = 0;
+  while (segs * (((tiles + kPieceCost) >> p->unit_shift) + 1) >= (1ull << 31)) ++p->unit_shift;
   uint64_t shares = 0;
   if (tiles > kWholeTiles && segs) {
-    shares = p->dp == 256 ? kSharesWide : kShares;
-    shares = segs * kSharesOfSegment < shares ? segs * kSharesOfSegment : shares;
+    shares = segs * kSharesOfSegment < kShares ? segs * kSharesOfSegment : kShares;
     const uint64_t useful = segs * (tiles + kPieceCost) / kMinShare + 1;
     shares = useful < shares ? useful : shares;
     shares = (shares + kWaves - 1) / kWaves * kWaves;
@@ -122,6 +124,10 @@ extern "C" int argus_decode_attend(const argus_attend_config* cfg, const argus_a
     return refuse(ARGUS_E_INVAL, "a required pointer is NULL");
   if ((rc = check_view(io->k, cfg->cache_type, "k")) != ARGUS_OK || (rc = check_view(io->v, cfg->cache_type, "v")) != ARGUS_OK)
     return rc;
+  for (const argus_page_view* w : {&io->k, &io->v})
+    if (w->page_stride < 0 || w->page_stride > (int64_t)(1ll << 35) || w->token_stride < 0 ||
+        w->token_stride * (int64_t)cfg->page_size > 0x3FFFFFFFll)
+      return refuse(ARGUS_E_CAPACITY, "a page's stride, or its tokens' times page_size, is out of range");
   if (!aligned_to(io->d_q, 16) || io->q_seq_stride % 8 || io->q_head_stride % 8 || !aligned_to(io->d_out, 16) ||
       !aligned_to(io->d_table, 4) || !aligned_to(io->d_lens, 4) || !aligned_to(io->d_k_scale, 4) ||
       !aligned_to(io->d_v_scale, 4) || !aligned_to(io->d_lse, 4))
@@ -145,8 +151,8 @@ extern "C" int argus_decode_attend(const argus_attend_config* cfg, const argus_a
   a.q = (const uint16_t*)io->d_q;
   a.q_seq = io->q_seq_stride, a.q_head = io->q_head_stride;
   a.k = (const uint8_t*)io->k.base, a.v = (const uint8_t*)io->v.base;
-  a.k_page = io->k.page_stride * e, a.k_head = io->k.head_stride * e, a.k_tok = io->k.token_stride * e;
-  a.v_page = io->v.page_stride * e, a.v_head = io->v.head_stride * e, a.v_tok = io->v.token_stride * e;
+  a.k_page = (uint32_t)(io->k.page_stride * e / 16), a.k_head = io->k.head_stride * e, a.k_tok = (uint32_t)(io->k.token_stride * e);
+  a.v_page = (uint32_t)(io->v.page_stride * e / 16), a.v_head = io->v.head_stride * e, a.v_tok = (uint32_t)(io->v.token_stride * e);
   a.table = io->d_table, a.table_stride = io->table_stride, a.lens = io->d_lens;
   a.k_scale = io->d_k_scale, a.v_scale = io->d_v_scale;
   a.out = (uint16_t*)io->d_out, a.lse = io->d_lse;
@@ -157,6 +163,7 @@ extern "C" int argus_decode_attend(const argus_attend_config* cfg, const argus_a
   a.HS = p.hs, a.row_tiles = p.row_tiles;
   a.shift = log2_of(cfg->page_size), a.num_pages = cfg->num_pages, a.columns = cfg->columns;
   a.window = cfg->window, a.sinks = cfg->sinks;
+  a.unit_shift = p.unit_shift;
   a.shares = p.shares, a.by_seg = p.segs <= p.shares, a.scale = cfg->scale;
   a.marks = take_marks(markers, p.grid, per_wave);
   hipStream_t st = (hipStream_t)stream_v;
