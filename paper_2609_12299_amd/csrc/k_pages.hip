@@ -882,8 +882,8 @@ extern "C" int argus_decode_compact(const argus_compact_config* cfg, const argus
     return refuse(ARGUS_E_CAPACITY, "sequences, columns or pages out of range");
   if ((cfg->seqs && (!io->d_table || !io->d_new_table)) || !io->d_refs || !io->d_new_refs || !io->d_map || !io->d_counters)
     return refuse(ARGUS_E_INVAL, "a required pointer is NULL");
-  if ((cfg->seqs && io->d_new_table == io->d_table) || io->d_new_refs == io->d_refs)
-    return refuse(ARGUS_E_INVAL, "the new table and refs are other buffers than the old");
+  if ((cfg->seqs && io->d_new_table == io->d_table) || io->d_new_refs == io->d_refs || io->d_map == io->d_refs || io->d_map == io->d_new_refs)
+    return refuse(ARGUS_E_INVAL, "the new table, refs and map are buffers of their own");
   if (!aligned_to(io->d_table, 4) || !aligned_to(io->d_refs, 4) || !aligned_to(io->d_new_table, 4) ||
       !aligned_to(io->d_new_refs, 4) || !aligned_to(io->d_map, 4) || !aligned_to(io->d_counters, 4))
     return refuse(ARGUS_E_ALIGN, "tables lie on 4 bytes");
