@@ -626,11 +626,11 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend_shared(A
   mk.end(ARGUS_REGION_ATTEND);
 }
 
-// Four rows of a segment that was left in pieces: piece 0 is the second of its
-// first share, piece i the first of share i further on.
-template <int T, int DP, int NQ>
+// Rows of a segment that was left in pieces: piece 0 is the second of its first
+// share, piece i the first of share i further on.
+template <int T, int DP, int NQ, int ROWS>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
-  constexpr uint32_t kRows = 4, kQuads = DP / 4, kParts = kThreads / (kQuads * kRows);
+  constexpr uint32_t kRows = ROWS, kQuads = DP / 4, kParts = kThreads / (kQuads * kRows);
   using Hf = Half<T>;
   __shared__ float s_m[kRows][kParts], s_l[kRows][kParts];
   __shared__ __align__(16) float s_o[kRows][kParts][DP];
@@ -705,8 +705,7 @@ void launch_attend_as(const AttendArgs& a, uint32_t grid, hipStream_t st) {
 }
 
 // The head size rounded up, and as many column tiles as the group needs: two
-// read the cache once for up to 32 query heads (at 256 their registers would
-// spill, and a group beyond 16 reads it again).
+// read the cache once for up to 32 query heads; a group beyond 32 reads it again.
 template <int T, bool F8>
 void launch_attend_type(const AttendArgs& a, uint32_t grid, hipStream_t st) {
   if (a.D <= 64)
@@ -714,21 +713,28 @@ void launch_attend_type(const AttendArgs& a, uint32_t grid, hipStream_t st) {
   else if (a.D <= 128)
     a.G <= 16 ? launch_attend_as<T, F8, 128, 1>(a, grid, st) : launch_attend_as<T, F8, 128, 2>(a, grid, st);
   else
-    launch_attend_as<T, F8, 256, 1>(a, grid, st);
+    a.G <= 16 ? launch_attend_as<T, F8, 256, 1>(a, grid, st) : launch_attend_as<T, F8, 256, 2>(a, grid, st);
+}
+
+template <int T, int ROWS>
+void launch_join_rows(const AttendArgs& a, dim3 grid, hipStream_t st) {
+  const bool two = a.G > 16;
+  const dim3 b(kThreads);
+  if (a.D <= 64) {
+    if (two) hipLaunchKernelGGL((k_attend_join<T, 64, 2, ROWS>), grid, b, 0, st, a);
+    else hipLaunchKernelGGL((k_attend_join<T, 64, 1, ROWS>), grid, b, 0, st, a);
+  } else if (a.D <= 128) {
+    if (two) hipLaunchKernelGGL((k_attend_join<T, 128, 2, ROWS>), grid, b, 0, st, a);
+    else hipLaunchKernelGGL((k_attend_join<T, 128, 1, ROWS>), grid, b, 0, st, a);
+  } else {
+    if (two) hipLaunchKernelGGL((k_attend_join<T, 256, 2, ROWS>), grid, b, 0, st, a);
+    else hipLaunchKernelGGL((k_attend_join<T, 256, 1, ROWS>), grid, b, 0, st, a);
+  }
 }
 
 template <int T>
-void launch_join_type(const AttendArgs& a, dim3 grid, hipStream_t st) {
-  const bool two = a.G > 16;
-  if (a.D <= 64) {
-    if (two) hipLaunchKernelGGL((k_attend_join<T, 64, 2>), grid, dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL((k_attend_join<T, 64, 1>), grid, dim3(kThreads), 0, st, a);
-  } else if (a.D <= 128) {
-    if (two) hipLaunchKernelGGL((k_attend_join<T, 128, 2>), grid, dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL((k_attend_join<T, 128, 1>), grid, dim3(kThreads), 0, st, a);
-  } else {
-    hipLaunchKernelGGL((k_attend_join<T, 256, 1>), grid, dim3(kThreads), 0, st, a);
-  }
+void launch_join_type(const AttendArgs& a, uint32_t rows, dim3 grid, hipStream_t st) {
+  rows == 1 ? launch_join_rows<T, 1>(a, grid, st) : launch_join_rows<T, 4>(a, grid, st);
 }
 
 // One source file each, so that they compile side by side.

@@ -41,11 +41,13 @@ namespace {
 // against 97 for 128 of 1000, 78.6 against 74.5 for the 8-bit batch), and no more
 // of one segment than are soon joined.
 constexpr uint32_t kShares = 256 * kWaves, kSharesOfSegment = 256;
+// A block joins one row where there are so few: more threads for the pieces of each.
+constexpr uint32_t kJoinBlocks = 1024;
 // Segments of at most this many tiles are not shared: a block each.
 constexpr uint32_t kWholeTiles = 16;
 
 struct Plan {
-  uint32_t dp, nq, row_tiles, hs, shares, segs, grid, opens, join_rows, unit_shift;
+  uint32_t dp, nq, row_tiles, hs, shares, segs, grid, opens, join_grid, rows_of_join, unit_shift;
   size_t o_at, open_at, bytes;
 };
 
@@ -67,7 +69,7 @@ int make_plan(const argus_attend_config* c, Plan* p) {
       (uint64_t)c->columns * c->page_size > 0x7FFFFFFFull || c->window > 0x7FFFFFFFu || c->sinks > 0x7FFFFFFFu)
     return refuse(ARGUS_E_CAPACITY, "pages, columns, window or sinks out of range");
   p->dp = c->head_dim <= 64 ? 64u : c->head_dim <= 128 ? 128u : 256u;
-  p->nq = p->dp < 256 && c->group > 16 ? 2u : 1u;
+  p->nq = c->group > 16 ? 2u : 1u;
   p->row_tiles = (c->group + 16 * p->nq - 1) / (16 * p->nq);
   p->hs = c->kv_heads * p->row_tiles;
   const uint64_t segs = (uint64_t)c->seqs * p->hs;
@@ -91,7 +93,9 @@ int make_plan(const argus_attend_config* c, Plan* p) {
   p->shares = (uint32_t)shares;
   p->grid = shares ? p->shares / kWaves : p->segs;
   p->opens = p->shares < p->segs ? p->shares : p->segs;
-  p->join_rows = c->group < 16 * p->nq ? c->group : 16 * p->nq;
+  const uint32_t join_rows = c->group < 16 * p->nq ? c->group : 16 * p->nq;
+  p->rows_of_join = p->opens * join_rows <= kJoinBlocks ? 1 : 4;
+  p->join_grid = (join_rows + p->rows_of_join - 1) / p->rows_of_join;
   const size_t rows = (size_t)shares * 2 * 16 * p->nq;
   p->o_at = up256(rows * 2 * sizeof(float));
   p->open_at = p->o_at + up256(rows * p->dp * sizeof(float));
@@ -139,7 +143,7 @@ extern "C" int argus_decode_attend(const argus_attend_config* cfg, const argus_a
   if (p.bytes && !aligned_to(d_workspace, 256)) return refuse(ARGUS_E_ALIGN, "the workspace lies on 256 bytes");
   if (workspace_bytes < p.bytes)
     return refuse(ARGUS_E_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
-  const uint64_t joins = p.shares ? (uint64_t)p.opens * ((p.join_rows + 3) / 4) : 0;
+  const uint64_t joins = p.shares ? (uint64_t)p.opens * p.join_grid : 0;
   const uint32_t per_wave = 6;  // its own region, and in it the place and the tokens
   const uint64_t records = ((uint64_t)p.grid * per_wave + joins * 2) * kWaves;
   if (!marks_fit(markers, records)) return refuse(ARGUS_E_CAPACITY, "%llu marker records do not fit", (unsigned long long)records);
@@ -171,7 +175,7 @@ extern "C" int argus_decode_attend(const argus_attend_config* cfg, const argus_a
   (f8 ? (bf ? launch_attend_bf16_f8 : launch_attend_fp16_f8) : (bf ? launch_attend_bf16 : launch_attend_fp16))(a, p.grid, st);
   if (p.shares) {
     a.marks = take_marks(markers, joins, 2);
-    (bf ? launch_join_type<0> : launch_join_type<1>)(a, dim3(p.opens, (p.join_rows + 3) / 4), st);
+    (bf ? launch_join_type<0> : launch_join_type<1>)(a, p.rows_of_join, dim3(p.opens, p.join_grid), st);
   }
   return hipGetLastError() == hipSuccess ? ARGUS_OK : refuse(ARGUS_E_HIP, "launch failed");
 }

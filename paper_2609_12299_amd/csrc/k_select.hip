@@ -37,6 +37,7 @@ constexpr uint32_t kList = 128;               // candidates of a wave
 // 16: 50.8, only when half full: 54.4; 96 x 8 rows of 128003 in bf16, k 8).
 constexpr uint32_t kRoom = 8;
 constexpr uint32_t kCands = 512;              // candidates of a group that are ranked by counting
+constexpr uint32_t kFew = 96;                 // and how many are soon ranked
 constexpr uint32_t kMaxK = 64, kMaxBeams = 64;
 
 struct SelectArgs {
@@ -259,6 +260,7 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
   __shared__ uint32_t s_n;
   __shared__ Pick s_cand[kCands];
   __shared__ Pick s_best[kWaves];
+  __shared__ uint64_t s_top[kThreads], s_bound;
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_SELECT_BEAMS);
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, group = blockIdx.x;
@@ -324,37 +326,53 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
     p->first = join64(~w, order_of(score));
     return score > -INFINITY;
   };
-  uint32_t top = 0;
+  uint64_t top = 0;
   for (uint32_t i0 = 0; i0 < total; i0 += kMine * kThreads) {
     if (i0) fetch(i0);
 #pragma unroll
     for (uint32_t c = 0; c < kMine; ++c) {
       Pick p;
-      if (pick_of(c, &p)) {
-        const uint32_t o = (uint32_t)(p.first >> 32);
-        top = o > top ? o : top;
-      }
+      if (pick_of(c, &p)) top = p.first > top ? p.first : top;
     }
   }
-  atomicMax(&s_list[tid & (a.lists - 1)], top);
+  atomicMax(&s_list[tid & (a.lists - 1)], (uint32_t)(top >> 32));
   __syncthreads();
-  uint32_t bound = s_list[lane & (a.lists - 1)];
+  uint32_t least = s_list[lane & (a.lists - 1)];
   for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t o = __shfl_xor(bound, d);
-    bound = o < bound ? o : bound;
+    const uint32_t o = __shfl_xor(least, d);
+    least = o < least ? o : least;
   }
-  for (uint32_t i0 = 0; i0 < total; i0 += kMine * kThreads) {
-    if (total > kMine * kThreads) fetch(i0);
+  uint64_t bound = join64(0u, least);
+  auto collect = [&]() {
+    for (uint32_t i0 = 0; i0 < total; i0 += kMine * kThreads) {
+      if (total > kMine * kThreads) fetch(i0);
 #pragma unroll
-    for (uint32_t c = 0; c < kMine; ++c) {
-      Pick p;
-      if (pick_of(c, &p) && (uint32_t)(p.first >> 32) >= bound) {
-        const uint32_t at = atomicAdd(&s_n, 1u);
-        if (at < kCands) s_cand[at] = p;
+      for (uint32_t c = 0; c < kMine; ++c) {
+        Pick p;
+        if (pick_of(c, &p) && p.first >= bound) {
+          const uint32_t at = atomicAdd(&s_n, 1u);
+          if (at < kCands) s_cand[at] = p;
+        }
       }
     }
+    __syncthreads();
+  };
+  collect();
+  if (s_n > kFew) {
+    // The sets' maxima lie too far apart (one beam ahead of the others, or many
+    // places to fill): the k-th of the threads' own maxima instead.  (Group of 16
+    // beams of 2072, k 32: 100 us a call without this, 20 with it.)
+    s_top[tid] = top;
+    __syncthreads();
+    if (tid == 0) s_n = 0;
+    uint32_t rank = 0;
+#pragma unroll 8
+    for (uint32_t o = 0; o < (uint32_t)kThreads; ++o) rank += s_top[o] > top || (s_top[o] == top && o < tid);
+    if (rank == a.K - 1) s_bound = top;
+    __syncthreads();
+    bound = s_bound;
+    collect();
   }
-  __syncthreads();
   const uint32_t n = s_n;
   auto put = [&](uint32_t r, const Pick& p) {
     const uint32_t w = ~(uint32_t)p.first;
