@@ -3,17 +3,16 @@
 // k_select_rows reads the logits once.  A wave takes a part of one row, 64 lanes
 // of 32 elements at a time, the next ones under way while it looks at them, and
 // keeps the sum of their exponentials and a list of candidates in LDS.  The
-// least that a candidate needs is known after the first step: of `lists` >= k
-// disjoint sets of lanes, the least of the sets' maxima has k elements at or
-// above it, and few more (about lists * ln(lists)).  From then on a step costs a
-// comparison of each lane's largest value; where some are above, the step's elements
+// least that a candidate needs is known after the first step: the k-th largest of
+// the lanes' maxima has k elements at or above it, and few more.  From then on a
+// step costs a comparison of each lane's largest value; where some are above, the step's elements
 // go to LDS and the wave looks through those of the lanes in question.  When the
 // list is half full, it is cut to its first k, and what the k-th has becomes the
 // least: the list never overflows, however many values are equal.
 //
 // k_select_beams, one block per group of beams, joins the parts' sums to the
-// rows' logarithms and picks among the rows' candidates by the same sets of
-// maxima, ranking those above by counting.
+// rows' logarithms and picks among the rows' candidates in the same way: the k-th
+// largest of the threads' maxima, and those at or above it ranked by counting.
 //
 // What bounds it: the reading of the logits, and the exponential of each (a
 // quarter of the rate of other instructions).
@@ -37,7 +36,6 @@ constexpr uint32_t kList = 128;               // candidates of a wave
 // 16: 50.8, only when half full: 54.4; 96 x 8 rows of 128003 in bf16, k 8).
 constexpr uint32_t kRoom = 8;
 constexpr uint32_t kCands = 512;              // candidates of a group that are ranked by counting
-constexpr uint32_t kFew = 96;                 // and how many are soon ranked
 constexpr uint32_t kMaxK = 64, kMaxBeams = 64;
 
 struct SelectArgs {
@@ -50,7 +48,8 @@ struct SelectArgs {
   uint8_t* new_finished;
   float2* sums;     // [rows][parts] c, sum of 2^(x log2 e - c)
   uint64_t* cands;  // [rows][parts][k] (value, token) as a key, 0: none; no order
-  uint32_t W, V, K, parts, lists;
+  uint32_t W, V, K, parts;
+  FastDiv by_group, by_row;  // by W * parts, by parts
   uint32_t steps;   // of a part
   uint32_t rows;
   int32_t eos;
@@ -72,9 +71,26 @@ ARGUS_DEV float of_word(uint32_t w, int half) {
   return (float)__builtin_bit_cast(_Float16, (uint16_t)(half ? w >> 16 : w));
 }
 
+// The largest value of the wave, without LDS.
 ARGUS_DEV float wave_max(float v) {
-  for (int d = 1; d < 64; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+  auto step = [&](auto ctrl, auto rows) {
+    const int o = __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), ctrl(), rows(), 0xF, false);
+    v = fmaxf(v, __builtin_bit_cast(float, o));
+  };
+#define ARGUS_K(x) []() constexpr { return x; }
+  step(ARGUS_K(kDppRowShr + 1), ARGUS_K(0xF));
+  step(ARGUS_K(kDppRowShr + 2), ARGUS_K(0xF));
+  step(ARGUS_K(kDppRowShr + 4), ARGUS_K(0xF));
+  step(ARGUS_K(kDppRowShr + 8), ARGUS_K(0xF));
+  step(ARGUS_K(kDppBcast15), ARGUS_K(0xA));
+  step(ARGUS_K(kDppBcast31), ARGUS_K(0xC));
+#undef ARGUS_K
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+ARGUS_DEV uint32_t wave_max_u32(uint32_t v) {
+  // (unsigned order as that of signed numbers, whose least the wave's helpers find)
+  const int32_t x = (int32_t)(~v ^ 0x80000000u);
+  return ~((uint32_t)rows_min32(row_min32(x)) ^ 0x80000000u);
 }
 ARGUS_DEV float wave_sum(float v) {
   for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
@@ -123,7 +139,7 @@ __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
       __builtin_amdgcn_wave_barrier();
       const uint64_t k0 = lane < n ? list[lane] : 0, k1 = lane + 64 < n ? list[lane + 64] : 0;
       uint32_t r0 = 0, r1 = 0;
-#pragma unroll 4
+#pragma unroll 8
       for (uint32_t i = 0; i < n; ++i) {
         const uint64_t o = list[i];
         r0 += o > k0;
@@ -188,15 +204,12 @@ __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
       for (uint32_t i = 0; i < kItems; ++i) part_sum[i % 4] += __builtin_amdgcn_exp2f(fmaf(x[i], m1, -c1));
       sum += (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
       if (step == 0) {
-        uint32_t lo = order_of(top);
-        for (uint32_t d = a.lists; d < 64; d <<= 1) {
-          const uint32_t o = __shfl_xor(lo, d);
-          lo = o > lo ? o : lo;
-        }
-        for (uint32_t d = 1; d < a.lists; d <<= 1) {
-          const uint32_t o = __shfl_xor(lo, d);
-          lo = o < lo ? o : lo;
-        }
+        // the k-th largest of the lanes' maxima: the least that fewer than k are above
+        const uint32_t mine = order_of(top);
+        uint32_t above = 0;
+#pragma unroll 16
+        for (int i = 0; i < 64; ++i) above += (uint32_t)__builtin_amdgcn_readlane((int)mine, i) > mine;
+        const uint32_t lo = ~wave_max_u32(above < a.K ? ~mine : 0u);
         least_value = value_of(lo);
         least = join64(0u, lo);  // below every key of this value
       }
@@ -256,16 +269,16 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
   constexpr uint32_t kMine = 4;  // candidates that a thread holds at a time
   __shared__ float s_lse[kMaxBeams], s_score[kMaxBeams];
   __shared__ uint32_t s_done[kMaxBeams];
-  __shared__ uint32_t s_list[kMaxK];
   __shared__ uint32_t s_n;
   __shared__ Pick s_cand[kCands];
   __shared__ Pick s_best[kWaves];
-  __shared__ uint64_t s_top[kThreads], s_bound;
+  __shared__ uint64_t s_top[kWaves][64], s_bound;
+  __shared__ uint32_t s_tops[kWaves];
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_SELECT_BEAMS);
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, group = blockIdx.x;
   // Candidate i: the i / parts-th of the list of part i % parts (of the whole
-  // group), so that each set of threads has candidates of all ranks.
+  // group), so that the first of all parts lie in threads of their own.
   const uint32_t parts = a.W * a.parts, total = parts * a.K;
   const uint64_t* cands = a.cands + (uint64_t)group * total;
   uint64_t key[kMine];
@@ -274,7 +287,7 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
 #pragma unroll
     for (uint32_t c = 0; c < kMine; ++c) {
       const uint32_t i = i0 + c * kThreads + tid;
-      const uint32_t r = i / parts, j = i - r * parts, w = j / a.parts;
+      const uint32_t r = divide(i, a.by_group), j = i - r * parts, w = divide(j, a.by_row);
       key[c] = i < total ? cands[(uint64_t)j * a.K + r] : 0;
       beam[c] = i < total ? w | (r == 0 && j == w * a.parts ? 256u : 0u) : 0xFFFFu;
     }
@@ -306,8 +319,10 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
       s_done[w] = done;
     }
   }
-  if (tid < a.lists) s_list[tid] = 0;
-  if (tid == 0) s_n = 0;
+  if (tid == 0) {
+    s_n = 0;
+    s_bound = ~0ull;
+  }
   __syncthreads();
   // What fetch() has brought, as a place in the order; false: no candidate.
   auto pick_of = [&](uint32_t c, Pick* p) {
@@ -335,44 +350,39 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
       if (pick_of(c, &p)) top = p.first > top ? p.first : top;
     }
   }
-  atomicMax(&s_list[tid & (a.lists - 1)], (uint32_t)(top >> 32));
+  // The k-th largest of these: in each wave those that fewer than k are above, then
+  // of all such.  (What one of a wave's others is above, k of that wave are above.)
+  uint32_t above = 0;
+#pragma unroll 16
+  for (int i = 0; i < 64; ++i)
+    above += join64((uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)top, i),
+                    (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(top >> 32), i)) > top;
+  const uint64_t mine = __ballot(above < a.K);
+  if (above < a.K) s_top[wave][__popcll(mine & lanemask_lt())] = top;
+  if (lane == 0) s_tops[wave] = (uint32_t)__popcll(mine);
   __syncthreads();
-  uint32_t least = s_list[lane & (a.lists - 1)];
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t o = __shfl_xor(least, d);
-    least = o < least ? o : least;
+  if (above < a.K) {
+    above = 0;
+    for (uint32_t w = 0; w < (uint32_t)kWaves; ++w) {
+#pragma unroll 4
+      for (uint32_t o = 0; o < s_tops[w]; ++o) above += s_top[w][o] > top;
+    }
+    if (above < a.K) atomicMin((unsigned long long*)&s_bound, (unsigned long long)top);
   }
-  uint64_t bound = join64(0u, least);
-  auto collect = [&]() {
-    for (uint32_t i0 = 0; i0 < total; i0 += kMine * kThreads) {
-      if (total > kMine * kThreads) fetch(i0);
+  __syncthreads();
+  const uint64_t bound = s_bound;
+  for (uint32_t i0 = 0; i0 < total; i0 += kMine * kThreads) {
+    if (total > kMine * kThreads) fetch(i0);
 #pragma unroll
-      for (uint32_t c = 0; c < kMine; ++c) {
-        Pick p;
-        if (pick_of(c, &p) && p.first >= bound) {
-          const uint32_t at = atomicAdd(&s_n, 1u);
-          if (at < kCands) s_cand[at] = p;
-        }
+    for (uint32_t c = 0; c < kMine; ++c) {
+      Pick p;
+      if (pick_of(c, &p) && p.first >= bound) {
+        const uint32_t at = atomicAdd(&s_n, 1u);
+        if (at < kCands) s_cand[at] = p;
       }
     }
-    __syncthreads();
-  };
-  collect();
-  if (s_n > kFew) {
-    // The sets' maxima lie too far apart (one beam ahead of the others, or many
-    // places to fill): the k-th of the threads' own maxima instead.  (Group of 16
-    // beams of 2072, k 32: 100 us a call without this, 20 with it.)
-    s_top[tid] = top;
-    __syncthreads();
-    if (tid == 0) s_n = 0;
-    uint32_t rank = 0;
-#pragma unroll 8
-    for (uint32_t o = 0; o < (uint32_t)kThreads; ++o) rank += s_top[o] > top || (s_top[o] == top && o < tid);
-    if (rank == a.K - 1) s_bound = top;
-    __syncthreads();
-    bound = s_bound;
-    collect();
   }
+  __syncthreads();
   const uint32_t n = s_n;
   auto put = [&](uint32_t r, const Pick& p) {
     const uint32_t w = ~(uint32_t)p.first;
@@ -394,7 +404,7 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
     for (uint32_t c = tid; c < n; c += kThreads) {
       const Pick p = s_cand[c];
       uint32_t rank = 0;
-#pragma unroll 4
+#pragma unroll 8
       for (uint32_t o = 0; o < n; ++o) rank += before(s_cand[o], p);
       if (rank < a.K) put(rank, p);
     }
@@ -439,8 +449,15 @@ struct Plan {
   size_t cands_at, bytes;
 };
 
-// Waves that read the logits, all resident at once where there are so many steps.
-constexpr uint32_t kRowWaves = 256 * 4 * 4;
+// Waves that read the logits (4096 and 2048: 49.1 and 51.3 us against 46.7 for 96 x
+// 8 rows of 128003 in bf16).
+constexpr uint32_t kRowWaves = 3072;
+// More parts make shorter work of the rows and longer work of the group's
+// candidates: parts of one step where those stay below kGroupCands (2 x 8 rows of
+// 18641 in fp16, k 16: 17.6 us against 20.8 with three steps), else longer ones (8 x 8
+// rows of 128003 in fp32, k 8: 22.3 us with four steps against 28.8 with one), up to
+// kLongPart.
+constexpr uint32_t kGroupCands = 2048, kLongPart = 16;
 
 int make_plan(const argus_select_config* c, Plan* p) {
   if (!c) return refuse(ARGUS_E_INVAL, "no configuration");
@@ -453,7 +470,11 @@ int make_plan(const argus_select_config* c, Plan* p) {
   const uint64_t rows = (uint64_t)c->groups * c->beams;
   const uint32_t steps = (c->vocab + kStep - 1) / kStep;
   const uint64_t parts = rows ? kRowWaves / rows : 1;
-  p->parts = parts < 1 ? 1u : parts < steps ? (uint32_t)parts : steps;
+  uint32_t most = kGroupCands / (c->beams * c->k);
+  most = most < steps ? most : steps;
+  const uint32_t some = (steps + kLongPart - 1) / kLongPart;
+  most = most < some ? some : most;
+  p->parts = parts < 1 ? 1u : parts < most ? (uint32_t)parts : most;
   p->steps = (steps + p->parts - 1) / p->parts;
   p->parts = (steps + p->steps - 1) / p->steps;
   const uint64_t jobs = rows * p->parts;
@@ -510,8 +531,7 @@ extern "C" int argus_decode_select(const argus_select_config* cfg, const argus_s
   a.cands = (uint64_t*)((char*)d_workspace + p.cands_at);
   a.W = cfg->beams, a.V = cfg->vocab, a.K = cfg->k, a.parts = p.parts, a.eos = cfg->eos;
   a.steps = p.steps, a.rows = cfg->groups * cfg->beams;
-  a.lists = 1;
-  while (a.lists < a.K) a.lists <<= 1;
+  a.by_group = fast_div(a.W * a.parts), a.by_row = fast_div(a.parts);
   hipStream_t st = (hipStream_t)stream_v;
   a.marks = take_marks(markers, grid, 2);
   if (cfg->type == ARGUS_BF16) hipLaunchKernelGGL(k_select_rows<ARGUS_BF16>, dim3(grid), dim3(kThreads), 0, st, a);
