@@ -72,7 +72,8 @@ enum { ARGUS_BF16 = 0, ARGUS_FP16 = 1, ARGUS_FP32 = 2, ARGUS_FP8 = 3 /* e4m3, no
 
 /* One side (keys or values) of a paged cache of one layer: token t of page p,
  * head h, element d lies at base[p * page_stride + h * head_stride +
- * t * token_stride + d].  Base and strides are multiples of 16 bytes. */
+ * t * token_stride + d].  Base and strides are multiples of 16 bytes; for
+ * attend page_stride is 0..2^35 and page_size * token_stride below 2^30. */
 typedef struct argus_page_view {
   void* base;
   int64_t page_stride, head_stride, token_stride;

@@ -192,10 +192,11 @@ constexpr uint32_t kPageItems = 16;  // pages of a thread
 static_assert(kPageItems * kThreads == kPageTile, "a tile per block");
 // Calls of at most so many table entries and pages are planned by one block of
 // kSmallThreads, in one launch instead of three (step) or two (compact).  16
-// beams of 64 columns over 1024 pages: 19 us a call against 27; 512 of 256 over
-// 16384 pages by one block 311 against 25.  Compacting 640 pages: 17 us against
-// 22; 16384 pages by one block 235 against 229.
-constexpr uint32_t kSmallEntries = 4096, kSmallPages = 4096;
+// beams of 64 columns over 1024 pages: 19 us a call against 26 (15 us on the GPU
+// against 13, and less to launch); 56 of 51: 23.6 against 23.9, 22 us on the GPU; 512 of
+// 256 over 16384 pages by one block 311 against 25.  Compacting 640 pages: 17 us
+// against 22; 16384 pages by one block 235 against 229.
+constexpr uint32_t kSmallEntries = 2048, kSmallPages = 4096;
 constexpr uint32_t kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
 
 // Bit i: page p0 + i is in the pool and has (LIVE) or has not any reference.
@@ -652,6 +653,14 @@ int take_caches(const argus_page_planes* in, uint32_t n, Caches* out) {
   return ARGUS_OK;
 }
 
+// Blocks for the copies of at most n pages.
+uint32_t copy_blocks_for(const Caches& all, uint32_t n) {
+  uint64_t chunks = 0;
+  for (uint32_t i = 0; i < all.n; ++i) chunks += (uint64_t)n * all.c[i].planes * ((all.c[i].units + 255) / 256);
+  const uint64_t blocks = (chunks + kWaves - 1) / kWaves;
+  return blocks < kCopyBlocks ? (uint32_t)blocks : kCopyBlocks;
+}
+
 struct StepLayout {
   size_t best, lasts, ends, base, copies, free_list, words, state, bytes;
 };
@@ -811,7 +820,7 @@ extern "C" int argus_decode_step(const argus_step_config* cfg, const argus_step_
   const uint32_t tiles = (a.N + kPageTile - 1) / kPageTile;
   uint32_t clear = (a.N + kThreads - 1) / kThreads;
   clear = clear > 1024 ? 1024 : clear;
-  const uint32_t copy_blocks = a.caches.n && a.S ? kCopyBlocks : 0;
+  const uint32_t copy_blocks = copy_blocks_for(a.caches, a.S);
   hipStream_t st = (hipStream_t)stream_v;
   if ((uint64_t)a.S * a.P <= kSmallEntries && a.N <= kSmallPages) {
     // (the block's waves write their markers as those of four blocks)
@@ -907,7 +916,7 @@ extern "C" int argus_decode_compact(const argus_compact_config* cfg, const argus
   a.page_blocks = (a.N + kThreads - 1) / kThreads;
   const uint64_t entries = (uint64_t)a.S * a.P;
   a.row_blocks = (uint32_t)((entries + 4 * kThreads - 1) / (4 * kThreads));
-  const uint32_t copy_blocks = a.caches.n ? kCopyBlocks : 0;
+  const uint32_t copy_blocks = copy_blocks_for(a.caches, a.N / 2);
   const uint32_t moves = a.page_blocks + a.row_blocks + copy_blocks;
   const bool small = a.N <= kSmallPages;
   const uint64_t blocks = small ? (uint64_t)kSmallWaves / kWaves + moves : 2ull * a.tiles + moves;

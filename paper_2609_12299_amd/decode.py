@@ -179,7 +179,8 @@ def _t():
         _types.update({torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32,
                        torch.float8_e4m3fn: FP8})
         # (the handle alone: a tenth of the time of a stream object)
-        _raw_stream = torch._C._cuda_getCurrentRawStream
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                              lambda index: torch.cuda.current_stream(index).cuda_stream)
         _torch = torch
     return _torch
 
@@ -281,6 +282,8 @@ class _on:
 
 def _elsewhere(stream, dev) -> bool:
     """Whether the call leaves the current stream or device."""
+    if dev.type != "cuda":
+        _bad(f"tensors on a GPU, not on {dev}")
     return stream is not None or dev.index != _torch.cuda.current_device()
 
 

@@ -43,7 +43,7 @@ def attend(q, k, v, table, lens, scale, window=0, sinks=0, k_scale=None, v_scale
                 lse[s, h] = top + math.log(p.sum()) if top > -np.inf else -np.inf
                 # a score's error: its products and their sum (the products of 16-bit numbers are exact), then
                 # scale, k_scale and log2 e; a weight's: of its exponent, the exponential, and its two parts (2^-16)
-                dx = ((D + 2) * EPS * (np.abs(kh) @ np.abs(q64[s, h])) * scale + 6 * EPS * np.abs(x) + 4 * EPS * abs(top)).max()
+                dx = ((D + 2) * EPS * (np.abs(kh) @ np.abs(q64[s, h])) * abs(scale) + 6 * EPS * np.abs(x) + 4 * EPS * abs(top)).max()
                 rel = 2 * dx + 2.0 ** -16 + 2 * (len(at) + 16) * EPS
                 mean = (p[:, None] * np.abs(vh)).sum(0) / p.sum()
                 tol_o[s, h] = kinds * 1.01 * np.abs(o) + rel * mean + 2.0 ** -25

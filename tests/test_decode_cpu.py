@@ -289,3 +289,17 @@ def test_wrappers_check_types_and_shapes():
         decode._planes((pool,) * 5, 5, dev, out)
     m = MarkerBuffer(100, ctx_base=7, region_base=20, device="cpu")
     assert m.used == 0 and m.records().shape == (0, 16)
+
+
+def test_tensors_on_the_cpu_are_refused():
+    import torch
+
+    from paper_2609_12299_amd import ArgusError, append_tokens, attend_pages, compact_pages, select_beams, step_pages
+    q, c = torch.zeros(1, 4, 64, dtype=torch.bfloat16), torch.zeros(3, 2, 16, 64, dtype=torch.bfloat16)
+    one = torch.zeros(1, dtype=torch.int32)
+    tab = torch.zeros(1, 2, dtype=torch.int32)
+    for call in (lambda: attend_pages(q, c, c, tab, one), lambda: append_tokens(q[:, :2], q[:, :2], c, c, tab, one),
+                 lambda: step_pages(tab, one, None, None, 16, num_pages=3), lambda: compact_pages(tab, one),
+                 lambda: select_beams(torch.zeros(1, 2, 50), torch.zeros(1, 2), 2)):
+        with pytest.raises(ArgusError, match="on a GPU"):
+            call()

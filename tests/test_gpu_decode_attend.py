@@ -194,6 +194,60 @@ def test_weights_far_apart():
         check(a, run(a), kind)
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1e-33, 1e31, 40.0, -40.0])
+def test_scales(scale):
+    """None, negative ones, and such that the differences of scores have to come before the exponential."""
+    log(f"[gpu] attend scale {scale}")
+    for kind in ("bf16", "fp16"):
+        a = make(kind, [1, 100, 333], 2, 4, 64, 16, seed=9)
+        a["scale"] = scale
+        if abs(scale) > 1:  # scores a few units apart
+            a["q"] = (a["q"].float() / abs(scale)).to(a["q"].dtype) if scale < 1e30 else a["q"] * 0
+        check(a, run(a), f"{kind} {scale}")
+
+
+def test_scores_beyond_a_million():
+    """The maximum lies where a product's rounding would show in a weight."""
+    log("[gpu] attend far scores")
+    a = make("bf16", [400, 400], 1, 2, 64, 16, columns=40, junk=False)
+    k, t = a["k_cache"], a["table"]
+    a["q"] = torch.zeros_like(a["q"])
+    a["q"][:, :, 0], a["q"][:, :, 1] = 1.0, 1.0
+    a["scale"] = 1.0
+    for s, big in ((0, 2.0 ** 22), (1, -2.0 ** 30)):
+        for j in range(400):
+            row = torch.zeros(64)
+            row[0], row[1] = big, float(j % 4) / 2 if s == 0 else 0.0
+            k[t[s, j // 16], :, j % 16] = row.to(torch.bfloat16)
+    got = run(a)
+    w = torch.exp(torch.arange(400) % 4 / 2.0).double()
+    v = a["v_cache"]
+    for s, weights in ((0, w), (1, torch.ones(400).double())):
+        vv = torch.stack([v[t[s, j // 16], 0, j % 16] for j in range(400)]).double()
+        want = (weights[:, None] * vv).sum(0) / weights.sum()
+        # scores of 2^22 hold halves exactly
+        off = (got["out"][s].double().cpu() - want).abs()
+        assert (off <= 2.0 ** -8 * 1.01 * want.abs() + 2.0 ** -14 * vv.abs().mean()).all(), off.max()
+
+
+def test_tables_of_more_than_2_31_units():
+    """Work is shared out in groups of tiles where all tables could hold so much."""
+    log("[gpu] attend huge tables")
+    from paper_2609_12299_amd import attend_pages
+    H, ps, D, S, P = 64, 32, 8, 64, 1 << 20
+    a = make("bf16", [0, 1, 3000, 95, 700, 33], H, 1, D, ps, columns=96, junk=False)
+    g = on_gpu(a)
+    table = torch.full((S, P), -1, dtype=torch.int32, device="cuda")
+    table[:6, :96] = g["table"]
+    lens = torch.zeros(S, dtype=torch.int32, device="cuda")
+    lens[:6] = g["lens"]
+    q = torch.zeros((S, H, D), dtype=torch.bfloat16, device="cuda")
+    q[:6] = g["q"]
+    got = attend_pages(q, g["k_cache"], g["v_cache"], table, lens, scale=a["scale"], lse=True)
+    check(a, dict(out=got["out"][:6], lse=got["lse"][:6]), "huge tables")
+    assert (got["out"][6:] == 0).all() and (got["lse"][6:] == -math.inf).all()
+
+
 def test_strided_inputs():
     log("[gpu] attend strides")
     from paper_2609_12299_amd import attend_pages
