@@ -250,6 +250,9 @@ ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint
         if (!EXACT && !in) w.k[i][f] = (u32x4)(0u);
       }
     }
+    // Values are read once, whole lines at a time: not kept in the caches (four sequences
+    // of 262143 tokens 636 us against 707, 128 of 1000 86 against 95).  A load of keys
+    // takes half a line of 16 rows, and the other half has to be there for the next.
     uint32_t b = c * (VD * 4);
     if (!EXACT && b >= a.D * (F8 ? 1u : 2u)) b = 0;  // rows of O beyond the head size: not written
 #pragma unroll
@@ -259,12 +262,12 @@ ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint
       if constexpr (VD == 1) {
         w.v[i][0] = *reinterpret_cast<const uint32_t*>(r);
       } else if constexpr (VD == 2) {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(r);
+        const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(r));
         w.v[i][0] = x.x, w.v[i][1] = x.y;
       } else {
 #pragma unroll
         for (int j = 0; j < VD / 4; ++j) {
-          const u32x4 x = *reinterpret_cast<const u32x4*>(r + 16 * j);
+          const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(r + 16 * j));
           w.v[i][4 * j] = x.x, w.v[i][4 * j + 1] = x.y, w.v[i][4 * j + 2] = x.z, w.v[i][4 * j + 3] = x.w;
         }
       }
