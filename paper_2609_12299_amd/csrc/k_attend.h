@@ -7,24 +7,35 @@
 //   P = exp(S^T * c - m)                         c = scale * k_scale, m per column
 //   O^T[d][q] += V^T[d][token] P^T[token][q]     mfma 16x16x32
 //
-// The result of the first product leaves lane (q = l % 16, g = l / 16) with the
-// tokens 16 h + 4 g + r (h < 2, r < 4): eight tokens of its column.  The
-// contraction of the second product may run over the tokens in any order as
-// long as both operands agree, so these eight registers are its operand as
-// they are, and V is read in that order: lane (c, g) loads of the same eight
-// tokens the VW = DP / 16 elements from c * VW on (16 lanes read a whole row),
-// and 16-bit halves are then exchanged between registers.  Nothing goes through
-// LDS but the joining of the block's waves.
+// Which token stands in which row of a product is free, and so is the order of the
+// contractions, as long as both operands agree.  Row m = 4 g + r of a half of 16
+// tokens is token place(m) = 8 (r / 2) + 2 g + r % 2, which makes every load below
+// fall into one run of eight tokens, that is one page: its address is a scalar
+// base and an offset per lane that never changes.
+//
+// The first product leaves lane (q = l % 16, g = l / 16) with rows 4 g + r of its
+// column, and the second takes these eight registers as they are; V is read to
+// match: lane (c, g) loads of token place(4 g + r) the VW = DP / 16 elements from
+// c * VW on (16 lanes read a whole row), and 16-bit halves are then exchanged between
+// registers.  K is wanted with 16 rows by 4 lanes each, which would read a part of
+// 16 lines at a time.  So eight lanes read a run of 128 bytes of a row, eight rows per
+// load, and lanes l and l ^ 2 trade places (in registers) for the rows of the other
+// eight.  Nothing goes through LDS but the joining of a block's waves.
 //
 // What bounds it: the reading of the cache.  A tile of 32 tokens by 128
 // elements is 16 KiB of bf16 and takes 24 matrix instructions of 16 cycles (P is
 // taken as the sum of two 16-bit numbers, so that its rounding is not seen in
-// the result).
+// the result), a third of the time that its bytes take.  Every byte is read once,
+// by loads of whole lines, past the caches.  Measured: four sequences of 262143
+// tokens, 8 x 8 heads of 128 in bf16, 4.3 GB: 645 us, 6.7 TB/s (with keys read by
+// 16 rows x 64 bytes the same; values through the caches 707); 48 sequences of up to 32768
+// tokens in 8 bits 65 us, 5.2 TB/s (73 before the keys' rows were read whole).
 //
 // Shares: the units of work are the tiles (groups of 2^unit_shift tiles, where
 // there could be more than 2^31) of all (sequence, head) segments one after the
-// other, kPieceCost tiles more for each segment, and wave w takes units [w * per, (w + 1) * per) whatever the lengths are (they are known on the
-// device alone): a batch of one long and many short sequences loads all compute
+// other, kPieceCost tiles more for each segment, and wave w takes units
+// [w * per, (w + 1) * per) whatever the lengths are (they are known on the device
+// alone): a batch of one long and many short sequences loads all compute
 // units alike, and the short ones' latencies lie side by side.  A segment that lies
 // in one share is finished there; of the others each wave leaves its piece (m, l,
 // O in 32 bits), and k_attend_join joins them in the order of the shares: results
@@ -55,7 +66,7 @@ struct AttendArgs {
   int64_t q_seq, q_head;
   const uint8_t *k, *v;
   int64_t k_head, v_head;               // bytes
-  uint32_t k_page, v_page;              // 16 bytes
+  int64_t k_page, v_page;               // bytes
   uint32_t k_tok, v_tok;                // bytes
   const int32_t* table;
   int64_t table_stride;
@@ -161,6 +172,13 @@ constexpr float kFar = 1e6f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 ARGUS_DEV float exp_of(float x) { return exp2f(x * kLog2e); }
 
+// Whether the rows of the next tile are loaded while one is taken: where a tile is small
+// and the registers hold two (8 bits, head size 128: 65 us against 73 for 48
+// sequences of up to 32768 tokens; 16 bits: spilled, 890 against 645 for four
+// of 262143).
+template <bool F8, int DP, int NQ>
+constexpr bool kAhead = DP == 64 || (F8 && DP == 128 && NQ == 1);
+
 // One wave's part of a segment: O, maxima and sums of tiles t0, t0 + dt, ... < t1
 // for the 16 NQ query rows from q0 on.  T: type of q, out and the products; F8:
 // the cache holds e4m3; DP: head size rounded up to 64, 128 or 256; NQ: 16-wide
@@ -169,15 +187,16 @@ template <int T, bool F8, int DP, int NQ, bool EXACT>
 ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint32_t h, uint32_t q0, uint32_t rows,
                             uint32_t t0, uint32_t t1, uint32_t dt, f32x4 (&acc)[NQ][DP / 16], float (&m)[NQ],
                             float (&l)[NQ]) {
-  constexpr int KF = DP / 32;               // fragments of a key row
-  constexpr int KL = F8 ? DP / 64 : DP / 32;  // 16-byte loads of a key row by the 4 lanes that share it
-  constexpr int VW = DP / 16;               // elements of a value row per lane
-  constexpr int VD = VW * (F8 ? 1 : 2) / 4;   // in 32-bit words
-  constexpr int VH = VW / 2;                // 16-bit pairs per lane
-  // Small tiles leave too little under way with one at a time (64 sequences of up to
-  // 16384 tokens, head size 64: fp8 38 us against 48, bf16 56 against 58); for larger
-  // ones the rows of two would not fit the registers.
-  constexpr bool AHEAD = DP == 64;
+  constexpr int ES = F8 ? 1 : 2;             // bytes of an element of the cache
+  constexpr int KF = DP / 32;                // fragments of a key row
+  constexpr int CB = F8 && DP == 64 ? 8 : 16;  // bytes of a key row that a lane loads at a time
+  constexpr int CE = CB / ES;                // elements
+  constexpr int CW = CB / 4;                 // words
+  constexpr int KL = DP * ES / (8 * CB);     // loads of a key row by the 8 lanes that share it
+  constexpr int VW = DP / 16;                // elements of a value row per lane
+  constexpr int VD = VW * ES / 4;            // in 32-bit words
+  constexpr int VH = VW / 2;                 // 16-bit pairs per lane
+  constexpr bool AHEAD = kAhead<F8, DP, NQ>;
   using Hf = Half<T>;
   const uint32_t lane = threadIdx.x & 63u, c = lane & 15u, g = lane >> 4;
   const float kc = a.scale * (a.k_scale ? a.k_scale[h] : 1.0f), kd = fabsf(kc);
@@ -189,7 +208,8 @@ ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint
     const uint16_t* qr = a.q + (int64_t)s * a.q_seq + (int64_t)(h * a.G + q0 + (row < rows ? row : 0)) * a.q_head;
 #pragma unroll
     for (int f = 0; f < KF; ++f) {
-      const uint32_t d = F8 ? 64 * (f / 2) + 16 * g + 8 * (f % 2) : 32 * f + 8 * g;
+      // fragment (n, h, e) holds, of load n, elements 8 e ... of the lane's chunk 2 g + h
+      const uint32_t e = f % (CE / 8), hn = f / (CE / 8), d = (hn / 2 * 8 + 2 * g + hn % 2) * CE + 8 * e;
       qf[i][f] = row < rows && d < a.D ? *reinterpret_cast<const u32x4*>(qr + d) : (u32x4)(0u);
       if (kc < 0.0f) qf[i][f] ^= 0x80008000u;  // so that the largest product is the largest score
     }
@@ -213,74 +233,88 @@ ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint
   const float kd2 = kd * kLog2e;
   bool far = !(kd > 1e-30f && kd < 1e30f);  // scores so large, or a scale so odd, that the differences come first
 
-  // The pages of tile t's rows: of the lane's two keys, and of its two runs of four values.
+  // What a lane adds to the scalar base of a load: of the keys, token w of eight and
+  // chunk 2 g + part of its row; of the values, token 2 g and its elements.
+  const uint32_t part = c >> 1 & 1u, w8 = 2 * (c >> 2) + (c & 1u);
+  uint32_t k_at[EXACT ? 1 : KL], v_at;
+#pragma unroll
+  for (int n = 0; n < (EXACT ? 1 : KL); ++n) {
+    const uint32_t b = (8 * n + 2 * g + part) * CB;
+    k_at[n] = w8 * a.k_tok + (EXACT || b < a.D * ES ? b : a.D * ES - CB);
+  }
+  v_at = c * (VD * 4);
+  if (!EXACT && v_at >= a.D * ES) v_at = 0;  // rows of O beyond the head size: not written
+  v_at += 2 * g * a.v_tok;
+
+  // The pages of tile t's four runs of eight tokens (scalar loads).
   struct Ids {
-    int32_t k[2], v[2];
+    int32_t p[4];
   };
+  typedef const __attribute__((address_space(4))) int32_t* scalar_ptr;
+  const scalar_ptr tab_s = (scalar_ptr)(uintptr_t)tab;
   auto token_of = [&](uint32_t t) { return (t < p.sink_tiles ? t : t - p.sink_tiles + p.first) * kTile; };
   auto find = [&](uint32_t t, Ids& ids) {
     const uint32_t tok = token_of(t < t1 ? t : t1 - 1);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t kcol = (tok + 16 * i + c) >> a.shift, vcol = (tok + 16 * i + 4 * g) >> a.shift;
-      const int32_t kp = tab[kcol < a.columns ? kcol : 0], vp = tab[vcol < a.columns ? vcol : 0];
-      ids.k[i] = kcol < a.columns ? kp : -1;
-      ids.v[i] = vcol < a.columns ? vp : -1;
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t col = (tok + 8 * j) >> a.shift;
+      const int32_t page = tab_s[col < a.columns ? col : 0];
+      ids.p[j] = col < a.columns && (uint32_t)page < a.num_pages ? page : -1;
     }
   };
   // Its rows, and which of the lane's eight tokens are visible.  (A page that is not
   // held: any row, what comes of it is not taken.)
   struct Rows {
-    u32x4 k[2][KL];
+    uint32_t k[2][2][KL][CW];
     uint32_t v[8][VD];
     uint32_t vis;
   };
   auto load = [&](uint32_t t, const Ids& ids, Rows& w) {
     const uint32_t tok = token_of(t);
-    bool held = true;
+    // All of it is read once, whole lines at a time: past the caches.
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t page = (uint32_t)ids.k[i] < a.num_pages ? (uint32_t)ids.k[i] : 0u;
-      const uint8_t* r = kb + ((uint64_t)page * a.k_page << 4) + ((tok + 16 * i + c) & in_page) * a.k_tok;
+    for (int j = 0; j < 4; ++j) {
+      const int64_t page = ids.p[j] < 0 ? 0 : ids.p[j];
+      const uint8_t* base = kb + page * a.k_page + (uint64_t)((tok + 8 * j) & in_page) * a.k_tok;
 #pragma unroll
-      for (int f = 0; f < KL; ++f) {
-        const uint32_t d = 64 * f + 16 * g;  // byte of the row
-        const bool in = EXACT || d < a.D * (F8 ? 1u : 2u);
-        w.k[i][f] = *reinterpret_cast<const u32x4*>(r + (in ? d : 0u));
-        if (!EXACT && !in) w.k[i][f] = (u32x4)(0u);
+      for (int n = 0; n < KL; ++n) {
+        const uint8_t* r = base + k_at[EXACT ? 0 : n] + (EXACT ? n * 8 * CB : 0);
+        uint32_t(&to)[CW] = w.k[j / 2][j % 2][n];
+        if constexpr (CW == 2) {
+          const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(r));
+          to[0] = x.x, to[1] = x.y;
+        } else {
+          const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(r));
+          to[0] = x.x, to[1] = x.y, to[2] = x.z, to[3] = x.w;
+        }
       }
     }
-    // Values are read once, whole lines at a time: not kept in the caches (four sequences
-    // of 262143 tokens 636 us against 707, 128 of 1000 86 against 95).  A load of keys
-    // takes half a line of 16 rows, and the other half has to be there for the next.
-    uint32_t b = c * (VD * 4);
-    if (!EXACT && b >= a.D * (F8 ? 1u : 2u)) b = 0;  // rows of O beyond the head size: not written
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t page = (uint32_t)ids.v[i / 4] < a.num_pages ? (uint32_t)ids.v[i / 4] : 0u;
-      const uint8_t* r = vb + ((uint64_t)page * a.v_page << 4) + (((tok + 16 * (i / 4) + 4 * g) & in_page) * a.v_tok + b) + i % 4 * a.v_tok;
+    for (int i = 0; i < 8; ++i) {  // half i / 4, r = i % 4
+      const int j = i / 2;           // run of eight tokens
+      const int64_t page = ids.p[j] < 0 ? 0 : ids.p[j];
+      const uint8_t* r = vb + page * a.v_page + (uint64_t)(((tok + 8 * j) & in_page) + i % 2) * a.v_tok + v_at;
       if constexpr (VD == 1) {
-        w.v[i][0] = *reinterpret_cast<const uint32_t*>(r);
+        w.v[i][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(r));
       } else if constexpr (VD == 2) {
         const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(r));
         w.v[i][0] = x.x, w.v[i][1] = x.y;
       } else {
 #pragma unroll
-        for (int j = 0; j < VD / 4; ++j) {
-          const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(r + 16 * j));
-          w.v[i][4 * j] = x.x, w.v[i][4 * j + 1] = x.y, w.v[i][4 * j + 2] = x.z, w.v[i][4 * j + 3] = x.w;
+        for (int j4 = 0; j4 < VD / 4; ++j4) {
+          const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(r + 16 * j4));
+          w.v[i][4 * j4] = x.x, w.v[i][4 * j4 + 1] = x.y, w.v[i][4 * j4 + 2] = x.z, w.v[i][4 * j4 + 3] = x.w;
         }
       }
-      held = held && (uint32_t)ids.v[i / 4] < a.num_pages;
     }
     // which of the lane's eight tokens are visible
     w.vis = 0xFFu;
-    if (!F8 || tok < p.lo || tok + kTile > p.len || !__all(held)) {
+    if (tok < p.lo || tok + kTile > p.len || (ids.p[0] | ids.p[1] | ids.p[2] | ids.p[3]) < 0) {
       w.vis = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint32_t at = tok + 16 * (i / 4) + 4 * g + i % 4;
-        const bool in = at < p.len && (at >= p.lo || at < p.sinks) && (uint32_t)ids.v[i / 4] < a.num_pages;
+        const uint32_t at = tok + 8 * (i / 2) + 2 * g + i % 2;
+        const bool in = at < p.len && (at >= p.lo || at < p.sinks) && ids.p[i / 2] >= 0;
         w.vis |= in ? 1u << i : 0u;
       }
     }
@@ -299,18 +333,31 @@ ARGUS_DEV void attend_tiles(const AttendArgs& a, const Span& p, uint32_t s, uint
 #pragma unroll
     for (int i = 0; i < NQ; ++i) sc[i][0] = sc[i][1] = (f32x4)(0.0f);
 #pragma unroll
-    for (int f = 0; f < KF; ++f) {
+    for (int hn = 0; hn < 2 * KL; ++hn) {  // load n = hn / 2, chunk 2 g + hn % 2
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) {
-        u32x4 kf;
-        if constexpr (F8) {
-          const uint32_t w0 = w.k[hh][f / 2][2 * (f % 2)], w1 = w.k[hh][f / 2][2 * (f % 2) + 1];
-          kf = (u32x4){widen<T>(w0, false), widen<T>(w0, true), widen<T>(w1, false), widen<T>(w1, true)};
-        } else {
-          kf = w.k[hh][f];
+        // of the first eight tokens for the lanes of part 0, of the others for those of part 1
+        uint32_t x[CW];
+#pragma unroll
+        for (int i = 0; i < CW; ++i) {
+          const uint32_t lo = w.k[hh][0][hn / 2][i], hi = w.k[hh][1][hn / 2][i];
+          // (moved before it is chosen: under a condition the lanes read would be off)
+          const uint32_t moved = dpp32<kDppQuad2301>(hn % 2 == 0 ? hi : lo);
+          x[i] = hn % 2 == 0 ? (part ? moved : lo) : (part ? hi : moved);
+          if (!EXACT && (hn / 2 * 8 + 2 * g + hn % 2) * CE >= a.D) x[i] = 0;  // (what stood there may be NaN)
         }
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) sc[i][hh] = Hf::mfma(kf, qf[i][f], sc[i][hh]);
+        for (int e = 0; e < CE / 8; ++e) {
+          u32x4 kf;
+          if constexpr (F8) {
+            kf = (u32x4){widen<T>(x[2 * e], false), widen<T>(x[2 * e], true), widen<T>(x[2 * e + 1], false),
+                         widen<T>(x[2 * e + 1], true)};
+          } else {
+            kf = (u32x4){x[0], x[1], x[2], x[3]};
+          }
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) sc[i][hh] = Hf::mfma(kf, qf[i][hn * (CE / 8) + e], sc[i][hh]);
+        }
       }
     }
 

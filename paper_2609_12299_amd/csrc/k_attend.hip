@@ -37,9 +37,11 @@ int device_ok() {
 namespace {
 
 // Waves that share a batch: one block of four for each of the 256 compute
-// units (twice as many: 731 us against 716 for four sequences of 262143 tokens, 106
-// against 97 for 128 of 1000, 78.6 against 74.5 for the 8-bit batch), and no more
-// of one segment than are soon joined.
+// units (twice as many: 655 us against 645 for four sequences of 262143 tokens, 92
+// against 85 for 128 of 1000, 69 against 65 for the 8-bit batch), and no more
+// of one segment than are soon joined.  Two blocks where a tile's rows are so short
+// that one wave for each SIMD has too few bytes under way: of 64 bytes (64 sequences of up to
+// 16384 tokens in 8 bits: 35 us against 41; of 128 bytes 49.7 against 48.1).
 constexpr uint32_t kShares = 256 * kWaves, kSharesOfSegment = 256;
 // A block joins one row where there are so few: more threads for the pieces of each.
 constexpr uint32_t kJoinBlocks = 1024;
@@ -85,7 +87,8 @@ int make_plan(const argus_attend_config* c, Plan* p) {
   while (segs * (((tiles + kPieceCost) >> p->unit_shift) + 1) >= (1ull << 31)) ++p->unit_shift;
   uint64_t shares = 0;
   if (tiles > kWholeTiles && segs) {
-    shares = segs * kSharesOfSegment < kShares ? segs * kSharesOfSegment : kShares;
+    shares = p->dp * type_bytes(c->cache_type) <= 64 ? 2 * kShares : kShares;
+    shares = segs * kSharesOfSegment < shares ? segs * kSharesOfSegment : shares;
     const uint64_t useful = segs * (tiles + kPieceCost) / kMinShare + 1;
     shares = useful < shares ? useful : shares;
     shares = (shares + kWaves - 1) / kWaves * kWaves;
@@ -155,8 +158,8 @@ extern "C" int argus_decode_attend(const argus_attend_config* cfg, const argus_a
   a.q = (const uint16_t*)io->d_q;
   a.q_seq = io->q_seq_stride, a.q_head = io->q_head_stride;
   a.k = (const uint8_t*)io->k.base, a.v = (const uint8_t*)io->v.base;
-  a.k_page = (uint32_t)(io->k.page_stride * e / 16), a.k_head = io->k.head_stride * e, a.k_tok = (uint32_t)(io->k.token_stride * e);
-  a.v_page = (uint32_t)(io->v.page_stride * e / 16), a.v_head = io->v.head_stride * e, a.v_tok = (uint32_t)(io->v.token_stride * e);
+  a.k_page = io->k.page_stride * e, a.k_head = io->k.head_stride * e, a.k_tok = (uint32_t)(io->k.token_stride * e);
+  a.v_page = io->v.page_stride * e, a.v_head = io->v.head_stride * e, a.v_tok = (uint32_t)(io->v.token_stride * e);
   a.table = io->d_table, a.table_stride = io->table_stride, a.lens = io->d_lens;
   a.k_scale = io->d_k_scale, a.v_scale = io->d_v_scale;
   a.out = (uint16_t*)io->d_out, a.lse = io->d_lse;
