@@ -39,14 +39,19 @@ namespace {
 // Waves that share a batch: one block of four for each of the 256 compute
 // units (twice as many: 655 us against 645 for four sequences of 262143 tokens, 92
 // against 85 for 128 of 1000, 69 against 65 for the 8-bit batch), and no more
-// of one segment than are soon joined.  Two blocks where a tile's rows are so short
+// of one segment than are soon joined (one of 131072 tokens, 1 x 8 heads of 128: 36 us
+// with 256, 33 with 512).  Two blocks where a tile's rows are so short
 // that one wave for each SIMD has too few bytes under way: of 64 bytes (64 sequences of up to
 // 16384 tokens in 8 bits: 35 us against 41; of 128 bytes 49.7 against 48.1).
-constexpr uint32_t kShares = 256 * kWaves, kSharesOfSegment = 256;
-// A block joins one row where there are so few: more threads for the pieces of each.
+constexpr uint32_t kShares = 256 * kWaves, kSharesOfSegment = 512;
+// A block joins one row where there are so few: more threads for the pieces of each
+// (a sequence of 32768 tokens, 1 x 8 heads of 128: 19 us against 29 by four rows; 96
+// of up to 8192, 8 x 4 heads: 75 by four rows, 77 by one).
 constexpr uint32_t kJoinBlocks = 1024;
-// Segments of at most this many tiles are not shared: a block each.
-constexpr uint32_t kWholeTiles = 16;
+// Segments of at most this many tiles are not shared: a block each, and no joining
+// (64 sequences of 512 tokens, 8 x 4 heads of 128: 23 us against 30 shared; of 1024 tokens 45
+// against 52, and 4 of them 14.7 both; at head size 256, 4 of 1024: 34 against 25).
+uint32_t whole_tiles(uint32_t dp) { return dp == 256 ? 16u : 32u; }
 
 struct Plan {
   uint32_t dp, nq, row_tiles, hs, shares, segs, grid, opens, join_grid, rows_of_join, unit_shift;
@@ -86,7 +91,7 @@ int make_plan(const argus_attend_config* c, Plan* p) {
   p->unit_shift = 0;
   while (segs * (((tiles + kPieceCost) >> p->unit_shift) + 1) >= (1ull << 31)) ++p->unit_shift;
   uint64_t shares = 0;
-  if (tiles > kWholeTiles && segs) {
+  if (tiles > whole_tiles(p->dp) && segs) {
     shares = p->dp * type_bytes(c->cache_type) <= 64 ? 2 * kShares : kShares;
     shares = segs * kSharesOfSegment < shares ? segs * kSharesOfSegment : shares;
     const uint64_t useful = segs * (tiles + kPieceCost) / kMinShare + 1;

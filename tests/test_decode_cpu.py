@@ -131,10 +131,11 @@ def test_attend_workspace_sizes(dec):
                                                        w=0, s=0, scale=1.0, pad=0), **kw}[k] for k in
                                                  ("v", "q", "c", "seqs", "h", "g", "d", "ps", "n", "cols", "w", "s", "scale", "pad")])
     size = lambda **kw: dec.argus_decode_attend_workspace_bytes(cfg(**kw))
-    assert size() == 0 and size(cols=33) > 0 and size(cols=4096, w=400) == 0
+    assert size() == 0 and size(cols=64) == 0 and size(cols=65) > 0 and size(cols=4096, w=400) == 0
+    assert size(d=256) == 0 and size(cols=33, d=256) > 0
     most = 1024 * 2 * 32 * (128 + 2) * 4 + 1024 * 16 + 1024
     for seqs in (1, 7, 300, 1 << 20):
-        for cols in (33, 4096, 1 << 26):
+        for cols in (65, 4096, 1 << 26):
             assert 0 < size(seqs=seqs, cols=cols, g=32, d=128) <= most
     assert size(seqs=0, cols=4096) == 0
 

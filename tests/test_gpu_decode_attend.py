@@ -115,6 +115,16 @@ def test_shared_over_blocks(lens, kind, D, G):
     check(a, run(a), f"{lens[:4]} {kind}")
 
 
+@pytest.mark.parametrize("kind,q_kind", [("bf16", None), ("fp16", None), ("fp8", "bf16"), ("fp8", "fp16")])
+@pytest.mark.parametrize("D", [16, 64, 80, 96, 128, 144, 256])
+@pytest.mark.parametrize("columns", [64, 130])
+def test_head_sizes_over_longer_tables(kind, q_kind, D, columns):
+    """A block per sequence up to 1024 tokens, shared over the waves beyond; 8 bits and 16, whole rows and parts."""
+    log(f"[gpu] attend {kind} {q_kind} D={D} columns {columns}")
+    a = make(kind, [1, 997, 0, 17, 513, columns * 16], 2, 5, D, 16, q_kind, columns=columns, window=0 if D % 32 else 900, sinks=3)
+    check(a, run(a), f"{kind} {D} {columns}")
+
+
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 4), (33, 64), (100, 5), (128, 31), (5000, 7), (64, 5000)])
 @pytest.mark.parametrize("columns", [20, 200])
 def test_window_and_sinks(window, sinks, columns):
