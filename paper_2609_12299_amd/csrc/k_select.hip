@@ -46,7 +46,7 @@ struct SelectArgs {
   float* new_scores;
   int32_t *parents, *tokens;
   uint8_t* new_finished;
-  float2* sums;     // [rows][parts] c, sum of 2^(x log2 e - c)
+  float2* sums;     // [rows][parts] place (place_of), sum
   uint64_t* cands;  // [rows][parts][k] (value, token) as a key, 0: none; no order
   uint32_t W, V, K, parts;
   FastDiv by_group, by_row;  // by W * parts, by parts
@@ -99,7 +99,14 @@ ARGUS_DEV float wave_sum(float v) {
 
 // How far a value may rise above the reference of the exponentials.
 constexpr float kSlack = 8.0f;
-constexpr float kLarge = 1e37f;
+// An exponential is 2^(x log2 e - c1), one multiply-add; from references of this size
+// on the rounding of c1 would show in that, and the difference comes first.
+constexpr float kFar = 1e6f;
+// Where a sum stands: half of c1, or the reference itself from kFar on, so that these
+// numbers are in the references' order (c1 / 2 is at most 0.73 kFar).
+ARGUS_DEV float place_of(float ref, float c1) { return fabsf(ref) < kFar ? 0.5f * c1 : ref; }
+// What a sum at place p is worth at place q >= p.
+ARGUS_DEV float moved(float p, float q) { return __builtin_amdgcn_exp2f((p - q) * (fabsf(q) < kFar ? 2.0f : kLog2e)); }
 
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
@@ -161,19 +168,17 @@ __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
       if (want) list[n + (uint32_t)__popcll(take & lanemask_lt())] = key;
       n += (uint32_t)__popcll(take);
     };
-    // The sum is of 2^(x m1 - c1), about exp(x - ref).  c is c1, or ref itself where
-    // that is so large that times log2 e it might overflow: then all that counts
-    // is which values equal it.
-    float ref = -INFINITY, c = -INFINITY, m1 = kLog2e, c1 = 0.0f, sum = 0.0f;
+    // The sum is of 2^(x log2 e - c1), about exp(x - ref).
+    float ref = -INFINITY, c = -INFINITY, c1 = 0.0f, sum = 0.0f;
+    bool far = false;
     auto refer = [&](float to) {
       ref = to;
       if (ref == -INFINITY) return;
-      const bool fine = fabsf(ref) < kLarge;
-      m1 = fine ? kLog2e : 0x1p-20f;
-      c1 = ref * m1;
+      far = fabsf(ref) >= kFar;
+      c1 = ref * kLog2e;
       const float was = c;
-      c = fine ? c1 : ref;
-      sum *= was == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(was - c);
+      c = place_of(ref, c1);
+      sum *= was == -INFINITY ? 0.0f : moved(was, c);
     };
     if (part == 0) {  // what lies before and behind the vectors: at most 2 * (kPer - 1) elements
       const uint32_t j = lane < kPer ? lane : tail + lane - kPer;
@@ -184,7 +189,7 @@ __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
         else x = of_word<TYPE>(*reinterpret_cast<const uint16_t*>(base + (uint64_t)j * kBytes), 0);
       }
       refer(wave_max(x));
-      sum = __builtin_amdgcn_exp2f(fmaf(x, m1, -c1));
+      sum = __builtin_amdgcn_exp2f(far ? (x - ref) * kLog2e : fmaf(x, kLog2e, -c1));
       append(x > -INFINITY, key_of(x, j));
     }
     auto look = [&](uint32_t step, const u32x4 (&w)[kVecs]) {
@@ -201,8 +206,13 @@ __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
       for (uint32_t i = 1; i < kItems; ++i) top = fmaxf(top, x[i]);
       if (__any(top > ref + kSlack)) refer(fmaxf(ref, wave_max(top)));
       float part_sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (!far) {
 #pragma unroll
-      for (uint32_t i = 0; i < kItems; ++i) part_sum[i % 4] += __builtin_amdgcn_exp2f(fmaf(x[i], m1, -c1));
+        for (uint32_t i = 0; i < kItems; ++i) part_sum[i % 4] += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, -c1));
+      } else {
+#pragma unroll
+        for (uint32_t i = 0; i < kItems; ++i) part_sum[i % 4] += __builtin_amdgcn_exp2f((x[i] - ref) * kLog2e);
+      }
       sum += (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
       if (step == 0) {
         // the k-th largest of the lanes' maxima: the least that fewer than k are above
@@ -268,7 +278,7 @@ ARGUS_DEV bool before(const Pick& x, const Pick& y) { return x.first > y.first |
 
 __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
   constexpr uint32_t kMine = 4;  // candidates that a thread holds at a time
-  __shared__ float s_lse[kMaxBeams], s_score[kMaxBeams];
+  __shared__ float s_lse[kMaxBeams], s_rest[kMaxBeams], s_score[kMaxBeams];
   __shared__ uint32_t s_done[kMaxBeams];
   __shared__ uint32_t s_n;
   __shared__ Pick s_cand[kCands];
@@ -304,18 +314,22 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
         const float2 v = a.sums[(uint64_t)row * a.parts + c];
         const float most = fmaxf(top, v.x);
         // (a part without a value leaves 0, a NaN stays)
-        sum = sum * (top == -INFINITY ? 1.0f : exp2f(top - most)) + v.y * (v.x == -INFINITY ? 1.0f : exp2f(v.x - most));
+        sum = sum * (top == -INFINITY ? 1.0f : moved(top, most)) + v.y * (v.x == -INFINITY ? 1.0f : moved(v.x, most));
         top = most;
       }
     }
     for (int d = 1; d < 16; d <<= 1) {
       const float o = __shfl_xor(top, d), os = __shfl_xor(sum, d), most = fmaxf(top, o);
-      sum = sum * (top == -INFINITY ? 1.0f : exp2f(top - most)) + os * (o == -INFINITY ? 1.0f : exp2f(o - most));
+      sum = sum * (top == -INFINITY ? 1.0f : moved(top, most)) + os * (o == -INFINITY ? 1.0f : moved(o, most));
       top = most;
     }
     if (tid % 16 == 0) {
-      // (the difference of top to its 32 bits times ln 2 would show: in 64 bits)
-      s_lse[w] = fabsf(top) < kLarge ? (float)(((double)top + (double)log2f(sum)) * 0.69314718055994530942) : top + logf(sum);
+      // The logarithm, taken off a logit in two steps: of one number near 10^6 the rounding
+      // would show, and 10^10 leaves no place for the sum's.
+      // (What lies in the sum has kLog2e's rounding in its exponents, and so has top.)
+      const double lse = 2.0 * (double)top * (1.0 / (double)kLog2e) + (double)log2f(sum) * 0.69314718055994530942;
+      s_lse[w] = fabsf(top) < kFar ? (float)lse : top;
+      s_rest[w] = fabsf(top) < kFar ? (float)(lse - (double)(float)lse) : logf(sum);
       s_score[w] = score;
       s_done[w] = done;
     }
@@ -337,7 +351,7 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
     } else {
       p->key = key[c];
       if (p->key == 0) return false;
-      score = s_score[w] + (value_of((uint32_t)(p->key >> 32)) - s_lse[w]);
+      score = s_score[w] + (value_of((uint32_t)(p->key >> 32)) - s_lse[w] - s_rest[w]);
     }
     p->first = join64(~w, order_of(score));
     return score > -INFINITY;
@@ -469,6 +483,7 @@ int make_plan(const argus_select_config* c, Plan* p) {
   if (c->vocab < 1 || c->vocab > (1u << 24)) return refuse(ARGUS_E_INVAL, "vocab %u (1..2^24)", c->vocab);
   if (c->groups > (1u << 20)) return refuse(ARGUS_E_CAPACITY, "groups %u", c->groups);
   const uint64_t rows = (uint64_t)c->groups * c->beams;
+  if (rows > (uint64_t)kMaxBlocks * kWaves) return refuse(ARGUS_E_CAPACITY, "groups %u x beams %u", c->groups, c->beams);
   const uint32_t steps = (c->vocab + kStep - 1) / kStep;
   const uint64_t parts = rows ? kRowWaves / rows : 1;
   uint32_t most = kGroupCands / (c->beams * c->k);

@@ -150,8 +150,8 @@ def select(logits, scores, k, finished=None, eos=-1):
             row = x[g, w]
             with np.errstate(all="ignore"):
                 top = row.max()
-                lse = top + np.log(np.exp(row - top).sum())
-                val = base + (row - lse)
+                # (in this order: at 10^30 top + log has no place for the logarithm, in 64 bits either)
+                val = base + ((row - top) - np.log(np.exp(row - top).sum()))
             ok = np.nonzero(val > -np.inf)[0]
             best = ok[np.lexsort((ok, -row[ok]))][:k]
             cands += [(-val[t], w, -row[t], int(t)) for t in best]

@@ -144,3 +144,22 @@ def test_rows_beyond_32_bits():
     got = select_beams(x, torch.zeros((G, W), device="cuda"), 2)
     assert (got["tokens"] == torch.tensor([77, V - 1], device="cuda")).all()
     assert torch.equal(got["parents"].cpu(), torch.arange(2 * G).reshape(G, 2).int())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+def test_logits_of_any_size(kind):
+    """Rows of one value, of one that stands out, and rows whose parts lie far apart: the logarithm of
+    the sum is as good for values of 10^36 as for those of 10."""
+    log(f"[gpu] select sizes of logits {kind}")
+    sizes = [3.0, 9e4, 5e5, 9.9e5, 1.1e6, 1e9, 1e10, 3e30, 8e36, 1.5e37, 3e38]
+    V = 20000
+    x = torch.zeros(2 * len(sizes) + 1, 2, V)
+    for i, c in enumerate(sizes):
+        x[2 * i], x[2 * i + 1] = c, -c
+        x[2 * i:2 * i + 2, 1, V - 3] += c / 64
+    x[-1, 0], x[-1, 1] = 100.0, -2e6
+    x[-1, 0, V - 3] = 2e6
+    x[-1, 1, :300] = -5.0
+    x = x.to(TYPES[kind])
+    s = torch.tensor([-1.0, -4.0 / 3.0]).repeat(len(x), 1)
+    check(x, s, 6)
