@@ -142,7 +142,8 @@ typedef struct argus_append_config {
   uint32_t page_size;    /* a power of two, 8..65536 */
   uint32_t num_pages;
   uint32_t columns;
-  uint32_t rows;         /* 0..2^31 - 1; seqs where d_offsets is NULL */
+  uint32_t rows;         /* seqs where d_offsets is NULL; 0..2^24 - 1, and to 2^28 - 16 where a row's
+                            keys and values take at most 1024 bytes of the cache */
 } argus_append_config;
 
 typedef struct argus_append_io {
@@ -281,7 +282,7 @@ int argus_decode_compact(const argus_compact_config* cfg, const argus_compact_io
 typedef struct argus_select_config {
   uint32_t abi_version;
   uint32_t type;          /* ARGUS_BF16, ARGUS_FP16, ARGUS_FP32 */
-  uint32_t groups, beams; /* 0..2^20; 1..64 */
+  uint32_t groups, beams; /* 0..2^20; 1..64; below 2^26 rows in all */
   uint32_t vocab;         /* 1..2^24 */
   uint32_t k;             /* 1..64 */
   int32_t eos;            /* < 0: none (finished beams then have token eos as it is) */

@@ -14,6 +14,7 @@ namespace decode {
 
 constexpr int kThreads = 256;  // of a block, where nothing else is said
 constexpr int kWaves = kThreads / 64;
+constexpr uint32_t kMaxBlocks = (1u << 24) - 1;  // of kThreads: a launch has less than 2^32 threads
 
 // ---------------------------------------------------------------- markers
 

@@ -91,7 +91,7 @@ int make_plan(const argus_attend_config* c, Plan* p) {
   p->unit_shift = 0;
   while (segs * (((tiles + kPieceCost) >> p->unit_shift) + 1) >= (1ull << 31)) ++p->unit_shift;
   uint64_t shares = 0;
-  if (tiles > whole_tiles(p->dp) && segs) {
+  if ((tiles > whole_tiles(p->dp) || segs > kMaxBlocks) && segs) {
     shares = p->dp * type_bytes(c->cache_type) <= 64 ? 2 * kShares : kShares;
     shares = segs * kSharesOfSegment < shares ? segs * kSharesOfSegment : shares;
     const uint64_t useful = segs * (tiles + kPieceCost) / kMinShare + 1;

@@ -738,6 +738,7 @@ extern "C" int argus_decode_append(const argus_append_config* cfg, const argus_a
   a.tokens = cfg->rows >= 4096 ? 1024 / per_token : 1;
   a.tokens = a.tokens < 1 ? 1 : a.tokens > kMaxTokens ? kMaxTokens : a.tokens;
   const uint32_t blocks = (cfg->rows + a.tokens - 1) / a.tokens;
+  if (blocks > kMaxBlocks) return refuse(ARGUS_E_CAPACITY, "%u rows in one call", cfg->rows);
   if (!marks_fit(markers, (uint64_t)blocks * kWaves * 2)) return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
   if (cfg->rows == 0 || cfg->seqs == 0) return ARGUS_OK;
   if ((rc = device_ok()) != ARGUS_OK) return rc;

@@ -3,8 +3,11 @@
 The functions named ``argus_decode_*`` are one-to-one wrappers (argument
 marshalling only).  The others take torch CUDA tensors: they check what the C
 side cannot see (types, shapes, devices), allocate outputs and the workspace,
-and enqueue on the current torch stream or the one given.  Every step of the
-computation runs in the HIP kernels of libargus_attr.so; there is no fallback.
+and enqueue on the current torch stream or the one given.  A stream that is given is
+not made to wait for the current one, nor the current one for it: the order of their
+work is the caller's, and what a call returns is valid once its stream has come that
+far.  Every step of the computation runs in the HIP kernels of libargus_attr.so; there
+is no fallback.
 """
 from __future__ import annotations
 
@@ -240,6 +243,8 @@ def _planes(caches, num_pages: int, dev, out) -> None:
                 run *= n
         p = out[i]
         p.base, p.plane_stride, p.page_stride = c.data_ptr(), st[0] * e, st[1] * e
+        if run * e >= 1 << 32:
+            _bad(f"caches[{i}]: a page of {run * e} bytes")
         p.planes, p.page_bytes = shape[0], run * e
 
 
@@ -267,11 +272,16 @@ class MarkerBuffer:
 
 class _on:
     """A call on another stream than the current one, or on another device: allocations belong to
-    that stream, so that the allocator hands their memory on in its order."""
+    that stream, so that the allocator hands their memory on in its order, and the memory of
+    the tensors that the call uses is not handed on before the stream is done with them."""
 
-    def __init__(self, stream, dev):
+    def __init__(self, stream, dev, *used):
         t = _torch
         self.ctx = t.cuda.stream(stream) if stream is not None else t.cuda.device(dev)
+        if stream is not None:
+            for x in used:
+                if x is not None and x.is_cuda:
+                    x.record_stream(stream)
 
     def __enter__(self):
         return self.ctx.__enter__()
@@ -305,6 +315,10 @@ def _done(rc: int, call: str) -> None:
         raise ArgusError(rc, f"{call}: {argus_decode_last_error()}")
 
 
+def _buffer(markers):
+    return None if markers is None else markers.buffer
+
+
 def _marks(markers):
     return None if markers is None else ctypes.byref(markers.c)
 
@@ -325,7 +339,7 @@ def attend_pages(q, k_cache, v_cache, table, lens, scale: float | None = None, w
     t = _t()
     dev = q.device
     if _elsewhere(stream, dev):
-        with _on(stream, dev):
+        with _on(stream, dev, q, k_cache, v_cache, table, lens, k_scale, v_scale, out, _buffer(markers)):
             return attend_pages(q, k_cache, v_cache, table, lens, scale, window, sinks, k_scale, v_scale, lse,
                                 out, markers)
     qs = q.stride()
@@ -379,7 +393,7 @@ def append_tokens(new_k, new_v, k_cache, v_cache, table, starts, offsets=None, k
     _t()
     dev = k_cache.device
     if _elsewhere(stream, dev):
-        with _on(stream, dev):
+        with _on(stream, dev, new_k, new_v, k_cache, v_cache, table, starts, offsets, k_scale, v_scale, _buffer(markers)):
             return append_tokens(new_k, new_v, k_cache, v_cache, table, starts, offsets, k_scale, v_scale, markers)
     ks, vs = new_k.stride(), new_v.stride()
     k, v = _view(k_cache, "k_cache", dev), _view(v_cache, "v_cache", dev)
@@ -418,7 +432,7 @@ def step_pages(table, lens, parents, grow, page_size: int, held=None, num_pages:
     t = _t()
     dev = table.device
     if _elsewhere(stream, dev):
-        with _on(stream, dev):
+        with _on(stream, dev, table, lens, parents, grow, held, *caches, _buffer(markers)):
             return step_pages(table, lens, parents, grow, page_size, held, num_pages, caches, window, sinks, markers)
     if num_pages is None:
         if held is None and len(caches) == 0:
@@ -455,7 +469,7 @@ def compact_pages(table, refs, caches=(), markers=None, stream=None) -> dict:
     t = _t()
     dev = table.device
     if _elsewhere(stream, dev):
-        with _on(stream, dev):
+        with _on(stream, dev, table, refs, *caches, _buffer(markers)):
             return compact_pages(table, refs, caches, markers)
     tab, tab_stride = _table(table, "table", dev)
     S, P = table.shape
@@ -488,7 +502,7 @@ def select_beams(logits, scores, k: int, finished=None, eos: int = -1, markers=N
     t = _t()
     dev = logits.device
     if _elsewhere(stream, dev):
-        with _on(stream, dev):
+        with _on(stream, dev, logits, scores, finished, _buffer(markers)):
             return select_beams(logits, scores, k, finished, eos, markers)
     lt = _type(logits, (BF16, FP16, FP32), "logits")
     ls = logits.stride()

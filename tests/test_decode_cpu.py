@@ -304,3 +304,32 @@ def test_tensors_on_the_cpu_are_refused():
                  lambda: select_beams(torch.zeros(1, 2, 50), torch.zeros(1, 2), 2)):
         with pytest.raises(ArgusError, match="on a GPU"):
             call()
+
+
+def test_launches_stay_within_their_limits(dec):
+    """Calls of more threads than a launch can have: refused, or in another form."""
+    many = dec.argus_append_config(dec.ABI_VERSION, 0, 0, 1, 1, 8, 8, 10, 10, 1 << 29)
+    io = dec.argus_append_io(FAKE, FAKE, 8, 8, 8, 8, view(dec), view(dec), FAKE, 10, FAKE, FAKE, None, None)
+    assert dec.argus_decode_append(many, io, None, None) == -4  # ARGUS_E_CAPACITY
+    assert "rows" in dec.argus_decode_last_error()
+    cfg = dec.argus_select_config(dec.ABI_VERSION, 0, 1 << 20, 64, 8, 1, -1, 0)
+    assert dec.argus_decode_select_workspace_bytes(cfg) == (1 << 64) - 1
+    cfg.beams = 32
+    assert dec.argus_decode_select_workspace_bytes(cfg) < 1 << 40
+    # 2^24 segments of one page: shared out, as a block for each would be too many
+    a = dec.argus_attend_config(dec.ABI_VERSION, 0, 0, 1 << 20, 8, 1, 8, 8, 10, 1, 0, 0, 1.0, 0)
+    assert dec.argus_decode_attend_workspace_bytes(a) == 0
+    a.kv_heads = 16
+    assert 0 < dec.argus_decode_attend_workspace_bytes(a) < 1 << 32
+
+
+def test_page_bytes_beyond_32_bits():
+    torch = pytest.importorskip("torch")
+    from paper_2609_12299_amd import decode
+    from paper_2609_12299_amd.attr import ArgusError
+    out = (decode.argus_page_planes * decode.MAX_CACHES)()
+    fine, wide = (torch.empty((1, 2, n), dtype=torch.uint8, device="meta") for n in ((1 << 32) - 16, 1 << 32))
+    decode._planes([fine], 2, fine.device, out)
+    assert out[0].page_bytes == (1 << 32) - 16
+    with pytest.raises(ArgusError):
+        decode._planes([wide], 2, wide.device, out)

@@ -325,3 +325,23 @@ def test_no_sequences():
     a = on_gpu(make("bf16", [5], 2, 4, 64, 16))
     a.update(q=a["q"][:0], table=a["table"][:0], lens=a["lens"][:0])
     assert attend_pages(**a, lse=True)["out"].shape == (0, 8, 64)
+
+
+def test_more_segments_than_blocks():
+    """2^24 sequences by heads: more than a launch of a block each could have."""
+    from paper_2609_12299_amd import attend_pages
+    log("[gpu] attend 2^24 segments")
+    S, H, N, D = 1 << 20, 16, 1000, 8
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    v = torch.randn((N, H, 8, D), generator=gen, device="cuda").bfloat16()
+    k = torch.randn((N, H, 8, D), generator=gen, device="cuda").bfloat16()
+    q = torch.randn((S, H, D), generator=gen, device="cuda").bfloat16()
+    table = torch.randint(0, N, (S, 1), generator=gen, device="cuda").int()
+    lens = torch.ones(S, dtype=torch.int32, device="cuda")
+    lens[::7] = 0
+    got = attend_pages(q, k, v, table, lens, lse=True)
+    want = v[table[:, 0].long(), :, 0]
+    want[::7] = 0
+    # one weight over itself: the value, rounded once
+    assert ((got["out"].float() - want.float()).abs() <= want.float().abs() * 2.0 ** -8).all()
+    assert (got["lse"][::7] == -math.inf).all() and torch.isfinite(got["lse"][1::7]).all()
