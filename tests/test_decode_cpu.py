@@ -333,3 +333,23 @@ def test_page_bytes_beyond_32_bits():
     assert out[0].page_bytes == (1 << 32) - 16
     with pytest.raises(ArgusError):
         decode._planes([wide], 2, wide.device, out)
+
+
+def test_packed_layouts_are_the_structures(dec):
+    """What the wrappers pack as bytes is what the structures hold, field by field."""
+    view1, view2 = dec.argus_page_view(1, 2, 3, 4), dec.argus_page_view(5, 6, 7, 8)
+    caches = dec._CACHES(*(dec.argus_page_planes(i + 1, 2, 3, 4, 5 + i) for i in range(dec.MAX_CACHES)))
+    flat = [1, 2, 3, 4, 5, 6, 7, 8]
+    for layout, struct, packed, fields in (
+            (dec._ATTEND_CONFIG, dec.argus_attend_config, [*range(12), 0.25, 13], None),
+            (dec._ATTEND_IO, dec.argus_attend_io, [11, -2, 3, *flat, *range(20, 27)], [11, -2, 3, view1, view2, *range(20, 27)]),
+            (dec._APPEND_CONFIG, dec.argus_append_config, [*range(10)], None),
+            (dec._APPEND_IO, dec.argus_append_io, [*range(6), *flat, *range(20, 26)], [*range(6), view1, view2, *range(20, 26)]),
+            (dec._STEP_CONFIG, dec.argus_step_config, [*range(10)], None),
+            (dec._STEP_IO, dec.argus_step_io, [*range(10), bytes(caches)], [*range(10), caches]),
+            (dec._COMPACT_CONFIG, dec.argus_compact_config, [*range(6)], None),
+            (dec._COMPACT_IO, dec.argus_compact_io, [*range(7), bytes(caches)], [*range(7), caches]),
+            (dec._SELECT_CONFIG, dec.argus_select_config, [*range(6), -1, 7], None),
+            (dec._SELECT_IO, dec.argus_select_io, [*range(9)], None)):
+        assert layout.pack(*packed) == bytes(struct(*(fields or packed))), struct
+        assert layout.size == ctypes.sizeof(struct)
