@@ -226,9 +226,10 @@ typedef struct argus_step_io {
   const int32_t* d_parents;  /* [new_seqs], or NULL: the sequences stay (new_seqs == old_seqs) */
   const int32_t* d_grow;     /* [new_seqs], or NULL: 0 */
   const int32_t* d_held;     /* [num_pages], or NULL: 0 */
-  int32_t* d_new_table;      /* out [new_seqs][columns], dense; not the old one */
-  int32_t* d_new_lens;       /* out [new_seqs]; not the old one */
-  int32_t* d_refs;           /* out [num_pages]; not held */
+  /* the outputs overlap none of the inputs */
+  int32_t* d_new_table;      /* out [new_seqs][columns], dense */
+  int32_t* d_new_lens;       /* out [new_seqs] */
+  int32_t* d_refs;           /* out [num_pages] */
   int32_t* d_counters;       /* out [ARGUS_ST_NUM_COUNTERS] */
   argus_page_planes caches[ARGUS_MAX_CACHES];
 } argus_step_io;

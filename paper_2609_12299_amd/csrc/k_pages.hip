@@ -192,21 +192,21 @@ struct StepArgs {
 constexpr uint32_t kPageTile = 4096;
 constexpr uint32_t kPageItems = 16;  // pages of a thread
 static_assert(kPageItems * kThreads == kPageTile, "a tile per block");
-// Calls of at most so many table entries and pages are planned by one block of
-// kSmallThreads, in one launch instead of three (step) or two (compact).  16
-// beams of 64 columns over 1024 pages: 19 us a call against 26 (15 us on the GPU
-// against 13, and less to launch); 56 of 51: 23.6 against 23.9, 22 us on the GPU; 512 of
-// 256 over 16384 pages by one block 311 against 25.  Compacting 640 pages: 17 us
-// against 22; 16384 pages by one block 235 against 229.
-constexpr uint32_t kSmallEntries = 2048, kSmallPages = 4096;
+// Calls of at most so many table entries and pages are planned by every block for
+// itself, in LDS, in one launch: what a call costs is its launches (3.5 us of the
+// host each) and the ways to memory one after the other.  Steps over 4096 pages,
+// with keys and values of one layer: 4096 entries 15.1 us a call against 22.2 by four
+// launches, 8192 18.9 against 21.8, 16384 28.3 against 22.0.  Compaction: 4096
+// pages 15.5 us against 21.7 by three launches (4097); more do not fit 16 bits of a thread.
+constexpr uint32_t kSmallEntries = 8192, kSmallRows = 2048, kSmallPages = 4096;
 constexpr uint32_t kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
+constexpr uint32_t kSmallBlocks = 256;  // one for each compute unit: their LDS is taken
 
 // Bit i: page p0 + i is in the pool and has (LIVE) or has not any reference.
-// AGENT: the counts were changed by atomics of this kernel, which do not pass the L1.
-template <bool LIVE, bool AGENT>
+template <bool LIVE>
 ARGUS_DEV uint32_t page_flags(const int32_t* refs, uint32_t p0, uint32_t N) {
   int32_t v[kPageItems];
-  if (!AGENT && p0 + kPageItems <= N && ((uintptr_t)refs & 15u) == 0) {
+  if (p0 + kPageItems <= N && ((uintptr_t)refs & 15u) == 0) {
 #pragma unroll
     for (uint32_t i = 0; i < kPageItems; i += 4) {
       const int4 q = *reinterpret_cast<const int4*>(refs + p0 + i);
@@ -216,8 +216,7 @@ ARGUS_DEV uint32_t page_flags(const int32_t* refs, uint32_t p0, uint32_t N) {
 #pragma unroll
     for (uint32_t i = 0; i < kPageItems; ++i) {
       const bool in = p0 + i < N;
-      const uint32_t* at = (const uint32_t*)refs + (in ? p0 + i : 0);
-      const int32_t x = AGENT ? (int32_t)ld_agent(at) : (int32_t)*at;
+      const int32_t x = refs[in ? p0 + i : 0];
       v[i] = in ? x : (LIVE ? 0 : 1);
     }
   }
@@ -324,9 +323,8 @@ ARGUS_DEV bool writes_on(const StepArgs& a, uint32_t s, int32_t e) {
 }
 
 // Fresh pages that the sequences before each one take, by one block.
-template <uint32_t THREADS>
 ARGUS_DEV void plan_rows(const StepArgs& a, uint32_t* s_wave) {
-  constexpr uint32_t kRows = 4;  // of a thread
+  constexpr uint32_t kRows = 4, THREADS = kThreads;
   uint32_t pages = 0, copies = 0;  // before
   for (uint32_t s0 = 0; s0 < a.S; s0 += THREADS * kRows) {
     int2 e[kRows];
@@ -434,13 +432,13 @@ __global__ __launch_bounds__(kThreads) void k_step_plan(StepArgs a) {
   mk.begin(ARGUS_REGION_STEP_PLAN);
   const uint32_t tid = threadIdx.x;
   if (blockIdx.x == 0) {
-    plan_rows<kThreads>(a, s_wave);
+    plan_rows(a, s_wave);
   } else {
     // Tiles are taken in order, so a block waits for running blocks alone.
     if (tid == 0) s_tile = atomicAdd(&a.state[0], 1u);
     __syncthreads();
     const uint32_t tile = s_tile, p0 = tile * kPageTile + tid * kPageItems;
-    const uint32_t free = page_flags<false, false>(a.refs, p0, a.N);
+    const uint32_t free = page_flags<false>(a.refs, p0, a.N);
     uint32_t total;
     uint32_t at = block_scan<kWaves>((uint32_t)__popc(free), s_wave, &total);
     if (tid < 64) {
@@ -476,42 +474,133 @@ __global__ __launch_bounds__(kThreads) void k_step_place(StepArgs a) {
   mk.end(ARGUS_REGION_STEP_PLACE);
 }
 
-// All of a small call but its copies, by one block.  What its atomics change is
-// read past the L1.
+// A small call: every block plans all of it for itself, in LDS, then the blocks share the
+// copies.  Block 0 writes the tables.  One launch.
 __global__ __launch_bounds__(kSmallThreads) void k_step_small(StepArgs a) {
-  __shared__ uint32_t s_wave[kSmallWaves];
+  constexpr uint32_t kPages = kSmallPages / kSmallThreads;  // of a thread
+  constexpr uint32_t kRows = kSmallRows / kSmallThreads;
+  __shared__ uint32_t s_wave[kSmallWaves], s_count[ARGUS_ST_NUM_COUNTERS];
+  __shared__ uint32_t s_refs[kSmallPages], s_lasts[kSmallPages];
+  __shared__ unsigned long long s_best[kSmallPages];
+  __shared__ uint16_t s_free[kSmallPages];
+  __shared__ int2 s_ends[kSmallRows];      // as StepArgs::ends
+  __shared__ uint2 s_copies[kSmallRows];   // as StepArgs::copies
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_STEP_PLAN);
   const uint32_t tid = threadIdx.x;
-  for (uint32_t p = tid; p < a.N; p += kSmallThreads) clear_page(a, p);
-  if (tid < ARGUS_ST_NUM_COUNTERS) a.counters[tid] = 0;
+  const bool writes = blockIdx.x == 0;
+#pragma unroll
+  for (uint32_t i = 0; i < kPages; ++i) {
+    const uint32_t p = tid + i * kSmallThreads;
+    const int32_t h = a.held && p < a.N ? a.held[p] : 0;
+    s_refs[p] = h < 0 ? 0u : (uint32_t)h;
+    s_lasts[p] = 0;
+    s_best[p] = 0;
+  }
+  if (tid < ARGUS_ST_NUM_COUNTERS) s_count[tid] = 0;
   __syncthreads();
-  const uint32_t rows = kSmallThreads / a.row_lanes;
-  for (uint32_t s = tid / a.row_lanes; s < a.S; s += rows) claim_row(a, s, tid % a.row_lanes, a.row_lanes);
-  __syncthreads();
-  plan_rows<kSmallThreads>(a, s_wave);
-  uint32_t n_free = 0;
-  for (uint32_t p = 0; p < a.N; p += kSmallThreads * kPageItems) {
-    const uint32_t p0 = p + tid * kPageItems;
-    const uint32_t free = page_flags<false, true>(a.refs, p0, a.N);
-    uint32_t total;
-    uint32_t at = n_free + block_scan<kSmallWaves>((uint32_t)__popc(free), s_wave, &total);
-    for (uint32_t f = free; f; f &= f - 1) a.free_list[at++] = p0 + (uint32_t)__builtin_ctz(f);
-    n_free += total;
+
+  // the entries that the sequences take over, and who has which page
+  const uint32_t rows = kSmallThreads / a.row_lanes, c0 = tid % a.row_lanes;
+  for (uint32_t s = tid / a.row_lanes; s < a.S; s += rows) {
+    const Row r = row_of(a, s);
+    const bool inside = ends_inside(a, r);
+    for (uint32_t c = c0; c < a.P; c += a.row_lanes) {
+      const int32_t e = entry_of(a, r, c);
+      if (writes && (c < r.used || c >= r.need)) a.new_table[(int64_t)s * a.P + c] = e;
+      const bool last = c + 1 == r.used && inside;
+      if (e >= 0) {
+        atomicAdd(&s_refs[e], 1u);
+        if (last) {
+          atomicMax(&s_best[e], (unsigned long long)(r.len + 1) << 32 | (0xFFFFFFFFu - s));
+          atomicAdd(&s_lasts[e], 1u);
+        }
+      }
+      if (c + 1 == r.used || (r.used == 0 && c == 0))
+        s_ends[s] = make_int2(last && r.grown > r.len ? e : -1, (int32_t)(r.need - r.used));
+    }
+    if (writes && c0 == 0) {
+      a.new_lens[s] = (int32_t)r.grown;
+      if (r.bad) atomicAdd(&s_count[ARGUS_ST_BAD_PARENT], 1u);
+      if (r.cut) atomicAdd(&s_count[ARGUS_ST_CUT], 1u);
+    }
   }
   __syncthreads();
-  for (uint32_t s = tid / a.row_lanes; s < a.S; s += rows) place_row(a, s, tid % a.row_lanes, a.row_lanes, n_free);
-  if (tid == 0) {
-    a.state[1] = n_free;
-    count_pages(a, n_free, a.state[2]);
+
+  // the free pages in order
+  uint32_t free = 0, n_free;
+#pragma unroll
+  for (uint32_t i = 0; i < kPages; ++i) {
+    const uint32_t p = tid * kPages + i;
+    free |= p < a.N && s_refs[p] == 0 ? 1u << i : 0u;
+  }
+  uint32_t at = block_scan<kSmallWaves>((uint32_t)__popc(free), s_wave, &n_free);
+  for (uint32_t f = free; f; f &= f - 1) s_free[at++] = (uint16_t)(tid * kPages + (uint32_t)__builtin_ctz(f));
+  // the fresh pages that the sequences before each one take; at most kSmallRows
+  uint32_t need = 0, copies = 0, needed, copied;
+  int2 e[kRows];
+#pragma unroll
+  for (uint32_t i = 0; i < kRows; ++i) {
+    const uint32_t s = tid * kRows + i;
+    e[i] = s < a.S ? s_ends[s] : make_int2(-1, 0);
+    if (e[i].x >= 0) {
+      const uint32_t p = (uint32_t)e[i].x;
+      if ((a.held == nullptr || a.held[p] <= 0) && s_lasts[p] == s_refs[p] && (uint32_t)s_best[p] == 0xFFFFFFFFu - s) e[i].x = -1;
+    }
+    need += (uint32_t)e[i].y + (e[i].x >= 0);
+    copies += e[i].x >= 0;
+  }
+  uint32_t base = block_scan<kSmallWaves>(need, s_wave, &needed);
+  uint32_t at_c = block_scan<kSmallWaves>(copies, s_wave, &copied);
+#pragma unroll
+  for (uint32_t i = 0; i < kRows; ++i) {
+    const uint32_t s = tid * kRows + i;
+    if (s < a.S) s_ends[s] = make_int2((int32_t)base, e[i].x);
+    if (e[i].x >= 0) s_copies[at_c++] = make_uint2((uint32_t)e[i].x, base);
+    base += (uint32_t)e[i].y + (e[i].x >= 0);
+  }
+  __syncthreads();
+  auto fresh = [&](uint32_t rank) { return rank < n_free ? (int32_t)s_free[rank] : -1; };
+
+  if (writes) {  // fresh pages into the tables
+    for (uint32_t s = tid / a.row_lanes; s < a.S; s += rows) {
+      const Row r = row_of(a, s);
+      const uint32_t first = (uint32_t)s_ends[s].x;
+      const int32_t old = s_ends[s].y;
+      const uint32_t copy = old >= 0;
+      for (uint32_t c = r.used + c0; c < r.need; c += a.row_lanes) {
+        const int32_t page = fresh(first + copy + c - r.used);
+        a.new_table[(int64_t)s * a.P + c] = page;
+        if (page >= 0) s_refs[page] = 1;
+      }
+      if (copy && c0 == 0) {
+        const int32_t page = fresh(first);
+        a.new_table[(int64_t)s * a.P + r.used - 1] = page;
+        if (page >= 0) {
+          s_refs[page] = 1;
+          atomicAdd(&s_count[ARGUS_ST_COPIED], 1u);
+        }
+        if (atomicSub(&s_refs[old], 1u) == 1u) atomicSub(&s_count[ARGUS_ST_LIVE], 1u);
+      }
+    }
+    __syncthreads();
+    if (tid < ARGUS_ST_NUM_COUNTERS) {
+      const uint32_t got = needed < n_free ? needed : n_free;
+      a.counters[tid] = (int32_t)(tid == ARGUS_ST_NEEDED ? needed : tid == ARGUS_ST_SHORT ? needed - got
+                                  : s_count[tid] + (tid == ARGUS_ST_LIVE ? a.N - n_free + got : 0u));
+    }
+    for (uint32_t p = tid; p < a.N; p += kSmallThreads) a.refs[p] = (int32_t)s_refs[p];
   }
   mk.end(ARGUS_REGION_STEP_PLAN);
-}
-
-__global__ __launch_bounds__(kThreads) void k_step_copy(StepArgs a) {
-  WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_STEP_PLACE);
-  copy_step(a, __builtin_amdgcn_readfirstlane(blockIdx.x * kWaves + threadIdx.x / 64), gridDim.x * kWaves);
+  copy_pages(a.caches, copied, __builtin_amdgcn_readfirstlane(blockIdx.x * kSmallWaves + tid / 64), gridDim.x * kSmallWaves,
+             [&](uint32_t i, uint32_t* src, uint32_t* dst) {
+               const uint2 c = s_copies[i];
+               if (c.y >= n_free) return false;
+               *src = c.x;
+               *dst = s_free[c.y];
+               return true;
+             });
   mk.end(ARGUS_REGION_STEP_PLACE);
 }
 
@@ -538,7 +627,7 @@ __global__ __launch_bounds__(kThreads) void k_compact_count(CompactArgs a) {
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_COMPACT_COUNT);
   uint32_t total;
-  block_scan<kWaves>((uint32_t)__popc(page_flags<true, false>(a.refs, blockIdx.x * kPageTile + threadIdx.x * kPageItems, a.N)),
+  block_scan<kWaves>((uint32_t)__popc(page_flags<true>(a.refs, blockIdx.x * kPageTile + threadIdx.x * kPageItems, a.N)),
                      s_wave, &total);
   if (threadIdx.x == 0) a.tile_live[blockIdx.x] = total;
   mk.end(ARGUS_REGION_COMPACT_COUNT);
@@ -572,7 +661,7 @@ __global__ __launch_bounds__(kThreads) void k_compact_plan(CompactArgs a) {
     before += t < blockIdx.x ? v : 0u;
   }
   const uint32_t p0 = blockIdx.x * kPageTile + tid * kPageItems;
-  const uint32_t live = page_flags<true, false>(a.refs, p0, a.N);
+  const uint32_t live = page_flags<true>(a.refs, p0, a.N);
   uint32_t total, all, all_before;
   block_scan<kWaves>(n, s_wave, &all);
   block_scan<kWaves>(before, s_wave, &all_before);
@@ -585,36 +674,18 @@ __global__ __launch_bounds__(kThreads) void k_compact_plan(CompactArgs a) {
   mk.end(ARGUS_REGION_COMPACT_PLAN);
 }
 
-// Both of them for a small pool, by one block.
-__global__ __launch_bounds__(kSmallThreads) void k_compact_small(CompactArgs a) {
-  __shared__ uint32_t s_wave[kSmallWaves];
-  WaveMarks mk(a.marks);
-  mk.begin(ARGUS_REGION_COMPACT_PLAN);
-  const uint32_t p0 = threadIdx.x * kPageItems;
-  const uint32_t live = page_flags<true, false>(a.refs, p0, a.N);
-  uint32_t n;
-  const uint32_t rank = block_scan<kSmallWaves>((uint32_t)__popc(live), s_wave, &n);
-  rank_pages(a, p0, live, rank, n);
-  if (threadIdx.x == 0) {
-    a.state[0] = n;
-    if (n == a.N) a.state[1] = n;
-  }
-  mk.end(ARGUS_REGION_COMPACT_PLAN);
-}
-static_assert(kSmallPages <= kSmallThreads * kPageItems, "a small pool in one round");
-
-__global__ __launch_bounds__(kThreads) void k_compact_move(CompactArgs a) {
-  WaveMarks mk(a.marks);
-  mk.begin(ARGUS_REGION_COMPACT_MOVE);
-  const uint32_t n = a.state[0], stay = a.state[1];
+// A block's part of the move: pages, table entries or copies.  PLAN: live(p), rank(p), the
+// live pages below p, and the i-th hole() and mover().
+template <class Plan>
+ARGUS_DEV void move_block(const CompactArgs& a, uint32_t n, uint32_t stay, const Plan& plan) {
   uint32_t b = blockIdx.x;
   if (b < a.page_blocks) {
     const uint32_t p = b * kThreads + threadIdx.x;
     if (p < a.N) {
       const int32_t refs = a.refs[p];
-      const uint32_t rank = a.rank[p];
-      a.map[p] = refs <= 0 ? -1 : p < n ? (int32_t)p : (int32_t)a.holes[rank - stay];
-      a.new_refs[p] = p >= n ? 0 : refs > 0 ? refs : a.refs[a.movers[stay + p - rank]];
+      const uint32_t rank = plan.rank(p);
+      a.map[p] = refs <= 0 ? -1 : p < n ? (int32_t)p : (int32_t)plan.hole(rank - stay);
+      a.new_refs[p] = p >= n ? 0 : refs > 0 ? refs : a.refs[plan.mover(p - rank)];
     }
     if (b == 0 && threadIdx.x < ARGUS_CO_NUM_COUNTERS)
       a.counters[threadIdx.x] = threadIdx.x == ARGUS_CO_LIVE ? (int32_t)n : threadIdx.x == ARGUS_CO_MOVED ? (int32_t)(n - stay) : 0;
@@ -624,7 +695,7 @@ __global__ __launch_bounds__(kThreads) void k_compact_move(CompactArgs a) {
       const uint32_t s = (uint32_t)(e / a.P), c = (uint32_t)(e % a.P);
       const int32_t p = a.table[(int64_t)s * a.table_stride + c];
       int32_t to = -1;
-      if ((uint32_t)p < a.N && a.refs[p] > 0) to = (uint32_t)p < n ? p : (int32_t)a.holes[a.rank[p] - stay];
+      if ((uint32_t)p < a.N && plan.live((uint32_t)p)) to = (uint32_t)p < n ? p : (int32_t)plan.hole(plan.rank((uint32_t)p) - stay);
       a.new_table[e] = to;
     }
   } else {
@@ -632,11 +703,72 @@ __global__ __launch_bounds__(kThreads) void k_compact_move(CompactArgs a) {
     const uint32_t wave = __builtin_amdgcn_readfirstlane(b * kWaves + threadIdx.x / 64);
     copy_pages(a.caches, n - stay, wave, (gridDim.x - a.page_blocks - a.row_blocks) * kWaves,
                [&](uint32_t i, uint32_t* src, uint32_t* dst) {
-                 *src = a.movers[stay + i];
-                 *dst = a.holes[i];
+                 *src = plan.mover(i);
+                 *dst = plan.hole(i);
                  return true;
                });
   }
+}
+
+struct LargePlan {
+  const CompactArgs& a;
+  uint32_t stay;
+  ARGUS_DEV bool live(uint32_t p) const { return a.refs[p] > 0; }
+  ARGUS_DEV uint32_t rank(uint32_t p) const { return a.rank[p]; }
+  ARGUS_DEV uint32_t hole(uint32_t i) const { return a.holes[i]; }
+  ARGUS_DEV uint32_t mover(uint32_t i) const { return a.movers[stay + i]; }
+};
+
+__global__ __launch_bounds__(kThreads) void k_compact_move(CompactArgs a) {
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_COMPACT_MOVE);
+  const uint32_t n = a.state[0], stay = a.state[1];
+  move_block(a, n, stay, LargePlan{a, stay});
+  mk.end(ARGUS_REGION_COMPACT_MOVE);
+}
+
+// A small pool is planned by every block for itself, in LDS: one launch.
+struct SmallPlan {
+  uint32_t n, stay;
+  const uint16_t *flags, *base, *holes, *movers;  // of 16 pages: which live, how many before; lists, the movers' backwards
+  ARGUS_DEV bool live(uint32_t p) const { return flags[p / kPageItems] >> (p % kPageItems) & 1u; }
+  ARGUS_DEV uint32_t rank(uint32_t p) const {
+    return base[p / kPageItems] + (uint32_t)__popc(flags[p / kPageItems] & ((1u << (p % kPageItems)) - 1u));
+  }
+  ARGUS_DEV uint32_t hole(uint32_t i) const { return holes[i]; }
+  ARGUS_DEV uint32_t mover(uint32_t i) const { return movers[n - stay - 1 - i]; }
+};
+static_assert(kSmallPages == kPageTile && kPageItems == 16 && kSmallPages <= 65536, "a tile, flags and numbers in 16 bits");
+
+__global__ __launch_bounds__(kThreads) void k_compact_small(CompactArgs a) {
+  __shared__ uint32_t s_wave[kWaves];
+  __shared__ uint16_t s_flags[kThreads], s_base[kThreads], s_holes[kSmallPages / 2], s_movers[kSmallPages / 2];
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_COMPACT_PLAN);
+  const uint32_t tid = threadIdx.x, p0 = tid * kPageItems;
+  const uint32_t live = page_flags<true>(a.refs, p0, a.N);
+  uint32_t n;
+  const uint32_t first = block_scan<kWaves>((uint32_t)__popc(live), s_wave, &n);
+  s_flags[tid] = (uint16_t)live;
+  s_base[tid] = (uint16_t)first;
+  // No more than half of the pages: as many holes below n as movers from n on.
+  uint32_t rank = first;
+#pragma unroll
+  for (uint32_t i = 0; i < kPageItems; ++i) {
+    const uint32_t p = p0 + i;
+    if (live >> i & 1u) {
+      if (p >= n) s_movers[n - 1 - rank] = (uint16_t)p;
+      ++rank;
+    } else if (p < n) {
+      s_holes[p - rank] = (uint16_t)p;
+    }
+  }
+  __syncthreads();
+  SmallPlan plan{n, n, s_flags, s_base, s_holes, s_movers};
+  if (n < a.N) plan.stay = plan.rank(n);
+  mk.end(ARGUS_REGION_COMPACT_PLAN);
+  mk.begin(ARGUS_REGION_COMPACT_MOVE);
+  move_block(a, n, plan.stay, plan);
   mk.end(ARGUS_REGION_COMPACT_MOVE);
 }
 
@@ -825,17 +957,15 @@ extern "C" int argus_decode_step(const argus_step_config* cfg, const argus_step_
   clear = clear > 1024 ? 1024 : clear;
   const uint32_t copy_blocks = copy_blocks_for(a.caches, a.S);
   hipStream_t st = (hipStream_t)stream_v;
-  if ((uint64_t)a.S * a.P <= kSmallEntries && a.N <= kSmallPages) {
-    // (the block's waves write their markers as those of four blocks)
-    if (!marks_fit(markers, ((uint64_t)kSmallWaves / kWaves + copy_blocks) * kWaves * 2))
-      return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
+  if ((uint64_t)a.S * a.P <= kSmallEntries && a.S <= kSmallRows && a.N <= kSmallPages) {
+    // (a block's waves write their markers as those of four blocks)
+    constexpr uint32_t kBlocks = kSmallWaves / kWaves;
+    const uint32_t wanted = (copy_blocks + kBlocks - 1) / kBlocks;
+    const uint32_t blocks = wanted < 1 ? 1 : wanted < kSmallBlocks ? wanted : kSmallBlocks;
+    if (!marks_fit(markers, (uint64_t)blocks * kSmallWaves * 4)) return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
     if ((rc = device_ok()) != ARGUS_OK) return rc;
-    a.marks = take_marks(markers, kSmallWaves / kWaves, 2);
-    hipLaunchKernelGGL(k_step_small, dim3(1), dim3(kSmallThreads), 0, st, a);
-    if (copy_blocks) {
-      a.marks = take_marks(markers, copy_blocks, 2);
-      hipLaunchKernelGGL(k_step_copy, dim3(copy_blocks), dim3(kThreads), 0, st, a);
-    }
+    a.marks = take_marks(markers, (uint64_t)blocks * kBlocks, 4);
+    hipLaunchKernelGGL(k_step_small, dim3(blocks), dim3(kSmallThreads), 0, st, a);
     return hipGetLastError() == hipSuccess ? ARGUS_OK : refuse(ARGUS_E_HIP, "launch failed");
   }
   const uint32_t grid[4] = {clear, a.rows_blocks, tiles + 1, a.rows_blocks + copy_blocks};
@@ -922,20 +1052,20 @@ extern "C" int argus_decode_compact(const argus_compact_config* cfg, const argus
   const uint32_t copy_blocks = copy_blocks_for(a.caches, a.N / 2);
   const uint32_t moves = a.page_blocks + a.row_blocks + copy_blocks;
   const bool small = a.N <= kSmallPages;
-  const uint64_t blocks = small ? (uint64_t)kSmallWaves / kWaves + moves : 2ull * a.tiles + moves;
-  if (!marks_fit(markers, blocks * kWaves * 2)) return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
+  const uint64_t blocks = 2ull * (small ? 0 : a.tiles) + moves;
+  if (!marks_fit(markers, (blocks + (small ? moves : 0)) * kWaves * 2)) return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
   if ((rc = device_ok()) != ARGUS_OK) return rc;
   hipStream_t st = (hipStream_t)stream_v;
   if (small) {
-    a.marks = take_marks(markers, kSmallWaves / kWaves, 2);
-    hipLaunchKernelGGL(k_compact_small, dim3(1), dim3(kSmallThreads), 0, st, a);
+    a.marks = take_marks(markers, moves, 4);
+    hipLaunchKernelGGL(k_compact_small, dim3(moves), dim3(kThreads), 0, st, a);
   } else {
     a.marks = take_marks(markers, a.tiles, 2);
     hipLaunchKernelGGL(k_compact_count, dim3(a.tiles), dim3(kThreads), 0, st, a);
     a.marks = take_marks(markers, a.tiles, 2);
     hipLaunchKernelGGL(k_compact_plan, dim3(a.tiles), dim3(kThreads), 0, st, a);
+    a.marks = take_marks(markers, moves, 2);
+    hipLaunchKernelGGL(k_compact_move, dim3(moves), dim3(kThreads), 0, st, a);
   }
-  a.marks = take_marks(markers, moves, 2);
-  hipLaunchKernelGGL(k_compact_move, dim3(moves), dim3(kThreads), 0, st, a);
   return hipGetLastError() == hipSuccess ? ARGUS_OK : refuse(ARGUS_E_HIP, "launch failed");
 }
