@@ -30,7 +30,7 @@ struct WaveMarks {
   uint32_t ctx = 0, region = 0;
   ARGUS_DEV WaveMarks(const Marks& m) {
     if (m.rec) {
-      const uint32_t wave = __builtin_amdgcn_readfirstlane((blockIdx.y * gridDim.x + blockIdx.x) * (blockDim.x / 64) + threadIdx.x / 64);
+      const uint32_t wave = __builtin_amdgcn_readfirstlane(((blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x) * (blockDim.x / 64) + threadIdx.x / 64);
       at = m.rec + (uint64_t)wave * m.per_wave;
       ctx = m.ctx + wave;
       region = m.region;

@@ -676,14 +676,15 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend_shared(A
   mk.end(ARGUS_REGION_ATTEND);
 }
 
-// Rows of a segment that was left in pieces: piece 0 is the second of its first
-// share, piece i the first of share i further on.
-template <int T, int DP, int NQ, int ROWS>
+// ROWS rows by COLS elements of a segment that was left in pieces: piece 0 is the second
+// of its first share, piece i the first of share i further on.
+template <int T, int DP, int NQ, int ROWS, int COLS>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
-  constexpr uint32_t kRows = ROWS, kQuads = DP / 4, kParts = kThreads / (kQuads * kRows);
+  constexpr uint32_t kRows = ROWS, kQuads = COLS / 4, kParts = kThreads / (kQuads * kRows);
   using Hf = Half<T>;
-  __shared__ float s_m[kRows][kParts], s_l[kRows][kParts];
-  __shared__ __align__(16) float s_o[kRows][kParts][DP];
+  static_assert(ROWS == 1 || ROWS == kWaves, "a row for the block, or one for each wave");
+  __shared__ float s_m[kWaves], s_l[kWaves];
+  __shared__ __align__(16) float s_o[kWaves][COLS];
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_ATTEND_JOIN);
   const uint4 open = a.open[blockIdx.x];
@@ -691,7 +692,8 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
     const uint32_t s = open.x / a.HS, hs = open.x % a.HS, n = open.z - open.y + 1;
     const uint32_t h = hs / a.row_tiles, q0 = (hs % a.row_tiles) * 16 * NQ;
     const uint32_t rows = a.G - q0 < 16u * NQ ? a.G - q0 : 16u * NQ;
-    const uint32_t tid = threadIdx.x, r4 = tid / (kQuads * kParts), part = tid / kQuads % kParts, d = (tid % kQuads) * 4;
+    const uint32_t tid = threadIdx.x, r4 = tid / (kQuads * kParts), part = tid / kQuads % kParts, q4 = (tid % kQuads) * 4;
+    const uint32_t d = blockIdx.z * COLS + q4;
     const uint32_t row = blockIdx.y * kRows + r4, at = row < rows ? row : 0;
     float m = -INFINITY, l = 0.0f;
     f32x4 o = (f32x4)(0.0f);
@@ -720,18 +722,34 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
       }
       m = top;
     }
-    if (d == 0) s_m[r4][part] = m, s_l[r4][part] = l;
-    *reinterpret_cast<f32x4*>(&s_o[r4][part][d]) = o;
-    __syncthreads();
-    if (part == 0 && row < rows && d < a.D) {
-      float top = m, sum = 0.0f;
-      for (uint32_t i = 1; i < kParts; ++i) top = fmaxf(top, s_m[r4][i]);
-      o = (f32x4)(0.0f);
-      for (uint32_t i = 0; i < kParts; ++i) {
-        const float w = s_m[r4][i] == -INFINITY ? 1.0f : exp_of(s_m[r4][i] - top);
-        sum += s_l[r4][i] * w;
-        o += *reinterpret_cast<const f32x4*>(&s_o[r4][i][d]) * w;
+    // the parts of a wave, then the waves
+#pragma unroll
+    for (uint32_t x = kQuads; x < 64; x <<= 1) {
+      const float m2 = __shfl_xor(m, x), l2 = __shfl_xor(l, x), top = fmaxf(m, m2);
+      const float w = m == -INFINITY ? 1.0f : exp_of(m - top), w2 = m2 == -INFINITY ? 1.0f : exp_of(m2 - top);
+      l = l * w + l2 * w2;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] = o[j] * w + __shfl_xor(o[j], x) * w2;
+      m = top;
+    }
+    float top = m, sum = l;
+    if constexpr (ROWS == 1) {
+      if ((tid & 63u) < kQuads) {
+        if (q4 == 0) s_m[tid >> 6] = m, s_l[tid >> 6] = l;
+        *reinterpret_cast<f32x4*>(&s_o[tid >> 6][q4]) = o;
       }
+      __syncthreads();
+      top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+      sum = 0.0f;
+      o = (f32x4)(0.0f);
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        const float w = s_m[i] == -INFINITY ? 1.0f : exp_of(s_m[i] - top);
+        sum += s_l[i] * w;
+        o += *reinterpret_cast<const f32x4*>(&s_o[i][q4]) * w;
+      }
+    }
+    if (part == 0 && row < rows && d < a.D) {
       const uint64_t out = (uint64_t)s * a.H * a.G + (uint64_t)h * a.G + q0 + row;
       const float inv = sum == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[h] : 1.0f) / sum;
       *reinterpret_cast<u32x2*>(a.out + out * a.D + d) = (u32x2){Hf::pack(o.x * inv, o.y * inv), Hf::pack(o.z * inv, o.w * inv)};
@@ -766,25 +784,27 @@ void launch_attend_type(const AttendArgs& a, uint32_t grid, hipStream_t st) {
     a.G <= 16 ? launch_attend_as<T, F8, 256, 1>(a, grid, st) : launch_attend_as<T, F8, 256, 2>(a, grid, st);
 }
 
-template <int T, int ROWS>
-void launch_join_rows(const AttendArgs& a, dim3 grid, hipStream_t st) {
-  const bool two = a.G > 16;
+// What a block joins: four rows, one row, or 32 elements of one, for up to 2, 8 and 32 pieces
+// side by side at head size 128.
+enum JoinForm : uint32_t { kJoinFourRows, kJoinRow, kJoinPart };
+constexpr int kJoinCols = 32;
+
+template <int T, int DP, int NQ>
+void launch_join_as(const AttendArgs& a, JoinForm form, dim3 g, hipStream_t st) {
   const dim3 b(kThreads);
-  if (a.D <= 64) {
-    if (two) hipLaunchKernelGGL((k_attend_join<T, 64, 2, ROWS>), grid, b, 0, st, a);
-    else hipLaunchKernelGGL((k_attend_join<T, 64, 1, ROWS>), grid, b, 0, st, a);
-  } else if (a.D <= 128) {
-    if (two) hipLaunchKernelGGL((k_attend_join<T, 128, 2, ROWS>), grid, b, 0, st, a);
-    else hipLaunchKernelGGL((k_attend_join<T, 128, 1, ROWS>), grid, b, 0, st, a);
-  } else {
-    if (two) hipLaunchKernelGGL((k_attend_join<T, 256, 2, ROWS>), grid, b, 0, st, a);
-    else hipLaunchKernelGGL((k_attend_join<T, 256, 1, ROWS>), grid, b, 0, st, a);
-  }
+  if (form == kJoinPart) hipLaunchKernelGGL((k_attend_join<T, DP, NQ, 1, kJoinCols>), g, b, 0, st, a);
+  else if (form == kJoinRow) hipLaunchKernelGGL((k_attend_join<T, DP, NQ, 1, DP>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((k_attend_join<T, DP, NQ, 4, DP>), g, b, 0, st, a);
 }
 
 template <int T>
-void launch_join_type(const AttendArgs& a, uint32_t rows, dim3 grid, hipStream_t st) {
-  rows == 1 ? launch_join_rows<T, 1>(a, grid, st) : launch_join_rows<T, 4>(a, grid, st);
+void launch_join_type(const AttendArgs& a, JoinForm form, dim3 g, hipStream_t st) {
+  if (a.D <= 64)
+    a.G <= 16 ? launch_join_as<T, 64, 1>(a, form, g, st) : launch_join_as<T, 64, 2>(a, form, g, st);
+  else if (a.D <= 128)
+    a.G <= 16 ? launch_join_as<T, 128, 1>(a, form, g, st) : launch_join_as<T, 128, 2>(a, form, g, st);
+  else
+    a.G <= 16 ? launch_join_as<T, 256, 1>(a, form, g, st) : launch_join_as<T, 256, 2>(a, form, g, st);
 }
 
 // One source file each, so that they compile side by side.

@@ -38,23 +38,27 @@ namespace {
 
 // Waves that share a batch: one block of four for each of the 256 compute
 // units (twice as many: 655 us against 645 for four sequences of 262143 tokens, 92
-// against 85 for 128 of 1000, 69 against 65 for the 8-bit batch), and no more
-// of one segment than are soon joined (one of 131072 tokens, 1 x 8 heads of 128: 36 us
-// with 256, 33 with 512).  Two blocks where a tile's rows are so short
+// against 85 for 128 of 1000, 69 against 65 for the 8-bit batch).  All of them may
+// fall to one segment (one of 131072 tokens, 1 x 8 heads of 128: 24 us, with at most 512 27,
+// with 256 34).  Two blocks where a tile's rows are so short
 // that one wave for each SIMD has too few bytes under way: of 64 bytes (64 sequences of up to
 // 16384 tokens in 8 bits: 35 us against 41; of 128 bytes 49.7 against 48.1).
-constexpr uint32_t kShares = 256 * kWaves, kSharesOfSegment = 512;
-// A block joins one row where there are so few: more threads for the pieces of each
-// (a sequence of 32768 tokens, 1 x 8 heads of 128: 19 us against 29 by four rows; 96
-// of up to 8192, 8 x 4 heads: 75 by four rows, 77 by one).
-constexpr uint32_t kJoinBlocks = 1024;
+constexpr uint32_t kShares = 256 * kWaves, kSharesOfSegment = 1024;
+// A block of the join takes 32 elements of a row where segments may lie in so many pieces
+// (a sequence of 32768 tokens, 1 x 8 heads of 128: 16.3 us against 18.6 by whole rows; of
+// 8192, 66 pieces, 15.8 against 15.2); a row where there are so few of them (6 sequences of up to 3111,
+// 8 x 4 heads: 15.9 us against 16.8 by four rows), else four (10 of 8502 with a window of
+// 1060, 2 x 24 heads: 18.6 us against 19.2 by one row).
+constexpr uint32_t kManyPieces = 64, kFewRows = 256;
 // Segments of at most this many tiles are not shared: a block each, and no joining
 // (64 sequences of 512 tokens, 8 x 4 heads of 128: 23 us against 30 shared; of 1024 tokens 45
 // against 52, and 4 of them 14.7 both; at head size 256, 4 of 1024: 34 against 25).
 uint32_t whole_tiles(uint32_t dp) { return dp == 256 ? 16u : 32u; }
 
 struct Plan {
-  uint32_t dp, nq, row_tiles, hs, shares, segs, grid, opens, join_grid, rows_of_join, unit_shift;
+  uint32_t dp, nq, row_tiles, hs, shares, segs, grid, opens, unit_shift;
+  JoinForm join;
+  uint32_t join_y, join_z;
   size_t o_at, open_at, bytes;
 };
 
@@ -102,8 +106,9 @@ int make_plan(const argus_attend_config* c, Plan* p) {
   p->grid = shares ? p->shares / kWaves : p->segs;
   p->opens = p->shares < p->segs ? p->shares : p->segs;
   const uint32_t join_rows = c->group < 16 * p->nq ? c->group : 16 * p->nq;
-  p->rows_of_join = p->opens * join_rows <= kJoinBlocks ? 1 : 4;
-  p->join_grid = (join_rows + p->rows_of_join - 1) / p->rows_of_join;
+  p->join = p->shares >= (uint64_t)p->segs * kManyPieces ? kJoinPart : p->opens * join_rows <= kFewRows ? kJoinRow : kJoinFourRows;
+  p->join_y = p->join == kJoinFourRows ? (join_rows + 3) / 4 : join_rows;
+  p->join_z = p->join == kJoinPart ? (c->head_dim + kJoinCols - 1) / kJoinCols : 1;
   const size_t rows = (size_t)shares * 2 * 16 * p->nq;
   p->o_at = up256(rows * 2 * sizeof(float));
   p->open_at = p->o_at + up256(rows * p->dp * sizeof(float));
@@ -151,7 +156,7 @@ extern "C" int argus_decode_attend(const argus_attend_config* cfg, const argus_a
   if (p.bytes && !aligned_to(d_workspace, 256)) return refuse(ARGUS_E_ALIGN, "the workspace lies on 256 bytes");
   if (workspace_bytes < p.bytes)
     return refuse(ARGUS_E_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
-  const uint64_t joins = p.shares ? (uint64_t)p.opens * p.join_grid : 0;
+  const uint64_t joins = p.shares ? (uint64_t)p.opens * p.join_y * p.join_z : 0;
   const uint32_t per_wave = 6;  // its own region, and in it the place and the tokens
   const uint64_t records = ((uint64_t)p.grid * per_wave + joins * 2) * kWaves;
   if (!marks_fit(markers, records)) return refuse(ARGUS_E_CAPACITY, "%llu marker records do not fit", (unsigned long long)records);
@@ -183,7 +188,7 @@ extern "C" int argus_decode_attend(const argus_attend_config* cfg, const argus_a
   (f8 ? (bf ? launch_attend_bf16_f8 : launch_attend_fp16_f8) : (bf ? launch_attend_bf16 : launch_attend_fp16))(a, p.grid, st);
   if (p.shares) {
     a.marks = take_marks(markers, joins, 2);
-    (bf ? launch_join_type<0> : launch_join_type<1>)(a, p.rows_of_join, dim3(p.opens, p.join_grid), st);
+    (bf ? launch_join_type<0> : launch_join_type<1>)(a, p.join, dim3(p.opens, p.join_y, p.join_z), st);
   }
   return hipGetLastError() == hipSuccess ? ARGUS_OK : refuse(ARGUS_E_HIP, "launch failed");
 }
