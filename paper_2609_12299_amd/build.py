@@ -102,12 +102,12 @@ def resources() -> str:
     if filt and names:
         out = subprocess.run([filt], input="\n".join(names), capture_output=True, text=True).stdout
         for r, d in zip(rows, out.splitlines()):
-            r["kernel"] = d.split("(")[0]
-    head = (f"{'kernel':48s} {'file':14s} VGPR AGPR SGPR spill sspill scratch waves/SIMD   LDS B"
+            r["kernel"] = d.replace("(anonymous namespace)::", "").split("(")[0]
+    head = (f"{'kernel':64s} {'file':19s} VGPR AGPR SGPR spill sspill scratch waves/SIMD   LDS B"
             "\n(spill: VGPRs spilled to scratch; sspill: SGPRs spilled to VGPR lanes)")
     lines = [head]
     for r in rows:
-        lines.append(f"{r['kernel'][:48]:48s} {r['file']:14s} {r.get('VGPRs', 0):4d} "
+        lines.append(f"{r['kernel'][:64]:64s} {r['file']:19s} {r.get('VGPRs', 0):4d} "
                      f"{r.get('AGPRs', 0):4d} {r.get('TotalSGPRs', 0):4d} {r.get('VGPRs Spill', 0):5d} "
                      f"{r.get('SGPRs Spill', 0):6d} "
                      f"{r.get('ScratchSize [bytes/lane]', 0):7d} "

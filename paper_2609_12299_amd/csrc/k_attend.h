@@ -27,9 +27,10 @@
 // taken as the sum of two 16-bit numbers, so that its rounding is not seen in
 // the result), a third of the time that its bytes take.  Every byte is read once,
 // by loads of whole lines, past the caches.  Measured: four sequences of 262143
-// tokens, 8 x 8 heads of 128 in bf16, 4.3 GB: 645 us, 6.7 TB/s (with keys read by
+// tokens, 8 x 8 heads of 128 in bf16, 4.3 GB: 643 us, 6.7 TB/s (with keys read by
 // 16 rows x 64 bytes the same; values through the caches 707); 48 sequences of up to 32768
-// tokens in 8 bits 65 us, 5.2 TB/s (73 before the keys' rows were read whole).
+// tokens in 8 bits 64 us, 5.3 TB/s (73 before the keys' rows were read whole), 62 us for
+// the shares and 6 for the joins.
 //
 // Shares: the units of work are the tiles (groups of 2^unit_shift tiles, where
 // there could be more than 2^31) of all (sequence, head) segments one after the
@@ -174,8 +175,9 @@ ARGUS_DEV float exp_of(float x) { return exp2f(x * kLog2e); }
 
 // Whether the rows of the next tile are loaded while one is taken: where a tile is small
 // and the registers hold two (8 bits, head size 128: 65 us against 73 for 48
-// sequences of up to 32768 tokens; 16 bits: spilled, 890 against 645 for four
-// of 262143).
+// sequences of up to 32768 tokens; two column tiles of it 60 against 41 for 20 of up to 20000, 4
+// x 24 heads; 16 bits 867 against 638 for four of 262143, 8 bits at head size 256 184
+// against 170 for 8 of 30000).
 template <bool F8, int DP, int NQ>
 constexpr bool kAhead = DP == 64 || (F8 && DP == 128 && NQ == 1);
 
