@@ -7,7 +7,7 @@
 // the lanes' maxima has k elements at or above it, and few more.  From then on a
 // step costs a comparison of each lane's largest value; where some are above, the step's elements
 // go to LDS and the wave looks through those of the lanes in question.  When the
-// list is half full, it is cut to its first k, and what the k-th has becomes the
+// list may not hold 64 more, it is cut to its first k, and what the k-th has becomes the
 // least: the list never overflows, however many values are equal.
 //
 // k_select_beams, one block per group of beams, joins the parts' sums to the
@@ -31,10 +31,13 @@ typedef uint16_t any_u16 __attribute__((may_alias));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint32_t kItems = 32;               // elements of a lane per step
 constexpr uint32_t kStep = kItems * 64;
-constexpr uint32_t kList = 128;               // candidates of a wave
+// Candidates of a wave.  A cut counts, for each, those above it: the more room there is beyond
+// 64, the rarer it is for a large k (32 x 4 rows of 128003, k 64: 188 us with 128, 71 with 192,
+// 72 with 256; finding the k-th key bit by bit instead 54 against 43 for k 8).
+constexpr uint32_t kList = 192;
 // Beyond its k a list holds so many before it is cut at the end of a step: the
 // sooner the least rises, the fewer lanes are looked through (0: 51.5 us, 8: 50.1,
-// 16: 50.8, only when half full: 54.4; 96 x 8 rows of 128003 in bf16, k 8).
+// 16: 50.8, only when half full: 54.4, with lists of 128; 96 x 8 rows of 128003 in bf16, k 8).
 constexpr uint32_t kRoom = 8;
 constexpr uint32_t kCands = 512;              // candidates of a group that are ranked by counting
 constexpr uint32_t kMaxK = 64, kMaxBeams = 64;
@@ -143,20 +146,32 @@ __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
     uint32_t n = 0;           // candidates in the list
     uint64_t least = 0;       // their keys are above it
     float least_value = -INFINITY;
-    // The list cut to its first k, in order.
-    auto cut = [&]() {
-      __builtin_amdgcn_wave_barrier();
-      const uint64_t k0 = lane < n ? list[lane] : 0, k1 = lane + 64 < n ? list[lane + 64] : 0;
-      uint32_t r0 = 0, r1 = 0;
+    // The list cut to its first k, in order: each lane counts what is above its keys, C of them.
+    auto rank = [&](auto keys) {
+      constexpr uint32_t C = keys();
+      uint64_t key[C];
+      uint32_t above[C];
+#pragma unroll
+      for (uint32_t c = 0; c < C; ++c) {
+        key[c] = lane + 64 * c < n ? list[lane + 64 * c] : 0;
+        above[c] = 0;
+      }
 #pragma unroll 8
       for (uint32_t i = 0; i < n; ++i) {
         const uint64_t o = list[i];
-        r0 += o > k0;
-        r1 += o > k1;
+#pragma unroll
+        for (uint32_t c = 0; c < C; ++c) above[c] += o > key[c];
       }
       __builtin_amdgcn_wave_barrier();
-      if (lane < n && r0 < a.K) list[r0] = k0;
-      if (lane + 64 < n && r1 < a.K) list[r1] = k1;
+#pragma unroll
+      for (uint32_t c = 0; c < C; ++c)
+        if (lane + 64 * c < n && above[c] < a.K) list[above[c]] = key[c];
+    };
+    auto cut = [&]() {
+      __builtin_amdgcn_wave_barrier();
+      if (n <= 64) rank([]() constexpr { return 1u; });
+      else if (n <= 128) rank([]() constexpr { return 2u; });
+      else rank([]() constexpr { return kList / 64; });
       __builtin_amdgcn_wave_barrier();
       n = n < a.K ? n : a.K;
       if (n == a.K) {
@@ -233,7 +248,7 @@ __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
         __builtin_amdgcn_wave_barrier();
         // two lanes' 32 elements at a time
         while (hot) {
-          if (n > kList / 2) cut();
+          if (n > kList - 64) cut();
           const uint32_t l0 = (uint32_t)__builtin_ctzll(hot);
           hot &= hot - 1;
           const uint32_t l1 = hot ? (uint32_t)__builtin_ctzll(hot) : l0;
@@ -472,8 +487,9 @@ constexpr uint32_t kRowWaves = 3072;
 // candidates: parts of one step where those stay below kGroupCands (2 x 8 rows of
 // 18641 in fp16, k 16: 17.6 us against 20.8 with three steps), else longer ones (8 x 8
 // rows of 128003 in fp32, k 8: 22.3 us with four steps against 28.8 with one), up to
-// kLongPart.
-constexpr uint32_t kGroupCands = 2048, kLongPart = 16;
+// kLongPart.  The lists of a large k are what costs in a part: 128 k candidates there (4 x 16 rows of
+// 128003, k 32: 49 us against 54; 32 x 4, k 64: 74 against 71; 1 x 4, k 64: 60 against 68).
+constexpr uint32_t kGroupCands = 2048, kCandsOfK = 128, kLongPart = 16;
 
 int make_plan(const argus_select_config* c, Plan* p) {
   if (!c) return refuse(ARGUS_E_INVAL, "no configuration");
@@ -487,7 +503,7 @@ int make_plan(const argus_select_config* c, Plan* p) {
   if (rows > (uint64_t)kMaxBlocks * kWaves) return refuse(ARGUS_E_CAPACITY, "groups %u x beams %u", c->groups, c->beams);
   const uint32_t steps = (c->vocab + kStep - 1) / kStep;
   const uint64_t parts = rows ? kRowWaves / rows : 1;
-  uint32_t most = kGroupCands / (c->beams * c->k);
+  uint32_t most = (kCandsOfK * c->k > kGroupCands ? kCandsOfK * c->k : kGroupCands) / (c->beams * c->k);
   most = most < steps ? most : steps;
   const uint32_t some = (steps + kLongPart - 1) / kLongPart;
   most = most < some ? some : most;

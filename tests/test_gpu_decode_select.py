@@ -163,3 +163,19 @@ def test_logits_of_any_size(kind):
     x = x.to(TYPES[kind])
     s = torch.tensor([-1.0, -4.0 / 3.0]).repeat(len(x), 1)
     check(x, s, 6)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("k", [31, 32, 33, 63, 64])
+def test_large_k(kind, k):
+    """Lists that fill up within a step, rows that rise (every element is among the best so far) and
+    rows of few values."""
+    log(f"[gpu] select large k {kind} {k}")
+    G, W, V = 3, 2, 30011
+    gen = torch.Generator().manual_seed(k)
+    x = torch.randn(G, W, V, generator=gen) * 2.5
+    x[1] = torch.arange(V) / 4000.0
+    x[2] = torch.randint(0, 3, (W, V), generator=gen).float()
+    x = ((x * 32).round() / 32).clamp(-7.9, 7.9).to(TYPES[kind])
+    s = (torch.logsumexp(x.double(), 2) - 9.0 + torch.arange(W) / (32.0 * W)).float()
+    check(x, s, k)
