@@ -372,14 +372,13 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
     p->first = join64(~w, order_of(score));
     return score > -INFINITY;
   };
+  // (The first of all lists are enough for a bound: 2 x 16 rows of 17365 in fp32, k 32: 28.4 us against
+  // 31.0 with all of them.)
   uint64_t top = 0;
-  for (uint32_t i0 = 0; i0 < total; i0 += kMine * kThreads) {
-    if (i0) fetch(i0);
 #pragma unroll
-    for (uint32_t c = 0; c < kMine; ++c) {
-      Pick p;
-      if (pick_of(c, &p)) top = p.first > top ? p.first : top;
-    }
+  for (uint32_t c = 0; c < kMine; ++c) {
+    Pick p;
+    if (pick_of(c, &p)) top = p.first > top ? p.first : top;
   }
   // The k-th largest of these: in each wave those that fewer than k are above, then
   // of all such.  (What one of a wave's others is above, k of that wave are above.)
@@ -403,7 +402,7 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
   __syncthreads();
   const uint64_t bound = s_bound;
   for (uint32_t i0 = 0; i0 < total; i0 += kMine * kThreads) {
-    if (total > kMine * kThreads) fetch(i0);
+    if (i0) fetch(i0);
 #pragma unroll
     for (uint32_t c = 0; c < kMine; ++c) {
       Pick p;
@@ -488,7 +487,8 @@ constexpr uint32_t kRowWaves = 3072;
 // 18641 in fp16, k 16: 17.6 us against 20.8 with three steps), else longer ones (8 x 8
 // rows of 128003 in fp32, k 8: 22.3 us with four steps against 28.8 with one), up to
 // kLongPart.  The lists of a large k are what costs in a part: 128 k candidates there (4 x 16 rows of
-// 128003, k 32: 49 us against 54; 32 x 4, k 64: 74 against 71; 1 x 4, k 64: 60 against 68).
+// 128003, k 32: 49 us against 54; 32 x 4, k 64: 74 against 71; 1 x 4, k 64: 60 against 68; with a
+// bound from the first of all lists since then 45, 68 and 51, with 256 k 43, 68 and 53).
 constexpr uint32_t kGroupCands = 2048, kCandsOfK = 128, kLongPart = 16;
 
 int make_plan(const argus_select_config* c, Plan* p) {
