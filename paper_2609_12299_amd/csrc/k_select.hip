@@ -107,10 +107,17 @@ constexpr float kSlack = 8.0f;
 // on the rounding of c1 would show in that, and the difference comes first.
 constexpr float kFar = 1e6f;
 // Where a sum stands: half of c1, or the reference itself from kFar on, so that these
-// numbers are in the references' order (c1 / 2 is at most 0.73 kFar).
+// numbers are in the references' order (c1 / 2 is at most 0.73 kFar) and their size says
+// which it is.
 ARGUS_DEV float place_of(float ref, float c1) { return fabsf(ref) < kFar ? 0.5f * c1 : ref; }
-// What a sum at place p is worth at place q >= p.
-ARGUS_DEV float moved(float p, float q) { return __builtin_amdgcn_exp2f((p - q) * (fabsf(q) < kFar ? 2.0f : kLog2e)); }
+// What a sum at place p is worth at place q >= p: a power of 2 with the difference of what the
+// sums' exponents are less, 2 p or p log2 e; where only one is near, in one multiply-add.
+ARGUS_DEV float moved(float p, float q) {
+  const bool near_p = fabsf(p) < kFar, near_q = fabsf(q) < kFar;
+  const float both = (p - q) * (near_q ? 2.0f : kLog2e);
+  const float mixed = near_p ? fmaf(-q, kLog2e, 2.0f * p) : fmaf(p, kLog2e, -2.0f * q);
+  return __builtin_amdgcn_exp2f(near_p == near_q ? both : mixed);
+}
 
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {

@@ -179,3 +179,39 @@ def test_large_k(kind, k):
     x = ((x * 32).round() / 32).clamp(-7.9, 7.9).to(TYPES[kind])
     s = (torch.logsumexp(x.double(), 2) - 9.0 + torch.arange(W) / (32.0 * W)).float()
     check(x, s, k)
+
+
+def around_a_million(V, W, sign):
+    """Rows [5, W, V] in fp32 with values on both sides of sign * 10^6, in steps of 1/16, which 32 bits hold there."""
+    gen = torch.Generator().manual_seed(11)
+    x = torch.empty(5, W, V)
+    x[0] = sign * 1e6 - 0.0625  # of one value, one that stands out on the other side
+    x[0, :, V - 3] = sign * 1e6 + 0.5
+    x[1] = sign * 1e6 + 0.5     # the higher ones first
+    x[1, :, V // 3:] = sign * 1e6 - 0.25
+    x[2] = sign * 1e6 - 8.75 + (torch.randn(W, V, generator=gen) * 2.5 * 16).round() / 16
+    x[3] = sign * 1e6 + (torch.rand(V, generator=gen) * 20 - 10).mul_(16).round_() / 16
+    x[4] = sign * 1e6 - 10 + (20.0 * torch.arange(V) / V * 16).round() / 16  # and the maximum moves all the time
+    return x
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("W,k,V", [(2, 6, 20000), (64, 64, 20000), (2, 3, 4096), (1, 2, 9)])
+def test_logits_on_both_sides_of_a_million(sign, W, k, V):
+    """Where the form of the exponentials changes: a row's parts on either side (the first shape), and the
+    steps of one part (the second)."""
+    log(f"[gpu] select around {sign} 10^6: {W} x {V}")
+    x = around_a_million(V, W, sign)
+    s = (-1.0 - torch.arange(W) / 3.0).repeat(len(x), 1)
+    check(x, s, k)
+
+
+def test_rows_masked_by_a_sum():
+    """Beams of whose tokens all or some carry about -10^6, beside one that carries nothing."""
+    log("[gpu] select masked by a sum")
+    gen = torch.Generator().manual_seed(5)
+    x = (torch.randn(3, 4, 32000, generator=gen) * 2.5 * 16).round() / 16
+    x[:, 1] += -1e6 - 8.75
+    x[:, 2, ::2] += -1e6
+    x[:, 3] += 1e6 - 8.75
+    check(x, (-1.0 - torch.arange(4) / 3.0).repeat(3, 1), 8)
