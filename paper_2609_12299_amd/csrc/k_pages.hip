@@ -940,7 +940,8 @@ extern "C" int argus_decode_step(const argus_step_config* cfg, const argus_step_
   if ((cfg->old_seqs && (!io->d_table || !io->d_lens)) || (cfg->new_seqs && (!io->d_new_table || !io->d_new_lens)) ||
       !io->d_refs || !io->d_counters)
     return refuse(ARGUS_E_INVAL, "a required pointer is NULL");
-  if (io->d_new_table == io->d_table || (io->d_new_lens && io->d_new_lens == io->d_lens) || io->d_refs == io->d_held)
+  // (without sequences the tables may both be NULL)
+  if ((io->d_new_table && io->d_new_table == io->d_table) || (io->d_new_lens && io->d_new_lens == io->d_lens) || io->d_refs == io->d_held)
     return refuse(ARGUS_E_INVAL, "the new table, lens and refs are other buffers than the old");
   if (!aligned_to(io->d_table, 4) || !aligned_to(io->d_lens, 4) || !aligned_to(io->d_parents, 4) || !aligned_to(io->d_grow, 4) ||
       !aligned_to(io->d_held, 4) || !aligned_to(io->d_new_table, 4) || !aligned_to(io->d_new_lens, 4) ||

@@ -353,3 +353,12 @@ def test_packed_layouts_are_the_structures(dec):
             (dec._SELECT_IO, dec.argus_select_io, [*range(9)], None)):
         assert layout.pack(*packed) == bytes(struct(*(fields or packed))), struct
         assert layout.size == ctypes.sizeof(struct)
+
+
+def test_step_of_no_sequences_passes_its_checks(dec):
+    """0 old and 0 new sequences, all tables NULL as empty tensors give them: only the workspace is refused."""
+    none = dict.fromkeys(("d_table", "d_lens", "d_parents", "d_grow", "d_new_table", "d_new_lens"))
+    for held in (None, FAKE):
+        assert step(dec, dict(none, d_held=held), old_seqs=0, new_seqs=0, room=0) == -4
+        assert "workspace" in dec.argus_decode_last_error()
+    assert step(dec, dict(none, d_refs=FAKE), old_seqs=0, new_seqs=0, room=0) == -1

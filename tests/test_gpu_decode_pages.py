@@ -258,3 +258,14 @@ def test_compact(N, S, P, live):
             src, dst = (torch.tensor(x, device="cuda") for x in zip(*want[4]))
             b[:, dst] = b[:, src]
         assert torch.equal(c, b)
+
+
+@pytest.mark.parametrize("N", [32, 5000])
+@pytest.mark.parametrize("parents", [None, []])
+@pytest.mark.parametrize("hold", [False, True])
+def test_step_from_no_sequences_to_none(N, parents, hold):
+    """A batch that has run dry: the holds that are left are counted."""
+    log(f"[gpu] step of no sequences {N} {parents} {hold}")
+    held = [p % 3 - 1 for p in range(N)] if hold else None
+    check_step(np.zeros((0, 4), np.int32), [], parents, None, 8, N, held)
+    check_step(np.zeros((0, 4), np.int32), [], parents, [], 8, N, held)
