@@ -343,7 +343,11 @@ def _elsewhere(stream, dev) -> bool:
     """Whether the call leaves the current stream or device."""
     if dev.type != "cuda":
         _bad(f"tensors on a GPU, not on {dev}")
-    return stream is not None or dev.index != _device()
+    if stream is None:
+        return dev.index != _device()
+    if stream.device != dev:
+        _bad(f"a stream of {stream.device} for tensors on {dev}")
+    return True
 
 
 def _workspace(need: int, ints):

@@ -362,3 +362,18 @@ def test_step_of_no_sequences_passes_its_checks(dec):
         assert step(dec, dict(none, d_held=held), old_seqs=0, new_seqs=0, room=0) == -4
         assert "workspace" in dec.argus_decode_last_error()
     assert step(dec, dict(none, d_refs=FAKE), old_seqs=0, new_seqs=0, room=0) == -1
+
+
+def test_streams_of_another_device_are_refused():
+    """Such a stream cannot run the call, and another one in its place would not be what was asked for."""
+    from types import SimpleNamespace
+
+    import torch
+
+    from paper_2609_12299_amd import ArgusError, decode
+    decode._t()
+    first, second = torch.device("cuda", 0), torch.device("cuda", 1)
+    assert decode._elsewhere(SimpleNamespace(device=first), first)
+    assert decode._elsewhere(SimpleNamespace(device=second), second)
+    with pytest.raises(ArgusError, match="stream of cuda:1"):
+        decode._elsewhere(SimpleNamespace(device=second), first)
