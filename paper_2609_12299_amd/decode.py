@@ -372,8 +372,12 @@ def _buffer(markers):
     return None if markers is None else markers.buffer
 
 
-def _marks(markers):
-    return None if markers is None else ctypes.byref(markers.c)
+def _marks(markers, dev):
+    if markers is None:
+        return None
+    if markers.buffer.device != dev:
+        _bad(f"a MarkerBuffer on {markers.buffer.device} for tensors on {dev}")
+    return ctypes.byref(markers.c)
 
 
 def attend_pages(q, k_cache, v_cache, table, lens, scale: float | None = None, window: int = 0,
@@ -428,7 +432,7 @@ def attend_pages(q, k_cache, v_cache, table, lens, scale: float | None = None, w
                _scales(k_scale, H, "k_scale", dev), _scales(v_scale, H, "v_scale", dev), out.data_ptr(), l_ptr)
     need = _lib_attend_bytes(cfg)
     ws, ws_ptr = _workspace(need, table)
-    _done(_lib_attend(cfg, io, ws_ptr, need, _marks(markers), _raw_stream(dev.index)), "argus_decode_attend")
+    _done(_lib_attend(cfg, io, ws_ptr, need, _marks(markers, dev), _raw_stream(dev.index)), "argus_decode_attend")
     return res
 
 
@@ -466,7 +470,7 @@ def append_tokens(new_k, new_v, k_cache, v_cache, table, starts, offsets=None, k
                tab_stride, _ints(starts, (S,), "starts", dev),
                0 if offsets is None else _ints(offsets, (S + 1,), "offsets", dev),
                _scales(k_scale, H, "k_scale", dev), _scales(v_scale, H, "v_scale", dev))
-    _done(_lib_append(cfg, io, _marks(markers), _raw_stream(dev.index)), "argus_decode_append")
+    _done(_lib_append(cfg, io, _marks(markers, dev), _raw_stream(dev.index)), "argus_decode_append")
 
 
 def step_pages(table, lens, parents, grow, page_size: int, held=None, num_pages: int | None = None,
@@ -507,7 +511,7 @@ def step_pages(table, lens, parents, grow, page_size: int, held=None, num_pages:
                out["counters"].data_ptr(), _caches(caches, N, dev))
     need = argus_decode_step_workspace_bytes(S, N)
     ws, ws_ptr = _workspace(need, table)
-    _done(_lib_step(cfg, io, ws_ptr, need, _marks(markers), _raw_stream(dev.index)), "argus_decode_step")
+    _done(_lib_step(cfg, io, ws_ptr, need, _marks(markers, dev), _raw_stream(dev.index)), "argus_decode_step")
     return out
 
 
@@ -532,7 +536,7 @@ def compact_pages(table, refs, caches=(), markers=None, stream=None) -> dict:
                out["refs"].data_ptr(), out["map"].data_ptr(), out["counters"].data_ptr(), _caches(caches, N, dev))
     need = argus_decode_compact_workspace_bytes(N)
     ws, ws_ptr = _workspace(need, table)
-    _done(_lib_compact(cfg, io, ws_ptr, need, _marks(markers), _raw_stream(dev.index)), "argus_decode_compact")
+    _done(_lib_compact(cfg, io, ws_ptr, need, _marks(markers, dev), _raw_stream(dev.index)), "argus_decode_compact")
     return out
 
 
@@ -574,5 +578,5 @@ def select_beams(logits, scores, k: int, finished=None, eos: int = -1, markers=N
                parents.data_ptr(), out["tokens"].data_ptr(), out["finished"].data_ptr())
     need = _lib_select_bytes(cfg)
     ws, ws_ptr = _workspace(need, parents)
-    _done(_lib_select(cfg, io, ws_ptr, need, _marks(markers), _raw_stream(dev.index)), "argus_decode_select")
+    _done(_lib_select(cfg, io, ws_ptr, need, _marks(markers, dev), _raw_stream(dev.index)), "argus_decode_select")
     return out

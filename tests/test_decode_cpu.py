@@ -377,3 +377,15 @@ def test_streams_of_another_device_are_refused():
     assert decode._elsewhere(SimpleNamespace(device=second), second)
     with pytest.raises(ArgusError, match="stream of cuda:1"):
         decode._elsewhere(SimpleNamespace(device=second), first)
+
+
+def test_marker_buffers_of_another_device_are_refused():
+    """The kernels of one device do not write into the memory of another, or of the host."""
+    import torch
+
+    from paper_2609_12299_amd import ArgusError, MarkerBuffer, decode
+    m = MarkerBuffer(10, device="cpu")
+    assert decode._marks(None, torch.device("cuda", 0)) is None
+    assert decode._marks(m, torch.device("cpu")) is not None
+    with pytest.raises(ArgusError, match="MarkerBuffer on cpu"):
+        decode._marks(m, torch.device("cuda", 0))
