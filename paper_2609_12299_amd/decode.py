@@ -7,7 +7,8 @@ and enqueue on the current torch stream or the one given.  A stream that is give
 not made to wait for the current one, nor the current one for it: the order of their
 work is the caller's, and what a call returns is valid once its stream has come that
 far.  Every step of the computation runs in the HIP kernels of libargus_attr.so; there
-is no fallback.
+is no fallback.  The operators have no backward pass: a tensor that requires gradients
+is refused unless gradients are off (torch.no_grad).
 """
 from __future__ import annotations
 
@@ -231,6 +232,11 @@ def _pack(layout, *fields) -> bytes:
         _bad(f"sizes or strides out of range: {fields}")
 
 
+def _differentiable(name: str) -> None:
+    if _torch.is_grad_enabled():
+        _bad(f"{name} requires gradients, and there is no backward pass: detach it, or call under torch.no_grad()")
+
+
 def _type(x, allowed, name: str) -> int:
     got = _types.get(x.dtype)
     if got not in allowed:
@@ -257,6 +263,8 @@ def _scales(x, heads: int, name: str, dev):
         return 0
     if not (x.dtype == _torch.float32 and x.shape == (heads,) and x.device == dev and x.is_contiguous()):
         _bad(f"{name}: float32 [{heads}], dense, on {dev}")
+    if x.requires_grad:
+        _differentiable(name)
     return x.data_ptr()
 
 
@@ -275,6 +283,8 @@ def _planes(caches, num_pages: int, dev, out) -> None:
         st, shape, e = c.stride(), c.shape, c.element_size()
         if not (c.device == dev and len(shape) >= 3 and shape[1] == num_pages):
             _bad(f"caches[{i}]: [layers, {num_pages} pages, ...] on {dev}")
+        if c.requires_grad:
+            _differentiable(f"caches[{i}]")
         # a page is one run of memory, in whatever order its dimensions lie
         run = 1
         for step, n in sorted(zip(st[2:], shape[2:])):
@@ -405,6 +415,8 @@ def attend_pages(q, k_cache, v_cache, table, lens, scale: float | None = None, w
     S, heads, D = q.shape
     qt = _type(q, (BF16, FP16), "q")
     ct = _type(k_cache, (qt, FP8), "k_cache")
+    if q.requires_grad or k_cache.requires_grad or v_cache.requires_grad:
+        _differentiable("q, k_cache or v_cache")
     k, v = _view(k_cache, "k_cache", dev), _view(v_cache, "v_cache", dev)
     N, H, ps, kd = k_cache.shape
     if not (v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype and kd == D):
@@ -423,6 +435,8 @@ def attend_pages(q, k_cache, v_cache, table, lens, scale: float | None = None, w
         out = q.new_empty((S, heads, D))
     elif not (out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.is_contiguous()):
         _bad("out: like q, dense")
+    elif out.requires_grad:
+        _differentiable("out")
     res = dict(out=out)
     l_ptr = 0
     if lse:
@@ -458,6 +472,8 @@ def append_tokens(new_k, new_v, k_cache, v_cache, table, starts, offsets=None, k
     if not (len(ks) == len(vs) == 3 and (ks[2] == vs[2] == 1 or D == 1) and new_k.device == dev and new_v.device == dev):
         _bad(f"new_k, new_v: [rows, kv_heads, head_dim] with contiguous rows on {dev}")
     st = _type(new_k, (BF16, FP16), "new_k")
+    if new_k.requires_grad or new_v.requires_grad or k_cache.requires_grad or v_cache.requires_grad:
+        _differentiable("new_k, new_v, k_cache or v_cache")
     ct = _type(k_cache, (st, FP8), "k_cache")
     if not (v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype):
         _bad("k_cache and v_cache differ")
@@ -561,6 +577,8 @@ def select_beams(logits, scores, k: int, finished=None, eos: int = -1, markers=N
     G, W, V = logits.shape
     if not (scores.dtype == t.float32 and scores.shape == (G, W) and scores.device == dev and scores.is_contiguous()):
         _bad(f"scores: float32 {(G, W)}, dense, on {dev}")
+    if logits.requires_grad or scores.requires_grad:
+        _differentiable("logits or scores")
     done = 0
     if finished is not None:
         if not (finished.dtype in (t.bool, t.uint8) and finished.shape == (G, W) and finished.device == dev

@@ -389,3 +389,21 @@ def test_marker_buffers_of_another_device_are_refused():
     assert decode._marks(m, torch.device("cpu")) is not None
     with pytest.raises(ArgusError, match="MarkerBuffer on cpu"):
         decode._marks(m, torch.device("cuda", 0))
+
+
+def test_tensors_that_require_gradients_are_refused():
+    """There is no backward pass: a result without history would be taken for one of constants."""
+    import torch
+
+    from paper_2609_12299_amd import ArgusError, decode
+    decode._t()
+    dev = torch.device("cpu")
+    out = (decode.argus_page_planes * 4)()
+    cache = torch.zeros(2, 2, 8, 16, dtype=torch.bfloat16, requires_grad=True)
+    scale = torch.zeros(2, requires_grad=True)
+    for call in (lambda: decode._differentiable("q"), lambda: decode._scales(scale, 2, "k_scale", dev),
+                 lambda: decode._planes((cache,), 2, dev, out)):
+        with pytest.raises(ArgusError, match="no_grad"):
+            call()
+        with torch.no_grad():
+            call()
