@@ -176,7 +176,7 @@ def argus_decode_select(cfg, io, d_workspace, workspace_bytes, markers, stream) 
 
 _torch = None
 _types = {}
-_raw_stream = _device = None
+_raw_stream = _device = _written = None
 _lib_attend = _lib_attend_bytes = _lib_append = _lib_step = _lib_compact = _lib_select = _lib_select_bytes = None
 
 # The structures of the header, field by field (native alignment).
@@ -189,7 +189,7 @@ _SELECT_CONFIG, _SELECT_IO = struct.Struct("6IiI"), struct.Struct("Q2q 6Q")
 
 
 def _t():
-    global _torch, _raw_stream, _device, _lib_attend, _lib_attend_bytes, _lib_append, _lib_step, _lib_compact
+    global _torch, _raw_stream, _device, _written, _lib_attend, _lib_attend_bytes, _lib_append, _lib_step, _lib_compact
     global _lib_select, _lib_select_bytes
     if _torch is None:
         import torch
@@ -199,6 +199,8 @@ def _t():
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                               lambda index: torch.cuda.current_stream(index).cuda_stream)
         _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        # (of tensors that a call writes in place, so that autograd sees it where it has kept them)
+        _written = getattr(torch._C, "_increment_version", torch.autograd.graph.increment_version)
         lib = _library()
 
         def of(name, *types):
@@ -431,7 +433,8 @@ def attend_pages(q, k_cache, v_cache, table, lens, scale: float | None = None, w
         _bad(f"window {window}, sinks {sinks}")
     cfg = _pack(_ATTEND_CONFIG, ABI_VERSION, qt, ct, S, H, heads // H if heads else 1, D, ps, N, P, window, sinks,
                               D ** -0.5 if scale is None else scale, 0)
-    if out is None:
+    given = out is not None
+    if not given:
         out = q.new_empty((S, heads, D))
     elif not (out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.is_contiguous()):
         _bad("out: like q, dense")
@@ -447,6 +450,8 @@ def attend_pages(q, k_cache, v_cache, table, lens, scale: float | None = None, w
     need = _lib_attend_bytes(cfg)
     ws, ws_ptr = _workspace(need, table)
     _done(_lib_attend(cfg, io, ws_ptr, need, _marks(markers, dev), _raw_stream(dev.index)), "argus_decode_attend")
+    if given:
+        _written((out,))
     return res
 
 
@@ -487,6 +492,7 @@ def append_tokens(new_k, new_v, k_cache, v_cache, table, starts, offsets=None, k
                0 if offsets is None else _ints(offsets, (S + 1,), "offsets", dev),
                _scales(k_scale, H, "k_scale", dev), _scales(v_scale, H, "v_scale", dev))
     _done(_lib_append(cfg, io, _marks(markers, dev), _raw_stream(dev.index)), "argus_decode_append")
+    _written((k_cache, v_cache))
 
 
 def step_pages(table, lens, parents, grow, page_size: int, held=None, num_pages: int | None = None,
@@ -528,6 +534,7 @@ def step_pages(table, lens, parents, grow, page_size: int, held=None, num_pages:
     need = argus_decode_step_workspace_bytes(S, N)
     ws, ws_ptr = _workspace(need, table)
     _done(_lib_step(cfg, io, ws_ptr, need, _marks(markers, dev), _raw_stream(dev.index)), "argus_decode_step")
+    _written(caches)
     return out
 
 
@@ -553,6 +560,7 @@ def compact_pages(table, refs, caches=(), markers=None, stream=None) -> dict:
     need = argus_decode_compact_workspace_bytes(N)
     ws, ws_ptr = _workspace(need, table)
     _done(_lib_compact(cfg, io, ws_ptr, need, _marks(markers, dev), _raw_stream(dev.index)), "argus_decode_compact")
+    _written(caches)
     return out
 
 
