@@ -40,6 +40,10 @@ ARGUS_DEV float quotient(float x, float s, float y) {
   return r < -448.0f ? -448.0f : r;
 }
 
+// Scales that quotient() takes.  Outside (0, infinities and NaN among them) the reciprocal, or the
+// remainder of a quotient that is not rounded to zero, would leave the normal numbers of 32 bits.
+ARGUS_DEV bool ordinary(float s) { return fabsf(s) >= 0x1p-80f && fabsf(s) <= 0x1p80f; }
+
 template <int T>  // 0: bf16, 1: fp16
 ARGUS_DEV f32x2 pair(uint32_t w) {
   if constexpr (T == 0) {
@@ -109,11 +113,18 @@ __global__ __launch_bounds__(kThreads) void k_append(AppendArgs a) {
       const u32x4 lo = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + 2 * at));
       const u32x4 hi = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + 2 * at + 16));
       const float* scale = values ? a.v_scale : a.k_scale;
-      const float sc = scale ? scale[h] : 1.0f, inv = 1.0f / sc;
+      float sc = scale ? scale[h] : 1.0f, inv = 1.0f / sc;
+      f32x2 x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = pair<MODE - 1>(i < 4 ? lo[i] : hi[i - 4]);
+      if (!ordinary(sc)) {  // divided here, and by 1 below
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (f32x2){x[i].x / sc, x[i].y / sc};
+        sc = inv = 1.0f;
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const f32x2 p = pair<MODE - 1>(i < 2 ? lo[2 * i] : hi[2 * i - 4]);
-        const f32x2 q = pair<MODE - 1>(i < 2 ? lo[2 * i + 1] : hi[2 * i - 3]);
+        const f32x2 p = x[2 * i], q = x[2 * i + 1];
         int w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(p.x, sc, inv), quotient(p.y, sc, inv), 0, false);
         w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(q.x, sc, inv), quotient(q.y, sc, inv), w, true);
         out[i] = (uint32_t)w;

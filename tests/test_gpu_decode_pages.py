@@ -269,3 +269,24 @@ def test_step_from_no_sequences_to_none(N, parents, hold):
     held = [p % 3 - 1 for p in range(N)] if hold else None
     check_step(np.zeros((0, 4), np.int32), [], parents, None, 8, N, held)
     check_step(np.zeros((0, 4), np.int32), [], parents, [], 8, N, held)
+
+
+@pytest.mark.parametrize("source", ["bf16", "fp16"])
+@pytest.mark.parametrize("scale", [2.0 ** -149, 2.0 ** -140, 2.0 ** -129, 1.1 * 2.0 ** -127, 2.0 ** -126, 1.7 * 2.0 ** -119,
+                                   2.0 ** -100, 1.3 * 2.0 ** -81, 1.9 * 2.0 ** -80, 1.1 * 2.0 ** 80, 1.7 * 2.0 ** 118,
+                                   1.3 * 2.0 ** 127, float("inf"), 0.0, -0.5, -2.0 ** -130])
+def test_append_scales_of_any_size(source, scale):
+    """All numbers of 16 bits over scales whose reciprocal is no ordinary number, or whose products leave
+    remainders below the least number of 32 bits."""
+    from paper_2609_12299_amd import append_tokens
+    log(f"[gpu] append {source} over {scale}")
+    every = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(TYPES[source]).reshape(256, 1, 256)
+    s = torch.tensor([scale], dtype=torch.float64).float()
+    k, v = (torch.zeros(32, 1, 8, 256, dtype=torch.uint8, device="cuda").view(TYPES["fp8"]) for _ in range(2))
+    append_tokens(every.cuda(), every.cuda(), k, v, torch.arange(32, dtype=torch.int32, device="cuda")[None],
+                  ints([0]), ints([0, 256]), s.cuda(), s.cuda())
+    want = (every.float() / s).clamp(-448, 448).to(TYPES["fp8"]).float().reshape(-1)
+    for c in (k, v):
+        got = c.float().cpu().reshape(-1)
+        assert torch.equal(torch.isnan(got), torch.isnan(want))
+        assert torch.equal(got.nan_to_num(0), want.nan_to_num(0))
