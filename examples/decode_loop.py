@@ -109,7 +109,7 @@ def search(model: Model, prompts, beams: int, steps: int, eos: int = -1, markers
     for i in range(steps):
         mk = markers if i >= steps - marked else None
         tokens = d.select(logits, eos, mk)
-        # a beam without a candidate goes on as its own group's first, with a score of -inf
+        # a beam without a candidate goes on from itself, with a score of -inf: nothing selects it again
         alive = d.parents >= 0
         d.parents = torch.where(alive, d.parents, torch.arange(len(d.parents), device=d.parents.device).int())
         tokens = torch.where(alive, tokens, 0)
