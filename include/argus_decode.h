@@ -56,9 +56,10 @@ enum {
 /* A buffer of marker records.  A call that is given one adds its records
  * behind the first `used` and moves `used` on (ARGUS_E_CAPACITY, and nothing is
  * enqueued, where they do not fit); how many is known at the call.  One
- * context per wave (ctx_base + block * waves + wave), time in ticks of the
- * device's constant 100 MHz clock.  An operator's answers are the same with
- * and without markers. */
+ * context per wave (ctx_base + block * waves + wave; four waves a block, sixteen
+ * in a step that is one launch: ARGUS_REGION_STEP_PLAN and _PLACE without _CLEAR), time
+ * in ticks of the device's constant 100 MHz clock.  An operator's answers are
+ * the same with and without markers. */
 typedef struct argus_markers {
   argus_record* d_records; /* 16-byte aligned */
   uint64_t capacity;       /* records */

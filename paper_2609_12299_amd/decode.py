@@ -312,8 +312,9 @@ def _caches(caches, num_pages: int, dev) -> bytes:
 class MarkerBuffer:
     """Marker records that the operators write of their own regions: give it as
     `markers` to the calls of one stream, then `records()` to
-    RegionAttribution(num_regions=region_base + NUM_REGIONS).run.  Contexts are waves
-    (group_shift 2: blocks), time is in ticks of 10 ns."""
+    RegionAttribution(num_regions=region_base + NUM_REGIONS).run.  Contexts are waves, time
+    is in ticks of 10 ns.  Four contexts (group_shift 2) are a block, save of a step that is
+    one launch (few sequences and pages): its blocks have sixteen waves, four such groups each."""
 
     def __init__(self, capacity: int, ctx_base: int = 0, region_base: int = 0, device="cuda"):
         t = _t()

@@ -123,3 +123,23 @@ def test_example_runs():
                         "--prompt", "20"], capture_output=True, text=True, timeout=100)
     assert r.returncode == 0, r.stderr[-2000:]
     assert "0 mismatched, 0 unclosed, 0 orphans" in r.stdout and "attend.tokens" in r.stdout
+
+
+def test_contexts_of_a_block():
+    """Four contexts are a block, sixteen in a step that is one launch."""
+    from paper_2609_12299_amd import REGION_NAMES, MarkerBuffer, select_beams, step_pages
+    log("[gpu] contexts of a block")
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    m = MarkerBuffer(1 << 16, ctx_base=40)
+
+    def contexts(region):
+        torch.cuda.synchronize()
+        words = m.records().cpu().numpy().view(np.uint32).reshape(-1, 4)
+        m.clear()
+        return set(words[words[:, 3] & 0xFFFF == REGION_NAMES.index(region), 2].tolist())
+    step_pages(ints(0, 1).view(2, 1), ints(3, 4), None, ints(1, 1), 16, num_pages=100, markers=m)
+    assert m.used == 16 * 4 and contexts("step.plan") == set(range(40, 56))
+    step_pages(ints(0, 1).view(2, 1), ints(3, 4), None, ints(1, 1), 16, num_pages=5000, markers=m)
+    assert contexts("step.claim") == set(range(40, 44))
+    select_beams(torch.zeros(3, 2, 100, device="cuda"), torch.zeros(3, 2, device="cuda"), 2, markers=m)
+    assert contexts("select.beams") == set(range(40, 52))
