@@ -122,7 +122,8 @@ struct Half<0> {
   }
   // Two weights as the sum of two numbers each, none of them above the weight
   // and none 0 beside a weight that is not: times an infinite value, a
-  // negative or zero rest would make a NaN of infinity.
+  // negative or zero rest would make a NaN of infinity.  (It does where a weight is
+  // below what its type has: 2^-126 of the largest, in fp16 2^-31.)
   static ARGUS_DEV void split(float x, float y, uint32_t* hi, uint32_t* lo) {
     const uint32_t a = __builtin_bit_cast(uint32_t, x) | 1u, b = __builtin_bit_cast(uint32_t, y) | 1u;
     *hi = __builtin_amdgcn_perm(b, a, 0x07060302u);

@@ -37,22 +37,24 @@ int device_ok() {
 namespace {
 
 // Waves that share a batch: one block of four for each of the 256 compute
-// units (twice as many: 655 us against 645 for four sequences of 262143 tokens, 92
-// against 85 for 128 of 1000, 69 against 65 for the 8-bit batch).  All of them may
+// units (twice as many: 650 us against 640 for four sequences of 262143 tokens, 72
+// against 68 for the 8-bit batch).  All of them may
 // fall to one segment (one of 131072 tokens, 1 x 8 heads of 128: 24 us, with at most 512 27,
 // with 256 34).  Two blocks where a tile's rows are so short
 // that one wave for each SIMD has too few bytes under way: of 64 bytes (64 sequences of up to
-// 16384 tokens in 8 bits: 35 us against 41; of 128 bytes 49.7 against 48.1).
+// 16384 tokens in 8 bits: 36 us against 41; of 128 bytes 49.7 against 48.1).
 constexpr uint32_t kShares = 256 * kWaves, kSharesOfSegment = 1024;
 // A block of the join takes 32 elements of a row where segments may lie in so many pieces
-// (a sequence of 32768 tokens, 1 x 8 heads of 128: 16.3 us against 18.6 by whole rows; of
-// 8192, 66 pieces, 15.8 against 15.2); a row where there are so few of them (6 sequences of up to 3111,
-// 8 x 4 heads: 15.9 us against 16.8 by four rows), else four (10 of 8502 with a window of
-// 1060, 2 x 24 heads: 18.6 us against 19.2 by one row).
+// (the join of a sequence in 66 pieces, 1 x 8 heads of 128, takes 3.9 us by parts and by whole
+// rows, in 98 pieces 4.0 against 5.1, in 258 3.9 against 7.0, in 1024 7.8 against 18.1); a
+// row where there are so few of them (6 sequences of up to 3111, 8 x 4 heads: 15.8 us a call
+// against 16.7 by four rows), else four (10 of 8502 with a window of 1060, 2 x 24 heads: 18.3
+// us against 19.4 by one row).
 constexpr uint32_t kManyPieces = 64, kFewRows = 256;
 // Segments of at most this many tiles are not shared: a block each, and no joining
-// (64 sequences of 512 tokens, 8 x 4 heads of 128: 23 us against 30 shared; of 1024 tokens 45
-// against 52, and 4 of them 14.7 both; at head size 256, 4 of 1024: 34 against 25).
+// (64 sequences of 512 tokens, 8 x 4 heads of 128: 24 us against 30 shared; of 1024 tokens 44
+// against 50, and 4 of them 14.8 against 15.3; at head size 256, 4 of 512 18.7 against 23.1,
+// 4 of 1024 33 against 25).
 uint32_t whole_tiles(uint32_t dp) { return dp == 256 ? 16u : 32u; }
 
 struct Plan {

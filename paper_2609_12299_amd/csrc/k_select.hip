@@ -32,12 +32,13 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint32_t kItems = 32;               // elements of a lane per step
 constexpr uint32_t kStep = kItems * 64;
 // Candidates of a wave.  A cut counts, for each, those above it: the more room there is beyond
-// 64, the rarer it is for a large k (32 x 4 rows of 128003, k 64: 188 us with 128, 71 with 192,
-// 72 with 256; finding the k-th key bit by bit instead 54 against 43 for k 8).
+// 64, the rarer it is for a large k (32 x 4 rows of 128003, k 64: 174 us with 128, 68 with 192,
+// 71 with 256; 96 x 8 rows, k 8, 43.5, 43.1 and 43.2; finding the k-th key bit by bit
+// instead 54 against 43).
 constexpr uint32_t kList = 192;
 // Beyond its k a list holds so many before it is cut at the end of a step: the
-// sooner the least rises, the fewer lanes are looked through (0: 51.5 us, 8: 50.1,
-// 16: 50.8, only when half full: 54.4, with lists of 128; 96 x 8 rows of 128003 in bf16, k 8).
+// sooner the least rises, the fewer lanes are looked through (0: 43.4 us, 8: 43.1,
+// 16: 43.1, only when half full: 48.0; 96 x 8 rows of 128003 in bf16, k 8).
 constexpr uint32_t kRoom = 8;
 constexpr uint32_t kCands = 512;              // candidates of a group that are ranked by counting
 constexpr uint32_t kMaxK = 64, kMaxBeams = 64;
@@ -486,7 +487,7 @@ struct Plan {
   size_t cands_at, bytes;
 };
 
-// Waves that read the logits (4096 and 2048: 49.1 and 51.3 us against 46.7 for 96 x
+// Waves that read the logits (4096 and 2048: 44.2 and 49.9 us against 43.1 for 96 x
 // 8 rows of 128003 in bf16).
 constexpr uint32_t kRowWaves = 3072;
 // More parts make shorter work of the rows and longer work of the group's
