@@ -51,7 +51,7 @@ struct SelectArgs {
   float* new_scores;
   int32_t *parents, *tokens;
   uint8_t* new_finished;
-  float2* sums;     // [rows][parts] place (place_of), sum
+  float2* sums;     // [rows][parts] reference, sum of exp(x - reference)
   uint64_t* cands;  // [rows][parts][k] (value, token) as a key, 0: none; no order
   uint32_t W, V, K, parts;
   FastDiv by_group, by_row;  // by W * parts, by parts
@@ -107,18 +107,8 @@ constexpr float kSlack = 8.0f;
 // An exponential is 2^(x log2 e - c1), one multiply-add; from references of this size
 // on the rounding of c1 would show in that, and the difference comes first.
 constexpr float kFar = 1e6f;
-// Where a sum stands: half of c1, or the reference itself from kFar on, so that these
-// numbers are in the references' order (c1 / 2 is at most 0.73 kFar) and their size says
-// which it is.
-ARGUS_DEV float place_of(float ref, float c1) { return fabsf(ref) < kFar ? 0.5f * c1 : ref; }
-// What a sum at place p is worth at place q >= p: a power of 2 with the difference of what the
-// sums' exponents are less, 2 p or p log2 e; where only one is near, in one multiply-add.
-ARGUS_DEV float moved(float p, float q) {
-  const bool near_p = fabsf(p) < kFar, near_q = fabsf(q) < kFar;
-  const float both = (p - q) * (near_q ? 2.0f : kLog2e);
-  const float mixed = near_p ? fmaf(-q, kLog2e, 2.0f * p) : fmaf(p, kLog2e, -2.0f * q);
-  return __builtin_amdgcn_exp2f(near_p == near_q ? both : mixed);
-}
+// What a sum of exp(x - p) is worth as one of exp(x - q), q >= p.
+ARGUS_DEV float moved(float p, float q) { return __builtin_amdgcn_exp2f((p - q) * kLog2e); }
 
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
@@ -192,17 +182,20 @@ __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
       if (want) list[n + (uint32_t)__popcll(take & lanemask_lt())] = key;
       n += (uint32_t)__popcll(take);
     };
-    // The sum is of 2^(x log2 e - c1), about exp(x - ref).
-    float ref = -INFINITY, c = -INFINITY, c1 = 0.0f, sum = 0.0f;
+    // The sum is of 2^(x log2 e - c1), about exp(x - ref); far ones of exp(x - ref).  Either way a
+    // sum moves, near and far ones among each other too, with no rounding of c1 that shows.
+    float ref = -INFINITY, c1 = 0.0f, sum = 0.0f;
     bool far = false;
     auto refer = [&](float to) {
+      if (to == -INFINITY) return;
+      const float was = ref, c1_was = c1;
+      const bool far_was = far;
       ref = to;
-      if (ref == -INFINITY) return;
       far = fabsf(ref) >= kFar;
       c1 = ref * kLog2e;
-      const float was = c;
-      c = place_of(ref, c1);
-      sum *= was == -INFINITY ? 0.0f : moved(was, c);
+      if (was == -INFINITY) sum *= 0.0f;  // (a NaN stays)
+      else if (far) sum *= far_was ? moved(was, ref) : __builtin_amdgcn_exp2f(fmaf(-ref, kLog2e, c1_was));
+      else sum *= __builtin_amdgcn_exp2f(far_was ? fmaf(was, kLog2e, -c1) : c1_was - c1);
     };
     if (part == 0) {  // what lies before and behind the vectors: at most 2 * (kPer - 1) elements
       const uint32_t j = lane < kPer ? lane : tail + lane - kPer;
@@ -288,7 +281,8 @@ __global__ __launch_bounds__(kThreads) void k_select_rows(SelectArgs a) {
     }
     cut();
     sum = wave_sum(sum);
-    if (lane == 0) a.sums[job] = make_float2(c, sum);
+    if (!far && ref > -INFINITY) sum *= __builtin_amdgcn_exp2f(fmaf(-ref, kLog2e, c1));
+    if (lane == 0) a.sums[job] = make_float2(ref, sum);
     if (lane < a.K) a.cands[(uint64_t)job * a.K + lane] = lane < n ? list[lane] : 0;
   }
   mk.end(ARGUS_REGION_SELECT_ROWS);
@@ -302,7 +296,7 @@ ARGUS_DEV bool before(const Pick& x, const Pick& y) { return x.first > y.first |
 
 __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
   constexpr uint32_t kMine = 4;  // candidates that a thread holds at a time
-  __shared__ float s_lse[kMaxBeams], s_rest[kMaxBeams], s_score[kMaxBeams];
+  __shared__ float s_ref[kMaxBeams], s_log[kMaxBeams], s_score[kMaxBeams];
   __shared__ uint32_t s_done[kMaxBeams];
   __shared__ uint32_t s_n;
   __shared__ Pick s_cand[kCands];
@@ -348,12 +342,10 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
       top = most;
     }
     if (tid % 16 == 0) {
-      // The logarithm, taken off a logit in two steps: of one number near 10^6 the rounding
+      // The logarithm is taken off a logit in two steps: of one number near 10^6 the rounding
       // would show, and 10^10 leaves no place for the sum's.
-      // (What lies in the sum has kLog2e's rounding in its exponents, and so has top.)
-      const double lse = 2.0 * (double)top * (1.0 / (double)kLog2e) + (double)log2f(sum) * 0.69314718055994530942;
-      s_lse[w] = fabsf(top) < kFar ? (float)lse : top;
-      s_rest[w] = fabsf(top) < kFar ? (float)(lse - (double)(float)lse) : logf(sum);
+      s_ref[w] = top;
+      s_log[w] = logf(sum);
       s_score[w] = score;
       s_done[w] = done;
     }
@@ -375,7 +367,7 @@ __global__ __launch_bounds__(kThreads) void k_select_beams(SelectArgs a) {
     } else {
       p->key = key[c];
       if (p->key == 0) return false;
-      score = s_score[w] + (value_of((uint32_t)(p->key >> 32)) - s_lse[w] - s_rest[w]);
+      score = s_score[w] + (value_of((uint32_t)(p->key >> 32)) - s_ref[w] - s_log[w]);
     }
     p->first = join64(~w, order_of(score));
     return score > -INFINITY;
