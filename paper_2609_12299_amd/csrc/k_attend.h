@@ -167,10 +167,12 @@ ARGUS_DEV uint32_t widen(uint32_t w, bool hi) {
 // How far a score may rise above the running maximum before the maximum moves:
 // weights stay below 2^8, and the sums need no rescaling at most steps.
 constexpr float kSlack = 5.5f;
-// A weight is 2^(x kd2 - base), one multiply-add and the exponential.  Beyond
-// kFar the product's rounding would show in that, and near the largest float it
-// would overflow: then the difference of the scores first, and that to base 2.
-constexpr float kFar = 1e6f;
+// A weight is 2^(x kd2 - base), one multiply-add and the exponential.  The base, the
+// maximum to base 2, is rounded: all weights of one maximum are off alike, but not
+// those of another, before it moved or in another wave.  Up to kFar that is 2^-14.5 of
+// a weight.  Beyond it (at 2^15 it would be 2^-10, at 2^19 2^-6), and where a scale is so odd that the
+// product overflows, the difference of the scores comes first, and that to base 2.
+constexpr float kFar = 1024.0f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 ARGUS_DEV float exp_of(float x) { return exp2f(x * kLog2e); }
 

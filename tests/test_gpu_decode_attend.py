@@ -345,3 +345,32 @@ def test_more_segments_than_blocks():
     # one weight over itself: the value, rounded once
     assert ((got["out"].float() - want.float()).abs() <= want.float().abs() * 2.0 ** -8).all()
     assert (got["lse"][::7] == -math.inf).all() and torch.isfinite(got["lse"][1::7]).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("big", [2.0 ** 9, 2.0 ** 12, 2.0 ** 15, 2.0 ** 19, -2.0 ** 19])
+@pytest.mark.parametrize("tokens,columns", [(400, 40), (4000, 400)])
+def test_large_scores_that_climb(kind, big, tokens, columns):
+    """Large scores, exact in 32 bits, whose maximum moves from tile to tile and from wave to wave: a block
+    for all of them, and pieces that are joined.  What is left is the rounding of the result, the
+    exponentials (2^-22 each) and the weights' own (2^-16), with the maximum's below 2^-13."""
+    log(f"[gpu] attend climbing scores near {big} {kind} {tokens}")
+    a = make(kind, [tokens], 1, 2, 64, 16, columns=columns, junk=False)
+    k, t = a["k_cache"], a["table"]
+    a["scale"] = 1.0
+    a["q"] = torch.zeros_like(a["q"])
+    a["q"][:, :, 0], a["q"][:, :, 1] = 16.0, 1.0
+    j = torch.arange(tokens)
+    small = (j * 13.0 / tokens * 4).round() / 4 + (j % 4) / 4.0  # climbs by 13, in quarters
+    rows = torch.zeros(tokens, 64)
+    rows[:, 0], rows[:, 1] = big / 16, small
+    k[t[0, j // 16].long(), 0, j % 16] = rows.to(TYPES[kind])
+    got = run(a)
+    w = torch.exp((small - small.max()).double())
+    v = a["v_cache"][t[0, j // 16].long(), 0, j % 16].double()
+    want = (w[:, None] * v).sum(0) / w.sum()
+    mean = (w[:, None] * v.abs()).sum(0) / w.sum()
+    off = (got["out"][0].double().cpu() - want).abs()
+    assert (off <= ref.ROUND[TYPES[kind]] * 1.01 * want.abs() + 2.0 ** -13 * mean).all(), (off / mean).max()
+    lse = big + small.max().double() + torch.log(w.sum())
+    assert ((got["lse"][0].double().cpu() - lse).abs() <= 2.0 ** -23 * lse.abs() + 2.0 ** -13).all()
