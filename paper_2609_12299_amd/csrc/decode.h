@@ -24,7 +24,8 @@ struct Marks {
   uint32_t ctx, region, per_wave;
 };
 
-// A wave's markers.  Without a buffer each costs one scalar branch.
+// A wave's markers.  Without a buffer each costs one scalar branch; with one 0.2 to 0.4 us
+// of a short call, 1 to 2 of a long one (79376 of them in a call of 95 us: 97).
 struct WaveMarks {
   argus_record* at = nullptr;
   uint32_t ctx = 0, region = 0;

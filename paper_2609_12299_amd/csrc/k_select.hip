@@ -16,7 +16,7 @@
 //
 // What bounds it: the reading of the logits, and the exponential of each (a
 // quarter of the rate of other instructions): 96 x 8 rows of 128003 in bf16, 197 MB, k 8: 37 us
-// for the rows, 5.3 TB/s with the vector units busy 0.57 of the time, and 7 us for the beams.
+// for the rows, 5.3 TB/s with the vector units busy 0.55 of the time, and 7 us for the beams.
 #include "decode.h"
 
 namespace argus {
