@@ -7,7 +7,8 @@ per-region duration statistics, class overlap and ambiguity counts, and PC
 samples are attributed to those instances, computed by hand-written HIP
 kernels for gfx950 behind a C ABI (include/argus_attr.h).  The operators of a
 decode step, whose kernels write marker records of their own regions, stand
-beside it (include/argus_decode.h).
+beside it (include/argus_decode.h), and those of a prompt's pass over the same
+paged cache (include/argus_prompt.h).
 """
 from .attr import (ABI_VERSION, COUNTER_NAMES, FORCE_EVENT_SORT, FORCE_FULL_SORT,
                    FORCE_RECORD_RADIX, INSTANCE_DTYPE, NOALLOC_SCRATCH_BYTES, NUM_COUNTERS,
@@ -31,6 +32,10 @@ from .decode import (COMPACT_COUNTER_NAMES, NUM_REGIONS, REGION_NAMES, STEP_COUN
                      argus_decode_select, argus_decode_select_workspace_bytes, argus_decode_step,
                      argus_decode_step_workspace_bytes, attend_pages, compact_pages, select_beams,
                      step_pages)
+from .prompt import (ALL_REGION_NAMES, NUM_ALL_REGIONS, PROMPT_REGION_NAMES, argus_prompt_attend,
+                     argus_prompt_attend_workspace_bytes, argus_prompt_rotate, argus_prompt_score,
+                     argus_prompt_score_workspace_bytes, attend_chunks, rotary_frequencies,
+                     rotate_tokens, score_tokens)
 
 __all__ = [
     "ABI_VERSION", "COUNTER_NAMES", "FORCE_EVENT_SORT", "FORCE_FULL_SORT", "FORCE_RECORD_RADIX",
@@ -52,4 +57,8 @@ __all__ = [
     "argus_decode_compact_workspace_bytes", "argus_decode_last_error", "argus_decode_select",
     "argus_decode_select_workspace_bytes", "argus_decode_step", "argus_decode_step_workspace_bytes",
     "attend_pages", "compact_pages", "select_beams", "step_pages",
+    "ALL_REGION_NAMES", "NUM_ALL_REGIONS", "PROMPT_REGION_NAMES", "argus_prompt_attend",
+    "argus_prompt_attend_workspace_bytes", "argus_prompt_rotate", "argus_prompt_score",
+    "argus_prompt_score_workspace_bytes", "attend_chunks", "rotary_frequencies", "rotate_tokens",
+    "score_tokens",
 ]

@@ -18,7 +18,8 @@ LIB = os.path.join(HERE, "libargus_attr.so")
 SOURCES = ["attr_host.hip", "k_ingest.hip", "k_radix.hip", "k_match.hip", "k_resolve.hip", "k_merge.hip",
            "k_agg.hip", "k_overlap.hip", "k_samples.hip", "k_scope.hip", "trace_export.hip",
            "k_attend.hip", "k_attend_bf16.hip", "k_attend_fp16.hip", "k_attend_bf16_f8.hip",
-           "k_attend_fp16_f8.hip", "k_pages.hip", "k_select.hip"]
+           "k_attend_fp16_f8.hip", "k_pages.hip", "k_select.hip", "k_chunk.hip", "k_chunk_bf16.hip",
+           "k_chunk_fp16.hip", "k_chunk_bf16_f8.hip", "k_chunk_fp16_f8.hip", "k_rotate.hip", "k_score.hip"]
 ARCH = "gfx950"
 
 

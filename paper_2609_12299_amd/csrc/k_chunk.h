@@ -1,0 +1,574 @@
+// k_chunk.h -- attention of chunks of new tokens over a paged cache.
+//
+// The queries of one sequence that share a key/value head, `group` of them for each
+// new token, are rows r = token * group + head of one matrix; a block takes a tile of
+// them (32 rows a wave) and goes over the tokens that its rows see, KT at a time:
+//
+//   S^T[token][row] = K[token][d] Q^T[d][row]    mfma 32x32x16
+//   P = exp(S^T * c - m)                         c = scale * k_scale, m per row
+//   O^T[d][row] += V^T[d][token] P^T[token][row] mfma 32x32x16
+//
+// With rows as columns a lane holds 16 scores of one row, half a wave apart from the
+// other 16, and what the first product leaves in its registers is what the second takes:
+// which token stands at which place of a contraction is free. Keys and values go through
+// LDS, read once for the block; queries and O stay in registers.
+#pragma once
+
+#include "k_attend.h"
+#include "prompt.h"
+
+namespace argus {
+namespace prompt {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// Tokens of a step: two buffers of keys and values are 64 KiB at head sizes of 128 and 256.
+template <int DP>
+constexpr int kStepTokens = DP == 256 ? 32 : 64;
+
+struct ChunkArgs {
+  const uint16_t* q;
+  int64_t q_row, q_head;
+  const uint8_t *k, *v;
+  int64_t k_head, v_head, k_page, v_page;  // bytes
+  uint32_t k_tok, v_tok;                   // bytes
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t *lens, *offsets;
+  const float *k_scale, *v_scale;
+  uint16_t* out;
+  float* lse;
+  // shared out: what the plan leaves, and the pieces
+  uint64_t* head;    // [0] units of all items of one head, [1] units of a share, [2] items
+  uint64_t* cum;     // [slots + 1] units before an item
+  uint2* items;      // [slots] sequence, row tile
+  uint4* start;      // [shares] item, head, unit of it
+  uint4* open;       // [shares] item, head, its last share, 1 where a piece starts here and does not end
+  float* part_o;     // [shares][2][TR][DP]
+  float* part_ml;    // [shares][2][TR][2]
+  uint32_t S, rows, H, G, D;
+  uint32_t slots, shares, tile_shift;  // row tiles that there may be; rows of one
+  uint32_t step_shift;                 // tokens of a step
+  uint32_t shift, num_pages, columns, window, sinks;
+  FastDiv by_group;
+  float scale;
+  Marks marks;
+};
+
+// What of the cache a row tile looks at: steps [0, sink_steps), then steps from `first` on.
+struct Reach {
+  uint32_t s, row0, r0, rows;  // sequence, its first row, the tile's first row and how many it has
+  int32_t pos0;                // position of the sequence's first row
+  uint32_t len;                // tokens of the sequence
+  uint32_t sink_steps, first, steps;
+};
+
+// Row tile x of the batch: sequence s owns the slots from slot_of(s) on, one at least for
+// each of its row tiles, whatever lies before it: no sum over the sequences is needed.
+ARGUS_DEV uint32_t slot_of(const ChunkArgs& a, uint32_t s) {
+  return (uint32_t)(((uint64_t)row_at(a.offsets, s, a.rows) * a.G) >> a.tile_shift) + s;
+}
+
+// false: the slot has no rows.
+ARGUS_DEV bool reach_of(const ChunkArgs& a, uint32_t s, uint32_t rt, Reach* r) {
+  const uint32_t lo = row_at(a.offsets, s, a.rows), hi = row_at(a.offsets, s + 1, a.rows);
+  const uint32_t n = hi > lo ? hi - lo : 0;
+  const uint64_t r0 = (uint64_t)rt << a.tile_shift;
+  if (r0 >= (uint64_t)n * a.G) return false;
+  r->s = s, r->row0 = lo, r->r0 = (uint32_t)r0;
+  const uint32_t left = n * a.G - r->r0, most = 1u << a.tile_shift;
+  r->rows = left < most ? left : most;
+  const int32_t l = a.lens[s];
+  const uint32_t cap = a.columns << a.shift;
+  r->len = l < 0 ? 0u : ((uint32_t)l < cap ? (uint32_t)l : cap);
+  r->pos0 = (int32_t)r->len - (int32_t)n;
+  const int32_t p0 = r->pos0 + (int32_t)divide(r->r0, a.by_group);
+  const int32_t p1 = r->pos0 + (int32_t)divide(r->r0 + r->rows - 1, a.by_group);
+  const uint32_t end = p1 < 0 ? 0u : (uint32_t)p1 + 1;
+  const uint32_t low = a.window && p0 >= 0 && (uint32_t)p0 + 1 > a.window ? (uint32_t)p0 + 1 - a.window : 0u;
+  const uint32_t ones = (1u << a.step_shift) - 1, sinks = low ? a.sinks : 0u;
+  r->first = low >> a.step_shift;
+  r->sink_steps = (sinks + ones) >> a.step_shift;
+  if (r->sink_steps >= r->first) r->sink_steps = r->first = 0;
+  r->steps = r->sink_steps + ((end + ones) >> a.step_shift) - r->first;
+  if (r->steps == 0) r->steps = 1;  // rows that see nothing answer too
+  return true;
+}
+
+template <int T>
+ARGUS_DEV f32x16 mfma32(u32x4 x, u32x4 y, f32x16 c) {
+  if constexpr (T == 0)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
+}
+
+// A row of LDS has its chunks of 16 bytes in another order for each of 16 rows (8 at head
+// size 64), so that the rows that are read together, 16 of keys or 4 of values (four chunks each),
+// lie in different banks.
+template <int DP>
+ARGUS_DEV uint32_t swizzle(uint32_t row) {
+  return DP == 64 ? (row >> 1 & 1u) << 2 | (row >> 2 & 3u) : (row & 3u) << 2 | (row >> 2 & 3u);
+}
+
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+ARGUS_DEV u32x4 lds16(const lds_byte* p) { return *(const __attribute__((address_space(3))) u32x4*)p; }
+
+// 16 bytes of each lane from base + at to LDS, one lane's after the other's from `to` on. It
+// has no registers to write; who reads them waits for the loads' count first.
+ARGUS_DEV void to_lds(const uint8_t* base, uint32_t at, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(base), "s"(to) : "memory", "m0");
+}
+
+// Bits of 16-bit numbers whose exponent is all ones: infinities and NaN.
+template <int T>
+ARGUS_DEV uint32_t not_finite(uint32_t w) {
+  return T == 0 ? ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u : ((w & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
+}
+
+template <int T>
+constexpr uint32_t kFrac = T == 0 ? 7 : 10;  // bits of a fraction
+template <int T>
+constexpr uint32_t kFracs = ((1u << kFrac<T>) - 1) * 0x10001u;
+
+// O, maxima and sums of steps [t0, t1) of a row tile for one head.
+template <int T, bool F8, int DP, int W>
+ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint32_t t0, uint32_t t1, lds_byte* lds,
+                           f32x16 (&acc)[DP / 32], float& m, float& l) {
+  constexpr int KT = kStepTokens<DP>, HT = KT / 32;  // halves of a step
+  constexpr int KF = DP / 16, DB = DP / 32;          // fragments of a key row, 32-wide parts of O
+  constexpr int RW = KT / W, RUNS = RW / 8;     // rows that a wave loads, runs of eight tokens
+  constexpr uint32_t kRow = DP * 2, kSide = KT * kRow, kBuffer = 2 * kSide;
+  // a lane's part of a load: CE elements, NI loads a run, RI rows a load
+  constexpr int CE = F8 && DP > 64 ? 16 : 8, LR = DP / CE, RI = 64 / LR, NI = 8 / RI;
+  constexpr int CW = F8 ? CE / 4 : 4;
+  using Hf = Half<T>;
+  const uint32_t lane = threadIdx.x & 63u, c = lane & 31u, hk = lane >> 5;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const float kc = a.scale * (a.k_scale ? a.k_scale[h] : 1.0f), kd = fabsf(kc), kd2 = kd * kLog2e;
+  bool far = !(kd > 1e-30f && kd < 1e30f);  // scores so large, or a scale so odd, that the differences come first
+
+  // queries: lane (row c, half hk) holds elements 16 f + 8 hk ... of its row
+  u32x4 qf[KF];
+  const uint32_t at0 = 32 * wave, mine = at0 + c;
+  const bool in = mine < g.rows;
+  const uint32_t r = g.r0 + (in ? mine : 0), row_tok = divide(r, a.by_group), head = h * a.G + r - row_tok * a.G;
+  const uint16_t* qr = a.q + (int64_t)(g.row0 + row_tok) * a.q_row + (int64_t)head * a.q_head;
+#pragma unroll
+  for (int f = 0; f < KF; ++f) {
+    const uint32_t d = 16 * f + 8 * hk;
+    qf[f] = in && d < a.D ? *reinterpret_cast<const u32x4*>(qr + d) : (u32x4)(0u);
+    if (kc < 0.0f) qf[f] ^= 0x80008000u;  // so that the largest product is the largest score
+  }
+  // the row sees tokens below `end`, from `low` on (and the sinks)
+  const int32_t pos = g.pos0 + (int32_t)row_tok, end = in ? pos + 1 : 0, low = a.window ? pos + 1 - (int32_t)a.window : 0;
+  // of the wave's rows, as scalars; none: nothing is seen
+  const int32_t p_least = at0 < g.rows ? g.pos0 + (int32_t)divide(g.r0 + at0, a.by_group) : -1;
+  const int32_t p_most = at0 < g.rows ? g.pos0 + (int32_t)divide(g.r0 + (at0 + 32 < g.rows ? at0 + 31 : g.rows - 1), a.by_group) : -1;
+  m = -INFINITY;
+  l = 0.0f;
+#pragma unroll
+  for (int d = 0; d < DB; ++d) acc[d] = (f32x16)(0.0f);
+  float base = 0.0f;  // the maximum to base 2, less kRaise
+  // infinite values that the row has seen, a bit for each of the lane's elements (both: NaN)
+  uint32_t plus[DB / 2] = {}, minus[DB / 2] = {};
+
+  const int32_t* tab = a.table + (int64_t)g.s * a.table_stride;
+  const uint8_t* kb = a.k + (int64_t)h * a.k_head;
+  const uint8_t* vb = a.v + (int64_t)h * a.v_head;
+  const uint32_t in_page = (1u << a.shift) - 1;
+
+  // What a lane adds to the scalar base of a load, and whether it has anything to load.
+  const uint32_t lr = lane / LR, lc = lane % LR;
+  uint32_t k_at[RUNS][NI], v_at[RUNS][NI], loads = 0;
+#pragma unroll
+  for (int j = 0; j < RUNS; ++j)
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const uint32_t row = wave * RW + 8 * j + i * RI + lr;
+      const uint32_t chunk = F8 ? lc : lc ^ swizzle<DP>(row);
+      const uint32_t b = chunk * (F8 ? CE : 16);
+      k_at[j][i] = (i * RI + lr) * a.k_tok + b;
+      v_at[j][i] = (i * RI + lr) * a.v_tok + b;
+      loads |= chunk * CE < a.D ? 1u << (j * NI + i) : 0u;
+    }
+  const bool padded = a.D != DP;
+
+  auto token_of = [&](uint32_t t) { return (t < g.sink_steps ? t : t - g.sink_steps + g.first) * KT; };
+  // The pages of a step's runs of eight tokens, in the first lanes: the entries, and a step
+  // later (they are under way until then) what they say.
+  const uint32_t run_at = 8 * (lane % (KT / 8));
+  auto find = [&](uint32_t t) {
+    const uint32_t col = (token_of(t < t1 ? t : t1 - 1) + run_at) >> a.shift;
+    return tab[col < a.columns ? col : 0];
+  };
+  auto known = [&](uint32_t t, int32_t entry) {
+    const uint32_t col = (token_of(t < t1 ? t : t1 - 1) + run_at) >> a.shift;
+    return col < a.columns && (uint32_t)entry < a.num_pages ? entry : -1;
+  };
+  uint32_t staged[F8 ? 2 : 1][RUNS][NI][F8 ? CW : 1];
+  // Step t's keys and values on their way, into LDS or (8 bits) registers.  What lies behind
+  // the sequence's end or in no page is 0.
+  auto load = [&](uint32_t t, int32_t ids, lds_byte* to) {
+    const uint32_t tok = token_of(t);
+#pragma unroll
+    for (int j = 0; j < RUNS; ++j) {
+      const uint32_t run = wave * RUNS + j, first = tok + 8 * run;
+      const int32_t page = __builtin_amdgcn_readlane(ids, run);
+      const uint32_t place = first & in_page;
+      const uint8_t* ks = kb + (int64_t)(page < 0 ? 0 : page) * a.k_page + (uint64_t)place * a.k_tok;
+      const uint8_t* vs = vb + (int64_t)(page < 0 ? 0 : page) * a.v_page + (uint64_t)place * a.v_tok;
+      const uint32_t have = page < 0 || first >= g.len ? 0u : g.len - first;  // tokens of the run that there are
+      if constexpr (F8) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          typedef uint32_t words __attribute__((ext_vector_type(CW)));
+          words x = (words)(0u), y = (words)(0u);
+          if (i * RI + lr < have && (!padded || (loads >> (j * NI + i) & 1u))) {
+            x = *reinterpret_cast<const words*>(ks + k_at[j][i]);
+            y = *reinterpret_cast<const words*>(vs + v_at[j][i]);
+          }
+#pragma unroll
+          for (int w = 0; w < CW; ++w) staged[0][j][i][w] = x[w], staged[1][j][i][w] = y[w];
+        }
+      } else {
+        lds_byte* at = to + (wave * RW + 8 * j) * kRow;
+        const uint32_t side = (uint32_t)(uintptr_t)at;
+        auto bring = [&](int i) {
+          to_lds(ks, k_at[j][i], side + i * RI * kRow);
+          to_lds(vs, v_at[j][i], side + i * RI * kRow + kSide);
+        };
+        if (have >= 8 && !padded) {
+#pragma unroll
+          for (int i = 0; i < NI; ++i) bring(i);
+        } else {
+#pragma unroll
+          for (int i = 0; i < NI; ++i) {
+            const bool there = i * RI + lr < have;
+            if (there && (loads >> (j * NI + i) & 1u)) bring(i);
+            if (!there) {
+              *(__attribute__((address_space(3))) u32x4*)(at + i * RI * kRow + lane * 16) = (u32x4)(0u);
+              *(__attribute__((address_space(3))) u32x4*)(at + i * RI * kRow + kSide + lane * 16) = (u32x4)(0u);
+            }
+          }
+        }
+      }
+    }
+  };
+  auto land = [&](lds_byte* to) {
+    if constexpr (F8) {
+#pragma unroll
+      for (int side = 0; side < 2; ++side)
+#pragma unroll
+        for (int j = 0; j < RUNS; ++j)
+#pragma unroll
+          for (int i = 0; i < NI; ++i) {
+            const uint32_t row = wave * RW + 8 * j + i * RI + lr;
+            lds_byte* at = to + side * kSide + row * kRow;
+#pragma unroll
+            for (int e = 0; e < CE / 8; ++e) {
+              const uint32_t w0 = staged[side][j][i][2 * e], w1 = staged[side][j][i][2 * e + 1];
+              const u32x4 x = (u32x4){widen<T>(w0, false), widen<T>(w0, true), widen<T>(w1, false), widen<T>(w1, true)};
+              *(__attribute__((address_space(3))) u32x4*)(at + (((lc * (CE / 8) + e) ^ swizzle<DP>(row)) << 4)) = x;
+            }
+          }
+    }
+  };
+
+  // Where a lane's fragments lie: their addresses stay in registers, what differs beside them is
+  // in the instructions.
+  const uint32_t i16 = lane & 15u, piece = i16 & 3u, v_row = 4 * hk + (i16 >> 2);
+  uint32_t k_frag[KF], v_frag[DB][2];
+#pragma unroll
+  for (int f = 0; f < KF; ++f) {
+    k_frag[f] = (uint32_t)(uintptr_t)lds + c * kRow + (((2 * f + hk) ^ swizzle<DP>(c)) << 4);
+    asm volatile("" : "+v"(k_frag[f]));
+  }
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t chunk = 4 * d + 2 * (piece & 1u) + (lane >> 4 & 1u), row = v_row + 8 * e;
+      v_frag[d][e] = (uint32_t)(uintptr_t)lds + kSide + row * kRow + ((chunk ^ swizzle<DP>(row)) << 4) + (piece >> 1) * 8;
+      asm volatile("" : "+v"(v_frag[d][e]));
+    }
+  auto k_part = [&](uint32_t from, int th, int f) { return lds16((const lds_byte*)(uintptr_t)(k_frag[f] + (from + th * 32 * kRow))); };
+  // Fragment (d, f) of V^T: lane (m, hk) has tokens 16 f + 8 e + 4 hk + 0..3, e = 0, 1, of
+  // element 32 d + 16 (m / 4 % 2) + 4 (m / 8) + m % 4, so that a lane of O^T holds 16 elements in a row.
+  auto v_part = [&](uint32_t from, int d, int f) {
+    u32x4 x;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) s16x4*)(uintptr_t)(v_frag[d][e] + (from + 16 * f * kRow)));
+      x[2 * e] = __builtin_bit_cast(u32x2, y).x, x[2 * e + 1] = __builtin_bit_cast(u32x2, y).y;
+    }
+    return x;
+  };
+
+  auto take = [&](uint32_t t, int32_t ids, uint32_t from) {
+    const uint32_t tok = token_of(t);
+    const uint32_t held = (uint32_t)__ballot(ids >= 0) & ((1u << (KT / 8)) - 1);
+    // whether the rows see all of the step, or none
+    const int32_t e = (int32_t)tok + KT - 1;
+    const bool whole = e <= p_least && held == (1u << (KT / 8)) - 1 &&
+                       (!a.window || (int32_t)tok > p_most - (int32_t)a.window || e < (int32_t)a.sinks);
+    if ((int32_t)tok > p_most || !held || (a.window && e <= p_least - (int32_t)a.window && tok >= a.sinks)) return;
+
+    f32x16 sc[HT];
+#pragma unroll
+    for (int th = 0; th < HT; ++th) sc[th] = (f32x16)(0.0f);
+#pragma unroll
+    for (int f = 0; f < KF; ++f)
+#pragma unroll
+      for (int th = 0; th < HT; ++th) {
+        sc[th] = mfma32<T>(k_part(from, th, f), qf[f], sc[th]);
+      }
+
+    if (!whole) {
+      // of the lane's 16 HT tokens, tok + 4 hk + 0..3, + 8..11, ..., those below x
+      auto below = [&](int32_t x) {
+        const int32_t y = x - (int32_t)(tok + 4 * hk), k = y < 0 ? 0 : 4 * (y >> 3) + ((y & 7) < 4 ? y & 7 : 4);
+        return k < 32 ? (1u << k) - 1 : ~0u;
+      };
+      uint32_t vis = below(end) & (~below(low) | below((int32_t)a.sinks));
+      if (held != (1u << (KT / 8)) - 1) {
+        uint32_t by_four = 0;
+#pragma unroll
+        for (int i = 0; i < KT / 8; ++i) by_four |= held >> i & 1u ? 15u << (4 * i) : 0u;
+        vis &= by_four;
+      }
+#pragma unroll
+      for (int th = 0; th < HT; ++th)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[th][i] = vis >> (16 * th + i) & 1u ? sc[th][i] : -INFINITY;
+    }
+    float top = sc[0][0];
+#pragma unroll
+    for (int th = 0; th < HT; ++th)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[th][i]);
+    top = top == -INFINITY ? top : top * kd;  // (kd may be 0)
+    if (__any(top > m + kSlack)) {
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = fmaxf(m, top);
+      const float scale = m == -INFINITY ? 0.0f : exp_of(m - mn);
+      l *= scale;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) acc[d] *= scale;
+      m = mn;
+      base = mn == -INFINITY ? 0.0f : fmaf(mn, kLog2e, -Hf::kRaise);
+      far = far || __any(fabsf(mn) > kFar && mn != -INFINITY);
+    }
+    if (!far) {
+#pragma unroll
+      for (int th = 0; th < HT; ++th)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[th][i] = __builtin_amdgcn_exp2f(fmaf(sc[th][i], kd2, -base));
+    } else {
+      const float ms = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+      for (int th = 0; th < HT; ++th)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float x = sc[th][i], y = x == -INFINITY ? x : x * kd;
+          sc[th][i] = __builtin_amdgcn_exp2f(fmaf(y - ms, kLog2e, Hf::kRaise));
+        }
+    }
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    u32x4 p[2 * HT];
+#pragma unroll
+    for (int th = 0; th < HT; ++th) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[i % 4] += sc[th][i];
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) p[2 * th + i / 8][i / 2 % 4] = Hf::pack(sc[th][i], sc[th][i + 1]);
+    }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+
+#pragma unroll
+    for (int f = 0; f < 2 * HT; ++f)
+#pragma unroll
+      for (int d = 0; d < DB; ++d) acc[d] = mfma32<T>(v_part(from, d, f), p[f], acc[d]);
+  };
+
+  // Of a step that some of the block's rows do not see, the values that are not finite (0 times infinity
+  // would be NaN): noted where they are seen, and 0 from then on.  All waves look at the same
+  // values, so they come to the same answer.
+  const int32_t b_least = g.pos0 + (int32_t)divide(g.r0, a.by_group), b_most = g.pos0 + (int32_t)divide(g.r0 + g.rows - 1, a.by_group);
+  auto settle = [&](uint32_t t, int32_t ids, uint32_t from) {
+    const uint32_t tok = token_of(t);
+    const int32_t e = (int32_t)tok + KT - 1;
+    if (e <= b_least && (!a.window || (int32_t)tok > b_most - (int32_t)a.window || e < (int32_t)a.sinks)) return;
+    uint32_t odd = 0;
+#pragma unroll 4
+    for (uint32_t i = 0; i < kSide / 1024; ++i) {
+      const u32x4 x = lds16(lds + from + kSide + i * 1024 + lane * 16);
+      odd |= not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3]);
+    }
+    if (!__any(odd)) return;
+    const uint32_t held = (uint32_t)__ballot(ids >= 0);
+#pragma unroll 1
+    for (uint32_t j = 0; j < (uint32_t)KT; ++j) {
+      const int32_t at = (int32_t)(tok + j);
+      const bool seen = at < end && (at >= low || at < (int32_t)a.sinks) && (held >> (j / 8) & 1u);
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const u32x4 x = lds16(lds + from + kSide + j * kRow + (((4 * d + 2 * hk + i) ^ swizzle<DP>(j)) << 4));
+          uint32_t up = 0, down = 0;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t bad = seen ? not_finite<T>(x[w]) >> 15 : 0u, sign = x[w] >> 15 & 0x10001u;
+            const uint32_t nan = bad & ((x[w] & kFracs<T>) + kFracs<T>) >> kFrac<T>, u = nan | (bad & ~sign), v = nan | (bad & sign);
+            up |= ((u | u >> 15) & 3u) << (2 * w), down |= ((v | v >> 15) & 3u) << (2 * w);
+          }
+          plus[d / 2] |= up << (16 * (d % 2) + 8 * i), minus[d / 2] |= down << (16 * (d % 2) + 8 * i);
+        }
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (uint32_t i = threadIdx.x; i < kSide / 16; i += 64 * W) {
+      lds_byte* at = lds + from + kSide + i * 16;
+      u32x4 x = lds16(at);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) x[w] &= ~((not_finite<T>(x[w]) >> 15) * 0xFFFFu);
+      *(__attribute__((address_space(3))) u32x4*)at = x;
+    }
+    __syncthreads();
+  };
+
+  auto arrived = [&]() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  __syncthreads();  // what came before is done with the buffers
+  if (padded) {     // elements behind the head size stay 0
+    for (uint32_t i = threadIdx.x; i < 2 * kBuffer / 16; i += 64 * W)
+      *(__attribute__((address_space(3))) u32x4*)(lds + i * 16) = (u32x4)(0u);
+    __syncthreads();
+  }
+  int32_t ids = known(t0, find(t0)), next = find(t0 + 1);
+  load(t0, ids, lds);
+  land(lds);
+  auto step = [&](uint32_t t, uint32_t b) {
+    arrived();  // step t is there, and nobody reads step t - 1 any more
+    const int32_t after = find(t + 2);
+    next = known(t + 1, next);
+    if (t + 1 < t1) load(t + 1, next, lds + (kBuffer - b));
+    settle(t, ids, b);
+    take(t, ids, b);
+    if (t + 1 < t1) land(lds + (kBuffer - b));
+    ids = next, next = after;
+  };
+  for (uint32_t t = t0; t < t1; t += 2) {
+    step(t, 0);
+    if (t + 1 < t1) step(t + 1, kBuffer);
+  }
+  l += __shfl_xor(l, 32);
+  uint32_t seen = 0;
+#pragma unroll
+  for (int d = 0; d < DB / 2; ++d) seen |= plus[d] | minus[d];
+  if (__any(seen)) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        acc[d][i] += plus[d / 2] >> (16 * (d % 2) + i) & 1u ? INFINITY : 0.0f;
+        acc[d][i] -= minus[d / 2] >> (16 * (d % 2) + i) & 1u ? INFINITY : 0.0f;
+      }
+  }
+}
+
+template <int T, bool F8, int DP, int W>
+__global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void k_chunk(ChunkArgs a) {
+  constexpr int DB = DP / 32, KT = kStepTokens<DP>, TR = 32 * W;
+  using Hf = Half<T>;
+  __shared__ __align__(1024) uint8_t s_raw[4 * KT * DP * 2];
+  lds_byte* lds = (lds_byte*)s_raw;
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_CHUNK);
+  const uint32_t lane = threadIdx.x & 63u, c = lane & 31u, hk = lane >> 5;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  // O of the rows, or (slot: not done) a piece of it
+  auto put = [&](const Reach& g, uint32_t h, const f32x16 (&acc)[DB], float m, float l, bool done, uint64_t slot) {
+    const float vs = a.v_scale ? a.v_scale[h] : 1.0f;
+    const uint32_t mine = 32 * wave + c;
+    if (mine >= g.rows) return;
+    const uint32_t r = g.r0 + mine, tok = divide(r, a.by_group);
+    const uint64_t row = (uint64_t)(g.row0 + tok) * a.H * a.G + h * a.G + (r - tok * a.G);
+    const float inv = l == 0.0f ? 0.0f : vs / l;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+      const uint32_t e = 32 * d + 16 * hk;
+      if (done) {
+#pragma unroll
+        for (int i = 0; i < 16; i += 8)
+          if (e + i < a.D) {
+            u32x4 x;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) x[w] = Hf::pack(acc[d][i + 2 * w] * inv, acc[d][i + 2 * w + 1] * inv);
+            *reinterpret_cast<u32x4*>(a.out + row * a.D + e + i) = x;
+          }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<f32x4*>(a.part_o + (slot * TR + mine) * DP + e + i) =
+              (f32x4){acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
+      }
+    }
+    if (hk == 0) {
+      if (!done)
+        *reinterpret_cast<f32x2*>(a.part_ml + (slot * TR + mine) * 2) = (f32x2){m, l};
+      else if (a.lse)
+        a.lse[row] = l == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m - Hf::kRaise * kLn2) + logf(l);
+    }
+  };
+
+  f32x16 acc[DB];
+  float m, l;
+  Reach g;
+  if (a.shares == 0) {
+    // A row tile per block: those that see the most tokens first.
+    const uint32_t h = blockIdx.x % a.H, x = a.slots - 1 - blockIdx.x / a.H;
+    uint32_t lo = 0, hi = a.S;
+    while (hi - lo > 1) {  // the last sequence whose slots start at or before x
+      const uint32_t step = (hi - lo + 63) / 64, s = lo + lane * step;
+      const uint32_t n = (uint32_t)__popcll(__ballot(s < hi && slot_of(a, s < hi ? s : lo) <= x));
+      if (n == 0) break;
+      lo += (n - 1) * step;
+      hi = hi < lo + step ? hi : lo + step;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    const uint32_t first = slot_of(a, lo);
+    if (first <= x && reach_of(a, lo, x - first, &g)) {
+      chunk_steps<T, F8, DP, W>(a, g, h, 0, g.steps, lds, acc, m, l);
+      put(g, h, acc, m, l, true, 0);
+    }
+  }
+  mk.end(ARGUS_REGION_CHUNK);
+}
+
+template <int T, bool F8, int DP, int W>
+void launch_chunk_as(const ChunkArgs& a, uint32_t grid, hipStream_t st) {
+  hipLaunchKernelGGL((k_chunk<T, F8, DP, W>), dim3(grid), dim3(64 * W), 0, st, a);
+}
+
+template <int T, bool F8>
+void launch_chunk_type(const ChunkArgs& a, uint32_t grid, hipStream_t st) {
+  if (a.D <= 64) launch_chunk_as<T, F8, 64, 4>(a, grid, st);
+  else if (a.D <= 128) launch_chunk_as<T, F8, 128, 4>(a, grid, st);
+  else launch_chunk_as<T, F8, 256, 4>(a, grid, st);
+}
+
+// One source file each, so that they compile side by side.
+void launch_chunk_bf16(const ChunkArgs& a, uint32_t grid, hipStream_t st);
+void launch_chunk_fp16(const ChunkArgs& a, uint32_t grid, hipStream_t st);
+void launch_chunk_bf16_f8(const ChunkArgs& a, uint32_t grid, hipStream_t st);
+void launch_chunk_fp16_f8(const ChunkArgs& a, uint32_t grid, hipStream_t st);
+
+}  // namespace prompt
+}  // namespace argus

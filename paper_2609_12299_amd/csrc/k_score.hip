@@ -1,0 +1,443 @@
+// k_score.hip -- log probabilities of given tokens, with entropy, rank and the best alternatives.
+//
+// With d = x - max x, S = sum e^d and T = sum d e^d of a row:
+//
+//   ln p[t] = (x[t] - max x) - ln S        entropy = ln S - T / S
+//
+// Both are sums of numbers of one sign where the maximum is the row's own: T <= 0 <= ln S, so nothing
+// cancels. A lane keeps the maximum of what it has seen, exactly, and moves its sums where it
+// rises (S' = S e^m, T' = (T + m S) e^m, m <= 0 the old maximum less the new one); lanes, waves and parts
+// are joined in the same way, in a fixed order.
+//
+// A block reads a part of a row, its four waves 64 lanes of 32 elements in turn, the next
+// ones under way while it looks at them. The rank is a count of what is above the given token's own
+// logit, read first. The alternatives are kept as selection over beams keeps its candidates: a list in LDS
+// for each wave, with a least value that rises as the list is cut to its first.
+#include "prompt.h"
+#include "rows.h"
+
+namespace argus {
+namespace prompt {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr uint32_t kItems = 32;       // elements of a lane per step
+constexpr uint32_t kStep = kItems * 64;
+constexpr uint32_t kList = 192, kRoom = 8;  // candidates of a wave; beyond its k, before it is cut
+constexpr uint32_t kMaxTop = 64;
+constexpr uint32_t kCands = 512;      // of the parts of a row, ranked by counting
+
+struct Sums {
+  float top, s, t;  // maximum, sum of e^d, sum of d e^d
+  uint32_t above;
+};
+
+struct ScoreArgs {
+  const uint8_t* logits;
+  int64_t row_stride;  // bytes
+  const int32_t* tokens;
+  float *logprobs, *entropy;
+  int32_t* ranks;
+  float* top_logprobs;
+  int32_t* top_tokens;
+  Sums* sums;       // [rows][parts]
+  uint64_t* cands;  // [rows][parts][K] in order, 0: none
+  uint32_t V, K, parts, steps, rows;  // steps of a part
+  Marks marks;
+};
+
+ARGUS_DEV float power(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+
+// Sums about a larger maximum. (None yet: nothing to move; -inf - -inf would be NaN.)
+ARGUS_DEV void move(Sums& a, float to) {
+  if (a.top == -INFINITY) {
+    a.top = to;
+    return;
+  }
+  const float m = a.top - to, f = power(m);
+  a.t = m < -128.0f ? 0.0f * a.s : (a.t + m * a.s) * f;  // (a NaN stays)
+  a.s *= f;
+  a.top = to;
+}
+ARGUS_DEV void join(Sums& a, Sums b) {
+  const float to = fmaxf(a.top, b.top);
+  move(a, to);
+  move(b, to);
+  a.s += b.s, a.t += b.t, a.above += b.above;
+}
+
+// A row's numbers, once its sums are known. `lane`: of those that write its alternatives.
+struct Row {
+  float top, log, entropy;
+  bool fine;
+};
+ARGUS_DEV Row row_of(const Sums& a) {
+  Row r;
+  r.top = a.top;
+  r.log = logf(a.s);
+  r.entropy = r.log - a.t / a.s;
+  r.fine = a.s > 0.0f && a.s < INFINITY;
+  return r;
+}
+ARGUS_DEV void put_row(const ScoreArgs& a, uint32_t row, const Row& r, uint32_t above, int32_t token, float mine) {
+  const bool known = (uint32_t)token < a.V;
+  a.logprobs[row] = !r.fine ? NAN : known ? (mine - r.top) - r.log : -INFINITY;
+  a.entropy[row] = r.fine ? r.entropy : NAN;
+  a.ranks[row] = r.fine && known ? (int32_t)above : -1;
+}
+ARGUS_DEV void put_top(const ScoreArgs& a, uint32_t row, const Row& r, uint32_t i, uint64_t key) {
+  const uint64_t at = (uint64_t)row * a.K + i;
+  a.top_tokens[at] = r.fine && key ? (int32_t)~(uint32_t)key : -1;
+  a.top_logprobs[at] = !r.fine ? NAN : key ? (value_of((uint32_t)(key >> 32)) - r.top) - r.log : -INFINITY;
+}
+
+template <int TYPE>
+ARGUS_DEV float element(const uint8_t* base, uint32_t i) {
+  if constexpr (TYPE == ARGUS_FP32) return *reinterpret_cast<const float*>(base + (uint64_t)i * 4);
+  else return of_word<TYPE>(*reinterpret_cast<const uint16_t*>(base + (uint64_t)i * 2), 0);
+}
+
+template <int TYPE, bool TOP>
+__global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
+  constexpr uint32_t kBytes = TYPE == ARGUS_FP32 ? 4 : 2, kPer = 16 / kBytes, kVecs = kItems / kPer;
+  __shared__ uint64_t s_list[TOP ? kWaves : 1][TOP ? kList : 1];
+  __shared__ u32x4 s_step[TOP ? kWaves : 1][TOP ? kVecs * 64 : 1];
+  __shared__ Sums s_sums[kWaves];
+  __shared__ uint32_t s_n[kWaves];
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_SCORE_ROWS);
+  const uint32_t tid = threadIdx.x, lane = tid & 63u;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+  const uint8_t* base = a.logits + (int64_t)row * a.row_stride;
+  const int32_t token = a.tokens[row];
+  const bool known = (uint32_t)token < a.V;
+  const float mine = known ? element<TYPE>(base, (uint32_t)token) : INFINITY;
+  // Vectors lie on 16 bytes: `head` elements come before the first of `vecs`
+  // vectors, less than a vector behind the last.
+  uint32_t head = (uint32_t)(0 - (uintptr_t)base & 15u) / kBytes;
+  head = head < a.V ? head : a.V;
+  const uint32_t vecs = (a.V - head) / kPer, tail = head + vecs * kPer;
+  const u32x4* body = reinterpret_cast<const u32x4*>(base + head * kBytes);
+  const uint32_t all = (vecs + kVecs * 64 - 1) / (kVecs * 64);
+  const uint32_t end = (part + 1) * a.steps < all ? (part + 1) * a.steps : all;
+  auto load = [&](uint32_t step, u32x4 (&w)[kVecs]) {
+    const uint32_t v0 = step * kVecs * 64 + lane;
+#pragma unroll
+    for (uint32_t v = 0; v < kVecs; ++v) w[v] = __builtin_nontemporal_load(&body[v0 + v * 64 < vecs ? v0 + v * 64 : vecs - 1]);
+  };
+  Sums my{-INFINITY, 0.0f, 0.0f, 0u};
+  auto add = [&](float x) {  // (a NaN of x goes on, a d of -inf has no part)
+    const float d = x - (my.top == -INFINITY ? 0.0f : my.top), e = power(d);
+    my.s += e;
+    my.t += e * (d < -128.0f ? -128.0f : d);
+  };
+  // the wave's list
+  uint64_t* list = s_list[TOP ? wave : 0];
+  uint32_t n = 0;
+  uint64_t least = 0;
+  float least_value = -INFINITY;
+  auto rank = [&](auto keys) {
+    constexpr uint32_t C = keys();
+    uint64_t key[C];
+    uint32_t above[C];
+#pragma unroll
+    for (uint32_t c = 0; c < C; ++c) {
+      key[c] = lane + 64 * c < n ? list[lane + 64 * c] : 0;
+      above[c] = 0;
+    }
+#pragma unroll 8
+    for (uint32_t i = 0; i < n; ++i) {
+      const uint64_t o = list[i];
+#pragma unroll
+      for (uint32_t c = 0; c < C; ++c) above[c] += o > key[c];
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (uint32_t c = 0; c < C; ++c)
+      if (lane + 64 * c < n && above[c] < a.K) list[above[c]] = key[c];
+  };
+  auto cut = [&]() {
+    __builtin_amdgcn_wave_barrier();
+    if (n <= 64) rank([]() constexpr { return 1u; });
+    else if (n <= 128) rank([]() constexpr { return 2u; });
+    else rank([]() constexpr { return kList / 64; });
+    __builtin_amdgcn_wave_barrier();
+    n = n < a.K ? n : a.K;
+    if (n == a.K) {
+      least = list[a.K - 1];
+      least_value = value_of((uint32_t)(least >> 32));
+    }
+  };
+  auto append = [&](bool want, uint64_t key) {  // at most 64 at a time
+    const uint64_t take = __ballot(want);
+    if (want) list[n + (uint32_t)__popcll(take & lanemask_lt())] = key;
+    n += (uint32_t)__popcll(take);
+  };
+  bool first = true;
+  auto look = [&](uint32_t step, const u32x4 (&w)[kVecs]) {
+    float x[kItems];
+#pragma unroll
+    for (uint32_t i = 0; i < kItems; ++i) x[i] = of_word<TYPE>(w[i / kPer][(i % kPer) * kBytes / 4], i % (4 / kBytes));
+    const uint32_t v0 = step * kVecs * 64 + lane;
+    const bool last = (step + 1) * kVecs * 64 > vecs;
+    if (last) {
+#pragma unroll
+      for (uint32_t i = 0; i < kItems; ++i) x[i] = v0 + i / kPer * 64 < vecs ? x[i] : -INFINITY;
+    }
+    float top = x[0];
+#pragma unroll
+    for (uint32_t i = 1; i < kItems; ++i) top = fmaxf(top, x[i]);
+    if (__any(top > my.top)) move(my, fmaxf(my.top, top));
+#pragma unroll
+    for (uint32_t i = 0; i < kItems; ++i) add(x[i]);
+    // those above the token's logit; as large, and before it
+    const uint32_t e0 = head + step * kVecs * 64 * kPer, e1 = e0 + kVecs * 64 * kPer;
+    if ((uint32_t)token >= e1 && !last) {
+#pragma unroll
+      for (uint32_t i = 0; i < kItems; ++i) my.above += x[i] >= mine;
+    } else if ((uint32_t)token < e0 && !last) {
+#pragma unroll
+      for (uint32_t i = 0; i < kItems; ++i) my.above += x[i] > mine;
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < kItems; ++i)
+        my.above += v0 + i / kPer * 64 < vecs &&
+                    (x[i] > mine || (x[i] == mine && head + (v0 + i / kPer * 64) * kPer + i % kPer < (uint32_t)token));
+    }
+    if constexpr (TOP) {
+      if (first) {
+        // the k-th largest of the lanes' maxima: the least that fewer than k are above
+        first = false;
+        const uint32_t its = order_of(top);
+        uint32_t above = 0;
+#pragma unroll 16
+        for (int i = 0; i < 64; ++i) above += (uint32_t)__builtin_amdgcn_readlane((int)its, i) > its;
+        const uint32_t lo = ~wave_max_u32(above < a.K ? ~its : 0u);
+        const uint64_t bound = join64(0u, lo);  // below every key of this value
+        if (bound > least) least = bound, least_value = value_of(lo);
+      }
+      uint64_t hot = __ballot(top >= least_value && top > -INFINITY);
+      if (hot) {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (uint32_t v = 0; v < kVecs; ++v) s_step[wave][v * 64 + lane] = w[v];
+        __builtin_amdgcn_wave_barrier();
+        // two lanes' 32 elements at a time
+        while (hot) {
+          if (n > kList - 64) cut();
+          const uint32_t l0 = (uint32_t)__builtin_ctzll(hot);
+          hot &= hot - 1;
+          const uint32_t l1 = hot ? (uint32_t)__builtin_ctzll(hot) : l0;
+          const bool in = lane < kItems || l1 != l0;
+          hot &= hot - 1;
+          const uint32_t i = lane % kItems, at = (i / kPer) * 64 + (lane < kItems ? l0 : l1);
+          float y;
+          if constexpr (TYPE == ARGUS_FP32) y = reinterpret_cast<const any_f32*>(&s_step[wave][at])[i % kPer];
+          else y = of_word<TYPE>(reinterpret_cast<const any_u16*>(&s_step[wave][at])[i % kPer], 0);
+          const uint32_t tok = head + (step * kVecs * 64 + at) * kPer + i % kPer;
+          const uint64_t key = key_of(y, tok);
+          const bool there = step * kVecs * 64 + at < vecs;
+          append(in && there && y >= least_value && key > least && y > -INFINITY, key);
+        }
+        if (n > a.K + kRoom) cut();
+      }
+    }
+  };
+  if (part == 0 && wave == 0) {  // what lies before and behind the vectors: at most 2 * (kPer - 1) elements
+    const uint32_t j = lane < kPer ? lane : tail + lane - kPer;
+    const bool in = lane < kPer ? j < head : lane < 2 * kPer && j < a.V;
+    const float x = in ? element<TYPE>(base, j) : -INFINITY;
+    if (x > -INFINITY) my.top = x;
+    if (in) add(x);
+    my.above += in && (x > mine || (x == mine && j < (uint32_t)token));
+    if constexpr (TOP) append(x > -INFINITY, key_of(x, j));
+  }
+  u32x4 w0[kVecs], w1[kVecs];
+  uint32_t step = part * a.steps + wave;
+  if (step < end) {
+    load(step, w0);
+    for (; step + kWaves < end; step += 2 * kWaves) {
+      load(step + kWaves, w1);
+      look(step, w0);
+      load(step + 2 * kWaves < end ? step + 2 * kWaves : step, w0);
+      look(step + kWaves, w1);
+    }
+    if (step < end) look(step, w0);
+  }
+#pragma unroll 1
+  for (int d = 1; d < 64; d <<= 1)
+    join(my, Sums{__shfl_xor(my.top, d), __shfl_xor(my.s, d), __shfl_xor(my.t, d), (uint32_t)__shfl_xor((int)my.above, d)});
+  if constexpr (TOP) cut();
+  if (lane == 0) {
+    s_sums[wave] = my;
+    s_n[wave] = n;
+  }
+  __syncthreads();
+  Sums sum = s_sums[0];
+#pragma unroll 1
+  for (int w = 1; w < kWaves; ++w) join(sum, s_sums[w]);
+  if (a.parts == 1) {
+    const Row r = row_of(sum);
+    if (tid == 0) put_row(a, row, r, sum.above, token, mine);
+    if constexpr (TOP) {
+      // a wave's candidates are in order: those of the others that are above one of them
+      uint32_t total = 0;
+      for (int w = 0; w < kWaves; ++w) total += s_n[w];
+      if (lane < n) {
+        const uint64_t key = list[lane];
+        uint32_t above = lane;
+        for (int w = 0; w < kWaves; ++w) {
+          if (w == (int)wave) continue;
+          for (uint32_t i = 0; i < s_n[w]; ++i) above += s_list[w][i] > key;
+        }
+        if (above < a.K) put_top(a, row, r, above, key);
+      }
+      for (uint32_t i = total + tid; i < a.K; i += kThreads) put_top(a, row, r, i, 0);
+    }
+  } else {
+    if (tid == 0) a.sums[blockIdx.x] = sum;
+    if constexpr (TOP) {
+      uint64_t* to = a.cands + (uint64_t)blockIdx.x * a.K;
+      uint32_t total = 0;
+      for (int w = 0; w < kWaves; ++w) total += s_n[w];
+      if (lane < n) {
+        const uint64_t key = list[lane];
+        uint32_t above = lane;
+        for (int w = 0; w < kWaves; ++w) {
+          if (w == (int)wave) continue;
+          for (uint32_t i = 0; i < s_n[w]; ++i) above += s_list[w][i] > key;
+        }
+        if (above < a.K) to[above] = key;
+      }
+      for (uint32_t i = total + tid; i < a.K; i += kThreads) to[i] = 0;
+    }
+  }
+  mk.end(ARGUS_REGION_SCORE_ROWS);
+}
+
+// The parts of a row joined.
+template <int TYPE>
+__global__ __launch_bounds__(kThreads) void k_score_join(ScoreArgs a) {
+  __shared__ uint64_t s_cand[kCands];
+  WaveMarks mk(a.marks);
+  mk.begin(ARGUS_REGION_SCORE_JOIN);
+  const uint32_t tid = threadIdx.x, row = blockIdx.x, lane = tid & 63u;
+  const uint32_t total = a.parts * a.K;
+  for (uint32_t i = tid; i < total; i += kThreads) s_cand[i] = a.cands[(uint64_t)row * total + i];
+  Sums sum{-INFINITY, 0.0f, 0.0f, 0u};
+  for (uint32_t i = lane; i < a.parts; i += 64) join(sum, a.sums[(uint64_t)row * a.parts + i]);
+#pragma unroll 1
+  for (int d = 1; d < 64; d <<= 1)
+    join(sum, Sums{__shfl_xor(sum.top, d), __shfl_xor(sum.s, d), __shfl_xor(sum.t, d), (uint32_t)__shfl_xor((int)sum.above, d)});
+  const Row r = row_of(sum);
+  if (tid == 0) {
+    const int32_t token = a.tokens[row];
+    const float mine = (uint32_t)token < a.V ? element<TYPE>(a.logits + (int64_t)row * a.row_stride, (uint32_t)token) : 0.0f;
+    put_row(a, row, r, sum.above, token, mine);
+  }
+  __syncthreads();
+  for (uint32_t i = tid; i < total; i += kThreads) {
+    const uint64_t key = s_cand[i];
+    uint32_t above = 0, none = 0;
+    // places without a candidate come last, in their order
+    for (uint32_t o = 0; o < total; ++o) {
+      above += s_cand[o] > key;
+      none += s_cand[o] == key && o < i;
+    }
+    above += none;
+    if (above < a.K) put_top(a, row, r, above, key);
+  }
+  mk.end(ARGUS_REGION_SCORE_JOIN);
+}
+
+template <int TYPE>
+void launch_score(const ScoreArgs& a, uint32_t grid, hipStream_t st) {
+  if (a.K) hipLaunchKernelGGL((k_score_rows<TYPE, true>), dim3(grid), dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL((k_score_rows<TYPE, false>), dim3(grid), dim3(kThreads), 0, st, a);
+}
+
+struct Plan {
+  uint32_t parts, steps, grid;
+  size_t cands_at, bytes;
+};
+
+constexpr uint32_t kRowBlocks = 768;
+
+int make_plan(const argus_score_config* c, Plan* p) {
+  if (!c) return refuse(ARGUS_E_INVAL, "no configuration");
+  if (c->abi_version != ARGUS_ATTR_ABI_VERSION) return refuse(ARGUS_E_ABI, "abi_version %u", c->abi_version);
+  if (c->type > ARGUS_FP32) return refuse(ARGUS_E_INVAL, "logits are bf16, fp16 or fp32");
+  if (c->vocab < 1 || c->vocab > (1u << 24)) return refuse(ARGUS_E_INVAL, "vocab %u (1..2^24)", c->vocab);
+  if (c->top > kMaxTop) return refuse(ARGUS_E_INVAL, "top %u (0..64)", c->top);
+  if (c->rows > (1u << 22)) return refuse(ARGUS_E_CAPACITY, "rows %u", c->rows);
+  const uint32_t steps = (c->vocab + kStep - 1) / kStep;
+  uint32_t parts = c->rows ? kRowBlocks / c->rows : 1;
+  uint32_t most = (steps + kWaves - 1) / kWaves;
+  if (c->top && kCands / c->top < most) most = kCands / c->top;
+  parts = parts < most ? parts : most;
+  parts = parts < 1 ? 1 : parts;
+  p->steps = (steps + parts - 1) / parts;
+  p->parts = (steps + p->steps - 1) / p->steps;
+  p->grid = c->rows * p->parts;
+  p->cands_at = up256((size_t)p->grid * sizeof(Sums));
+  p->bytes = p->parts > 1 ? p->cands_at + up256((size_t)p->grid * c->top * sizeof(uint64_t)) : 0;
+  return ARGUS_OK;
+}
+
+}  // namespace
+}  // namespace prompt
+}  // namespace argus
+
+using namespace argus;
+using namespace argus::prompt;
+
+extern "C" size_t argus_prompt_score_workspace_bytes(const argus_score_config* cfg) {
+  accepted();
+  Plan p;
+  return make_plan(cfg, &p) == ARGUS_OK ? p.bytes : (size_t)-1;
+}
+
+extern "C" int argus_prompt_score(const argus_score_config* cfg, const argus_score_io* io, void* d_workspace,
+                                  size_t workspace_bytes, argus_markers* markers, void* stream_v) {
+  accepted();
+  Plan p;
+  int rc = make_plan(cfg, &p);
+  if (rc != ARGUS_OK) return rc;
+  if (!io || (cfg->rows && (!io->d_logits || !io->d_tokens || !io->d_logprobs || !io->d_entropy || !io->d_ranks ||
+                            (cfg->top && (!io->d_top_logprobs || !io->d_top_tokens)))))
+    return refuse(ARGUS_E_INVAL, "a required pointer is NULL");
+  const uint32_t e = type_bytes(cfg->type);
+  if (!aligned_to(io->d_logits, e) || !aligned_to(io->d_tokens, 4) || !aligned_to(io->d_logprobs, 4) ||
+      !aligned_to(io->d_entropy, 4) || !aligned_to(io->d_ranks, 4) ||
+      (cfg->top && (!aligned_to(io->d_top_logprobs, 4) || !aligned_to(io->d_top_tokens, 4))))
+    return refuse(ARGUS_E_ALIGN, "buffers lie on their elements' size");
+  if (marks_bad_all(markers)) return refuse(ARGUS_E_INVAL, "markers: alignment or region_base");
+  if (p.bytes && !d_workspace) return refuse(ARGUS_E_INVAL, "no workspace");
+  if (p.bytes && !aligned_to(d_workspace, 256)) return refuse(ARGUS_E_ALIGN, "the workspace lies on 256 bytes");
+  if (workspace_bytes < p.bytes) return refuse(ARGUS_E_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
+  const uint32_t joins = p.parts > 1 ? cfg->rows : 0;
+  if (!marks_fit(markers, ((uint64_t)p.grid + joins) * kWaves * 2))
+    return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
+  if (cfg->rows == 0) return ARGUS_OK;
+  if ((rc = device_ok()) != ARGUS_OK) return rc;
+  ScoreArgs a{};
+  a.logits = (const uint8_t*)io->d_logits, a.row_stride = io->row_stride * e, a.tokens = io->d_tokens;
+  a.logprobs = io->d_logprobs, a.entropy = io->d_entropy, a.ranks = io->d_ranks;
+  a.top_logprobs = io->d_top_logprobs, a.top_tokens = io->d_top_tokens;
+  a.sums = (Sums*)d_workspace;
+  a.cands = (uint64_t*)((char*)d_workspace + p.cands_at);
+  a.V = cfg->vocab, a.K = cfg->top, a.parts = p.parts, a.steps = p.steps, a.rows = cfg->rows;
+  hipStream_t st = (hipStream_t)stream_v;
+  a.marks = take_marks(markers, p.grid, 2);
+  if (cfg->type == ARGUS_BF16) launch_score<ARGUS_BF16>(a, p.grid, st);
+  else if (cfg->type == ARGUS_FP16) launch_score<ARGUS_FP16>(a, p.grid, st);
+  else launch_score<ARGUS_FP32>(a, p.grid, st);
+  if (joins) {
+    a.marks = take_marks(markers, joins, 2);
+    if (cfg->type == ARGUS_BF16) hipLaunchKernelGGL(k_score_join<ARGUS_BF16>, dim3(joins), dim3(kThreads), 0, st, a);
+    else if (cfg->type == ARGUS_FP16) hipLaunchKernelGGL(k_score_join<ARGUS_FP16>, dim3(joins), dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL(k_score_join<ARGUS_FP32>, dim3(joins), dim3(kThreads), 0, st, a);
+  }
+  return hipGetLastError() == hipSuccess ? ARGUS_OK : refuse(ARGUS_E_HIP, "launch failed");
+}
