@@ -43,7 +43,7 @@ struct ChunkArgs {
   uint64_t* head;    // [0] units of all items of one head, [1] units of a share, [2] items
   uint64_t* cum;     // [slots + 1] units before an item
   uint2* items;      // [slots] sequence, row tile
-  uint4* start;      // [shares] item, head, unit of it
+  uint4* start;      // [shares] item, head, unit of it, units
   uint4* open;       // [shares] item, head, its last share, 1 where a piece starts here and does not end
   float* part_o;     // [shares][2][TR][DP]
   float* part_ml;    // [shares][2][TR][2]
@@ -55,6 +55,25 @@ struct ChunkArgs {
   float scale;
   Marks marks;
 };
+
+constexpr uint32_t kMinShare = 4;   // units of a share, at least
+constexpr uint32_t kPieceCost = 2;  // what a row tile costs beside its steps, in steps
+
+// The thread's number and the kernel's arguments as values that the compiler knows nothing of: what follows
+// from them is worked out where it is used. Kept from one row tile to the next it would take
+// the registers that the steps need.
+ARGUS_DEV uint32_t fresh_thread() {
+  uint32_t tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  return tid;
+}
+ARGUS_DEV ChunkArgs fresh_args() {
+  auto p = (const __attribute__((address_space(4))) void*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  ChunkArgs a;
+  __builtin_memcpy(&a, (const void*)p, sizeof(a));
+  return a;
+}
 
 // What of the cache a row tile looks at: steps [0, sink_steps), then steps from `first` on.
 struct Reach {
@@ -68,6 +87,20 @@ struct Reach {
 // each of its row tiles, whatever lies before it: no sum over the sequences is needed.
 ARGUS_DEV uint32_t slot_of(const ChunkArgs& a, uint32_t s) {
   return (uint32_t)(((uint64_t)row_at(a.offsets, s, a.rows) * a.G) >> a.tile_shift) + s;
+}
+
+ARGUS_DEV uint32_t scalar(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+ARGUS_DEV const uint8_t* scalar(const uint8_t* p) {
+  const uint64_t x = (uint64_t)(uintptr_t)p;
+  return (const uint8_t*)(uintptr_t)join64(scalar((uint32_t)x), scalar((uint32_t)(x >> 32)));
+}
+// What all threads of a block have alike, as scalars.
+ARGUS_DEV Reach scalar(const Reach& r) {
+  Reach u;
+  u.s = scalar(r.s), u.row0 = scalar(r.row0), u.r0 = scalar(r.r0), u.rows = scalar(r.rows);
+  u.pos0 = (int32_t)scalar((uint32_t)r.pos0), u.len = scalar(r.len);
+  u.sink_steps = scalar(r.sink_steps), u.first = scalar(r.first), u.steps = scalar(r.steps);
+  return u;
 }
 
 // false: the slot has no rows.
@@ -116,9 +149,10 @@ typedef __attribute__((address_space(3))) uint8_t lds_byte;
 ARGUS_DEV u32x4 lds16(const lds_byte* p) { return *(const __attribute__((address_space(3))) u32x4*)p; }
 
 // 16 bytes of each lane from base + at to LDS, one lane's after the other's from `to` on. It
-// has no registers to write; who reads them waits for the loads' count first.
+// has no registers to write; who reads them waits for the loads' count first. (M0, which says where
+// to, holds nothing of the compiler's from one of its own instructions to another.)
 ARGUS_DEV void to_lds(const uint8_t* base, uint32_t at, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(base), "s"(to) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(base), "s"(to) : "memory");
 }
 
 // Bits of 16-bit numbers whose exponent is all ones: infinities and NaN.
@@ -144,8 +178,8 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
   constexpr int CE = F8 && DP > 64 ? 16 : 8, LR = DP / CE, RI = 64 / LR, NI = 8 / RI;
   constexpr int CW = F8 ? CE / 4 : 4;
   using Hf = Half<T>;
-  const uint32_t lane = threadIdx.x & 63u, c = lane & 31u, hk = lane >> 5;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t tid = fresh_thread(), lane = tid & 63u, c = lane & 31u, hk = lane >> 5;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float kc = a.scale * (a.k_scale ? a.k_scale[h] : 1.0f), kd = fabsf(kc), kd2 = kd * kLog2e;
   bool far = !(kd > 1e-30f && kd < 1e30f);  // scores so large, or a scale so odd, that the differences come first
 
@@ -217,8 +251,8 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
       const uint32_t run = wave * RUNS + j, first = tok + 8 * run;
       const int32_t page = __builtin_amdgcn_readlane(ids, run);
       const uint32_t place = first & in_page;
-      const uint8_t* ks = kb + (int64_t)(page < 0 ? 0 : page) * a.k_page + (uint64_t)place * a.k_tok;
-      const uint8_t* vs = vb + (int64_t)(page < 0 ? 0 : page) * a.v_page + (uint64_t)place * a.v_tok;
+      const uint8_t* ks = scalar(kb + (int64_t)(page < 0 ? 0 : page) * a.k_page + (uint64_t)place * a.k_tok);
+      const uint8_t* vs = scalar(vb + (int64_t)(page < 0 ? 0 : page) * a.v_page + (uint64_t)place * a.v_tok);
       const uint32_t have = page < 0 || first >= g.len ? 0u : g.len - first;  // tokens of the run that there are
       if constexpr (F8) {
 #pragma unroll
@@ -430,7 +464,7 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
     }
     __syncthreads();
 #pragma unroll 1
-    for (uint32_t i = threadIdx.x; i < kSide / 16; i += 64 * W) {
+    for (uint32_t i = tid; i < kSide / 16; i += 64 * W) {
       lds_byte* at = lds + from + kSide + i * 16;
       u32x4 x = lds16(at);
 #pragma unroll
@@ -446,7 +480,7 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
   };
   __syncthreads();  // what came before is done with the buffers
   if (padded) {     // elements behind the head size stay 0
-    for (uint32_t i = threadIdx.x; i < 2 * kBuffer / 16; i += 64 * W)
+    for (uint32_t i = tid; i < 2 * kBuffer / 16; i += 64 * W)
       *(__attribute__((address_space(3))) u32x4*)(lds + i * 16) = (u32x4)(0u);
     __syncthreads();
   }
@@ -482,19 +516,19 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
   }
 }
 
-template <int T, bool F8, int DP, int W>
-__global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void k_chunk(ChunkArgs a) {
+template <int T, bool F8, int DP, int W, bool SHARED>
+__global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : 2) void k_chunk(ChunkArgs a) {
   constexpr int DB = DP / 32, KT = kStepTokens<DP>, TR = 32 * W;
   using Hf = Half<T>;
   __shared__ __align__(1024) uint8_t s_raw[4 * KT * DP * 2];
   lds_byte* lds = (lds_byte*)s_raw;
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_CHUNK);
-  const uint32_t lane = threadIdx.x & 63u, c = lane & 31u, hk = lane >> 5;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-
   // O of the rows, or (slot: not done) a piece of it
-  auto put = [&](const Reach& g, uint32_t h, const f32x16 (&acc)[DB], float m, float l, bool done, uint64_t slot) {
+  auto put = [&](const ChunkArgs& a, const Reach& g, uint32_t h, const f32x16 (&acc)[DB], float m, float l, bool done,
+                 uint64_t slot) {
+    const uint32_t tid = fresh_thread(), c = tid & 31u, hk = tid >> 5 & 1u;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const float vs = a.v_scale ? a.v_scale[h] : 1.0f;
     const uint32_t mine = 32 * wave + c;
     if (mine >= g.rows) return;
@@ -531,8 +565,9 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void k_chunk(ChunkArgs a
   f32x16 acc[DB];
   float m, l;
   Reach g;
-  if (a.shares == 0) {
-    // A row tile per block: those that see the most tokens first.
+  if constexpr (!SHARED) {
+    // A row tile for the block: those that see the most tokens first.
+    const uint32_t lane = threadIdx.x & 63u;
     const uint32_t h = blockIdx.x % a.H, x = a.slots - 1 - blockIdx.x / a.H;
     uint32_t lo = 0, hi = a.S;
     while (hi - lo > 1) {  // the last sequence whose slots start at or before x
@@ -545,8 +580,37 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void k_chunk(ChunkArgs a
     lo = __builtin_amdgcn_readfirstlane(lo);
     const uint32_t first = slot_of(a, lo);
     if (first <= x && reach_of(a, lo, x - first, &g)) {
+      g = scalar(g);
       chunk_steps<T, F8, DP, W>(a, g, h, 0, g.steps, lds, acc, m, l);
-      put(g, h, acc, m, l, true, 0);
+      put(a, g, h, acc, m, l, true, 0);
+    }
+  } else {
+    // Shares that follow one another lie on one XCD, whose L2 then holds what the row tiles of a head
+    // read.
+    const uint32_t share = a.shares % 8 == 0 ? blockIdx.x % 8 * (a.shares / 8) + blockIdx.x / 8 : blockIdx.x;
+    const uint4 start = a.start[share];
+    uint32_t at = scalar(start.x), h = scalar(start.y), off = scalar(start.z), left = scalar(start.w);
+    if (threadIdx.x == 0) a.open[share] = make_uint4(0u, 0u, 0u, 0u);
+    while (left) {
+      const ChunkArgs b = fresh_args();
+      const uint2 item = b.items[at];
+      if (!reach_of(b, scalar(item.x), scalar(item.y), &g)) break;
+      g = scalar(g);
+      const uint32_t units = g.steps + kPieceCost, n = left < units - off ? left : units - off;
+      // its cost comes before its steps
+      const uint32_t t0 = off < kPieceCost ? 0 : off - kPieceCost, t1 = off + n < kPieceCost ? 0 : off + n - kPieceCost;
+      if (t0 < t1) {
+        const bool done = t0 == 0 && t1 == g.steps;
+        chunk_steps<T, F8, DP, W>(b, g, h, t0, t1, lds, acc, m, l);
+        const ChunkArgs e = fresh_args();
+        put(e, g, h, acc, m, l, done, 2ull * share + (t0 == 0 ? 1u : 0u));
+        // a row tile starts here and does not end: what is left of it is that of the shares behind
+        if (t0 == 0 && !done && threadIdx.x == 0)
+          e.open[share] = make_uint4(at, h, share + (uint32_t)((units - off - n + e.head[1] - 1) / e.head[1]), 1u);
+      }
+      left -= n;
+      off = 0;
+      if (left && ++at == (uint32_t)b.head[2]) at = 0, ++h;
     }
   }
   mk.end(ARGUS_REGION_CHUNK);
@@ -554,13 +618,16 @@ __global__ __launch_bounds__(64 * W, DP == 256 ? 1 : 2) void k_chunk(ChunkArgs a
 
 template <int T, bool F8, int DP, int W>
 void launch_chunk_as(const ChunkArgs& a, uint32_t grid, hipStream_t st) {
-  hipLaunchKernelGGL((k_chunk<T, F8, DP, W>), dim3(grid), dim3(64 * W), 0, st, a);
+  if (a.shares) hipLaunchKernelGGL((k_chunk<T, F8, DP, W, true>), dim3(grid), dim3(64 * W), 0, st, a);
+  else hipLaunchKernelGGL((k_chunk<T, F8, DP, W, false>), dim3(grid), dim3(64 * W), 0, st, a);
 }
 
+// Four waves a block, or eight that read the cache once for twice as many rows.
 template <int T, bool F8>
 void launch_chunk_type(const ChunkArgs& a, uint32_t grid, hipStream_t st) {
-  if (a.D <= 64) launch_chunk_as<T, F8, 64, 4>(a, grid, st);
-  else if (a.D <= 128) launch_chunk_as<T, F8, 128, 4>(a, grid, st);
+  const bool eight = a.tile_shift == 8;
+  if (a.D <= 64) eight ? launch_chunk_as<T, F8, 64, 8>(a, grid, st) : launch_chunk_as<T, F8, 64, 4>(a, grid, st);
+  else if (a.D <= 128) eight ? launch_chunk_as<T, F8, 128, 8>(a, grid, st) : launch_chunk_as<T, F8, 128, 4>(a, grid, st);
   else launch_chunk_as<T, F8, 256, 4>(a, grid, st);
 }
 
