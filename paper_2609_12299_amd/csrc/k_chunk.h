@@ -11,7 +11,20 @@
 // With rows as columns a lane holds 16 scores of one row, half a wave apart from the
 // other 16, and what the first product leaves in its registers is what the second takes:
 // which token stands at which place of a contraction is free. Keys and values go through
-// LDS, read once for the block; queries and O stay in registers.
+// LDS, read once for the block; queries and O stay in registers. Weights are rounded once, to the 16 bits that
+// the second product takes (to the nearest; in fp16 times 2^7, so that small ones keep their bits), their sums are
+// of the unrounded ones in 32 bits: a row's answer is off by half a step of a value at most.
+//
+// What bounds it. Long chunks: the matrix cores. One sequence of 16384 tokens, 8 x 8 heads of 128 in bf16
+// (4.4 TFLOP), takes 3.93 to 4.1 ms, 1070 to 1120 TFLOP/s; a library product of 8192^3 reaches 1220 to 1270 on this
+// card, whose clock falls to 2.0 GHz under either. The instructions of the two products alone go at 1380;
+// between them stand the exponentials and maxima of 64 tokens a row, which two waves of a SIMD overlap
+// little: half-blocks that take turns at them, and other priorities, measured the same. What gave time: eight
+// waves a block instead of four (4.5 to 4.05 ms), fragments that are read from LDS four matrix instructions
+// ahead (1 ahead 4.20, 4 3.94, 12 3.95), loads three steps ahead, straight into LDS.
+// Few tokens over long contexts: the cache's bytes. 4 sequences of 131000 tokens with 6 new ones each read
+// 2.1 GB in 341 us (6.3 TB/s, a plain read reaches 6.7). Prompts of a few hundred tokens: the steps of the longest row
+// tile, one after the other.
 #pragma once
 
 #include "k_attend.h"
@@ -23,9 +36,14 @@ namespace prompt {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// Tokens of a step: two buffers of keys and values are 64 KiB at head sizes of 128 and 256.
+// Tokens of a step: a buffer of keys and values is 32 KiB at head sizes of 128 and 256.
 template <int DP>
 constexpr int kStepTokens = DP == 256 ? 32 : 64;
+
+// Buffers of a step's keys and values: four where a block has a compute unit's LDS to itself, so that loads are
+// three steps ahead. In 8 bits the step under way lies in registers.
+template <bool F8, int DP, int W>
+constexpr int kBuffers = !F8 && (W == 8 || DP == 256) ? 4 : 2;
 
 struct ChunkArgs {
   const uint16_t* q;
@@ -39,25 +57,22 @@ struct ChunkArgs {
   const float *k_scale, *v_scale;
   uint16_t* out;
   float* lse;
-  // shared out: what the plan leaves, and the pieces
-  uint64_t* head;    // [0] units of all items of one head, [1] units of a share, [2] items
-  uint64_t* cum;     // [slots + 1] units before an item
-  uint2* items;      // [slots] sequence, row tile
-  uint4* start;      // [shares] item, head, unit of it, units
-  uint4* open;       // [shares] item, head, its last share, 1 where a piece starts here and does not end
-  float* part_o;     // [shares][2][TR][DP]
-  float* part_ml;    // [shares][2][TR][2]
+  // in pieces: what the plan leaves, and what the pieces do
+  uint64_t* head;    // [0] pieces of a head, [1] items that are cut, [2] most steps of a piece, [3] pieces of those
+  uint4* items;      // [slots] sequence, row tile, steps
+  uint4* joins;      // items that are cut: sequence, row tile, first piece, steps
+  uint4* pieces;     // sequence, row tile, steps from .. to; those of items that are cut first
+  float* part_o;     // [pieces of items that are cut][H][TR][DP]
+  float* part_ml;    // [...][H][TR][2]
   uint32_t S, rows, H, G, D;
-  uint32_t slots, shares, tile_shift;  // row tiles that there may be; rows of one
+  uint32_t slots, tile_shift;  // row tiles that there may be; rows of one
+  uint32_t blocks;             // that run at once; 0: a row tile each
   uint32_t step_shift;                 // tokens of a step
   uint32_t shift, num_pages, columns, window, sinks;
   FastDiv by_group;
   float scale;
   Marks marks;
 };
-
-constexpr uint32_t kMinShare = 4;   // units of a share, at least
-constexpr uint32_t kPieceCost = 2;  // what a row tile costs beside its steps, in steps
 
 // The thread's number and the kernel's arguments as values that the compiler knows nothing of: what follows
 // from them is worked out where it is used. Kept from one row tile to the next it would take
@@ -154,6 +169,38 @@ ARGUS_DEV u32x4 lds16(const lds_byte* p) { return *(const __attribute__((address
 ARGUS_DEV void to_lds(const uint8_t* base, uint32_t at, uint32_t to) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(base), "s"(to) : "memory");
 }
+// The same for some lanes of a wave all of whose lanes are active, without a branch.
+ARGUS_DEV void to_lds(const uint8_t* base, uint32_t at, uint32_t to, uint64_t lanes) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1" ::"v"(at), "s"(base),
+               "s"(to), "s"(lanes)
+               : "memory");
+}
+
+// What is read once, past the caches.
+ARGUS_DEV void to_lds_once(const uint8_t* base, uint32_t at, uint32_t to, uint64_t lanes) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %0, %1 nt\n\ts_mov_b64 exec, -1" ::"v"(at), "s"(base),
+               "s"(to), "s"(lanes)
+               : "memory");
+}
+// 4 bytes of each lane.
+ARGUS_DEV void to_lds_word(const uint8_t* base, uint32_t at, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(at), "s"(base), "s"(to) : "memory");
+}
+
+// The order of N matrix instructions that take a fragment each, of R reads from LDS: the reads are
+// A fragments ahead.
+constexpr int kFragsAhead = 4;
+template <int N, int R, int A>
+ARGUS_DEV void ahead() {
+  constexpr int kMatrix = 0x8, kRead = 0x100;
+  __builtin_amdgcn_sched_group_barrier(kRead, R * A, 0);
+#pragma unroll
+  for (int i = 0; i < N - A; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(kRead, R, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(kMatrix, A, 0);
+}
 
 // Bits of 16-bit numbers whose exponent is all ones: infinities and NaN.
 template <int T>
@@ -170,16 +217,18 @@ constexpr uint32_t kFracs = ((1u << kFrac<T>) - 1) * 0x10001u;
 template <int T, bool F8, int DP, int W>
 ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint32_t t0, uint32_t t1, lds_byte* lds,
                            f32x16 (&acc)[DP / 32], float& m, float& l) {
-  constexpr int KT = kStepTokens<DP>, HT = KT / 32;  // halves of a step
-  constexpr int KF = DP / 16, DB = DP / 32;          // fragments of a key row, 32-wide parts of O
-  constexpr int RW = KT / W, RUNS = RW / 8;     // rows that a wave loads, runs of eight tokens
-  constexpr uint32_t kRow = DP * 2, kSide = KT * kRow, kBuffer = 2 * kSide;
+  constexpr int KT = kStepTokens<DP>, HT = KT / 32;      // halves of a step
+  constexpr int KF = DP / 16, DB = DP / 32;              // fragments of a key row, 32-wide parts of O
+  constexpr uint32_t kRuns = KT / 8;                     // of eight tokens, in a step
+  constexpr int RUNS = kRuns / W;                        // that a wave loads
+  constexpr int NB = kBuffers<F8, DP, W>, PD = NB - 1;   // buffers; steps that loads are ahead
+  constexpr uint32_t kRow = DP * 2, kSide = KT * kRow;
   // a lane's part of a load: CE elements, NI loads a run, RI rows a load
   constexpr int CE = F8 && DP > 64 ? 16 : 8, LR = DP / CE, RI = 64 / LR, NI = 8 / RI;
   constexpr int CW = F8 ? CE / 4 : 4;
   using Hf = Half<T>;
   const uint32_t tid = fresh_thread(), lane = tid & 63u, c = lane & 31u, hk = lane >> 5;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t wave = scalar(tid >> 6);
   const float kc = a.scale * (a.k_scale ? a.k_scale[h] : 1.0f), kd = fabsf(kc), kd2 = kd * kLog2e;
   bool far = !(kd > 1e-30f && kd < 1e30f);  // scores so large, or a scale so odd, that the differences come first
 
@@ -206,91 +255,100 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
   for (int d = 0; d < DB; ++d) acc[d] = (f32x16)(0.0f);
   float base = 0.0f;  // the maximum to base 2, less kRaise
   // infinite values that the row has seen, a bit for each of the lane's elements (both: NaN)
-  uint32_t plus[DB / 2] = {}, minus[DB / 2] = {};
+  constexpr int kBits = (DB + 3) / 4;
+  uint64_t plus[kBits] = {}, minus[kBits] = {};
 
-  const int32_t* tab = a.table + (int64_t)g.s * a.table_stride;
-  const uint8_t* kb = a.k + (int64_t)h * a.k_head;
-  const uint8_t* vb = a.v + (int64_t)h * a.v_head;
+  auto token_of = [&](uint32_t t) { return (t < g.sink_steps ? t : t - g.sink_steps + g.first) * KT; };
   const uint32_t in_page = (1u << a.shift) - 1;
 
+  // The pages: a lane looks after one run of eight tokens, 64 / kRuns steps in a row. The table's entries
+  // come to LDS, where each wave has a place of its own for this group of steps and for the next,
+  // so that no register waits for them.
+  constexpr uint32_t kGroup = 64 / kRuns;
+  const uint8_t* tab = (const uint8_t*)(a.table + (int64_t)g.s * a.table_stride);
+  lds_byte* const ring = lds + 2 * NB * kSide + wave * 512;
+  auto column = [&](uint32_t s0) {
+    const uint32_t s = s0 + lane / kRuns;
+    return (token_of(s < t1 ? s : t1 - 1) + 8 * (lane % kRuns)) >> a.shift;
+  };
+  auto fetch = [&](uint32_t s0) {  // entries of steps from s0 on
+    const uint32_t col = column(s0);
+    to_lds_word(scalar(tab), (col < a.columns ? col : 0) * 4, (uint32_t)(uintptr_t)ring + ((s0 - t0) / kGroup & 1u) * 256);
+  };
+  uint64_t place_k, place_v, held64;
+  uint32_t tokens;  // of the lane's run that there are
+  auto use = [&](uint32_t s0) {
+    const int32_t entry = *(const __attribute__((address_space(3))) int32_t*)(ring + ((s0 - t0) / kGroup & 1u) * 256 + lane * 4);
+    const bool held = column(s0) < a.columns && (uint32_t)entry < a.num_pages;
+    const uint32_t s = s0 + lane / kRuns, first = token_of(s < t1 ? s : t1 - 1) + 8 * (lane % kRuns);
+    const uint32_t page = held ? (uint32_t)entry : 0u, place = first & in_page;
+    place_k = (uint64_t)page * (uint64_t)a.k_page + (uint64_t)place * a.k_tok;
+    place_v = (uint64_t)page * (uint64_t)a.v_page + (uint64_t)place * a.v_tok;
+    tokens = held && first < g.len ? g.len - first : 0u;
+    held64 = __ballot(held);
+  };
+
   // What a lane adds to the scalar base of a load, and whether it has anything to load.
+  const uint8_t* kb = a.k + (int64_t)h * a.k_head;
+  const uint8_t* vb = a.v + (int64_t)h * a.v_head;
   const uint32_t lr = lane / LR, lc = lane % LR;
   uint32_t k_at[RUNS][NI], v_at[RUNS][NI], loads = 0;
+  uint64_t lanes[RUNS][NI];
 #pragma unroll
   for (int j = 0; j < RUNS; ++j)
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const uint32_t row = wave * RW + 8 * j + i * RI + lr;
+      const uint32_t row = 8 * (wave * RUNS + j) + i * RI + lr;
       const uint32_t chunk = F8 ? lc : lc ^ swizzle<DP>(row);
       const uint32_t b = chunk * (F8 ? CE : 16);
-      k_at[j][i] = (i * RI + lr) * a.k_tok + b;
-      v_at[j][i] = (i * RI + lr) * a.v_tok + b;
-      loads |= chunk * CE < a.D ? 1u << (j * NI + i) : 0u;
+      const bool some = chunk * CE < a.D;
+      // (in 8 bits, behind the head size: elements of the row once more, taken off where they land)
+      k_at[j][i] = (i * RI + lr) * a.k_tok + (F8 && !some ? 0 : b);
+      v_at[j][i] = (i * RI + lr) * a.v_tok + (F8 && !some ? 0 : b);
+      loads |= some ? 1u << (j * NI + i) : 0u;
+      lanes[j][i] = __ballot(some);
     }
   const bool padded = a.D != DP;
-
-  auto token_of = [&](uint32_t t) { return (t < g.sink_steps ? t : t - g.sink_steps + g.first) * KT; };
-  // The pages of a step's runs of eight tokens, in the first lanes: the entries, and a step
-  // later (they are under way until then) what they say.
-  const uint32_t run_at = 8 * (lane % (KT / 8));
-  auto find = [&](uint32_t t) {
-    const uint32_t col = (token_of(t < t1 ? t : t1 - 1) + run_at) >> a.shift;
-    return tab[col < a.columns ? col : 0];
-  };
-  auto known = [&](uint32_t t, int32_t entry) {
-    const uint32_t col = (token_of(t < t1 ? t : t1 - 1) + run_at) >> a.shift;
-    return col < a.columns && (uint32_t)entry < a.num_pages ? entry : -1;
-  };
   uint32_t staged[F8 ? 2 : 1][RUNS][NI][F8 ? CW : 1];
-  // Step t's keys and values on their way, into LDS or (8 bits) registers.  What lies behind
-  // the sequence's end or in no page is 0.
-  auto load = [&](uint32_t t, int32_t ids, lds_byte* to) {
-    const uint32_t tok = token_of(t);
+  typedef uint32_t words __attribute__((ext_vector_type(CW)));
+  // Step s's keys (side 0) and values on their way, into LDS or (8 bits) registers. What lies behind
+  // the sequence's end or in no page is 0; where nothing does, without a look at that.
+  // (Four waves: few rows of a sequence, which read most of it once, past the caches. 4 sequences of 131000
+  // tokens with 6 new ones each 341 us against 384, 64 of up to 30000 with one 301 against 329, and batches in which
+  // row tiles share what they read the same.)
+  auto load = [&](uint32_t s, int buffer, auto all_of) {
+    constexpr bool all = all_of(), once = W == 4;
+    const uint32_t run0 = (s - t0) % kGroup * kRuns + wave * RUNS;
 #pragma unroll
-    for (int j = 0; j < RUNS; ++j) {
-      const uint32_t run = wave * RUNS + j, first = tok + 8 * run;
-      const int32_t page = __builtin_amdgcn_readlane(ids, run);
-      const uint32_t place = first & in_page;
-      const uint8_t* ks = scalar(kb + (int64_t)(page < 0 ? 0 : page) * a.k_page + (uint64_t)place * a.k_tok);
-      const uint8_t* vs = scalar(vb + (int64_t)(page < 0 ? 0 : page) * a.v_page + (uint64_t)place * a.v_tok);
-      const uint32_t have = page < 0 || first >= g.len ? 0u : g.len - first;  // tokens of the run that there are
-      if constexpr (F8) {
+    for (int side = 0; side < 2; ++side)
+#pragma unroll
+      for (int j = 0; j < RUNS; ++j) {
+        const uint64_t place = side ? place_v : place_k;
+        const uint8_t* from = scalar((side ? vb : kb) + join64(__builtin_amdgcn_readlane((uint32_t)place, run0 + j),
+                                                               __builtin_amdgcn_readlane((uint32_t)(place >> 32), run0 + j)));
+        const uint32_t have = all ? 8u : __builtin_amdgcn_readlane(tokens, run0 + j);
+        lds_byte* to = lds + (side * NB + buffer) * kSide + 8 * (wave * RUNS + j) * kRow;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-          typedef uint32_t words __attribute__((ext_vector_type(CW)));
-          words x = (words)(0u), y = (words)(0u);
-          if (i * RI + lr < have && (!padded || (loads >> (j * NI + i) & 1u))) {
-            x = *reinterpret_cast<const words*>(ks + k_at[j][i]);
-            y = *reinterpret_cast<const words*>(vs + v_at[j][i]);
-          }
+          const uint32_t at = (side ? v_at : k_at)[j][i];
+          if constexpr (F8) {
+            words x = (words)(0u);
+            if (all || i * RI + lr < have)
+              x = once ? __builtin_nontemporal_load(reinterpret_cast<const words*>(from + at)) : *reinterpret_cast<const words*>(from + at);
 #pragma unroll
-          for (int w = 0; w < CW; ++w) staged[0][j][i][w] = x[w], staged[1][j][i][w] = y[w];
-        }
-      } else {
-        lds_byte* at = to + (wave * RW + 8 * j) * kRow;
-        const uint32_t side = (uint32_t)(uintptr_t)at;
-        auto bring = [&](int i) {
-          to_lds(ks, k_at[j][i], side + i * RI * kRow);
-          to_lds(vs, v_at[j][i], side + i * RI * kRow + kSide);
-        };
-        if (have >= 8 && !padded) {
-#pragma unroll
-          for (int i = 0; i < NI; ++i) bring(i);
-        } else {
-#pragma unroll
-          for (int i = 0; i < NI; ++i) {
+            for (int w = 0; w < CW; ++w) staged[side][j][i][w] = x[w];
+          } else if constexpr (all) {
+            if constexpr (once) to_lds_once(from, at, (uint32_t)(uintptr_t)to + i * RI * kRow, lanes[j][i]);
+            else to_lds(from, at, (uint32_t)(uintptr_t)to + i * RI * kRow, lanes[j][i]);
+          } else {
             const bool there = i * RI + lr < have;
-            if (there && (loads >> (j * NI + i) & 1u)) bring(i);
-            if (!there) {
-              *(__attribute__((address_space(3))) u32x4*)(at + i * RI * kRow + lane * 16) = (u32x4)(0u);
-              *(__attribute__((address_space(3))) u32x4*)(at + i * RI * kRow + kSide + lane * 16) = (u32x4)(0u);
-            }
+            if (there && (loads >> (j * NI + i) & 1u)) to_lds(from, at, (uint32_t)(uintptr_t)to + i * RI * kRow);
+            if (!there) *(__attribute__((address_space(3))) u32x4*)(to + i * RI * kRow + lane * 16) = (u32x4)(0u);
           }
         }
       }
-    }
   };
-  auto land = [&](lds_byte* to) {
+  auto land = [&](int buffer) {
     if constexpr (F8) {
 #pragma unroll
       for (int side = 0; side < 2; ++side)
@@ -298,13 +356,14 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
         for (int j = 0; j < RUNS; ++j)
 #pragma unroll
           for (int i = 0; i < NI; ++i) {
-            const uint32_t row = wave * RW + 8 * j + i * RI + lr;
-            lds_byte* at = to + side * kSide + row * kRow;
+            const uint32_t row = 8 * (wave * RUNS + j) + i * RI + lr;
+            lds_byte* to = lds + (side * NB + buffer) * kSide + row * kRow;
+            const uint32_t some = loads >> (j * NI + i) & 1u ? ~0u : 0u;
 #pragma unroll
             for (int e = 0; e < CE / 8; ++e) {
-              const uint32_t w0 = staged[side][j][i][2 * e], w1 = staged[side][j][i][2 * e + 1];
+              const uint32_t w0 = staged[side][j][i][2 * e] & some, w1 = staged[side][j][i][2 * e + 1] & some;
               const u32x4 x = (u32x4){widen<T>(w0, false), widen<T>(w0, true), widen<T>(w1, false), widen<T>(w1, true)};
-              *(__attribute__((address_space(3))) u32x4*)(at + (((lc * (CE / 8) + e) ^ swizzle<DP>(row)) << 4)) = x;
+              *(__attribute__((address_space(3))) u32x4*)(to + (((lc * (CE / 8) + e) ^ swizzle<DP>(row)) << 4)) = x;
             }
           }
     }
@@ -324,53 +383,61 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const uint32_t chunk = 4 * d + 2 * (piece & 1u) + (lane >> 4 & 1u), row = v_row + 8 * e;
-      v_frag[d][e] = (uint32_t)(uintptr_t)lds + kSide + row * kRow + ((chunk ^ swizzle<DP>(row)) << 4) + (piece >> 1) * 8;
+      v_frag[d][e] = (uint32_t)(uintptr_t)lds + NB * kSide + row * kRow + ((chunk ^ swizzle<DP>(row)) << 4) + (piece >> 1) * 8;
       asm volatile("" : "+v"(v_frag[d][e]));
     }
-  auto k_part = [&](uint32_t from, int th, int f) { return lds16((const lds_byte*)(uintptr_t)(k_frag[f] + (from + th * 32 * kRow))); };
+  auto k_part = [&](int buffer, int th, int f) { return lds16((const lds_byte*)(uintptr_t)(k_frag[f] + (buffer * kSide + th * 32 * kRow))); };
   // Fragment (d, f) of V^T: lane (m, hk) has tokens 16 f + 8 e + 4 hk + 0..3, e = 0, 1, of
   // element 32 d + 16 (m / 4 % 2) + 4 (m / 8) + m % 4, so that a lane of O^T holds 16 elements in a row.
-  auto v_part = [&](uint32_t from, int d, int f) {
+  auto v_part = [&](int buffer, int d, int f) {
     u32x4 x;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (__attribute__((address_space(3))) s16x4*)(uintptr_t)(v_frag[d][e] + (from + 16 * f * kRow)));
+          (__attribute__((address_space(3))) s16x4*)(uintptr_t)(v_frag[d][e] + (buffer * kSide + 16 * f * kRow)));
       x[2 * e] = __builtin_bit_cast(u32x2, y).x, x[2 * e + 1] = __builtin_bit_cast(u32x2, y).y;
     }
     return x;
   };
 
-  auto take = [&](uint32_t t, int32_t ids, uint32_t from) {
-    const uint32_t tok = token_of(t);
-    const uint32_t held = (uint32_t)__ballot(ids >= 0) & ((1u << (KT / 8)) - 1);
-    // whether the rows see all of the step, or none
-    const int32_t e = (int32_t)tok + KT - 1;
-    const bool whole = e <= p_least && held == (1u << (KT / 8)) - 1 &&
-                       (!a.window || (int32_t)tok > p_most - (int32_t)a.window || e < (int32_t)a.sinks);
-    if ((int32_t)tok > p_most || !held || (a.window && e <= p_least - (int32_t)a.window && tok >= a.sinks)) return;
-
-    f32x16 sc[HT];
+  // Steps [from, to) behind the sinks' whose tokens rows of positions p0 to p1 all see.
+  struct Range {
+    uint32_t from, to;
+  };
+  auto all_seen = [&](int32_t p0, int32_t p1) {
+    const uint32_t shift = g.first - g.sink_steps;  // of a step's number behind the sinks' and its tokens'
+    const uint32_t lo = a.window && p1 >= 0 && (uint32_t)p1 + 1 > a.window ? (uint32_t)p1 + 1 - a.window : 0u;
+    Range x{(lo + KT - 1) / KT - shift, p0 < 0 ? 0u : ((uint32_t)p0 + 1) / KT - shift};
+    if ((lo + KT - 1) / KT < g.first || x.from < g.sink_steps) x.from = g.sink_steps;
+    if (p0 < 0 || ((uint32_t)p0 + 1) / KT < g.first || x.to < x.from) x.to = x.from;
+    return x;
+  };
+  const Range mine_all = all_seen(p_least, p_most);
+  const Range block_all = all_seen(g.pos0 + (int32_t)divide(g.r0, a.by_group), g.pos0 + (int32_t)divide(g.r0 + g.rows - 1, a.by_group));
+  constexpr uint32_t kHeld = (1u << kRuns) - 1;
+  f32x16 sc[HT];    // scores
+  u32x4 p[2 * HT];  // weights as the second product takes them
+  auto score = [&](int buffer) {
 #pragma unroll
     for (int th = 0; th < HT; ++th) sc[th] = (f32x16)(0.0f);
 #pragma unroll
     for (int f = 0; f < KF; ++f)
 #pragma unroll
-      for (int th = 0; th < HT; ++th) {
-        sc[th] = mfma32<T>(k_part(from, th, f), qf[f], sc[th]);
-      }
-
-    if (!whole) {
+      for (int th = 0; th < HT; ++th) sc[th] = mfma32<T>(k_part(buffer, th, f), qf[f], sc[th]);
+    ahead<KF * HT, 1, kFragsAhead>();
+  };
+  auto weigh = [&](uint32_t tok, uint32_t held, bool whole) {
+    if (__builtin_expect(!whole, 0)) {
       // of the lane's 16 HT tokens, tok + 4 hk + 0..3, + 8..11, ..., those below x
       auto below = [&](int32_t x) {
         const int32_t y = x - (int32_t)(tok + 4 * hk), k = y < 0 ? 0 : 4 * (y >> 3) + ((y & 7) < 4 ? y & 7 : 4);
         return k < 32 ? (1u << k) - 1 : ~0u;
       };
       uint32_t vis = below(end) & (~below(low) | below((int32_t)a.sinks));
-      if (held != (1u << (KT / 8)) - 1) {
+      if (held != kHeld) {
         uint32_t by_four = 0;
 #pragma unroll
-        for (int i = 0; i < KT / 8; ++i) by_four |= held >> i & 1u ? 15u << (4 * i) : 0u;
+        for (uint32_t i = 0; i < kRuns; ++i) by_four |= held >> i & 1u ? 15u << (4 * i) : 0u;
         vis &= by_four;
       }
 #pragma unroll
@@ -384,7 +451,7 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[th][i]);
     top = top == -INFINITY ? top : top * kd;  // (kd may be 0)
-    if (__any(top > m + kSlack)) {
+    if (__builtin_expect(__any(top > m + kSlack), 0)) {
       top = fmaxf(top, __shfl_xor(top, 32));
       const float mn = fmaxf(m, top);
       const float scale = m == -INFINITY ? 0.0f : exp_of(m - mn);
@@ -395,132 +462,178 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
       base = mn == -INFINITY ? 0.0f : fmaf(mn, kLog2e, -Hf::kRaise);
       far = far || __any(fabsf(mn) > kFar && mn != -INFINITY);
     }
-    if (!far) {
+    float sum[4];
 #pragma unroll
-      for (int th = 0; th < HT; ++th)
+    for (int th = 0; th < HT; ++th) {
+      float w[16];
+      if (__builtin_expect(!far, 1)) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[th][i] = __builtin_amdgcn_exp2f(fmaf(sc[th][i], kd2, -base));
-    } else {
-      const float ms = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-      for (int th = 0; th < HT; ++th)
+        for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(sc[th][i], kd2, -base));
+      } else {
+        const float ms = m == -INFINITY ? 0.0f : m;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const float x = sc[th][i], y = x == -INFINITY ? x : x * kd;
-          sc[th][i] = __builtin_amdgcn_exp2f(fmaf(y - ms, kLog2e, Hf::kRaise));
+          w[i] = __builtin_amdgcn_exp2f(fmaf(y - ms, kLog2e, Hf::kRaise));
         }
-    }
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    u32x4 p[2 * HT];
+      }
 #pragma unroll
-    for (int th = 0; th < HT; ++th) {
+      for (int i = 0; i < 16; ++i) sum[i % 4] = th == 0 && i < 4 ? w[i] : sum[i % 4] + w[i];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sum[i % 4] += sc[th][i];
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) p[2 * th + i / 8][i / 2 % 4] = Hf::pack(sc[th][i], sc[th][i + 1]);
+      for (int i = 0; i < 16; i += 2) p[2 * th + i / 8][i / 2 % 4] = Hf::pack(w[i], w[i + 1]);
     }
     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-
+  };
+  auto apply = [&](int buffer) {
 #pragma unroll
     for (int f = 0; f < 2 * HT; ++f)
 #pragma unroll
-      for (int d = 0; d < DB; ++d) acc[d] = mfma32<T>(v_part(from, d, f), p[f], acc[d]);
+      for (int d = 0; d < DB; ++d) acc[d] = mfma32<T>(v_part(buffer, d, f), p[f], acc[d]);
+    ahead<2 * HT * DB, 2, kFragsAhead>();
   };
 
   // Of a step that some of the block's rows do not see, the values that are not finite (0 times infinity
   // would be NaN): noted where they are seen, and 0 from then on.  All waves look at the same
   // values, so they come to the same answer.
-  const int32_t b_least = g.pos0 + (int32_t)divide(g.r0, a.by_group), b_most = g.pos0 + (int32_t)divide(g.r0 + g.rows - 1, a.by_group);
-  auto settle = [&](uint32_t t, int32_t ids, uint32_t from) {
-    const uint32_t tok = token_of(t);
-    const int32_t e = (int32_t)tok + KT - 1;
-    if (e <= b_least && (!a.window || (int32_t)tok > b_most - (int32_t)a.window || e < (int32_t)a.sinks)) return;
+  auto settle = [&](uint32_t t, uint32_t held, int buffer) {
+    if (__builtin_expect(t >= block_all.from && t < block_all.to, 1)) return;
+    lds_byte* const values = lds + (NB + buffer) * kSide;
     uint32_t odd = 0;
 #pragma unroll 4
     for (uint32_t i = 0; i < kSide / 1024; ++i) {
-      const u32x4 x = lds16(lds + from + kSide + i * 1024 + lane * 16);
+      const u32x4 x = lds16(values + i * 1024 + lane * 16);
       odd |= not_finite<T>(x[0]) | not_finite<T>(x[1]) | not_finite<T>(x[2]) | not_finite<T>(x[3]);
     }
-    if (!__any(odd)) return;
-    const uint32_t held = (uint32_t)__ballot(ids >= 0);
+    if (__builtin_expect(!__any(odd), 1)) return;
+    const uint32_t tok = token_of(t);
 #pragma unroll 1
     for (uint32_t j = 0; j < (uint32_t)KT; ++j) {
       const int32_t at = (int32_t)(tok + j);
       const bool seen = at < end && (at >= low || at < (int32_t)a.sinks) && (held >> (j / 8) & 1u);
+#pragma unroll 1
+      for (uint32_t e = 0; e < 2 * DB; ++e) {  // eight of the lane's elements
+        const u32x4 x = lds16(values + j * kRow + (((4 * (e / 2) + 2 * hk + e % 2) ^ swizzle<DP>(j)) << 4));
+        uint32_t up = 0, down = 0;
 #pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const u32x4 x = lds16(lds + from + kSide + j * kRow + (((4 * d + 2 * hk + i) ^ swizzle<DP>(j)) << 4));
-          uint32_t up = 0, down = 0;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const uint32_t bad = seen ? not_finite<T>(x[w]) >> 15 : 0u, sign = x[w] >> 15 & 0x10001u;
-            const uint32_t nan = bad & ((x[w] & kFracs<T>) + kFracs<T>) >> kFrac<T>, u = nan | (bad & ~sign), v = nan | (bad & sign);
-            up |= ((u | u >> 15) & 3u) << (2 * w), down |= ((v | v >> 15) & 3u) << (2 * w);
-          }
-          plus[d / 2] |= up << (16 * (d % 2) + 8 * i), minus[d / 2] |= down << (16 * (d % 2) + 8 * i);
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t bad = seen ? not_finite<T>(x[w]) >> 15 : 0u, sign = x[w] >> 15 & 0x10001u;
+          const uint32_t nan = bad & ((x[w] & kFracs<T>) + kFracs<T>) >> kFrac<T>, u = nan | (bad & ~sign), v = nan | (bad & sign);
+          up |= ((u | u >> 15) & 3u) << (2 * w), down |= ((v | v >> 15) & 3u) << (2 * w);
         }
+#pragma unroll
+        for (int k = 0; k < kBits; ++k)
+          if (e / 8 == (uint32_t)k) plus[k] |= (uint64_t)up << (8 * (e % 8)), minus[k] |= (uint64_t)down << (8 * (e % 8));
+      }
     }
     __syncthreads();
 #pragma unroll 1
     for (uint32_t i = tid; i < kSide / 16; i += 64 * W) {
-      lds_byte* at = lds + from + kSide + i * 16;
-      u32x4 x = lds16(at);
+      u32x4 x = lds16(values + i * 16);
 #pragma unroll
       for (int w = 0; w < 4; ++w) x[w] &= ~((not_finite<T>(x[w]) >> 15) * 0xFFFFu);
-      *(__attribute__((address_space(3))) u32x4*)at = x;
+      *(__attribute__((address_space(3))) u32x4*)(values + i * 16) = x;
     }
     __syncthreads();
   };
 
-  auto arrived = [&]() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __syncthreads();
+  // All waves have come this far, and what they wrote to LDS is there; of their loads all but the
+  // last N.
+  auto meet = [&](auto last_of) {
+    constexpr int N = last_of();
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
   };
-  __syncthreads();  // what came before is done with the buffers
-  if (padded) {     // elements behind the head size stay 0
-    for (uint32_t i = tid; i < 2 * kBuffer / 16; i += 64 * W)
+  constexpr auto none = []() constexpr { return 0; };
+  // loads of a wave that may still be under way when a step's own have to be there: those of the steps
+  // behind it
+  constexpr auto rest = []() constexpr { return (PD - 1) * 2 * RUNS * NI; };
+  constexpr auto some = []() constexpr { return false; };
+  constexpr auto every = []() constexpr { return true; };
+  meet(none);  // (what came before is done with the buffers)
+  fetch(t0);
+  if (padded) {  // elements behind the head size stay 0
+    for (uint32_t i = tid; i < 2 * NB * kSide / 16; i += 64 * W)
       *(__attribute__((address_space(3))) u32x4*)(lds + i * 16) = (u32x4)(0u);
-    __syncthreads();
   }
-  int32_t ids = known(t0, find(t0)), next = find(t0 + 1);
-  load(t0, ids, lds);
-  land(lds);
-  auto step = [&](uint32_t t, uint32_t b) {
-    arrived();  // step t is there, and nobody reads step t - 1 any more
-    const int32_t after = find(t + 2);
-    next = known(t + 1, next);
-    if (t + 1 < t1) load(t + 1, next, lds + (kBuffer - b));
-    settle(t, ids, b);
-    take(t, ids, b);
-    if (t + 1 < t1) land(lds + (kBuffer - b));
-    ids = next, next = after;
-  };
-  for (uint32_t t = t0; t < t1; t += 2) {
-    step(t, 0);
-    if (t + 1 < t1) step(t + 1, kBuffer);
-  }
-  l += __shfl_xor(l, 32);
-  uint32_t seen = 0;
+  meet(none);
+  use(t0);
+  fetch(t0 + kGroup);
+  uint32_t held[NB], sure = 0;  // of the steps that are loaded; how many of the last were loaded whole
 #pragma unroll
-  for (int d = 0; d < DB / 2; ++d) seen |= plus[d] | minus[d];
-  if (__any(seen)) {
+  for (int i = 0; i < PD; ++i) {
+    held[i] = (uint32_t)(held64 >> (i * kRuns)) & kHeld;
+    if (t0 + i < t1) load(t0 + i, i, some);
+    land(i);
+  }
+  auto step = [&](uint32_t t, auto buffer_of) {
+    constexpr int b = buffer_of(), nb = (b + PD) % NB;
+    // step t is there, and nobody reads step t - 1 any more
+    if (PD > 1 && __builtin_expect(sure >= PD - 1, 1)) meet(rest);
+    else meet(none);
+    const uint32_t s = t + PD;
+    if ((s - t0) % kGroup == 0) {
+      use(s);
+      fetch(s + kGroup);
+    }
+    held[nb] = (uint32_t)(held64 >> ((s - t0) % kGroup * kRuns)) & kHeld;
+    // (as a scalar: all lanes go into load, which sets the mask of those that do)
+    if (__builtin_expect(scalar(s >= block_all.from && s < block_all.to && s < t1 && held[nb] == kHeld ? 1u : 0u), 1)) {
+      load(s, nb, every);
+      ++sure;
+    } else {
+      if (s < t1) load(s, nb, some);
+      sure = 0;
+    }
+    settle(t, held[b], b);
+    // what the wave's rows see of the step: all of it, some, nothing
+    bool whole = true, live = true;
+    const uint32_t tok = token_of(t);
+    if (__builtin_expect(t < mine_all.from || t >= mine_all.to || held[b] != kHeld, 0)) {
+      const int32_t first = (int32_t)tok, last = first + KT - 1;
+      whole = last <= p_least && held[b] == kHeld &&
+              (!a.window || first > p_most - (int32_t)a.window || last < (int32_t)a.sinks);
+      live = first <= p_most && held[b] && !(a.window && last <= p_least - (int32_t)a.window && tok >= a.sinks);
+    }
+    if (__builtin_expect(live, 1)) {
+      score(b);
+      weigh(tok, held[b], whole);
+      apply(b);
+    }
+    if (s < t1) land(nb);
+  };
+  for (uint32_t t = t0; t < t1; t += NB) {
+    step(t, []() constexpr { return 0; });
+    if (t + 1 < t1) step(t + 1, []() constexpr { return 1; });
+    if constexpr (NB == 4) {
+      if (t + 2 < t1) step(t + 2, []() constexpr { return 2; });
+      if (t + 3 < t1) step(t + 3, []() constexpr { return 3; });
+    }
+  }
+  // (entries for steps that there are not: LDS is given back when the block ends)
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  l += __shfl_xor(l, 32);
+  uint64_t seen = 0;
+#pragma unroll
+  for (int k = 0; k < kBits; ++k) seen |= plus[k] | minus[k];
+  if (__any(seen != 0)) {
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        acc[d][i] += plus[d / 2] >> (16 * (d % 2) + i) & 1u ? INFINITY : 0.0f;
-        acc[d][i] -= minus[d / 2] >> (16 * (d % 2) + i) & 1u ? INFINITY : 0.0f;
+        acc[d][i] += plus[d / 4] >> (16 * (d % 4) + i) & 1u ? INFINITY : 0.0f;
+        acc[d][i] -= minus[d / 4] >> (16 * (d % 4) + i) & 1u ? INFINITY : 0.0f;
       }
   }
 }
 
-template <int T, bool F8, int DP, int W, bool SHARED>
-__global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : 2) void k_chunk(ChunkArgs a) {
+template <int T, bool F8, int DP, int W, bool PIECES>
+__global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : DP == 128 ? 2 : 3) void k_chunk(ChunkArgs a) {
   constexpr int DB = DP / 32, KT = kStepTokens<DP>, TR = 32 * W;
   using Hf = Half<T>;
-  __shared__ __align__(1024) uint8_t s_raw[4 * KT * DP * 2];
+  __shared__ __align__(1024) uint8_t s_raw[2 * kBuffers<F8, DP, W> * KT * DP * 2 + 512 * W];
   lds_byte* lds = (lds_byte*)s_raw;
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_CHUNK);
@@ -565,10 +678,10 @@ __global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : 2) void k_chunk(C
   f32x16 acc[DB];
   float m, l;
   Reach g;
-  if constexpr (!SHARED) {
+  const uint32_t h = blockIdx.x % a.H;
+  if constexpr (!PIECES) {
     // A row tile for the block: those that see the most tokens first.
-    const uint32_t lane = threadIdx.x & 63u;
-    const uint32_t h = blockIdx.x % a.H, x = a.slots - 1 - blockIdx.x / a.H;
+    const uint32_t lane = threadIdx.x & 63u, x = a.slots - 1 - blockIdx.x / a.H;
     uint32_t lo = 0, hi = a.S;
     while (hi - lo > 1) {  // the last sequence whose slots start at or before x
       const uint32_t step = (hi - lo + 63) / 64, s = lo + lane * step;
@@ -577,7 +690,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : 2) void k_chunk(C
       lo += (n - 1) * step;
       hi = hi < lo + step ? hi : lo + step;
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
+    lo = scalar(lo);
     const uint32_t first = slot_of(a, lo);
     if (first <= x && reach_of(a, lo, x - first, &g)) {
       g = scalar(g);
@@ -585,32 +698,15 @@ __global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : 2) void k_chunk(C
       put(a, g, h, acc, m, l, true, 0);
     }
   } else {
-    // Shares that follow one another lie on one XCD, whose L2 then holds what the row tiles of a head
-    // read.
-    const uint32_t share = a.shares % 8 == 0 ? blockIdx.x % 8 * (a.shares / 8) + blockIdx.x / 8 : blockIdx.x;
-    const uint4 start = a.start[share];
-    uint32_t at = scalar(start.x), h = scalar(start.y), off = scalar(start.z), left = scalar(start.w);
-    if (threadIdx.x == 0) a.open[share] = make_uint4(0u, 0u, 0u, 0u);
-    while (left) {
-      const ChunkArgs b = fresh_args();
-      const uint2 item = b.items[at];
-      if (!reach_of(b, scalar(item.x), scalar(item.y), &g)) break;
-      g = scalar(g);
-      const uint32_t units = g.steps + kPieceCost, n = left < units - off ? left : units - off;
-      // its cost comes before its steps
-      const uint32_t t0 = off < kPieceCost ? 0 : off - kPieceCost, t1 = off + n < kPieceCost ? 0 : off + n - kPieceCost;
-      if (t0 < t1) {
-        const bool done = t0 == 0 && t1 == g.steps;
-        chunk_steps<T, F8, DP, W>(b, g, h, t0, t1, lds, acc, m, l);
+    const uint32_t q = blockIdx.x / a.H;
+    if (q < (uint32_t)a.head[0]) {
+      const uint4 piece = a.pieces[q];
+      if (reach_of(a, scalar(piece.x), scalar(piece.y), &g)) {
+        g = scalar(g);
+        chunk_steps<T, F8, DP, W>(a, g, h, scalar(piece.z), scalar(piece.w), lds, acc, m, l);
         const ChunkArgs e = fresh_args();
-        put(e, g, h, acc, m, l, done, 2ull * share + (t0 == 0 ? 1u : 0u));
-        // a row tile starts here and does not end: what is left of it is that of the shares behind
-        if (t0 == 0 && !done && threadIdx.x == 0)
-          e.open[share] = make_uint4(at, h, share + (uint32_t)((units - off - n + e.head[1] - 1) / e.head[1]), 1u);
+        put(e, g, h, acc, m, l, q >= (uint32_t)e.head[3], (uint64_t)q * e.H + h);
       }
-      left -= n;
-      off = 0;
-      if (left && ++at == (uint32_t)b.head[2]) at = 0, ++h;
     }
   }
   mk.end(ARGUS_REGION_CHUNK);
@@ -618,17 +714,16 @@ __global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : 2) void k_chunk(C
 
 template <int T, bool F8, int DP, int W>
 void launch_chunk_as(const ChunkArgs& a, uint32_t grid, hipStream_t st) {
-  if (a.shares) hipLaunchKernelGGL((k_chunk<T, F8, DP, W, true>), dim3(grid), dim3(64 * W), 0, st, a);
+  if (a.blocks) hipLaunchKernelGGL((k_chunk<T, F8, DP, W, true>), dim3(grid), dim3(64 * W), 0, st, a);
   else hipLaunchKernelGGL((k_chunk<T, F8, DP, W, false>), dim3(grid), dim3(64 * W), 0, st, a);
 }
 
-// Four waves a block, or eight that read the cache once for twice as many rows.
 template <int T, bool F8>
 void launch_chunk_type(const ChunkArgs& a, uint32_t grid, hipStream_t st) {
-  const bool eight = a.tile_shift == 8;
-  if (a.D <= 64) eight ? launch_chunk_as<T, F8, 64, 8>(a, grid, st) : launch_chunk_as<T, F8, 64, 4>(a, grid, st);
-  else if (a.D <= 128) eight ? launch_chunk_as<T, F8, 128, 8>(a, grid, st) : launch_chunk_as<T, F8, 128, 4>(a, grid, st);
-  else launch_chunk_as<T, F8, 256, 4>(a, grid, st);
+  if (a.D <= 64) launch_chunk_as<T, F8, 64, 4>(a, grid, st);
+  else if (a.D > 128) launch_chunk_as<T, F8, 256, 4>(a, grid, st);
+  else if (a.tile_shift == 8) launch_chunk_as<T, F8, 128, 8>(a, grid, st);
+  else launch_chunk_as<T, F8, 128, 4>(a, grid, st);
 }
 
 // One source file each, so that they compile side by side.

@@ -6,23 +6,35 @@ namespace argus {
 namespace prompt {
 namespace {
 
-// The shares of a batch, by one block. Units are steps, and kPieceCost more for each row tile,
-// of all row tiles one after the other, of one head after the other; share i has units i * per and on.
+// The batch in pieces, by one block: the items (row tiles) of a head, and those of more than `most` steps in
+// equal pieces, which are the first in the list: they take the longest. Heads come innermost, so
+// that with eight of them each has an XCD, in whose L2 its keys and values are.
+//
+// With U steps of n items and C blocks at a time, pieces of U / C steps would end together; cut from
+// items of any length they are up to n more. So some lengths for one and for two rounds of blocks are
+// tried, none but those whose pieces are as few, and the shortest way is taken: rounds times (length + what
+// a piece costs), and what joining costs, all in steps; or nothing is cut. Where there are more items than two
+// rounds of blocks take, those of more than 2 U / C steps are cut, and the longer of the others come first.
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+constexpr uint32_t kPlanItems = 4096, kPlanSplit = 1024;
+constexpr uint32_t kLeastPiece = 4, kItemCost = 2, kPieceCost = 8, kJoinCost = 8;
 __global__ __launch_bounds__(kPlanThreads) void k_chunk_plan(ChunkArgs a) {
   __shared__ uint64_t s_units[kPlanWaves];
-  __shared__ uint32_t s_items[kPlanWaves];
+  __shared__ uint32_t s_items[kPlanWaves], s_most[kPlanWaves], s_pieces[kPlanWaves], s_split[kPlanWaves], s_length[kPlanWaves], s_cost[kPlanWaves];
+  __shared__ uint32_t s_steps[kPlanItems];
+  __shared__ uint4 s_join[kPlanSplit];
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_CHUNK_PLAN);
-  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-  uint64_t units = 0;  // of all slots before
-  uint32_t items = 0;
+  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = scalar(tid >> 6);
+  uint64_t units = 0;
+  uint32_t items = 0, longest = 0;
+  // items in the order of their slots, the last first
   for (uint32_t x0 = 0; x0 < a.slots; x0 += kPlanThreads) {
-    const uint32_t x = x0 + tid;
+    const uint32_t x = a.slots - 1 - x0 - tid;
     Reach g;
     bool real = false;
-    uint32_t s = 0, first = 0, mine = 0;
-    if (x < a.slots) {
+    uint32_t s = 0, first = 0;
+    if (x0 + tid < a.slots) {
       uint32_t hi = a.S;
       while (hi - s > 1) {  // the last sequence whose slots start at or before x
         const uint32_t mid = (s + hi) / 2;
@@ -30,71 +42,139 @@ __global__ __launch_bounds__(kPlanThreads) void k_chunk_plan(ChunkArgs a) {
       }
       first = slot_of(a, s);
       real = first <= x && reach_of(a, s, x - first, &g);
-      if (real) mine = g.steps + kPieceCost;
     }
-    // (64 lanes of at most 2^26 units each)
-    uint64_t incl = mine;
+    const uint32_t mine = real ? g.steps : 0;
+    uint64_t sum = mine;
+    uint32_t most = mine;
     for (int d = 1; d < 64; d <<= 1) {
-      const uint64_t o = __shfl_up(incl, d);
-      if ((int)lane >= d) incl += o;
+      sum += __shfl_xor(sum, d);
+      const uint32_t o = __shfl_xor(most, d);
+      most = o > most ? o : most;
     }
     const uint64_t there = __ballot(real);
-    if (lane == 63) s_units[wave] = incl, s_items[wave] = (uint32_t)__popcll(there);
+    if (lane == 0) s_units[wave] = sum, s_items[wave] = (uint32_t)__popcll(there), s_most[wave] = most;
     __syncthreads();
-    uint64_t before = units;
     uint32_t at = items;
     for (uint32_t w = 0; w < (uint32_t)kPlanWaves; ++w) {
-      if (w < wave) before += s_units[w], at += s_items[w];
+      if (w < wave) at += s_items[w];
       units += s_units[w], items += s_items[w];
+      longest = s_most[w] > longest ? s_most[w] : longest;
     }
     if (real) {
       at += (uint32_t)__popcll(there & lanemask_lt());
-      a.items[at] = make_uint2(s, x - first);
-      a.cum[at] = before + incl - mine;
+      a.items[at] = make_uint4(s, x - first, mine, 0u);
+      if (at < kPlanItems) s_steps[at] = mine;
     }
     __syncthreads();
   }
-  uint64_t per = (units * a.H + a.shares - 1) / a.shares;
-  per = per < kMinShare ? kMinShare : per;
-  if (tid == 0) {
-    a.cum[items] = units;
-    a.head[0] = units, a.head[1] = per, a.head[2] = items;
+  auto steps_of = [&](uint32_t i) { return items <= kPlanItems ? s_steps[i] : a.items[i].z; };
+  // lengths of a piece: rounds 1 and 2, with room for none, half and all of the items' last pieces
+  const uint64_t all = units * a.H, blocks = a.blocks, heads = (uint64_t)items * a.H;
+  uint32_t length = longest, cost = ~0u;
+  if (wave < 6) {
+    const uint64_t rounds = wave / 3 + 1, room = rounds * blocks - (heads * (wave % 3)) / 2;
+    bool fits = rounds * blocks > heads && items;
+    if (fits) {
+      const uint64_t l = (all + room - 1) / room;
+      length = l < kLeastPiece ? kLeastPiece : l < longest ? (uint32_t)l : longest;
+      uint32_t pieces = 0;
+      for (uint32_t i = lane; i < items; i += 64) pieces += (steps_of(i) + length - 1) / length;
+      for (int d = 1; d < 64; d <<= 1) pieces += __shfl_xor(pieces, d);
+      fits = (uint64_t)pieces * a.H <= rounds * blocks;
+      if (fits) cost = (uint32_t)rounds * (length + kPieceCost) + kJoinCost;
+    }
+    if (lane == 0) s_length[wave] = length, s_cost[wave] = cost;
   }
   __syncthreads();
-  for (uint32_t i = tid; i < a.shares; i += kPlanThreads) {
-    const uint64_t u = i * per;
-    if (u >= units * a.H) {
-      a.start[i] = make_uint4(0u, 0u, 0u, 0u);
-      continue;
+  // nothing cut: no joining, and as many rounds as there are items for
+  uint32_t limit;  // steps of an item that is not cut, at most
+  length = longest, cost = ~0u;
+  if (heads > 2 * blocks) {
+    const uint64_t l = (all + blocks - 1) / blocks;
+    length = l < kLeastPiece ? kLeastPiece : l < longest ? (uint32_t)l : longest;
+    limit = 2 * length;
+  } else {
+    // (one round, or one after the other as blocks end)
+    cost = (heads > blocks ? (uint32_t)(all / blocks) + longest / 2 : longest) + kItemCost;
+    for (int w = 0; w < 6; ++w)
+      if (s_cost[w] < cost) cost = s_cost[w], length = s_length[w];
+    limit = length;
+  }
+  auto parts_of = [&](uint32_t steps) { return steps > limit ? (steps + length - 1) / length : 1u; };
+  // how many items are cut, and in how many pieces all of them
+  uint32_t cut = 0, parts = 0, longer = 0;
+  for (uint32_t i = tid; i < items; i += kPlanThreads) {
+    const uint32_t n = steps_of(i), k = parts_of(n);
+    if (k > 1) ++cut, parts += k;
+    else if (2 * n > longest) ++longer;
+  }
+  for (int d = 1; d < 64; d <<= 1) cut += __shfl_xor(cut, d), parts += __shfl_xor(parts, d), longer += __shfl_xor(longer, d);
+  if (lane == 0) s_split[wave] = cut, s_pieces[wave] = parts, s_items[wave] = longer;
+  __syncthreads();
+  cut = parts = longer = 0;
+  for (int w = 0; w < kPlanWaves; ++w) cut += s_split[w], parts += s_pieces[w], longer += s_items[w];
+  if (tid == 0) a.head[0] = parts + items - cut, a.head[1] = cut;
+  uint32_t cuts = 0, cut_parts = 0, longs = 0, others = 0;  // before
+  for (uint32_t i0 = 0; i0 < items; i0 += kPlanThreads) {
+    __syncthreads();
+    const uint32_t i = i0 + tid;
+    const uint4 item = i < items ? a.items[i] : make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t k = i < items ? parts_of(item.z) : 0;
+    const bool is_long = k == 1 && 2 * item.z > longest;
+    const uint64_t is_cut = __ballot(k > 1), are_long = __ballot(is_long), is_one = __ballot(k == 1 && !is_long);
+    uint32_t incl = k > 1 ? k : 0;
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t o = __shfl_up(incl, d);
+      if ((int)lane >= d) incl += o;
     }
-    const uint32_t h = (uint32_t)(u / units);
-    const uint64_t r = u - h * units;
-    uint32_t lo = 0, hi = items;
+    if (lane == 63) s_pieces[wave] = incl, s_split[wave] = (uint32_t)__popcll(is_cut), s_items[wave] = (uint32_t)__popcll(is_one), s_most[wave] = (uint32_t)__popcll(are_long);
+    __syncthreads();
+    uint32_t part = cut_parts, j = cuts, one = others, lng = longs;
+    for (uint32_t w = 0; w < (uint32_t)kPlanWaves; ++w) {
+      if (w < wave) part += s_pieces[w], j += s_split[w], one += s_items[w], lng += s_most[w];
+      cut_parts += s_pieces[w], cuts += s_split[w], others += s_items[w], longs += s_most[w];
+    }
+    if (k > 1) {
+      const uint4 join = make_uint4(item.x, item.y, part + incl - k, item.z);
+      j += (uint32_t)__popcll(is_cut & lanemask_lt());
+      a.joins[j] = join;
+      s_join[j] = join;
+    } else if (k == 1) {
+      const uint32_t q = parts + (is_long ? lng + (uint32_t)__popcll(are_long & lanemask_lt())
+                                          : longer + one + (uint32_t)__popcll(is_one & lanemask_lt()));
+      a.pieces[q] = make_uint4(item.x, item.y, 0u, item.z);
+    }
+  }
+  __syncthreads();
+  for (uint32_t q = tid; q < parts; q += kPlanThreads) {
+    uint32_t lo = 0, hi = cut;
     while (hi - lo > 1) {
       const uint32_t mid = (lo + hi) / 2;
-      if (a.cum[mid] <= r) lo = mid; else hi = mid;
+      if (s_join[mid].z <= q) lo = mid; else hi = mid;
     }
-    const uint64_t left = units * a.H - u;
-    a.start[i] = make_uint4(lo, h, (uint32_t)(r - a.cum[lo]), (uint32_t)(left < per ? left : per));
+    const uint4 join = s_join[lo];
+    const uint32_t k = (join.w + length - 1) / length, len = (join.w + k - 1) / k, t0 = (q - join.z) * len;
+    a.pieces[q] = make_uint4(join.x, join.y, t0, t0 + len < join.w ? t0 + len : join.w);
   }
+  if (tid == 0) a.head[2] = length, a.head[3] = parts;
   mk.end(ARGUS_REGION_CHUNK_PLAN);
 }
 
-// Rows of a row tile that was left in pieces: piece 0 is the second of its first share, piece i the
-// first of share i further on.
+// Rows of an item that was left in pieces. A block takes kRows of them at a time.
 template <int T, int DP, int W>
 __global__ __launch_bounds__(kThreads) void k_chunk_join(ChunkArgs a) {
   constexpr uint32_t kQuads = DP / 4, kRows = kThreads / kQuads, TR = 32 * W;
   using Hf = Half<T>;
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_CHUNK_JOIN);
-  const uint4 open = a.open[blockIdx.x];
+  const uint32_t j = blockIdx.x / a.H, h = blockIdx.x % a.H;
   Reach g;
-  if (open.w && blockIdx.y * kRows < TR) {
-    const uint2 item = a.items[open.x];
-    const uint32_t h = open.y, n = open.z - blockIdx.x + 1;
-    const uint32_t mine = blockIdx.y * kRows + threadIdx.x / kQuads, d = threadIdx.x % kQuads * 4;
-    if (reach_of(a, item.x, item.y, &g) && mine < g.rows) {
+  if (j < (uint32_t)a.head[1]) {
+    const uint4 join = a.joins[j];
+    const uint32_t length = (uint32_t)a.head[2], n = (join.w + length - 1) / length;
+    const bool real = reach_of(a, join.x, join.y, &g);
+    const uint32_t d = threadIdx.x % kQuads * 4;
+    for (uint32_t mine = blockIdx.y * kRows + threadIdx.x / kQuads; real && mine < g.rows; mine += gridDim.y * kRows) {
       float m = -INFINITY, l = 0.0f;
       f32x4 o = (f32x4)(0.0f);
       constexpr uint32_t kDeep = 8;
@@ -103,22 +183,21 @@ __global__ __launch_bounds__(kThreads) void k_chunk_join(ChunkArgs a) {
         f32x4 v[kDeep];
         float top = m;
 #pragma unroll
-        for (uint32_t j = 0; j < kDeep; ++j) {
-          const uint32_t i = i0 + j < n ? i0 + j : 0;
-          const uint64_t x = (2ull * (blockIdx.x + i) + (i == 0 ? 1u : 0u)) * TR + mine;
-          ml[j] = *reinterpret_cast<const f32x2*>(a.part_ml + 2 * x);
-          v[j] = *reinterpret_cast<const f32x4*>(a.part_o + x * DP + d);
-          if (i0 + j >= n) ml[j] = (f32x2){-INFINITY, 0.0f}, v[j] = (f32x4)(0.0f);
-          top = fmaxf(top, ml[j].x);
+        for (uint32_t i = 0; i < kDeep; ++i) {
+          const uint64_t x = ((uint64_t)(join.z + (i0 + i < n ? i0 + i : 0)) * a.H + h) * TR + mine;
+          ml[i] = *reinterpret_cast<const f32x2*>(a.part_ml + 2 * x);
+          v[i] = *reinterpret_cast<const f32x4*>(a.part_o + x * DP + d);
+          if (i0 + i >= n) ml[i] = (f32x2){-INFINITY, 0.0f}, v[i] = (f32x4)(0.0f);
+          top = fmaxf(top, ml[i].x);
         }
         const float keep = m == -INFINITY ? 1.0f : exp_of(m - top);  // (nothing yet, or NaN)
         l *= keep;
         o *= keep;
 #pragma unroll
-        for (uint32_t j = 0; j < kDeep; ++j) {
-          const float w = ml[j].x == -INFINITY ? 1.0f : exp_of(ml[j].x - top);  // a maximum of -inf: zeros, or NaN
-          l += ml[j].y * w;
-          o += v[j] * w;
+        for (uint32_t i = 0; i < kDeep; ++i) {
+          const float w = ml[i].x == -INFINITY ? 1.0f : exp_of(ml[i].x - top);  // a maximum of -inf: zeros, or NaN
+          l += ml[i].y * w;
+          o += v[i] * w;
         }
         m = top;
       }
@@ -139,8 +218,7 @@ void launch_chunk_join(const ChunkArgs& a, dim3 g, hipStream_t st) {
   const dim3 b(kThreads);
   const bool eight = a.tile_shift == 8;
   if (a.D <= 64) {
-    if (eight) hipLaunchKernelGGL((k_chunk_join<T, 64, 8>), g, b, 0, st, a);
-    else hipLaunchKernelGGL((k_chunk_join<T, 64, 4>), g, b, 0, st, a);
+    hipLaunchKernelGGL((k_chunk_join<T, 64, 4>), g, b, 0, st, a);
   } else if (a.D <= 128) {
     if (eight) hipLaunchKernelGGL((k_chunk_join<T, 128, 8>), g, b, 0, st, a);
     else hipLaunchKernelGGL((k_chunk_join<T, 128, 4>), g, b, 0, st, a);
@@ -149,15 +227,27 @@ void launch_chunk_join(const ChunkArgs& a, dim3 g, hipStream_t st) {
   }
 }
 
-
-// Blocks that share a batch: as many as run at once, two on a compute unit (one at head sizes
-// beyond 128).
-uint32_t share_count(uint32_t tile_shift, uint32_t head_dim) { return head_dim > 128 || tile_shift == 8 ? 256u : 512u; }
-constexpr uint32_t kWholeSteps = 8;
+// Eight waves a block, that read the cache once for 256 rows, or four. Eight where sequences have so many
+// rows on the average, and there are so many tiles of them (4 prompts in chunks over 8 bits 1350 us against 1463 with
+// four, one of 16384 tokens 4.12 ms against 4.46; 16 prompts of up to 2000 tokens, 8 x 4 heads, 103 us against
+// 107), else four (proposals over 131000 tokens 342 us against 390 with eight, a batch of single tokens and
+// chunks 168 against 172, one prompt of 512 tokens 20.4 against 22.9, of 2048, 8 x 4 heads, 59.5 against 62.2; the
+// other way round is one of 512 over 8192 in the cache, 190 against 177: what is in the cache is not known
+// here), and at head size 64, whose blocks of four run three at a time on a compute unit (4 prompts of up to
+// 4000 tokens 158 us against 186 with eight).
+constexpr uint32_t kManyRows = 1024, kManyTiles = 512;
+// Blocks that run at once.
+uint32_t blocks_at_once(uint32_t tile_shift, uint32_t head_dim) {
+  return 256u * (head_dim > 128 || tile_shift == 8 ? 1 : head_dim > 64 ? 2 : 3);
+}
+// Row tiles of at most so many steps are not cut, and are found by their blocks: no plan and no joining (a
+// prompt of 2048 tokens 69.6 us against 74.4).
+constexpr uint32_t kWholeSteps = 32;
+constexpr uint32_t kJoinBlocks = 8;  // of an item, for its rows
 
 struct Plan {
-  uint32_t tile_shift, slots, grid, shares, joins, join_rows;
-  size_t ml_at, o_at, open_at, start_at, items_at, cum_at, bytes;
+  uint32_t tile_shift, slots, grid, blocks, joins;
+  size_t ml_at, o_at, items_at, joins_at, pieces_at, bytes;
 };
 
 int make_plan(const argus_chunk_config* c, Plan* p) {
@@ -178,7 +268,10 @@ int make_plan(const argus_chunk_config* c, Plan* p) {
   if (c->num_pages < 1 || c->num_pages > 0x7FFFFFFFu || c->columns < 1 ||
       (uint64_t)c->columns * c->page_size > 0x3FFFFFFFull || c->window > 0x3FFFFFFFu || c->sinks > 0x3FFFFFFFu)
     return refuse(ARGUS_E_CAPACITY, "pages, columns, window or sinks out of range");
-  p->tile_shift = c->head_dim > 128 ? 7 : 8;
+  const uint64_t rows = (uint64_t)c->rows * c->group;
+  p->tile_shift = c->head_dim > 64 && c->head_dim <= 128 && rows >= (uint64_t)kManyRows * c->seqs &&
+                          rows / 256 * c->kv_heads >= kManyTiles
+                      ? 8 : 7;
   p->slots = c->seqs ? ((c->rows * c->group) >> p->tile_shift) + c->seqs : 0;
   const uint64_t tiles = (uint64_t)p->slots * c->kv_heads;
   const uint32_t kt = c->head_dim > 128 ? 32 : 64, dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
@@ -188,25 +281,21 @@ int make_plan(const argus_chunk_config* c, Plan* p) {
     const uint64_t w = (c->window + (1u << p->tile_shift) / c->group + 2 * kt) / kt + 1 + (c->sinks + kt - 1) / kt;
     steps = w < steps ? w : steps;
   }
-  p->shares = 0;
-  if (tiles && c->rows && (steps > kWholeSteps || tiles > kMaxBlocks)) {
-    // (units of a share are counted in 32 bits)
-    if (tiles * (steps + kPieceCost) >= 1ull << 40) return refuse(ARGUS_E_CAPACITY, "rows x heads x tokens");
-    const uint64_t useful = tiles * (steps + kPieceCost) / kMinShare + 1;
-    p->shares = share_count(p->tile_shift, c->head_dim);
-    p->shares = useful < p->shares ? (uint32_t)useful : p->shares;
-  }
-  p->grid = p->shares ? p->shares : (uint32_t)tiles;
-  p->join_rows = (1u << p->tile_shift) * dp / 4 / kThreads;
-  p->joins = p->shares * p->join_rows;
-  const size_t rows = (size_t)p->shares * 2 << p->tile_shift;
+  p->blocks = tiles && c->rows && (steps > kWholeSteps || tiles > kMaxBlocks) ? blocks_at_once(p->tile_shift, c->head_dim) : 0;
+  // At most two pieces for each block that runs at once are of items that were cut, and so few more than
+  // the items are all pieces.
+  const uint64_t most = p->slots + 2 * p->blocks / c->kv_heads + 1, grid = p->blocks ? most * c->kv_heads : tiles;
+  if (grid > kMaxBlocks) return refuse(ARGUS_E_CAPACITY, "rows x heads");
+  p->grid = (uint32_t)grid;
+  const uint32_t cut = p->slots < p->blocks / c->kv_heads ? p->slots : p->blocks / c->kv_heads;
+  p->joins = p->blocks ? cut * c->kv_heads : 0;
+  const size_t part_rows = (size_t)2 * p->blocks << p->tile_shift;
   p->ml_at = 256;
-  p->o_at = p->ml_at + up256(rows * 2 * sizeof(float));
-  p->open_at = p->o_at + up256(rows * dp * sizeof(float));
-  p->start_at = p->open_at + up256((size_t)p->shares * 16);
-  p->items_at = p->start_at + up256((size_t)p->shares * 16);
-  p->cum_at = p->items_at + up256((size_t)p->slots * 8);
-  p->bytes = p->shares ? p->cum_at + up256(((size_t)p->slots + 1) * 8) : 0;
+  p->o_at = p->ml_at + up256(part_rows * 2 * sizeof(float));
+  p->items_at = p->o_at + up256(part_rows * dp * sizeof(float));
+  p->joins_at = p->items_at + up256((size_t)p->slots * 16);
+  p->pieces_at = p->joins_at + up256((size_t)(cut + 1) * 16);
+  p->bytes = p->blocks ? p->pieces_at + up256(most * 16) : 0;
   return ARGUS_OK;
 }
 
@@ -248,8 +337,8 @@ extern "C" int argus_prompt_attend(const argus_chunk_config* cfg, const argus_ch
   if (p.bytes && !aligned_to(d_workspace, 256)) return refuse(ARGUS_E_ALIGN, "the workspace lies on 256 bytes");
   if (workspace_bytes < p.bytes)
     return refuse(ARGUS_E_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
-  const uint64_t plans = p.shares ? kPlanThreads / kThreads : 0;
-  const uint64_t records = (p.grid + plans + p.joins) * 2 * kWaves;
+  const uint64_t plans = p.blocks ? kPlanThreads / kThreads : 0, waves = p.tile_shift == 8 ? 2 : 1;
+  const uint64_t records = (p.grid * waves + plans + (uint64_t)p.joins * kJoinBlocks) * 2 * kWaves;
   if (!marks_fit(markers, records)) return refuse(ARGUS_E_CAPACITY, "%llu marker records do not fit", (unsigned long long)records);
   if (cfg->seqs == 0 || cfg->rows == 0) return ARGUS_OK;
   if ((rc = device_ok()) != ARGUS_OK) return rc;
@@ -271,22 +360,21 @@ extern "C" int argus_prompt_attend(const argus_chunk_config* cfg, const argus_ch
   a.by_group = fast_div(cfg->group);
   a.scale = cfg->scale;
   hipStream_t st = (hipStream_t)stream_v;
-  a.shares = p.shares;
-  if (p.shares) {
+  a.blocks = p.blocks;
+  if (p.blocks) {
     char* ws = (char*)d_workspace;
     a.head = (uint64_t*)ws;
     a.part_ml = (float*)(ws + p.ml_at), a.part_o = (float*)(ws + p.o_at);
-    a.open = (uint4*)(ws + p.open_at), a.start = (uint4*)(ws + p.start_at);
-    a.items = (uint2*)(ws + p.items_at), a.cum = (uint64_t*)(ws + p.cum_at);
+    a.items = (uint4*)(ws + p.items_at), a.joins = (uint4*)(ws + p.joins_at), a.pieces = (uint4*)(ws + p.pieces_at);
     a.marks = take_marks(markers, plans, 2);
     hipLaunchKernelGGL(k_chunk_plan, dim3(1), dim3(kPlanThreads), 0, st, a);
   }
-  a.marks = take_marks(markers, p.grid, 2);
+  a.marks = take_marks(markers, p.grid * waves, 2);
   const bool f8 = cfg->cache_type == ARGUS_FP8, bf = cfg->q_type == ARGUS_BF16;
   (f8 ? (bf ? launch_chunk_bf16_f8 : launch_chunk_fp16_f8) : (bf ? launch_chunk_bf16 : launch_chunk_fp16))(a, p.grid, st);
-  if (p.shares) {
-    a.marks = take_marks(markers, p.joins, 2);
-    (bf ? launch_chunk_join<0> : launch_chunk_join<1>)(a, dim3(p.shares, p.join_rows), st);
+  if (p.joins) {
+    a.marks = take_marks(markers, (uint64_t)p.joins * kJoinBlocks, 2);
+    (bf ? launch_chunk_join<0> : launch_chunk_join<1>)(a, dim3(p.joins, kJoinBlocks), st);
   }
   return hipGetLastError() == hipSuccess ? ARGUS_OK : refuse(ARGUS_E_HIP, "launch failed");
 }
