@@ -9,10 +9,20 @@
 // rises (S' = S e^m, T' = (T + m S) e^m, m <= 0 the old maximum less the new one); lanes, waves and parts
 // are joined in the same way, in a fixed order.
 //
-// A block reads a part of a row, its four waves 64 lanes of 32 elements in turn, the next
-// ones under way while it looks at them. The rank is a count of what is above the given token's own
-// logit, read first. The alternatives are kept as selection over beams keeps its candidates: a list in LDS
-// for each wave, with a least value that rises as the list is cut to its first.
+// A block reads a part of a row, its four waves 64 lanes of 32 elements in turn. The next ones' loads go out once
+// these are in 32 bits and looked through for the maximum; the rest is done while they are under way, five to seven waves
+// on a SIMD (two sets of registers for them, three or four waves: 137 us where this takes 108). The rank is a count of what is above the given token's own
+// logit, read first. The k best are among what is not below the k-th largest of the block's 256 lanes' maxima,
+// whichever elements the lanes have seen: that bound is worked out after the first step of
+// each wave and again when a wave has seen twice as much, from what the others have noted by then. What is not below
+// it goes to a list of the wave in LDS, and the rest of the work is a few steps over some k candidates.
+//
+// What bounds it: reading the logits, and nearly as much the arithmetic, 7.5 instructions an element (the exponential
+// counts twice). Where a clamp is needed for minus infinities it is an eighth: steps go without until a sum
+// becomes NaN, and ranks are counted by the scalar unit. 2048 rows of 128003 in bf16 with 20 alternatives take 108 us,
+// 4.8 TB/s (a list of its own bound for each wave, a rank in each lane and a clamp of two instructions 143); 500 rows of
+// 65537 in 32 bits, some of it minus infinity, 26 us, 5.0 TB/s; one row of 32000, 5 alternatives, 14 us, two
+// launches.
 #include "prompt.h"
 #include "rows.h"
 
@@ -23,7 +33,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint32_t kItems = 32;       // elements of a lane per step
 constexpr uint32_t kStep = kItems * 64;
-constexpr uint32_t kList = 192, kRoom = 8;  // candidates of a wave; beyond its k, before it is cut
+constexpr uint32_t kList = 192;       // candidates of a wave
 constexpr uint32_t kMaxTop = 64;
 constexpr uint32_t kCands = 512;      // of the parts of a row, ranked by counting
 
@@ -65,6 +75,16 @@ ARGUS_DEV void join(Sums& a, Sums b) {
   move(b, to);
   a.s += b.s, a.t += b.t, a.above += b.above;
 }
+// A wave's, in all lanes.
+ARGUS_DEV void join_lanes(Sums& a) {
+  float to = a.top;
+  for (int d = 1; d < 64; d <<= 1) to = fmaxf(to, __shfl_xor(to, d));
+  move(a, to);
+  for (int d = 1; d < 64; d <<= 1) {
+    a.s += __shfl_xor(a.s, d), a.t += __shfl_xor(a.t, d);
+    a.above += (uint32_t)__shfl_xor((int)a.above, d);
+  }
+}
 
 // A row's numbers, once its sums are known. `lane`: of those that write its alternatives.
 struct Row {
@@ -102,6 +122,7 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
   constexpr uint32_t kBytes = TYPE == ARGUS_FP32 ? 4 : 2, kPer = 16 / kBytes, kVecs = kItems / kPer;
   __shared__ uint64_t s_list[TOP ? kWaves : 1][TOP ? kList : 1];
   __shared__ u32x4 s_step[TOP ? kWaves : 1][TOP ? kVecs * 64 : 1];
+  __shared__ float s_tops[TOP ? kThreads : 1];  // the lanes' maxima
   __shared__ Sums s_sums[kWaves];
   __shared__ uint32_t s_n[kWaves];
   WaveMarks mk(a.marks);
@@ -113,6 +134,8 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
   const int32_t token = a.tokens[row];
   const bool known = (uint32_t)token < a.V;
   const float mine = known ? element<TYPE>(base, (uint32_t)token) : INFINITY;
+  // the least number above it (what is as large and comes behind the token is not above)
+  const float beyond = value_of(order_of(mine) + 1);
   // Vectors lie on 16 bytes: `head` elements come before the first of `vecs`
   // vectors, less than a vector behind the last.
   uint32_t head = (uint32_t)(0 - (uintptr_t)base & 15u) / kBytes;
@@ -121,16 +144,25 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
   const u32x4* body = reinterpret_cast<const u32x4*>(base + head * kBytes);
   const uint32_t all = (vecs + kVecs * 64 - 1) / (kVecs * 64);
   const uint32_t end = (part + 1) * a.steps < all ? (part + 1) * a.steps : all;
-  auto load = [&](uint32_t step, u32x4 (&w)[kVecs]) {
-    const uint32_t v0 = step * kVecs * 64 + lane;
+  u32x4 w[kVecs];  // the step's that is looked at, then the next one's
+  auto load = [&](uint32_t step) {
+    const uint32_t v0 = step * kVecs * 64;
+    if (__builtin_expect(v0 + kVecs * 64 <= vecs, 1)) {
+      const u32x4* from = body + v0;
 #pragma unroll
-    for (uint32_t v = 0; v < kVecs; ++v) w[v] = __builtin_nontemporal_load(&body[v0 + v * 64 < vecs ? v0 + v * 64 : vecs - 1]);
+      for (uint32_t v = 0; v < kVecs; ++v) w[v] = __builtin_nontemporal_load(&from[lane + v * 64]);
+    } else {
+#pragma unroll
+      for (uint32_t v = 0; v < kVecs; ++v)
+        w[v] = __builtin_nontemporal_load(&body[v0 + lane + v * 64 < vecs ? v0 + lane + v * 64 : vecs - 1]);
+    }
   };
   Sums my{-INFINITY, 0.0f, 0.0f, 0u};
-  auto add = [&](float x) {  // (a NaN of x goes on, a d of -inf has no part)
-    const float d = x - (my.top == -INFINITY ? 0.0f : my.top), e = power(d);
+  uint32_t above = 0;  // of the wave's elements
+  auto add = [&](float x, float base) {  // (a NaN of x goes on in s, a d of -inf has no part)
+    const float d = x - base, e = power(d);
     my.s += e;
-    my.t += e * (d < -128.0f ? -128.0f : d);
+    my.t += e * fmaxf(d, -128.0f);
   };
   // the wave's list
   uint64_t* list = s_list[TOP ? wave : 0];
@@ -174,8 +206,26 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
     if (want) list[n + (uint32_t)__popcll(take & lanemask_lt())] = key;
     n += (uint32_t)__popcll(take);
   };
-  bool first = true;
-  auto look = [&](uint32_t step, const u32x4 (&w)[kVecs]) {
+  // The k-th largest of the lanes' maxima, for 16-bit logits in its upper 16 bits: the largest number that k of them
+  // are not below. What other waves note meanwhile may count or not.
+  auto raise = [&]() {
+    uint32_t its[kWaves], v = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      its[w] = order_of(__hip_atomic_load(&s_tops[w * 64 + lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
+#pragma unroll 1
+    for (uint32_t bit = 1u << 31; bit >= (kBytes == 4 ? 1u : 1u << 16); bit >>= 1) {
+      uint32_t many = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) many += (uint32_t)__popcll(__ballot(its[w] >= (v | bit)));
+      v = many >= a.K ? v | bit : v;
+    }
+    const uint64_t bound = join64(0u, v);  // below every key of this value
+    if (v > order_of(-INFINITY) && bound > least) least = bound, least_value = value_of(v);
+  };
+  uint32_t seen = 0, next = 4;  // steps of the wave; when the bound is worked out again
+  bool holes = false;  // minus infinities have been seen
+  auto look = [&](uint32_t step) {
     float x[kItems];
 #pragma unroll
     for (uint32_t i = 0; i < kItems; ++i) x[i] = of_word<TYPE>(w[i / kPer][(i % kPer) * kBytes / 4], i % (4 / kBytes));
@@ -188,59 +238,76 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
     float top = x[0];
 #pragma unroll
     for (uint32_t i = 1; i < kItems; ++i) top = fmaxf(top, x[i]);
-    if (__any(top > my.top)) move(my, fmaxf(my.top, top));
-#pragma unroll
-    for (uint32_t i = 0; i < kItems; ++i) add(x[i]);
-    // those above the token's logit; as large, and before it
-    const uint32_t e0 = head + step * kVecs * 64 * kPer, e1 = e0 + kVecs * 64 * kPer;
-    if ((uint32_t)token >= e1 && !last) {
-#pragma unroll
-      for (uint32_t i = 0; i < kItems; ++i) my.above += x[i] >= mine;
-    } else if ((uint32_t)token < e0 && !last) {
-#pragma unroll
-      for (uint32_t i = 0; i < kItems; ++i) my.above += x[i] > mine;
-    } else {
-#pragma unroll
-      for (uint32_t i = 0; i < kItems; ++i)
-        my.above += v0 + i / kPer * 64 < vecs &&
-                    (x[i] > mine || (x[i] == mine && head + (v0 + i / kPer * 64) * kPer + i % kPer < (uint32_t)token));
+    if (__any(top > my.top)) {
+      move(my, fmaxf(my.top, top));
+      if constexpr (TOP) __hip_atomic_store(&s_tops[tid], my.top, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
+    uint64_t hot = 0;
     if constexpr (TOP) {
-      if (first) {
-        // the k-th largest of the lanes' maxima: the least that fewer than k are above
-        first = false;
-        const uint32_t its = order_of(top);
-        uint32_t above = 0;
-#pragma unroll 16
-        for (int i = 0; i < 64; ++i) above += (uint32_t)__builtin_amdgcn_readlane((int)its, i) > its;
-        const uint32_t lo = ~wave_max_u32(above < a.K ? ~its : 0u);
-        const uint64_t bound = join64(0u, lo);  // below every key of this value
-        if (bound > least) least = bound, least_value = value_of(lo);
+      if (++seen == next) {
+        next *= 4;
+        raise();
       }
-      uint64_t hot = __ballot(top >= least_value && top > -INFINITY);
+      hot = __ballot(top >= least_value && top > -INFINITY);
       if (hot) {
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (uint32_t v = 0; v < kVecs; ++v) s_step[wave][v * 64 + lane] = w[v];
         __builtin_amdgcn_wave_barrier();
-        // two lanes' 32 elements at a time
-        while (hot) {
-          if (n > kList - 64) cut();
-          const uint32_t l0 = (uint32_t)__builtin_ctzll(hot);
-          hot &= hot - 1;
-          const uint32_t l1 = hot ? (uint32_t)__builtin_ctzll(hot) : l0;
-          const bool in = lane < kItems || l1 != l0;
-          hot &= hot - 1;
-          const uint32_t i = lane % kItems, at = (i / kPer) * 64 + (lane < kItems ? l0 : l1);
-          float y;
-          if constexpr (TYPE == ARGUS_FP32) y = reinterpret_cast<const any_f32*>(&s_step[wave][at])[i % kPer];
-          else y = of_word<TYPE>(reinterpret_cast<const any_u16*>(&s_step[wave][at])[i % kPer], 0);
-          const uint32_t tok = head + (step * kVecs * 64 + at) * kPer + i % kPer;
-          const uint64_t key = key_of(y, tok);
-          const bool there = step * kVecs * 64 + at < vecs;
-          append(in && there && y >= least_value && key > least && y > -INFINITY, key);
-        }
-        if (n > a.K + kRoom) cut();
+      }
+    }
+    if (step + kWaves < end) load(step + kWaves);
+    float base = my.top == -INFINITY ? 0.0f : my.top;
+    const float s0 = my.s, t0 = my.t;
+    if (!holes) {
+#pragma unroll
+      for (uint32_t i = 0; i < kItems; ++i) {
+        const float d = x[i] - base, e = power(d);
+        my.s += e;
+        my.t += e * d;
+        if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+      }
+      holes = __any(my.t != my.t);  // 0 times infinity
+      if (holes) my.s = s0, my.t = t0;
+    }
+    if (holes) {
+      asm volatile("" : "+v"(base));  // (worked out anew: kept from above, it would take 64 registers)
+#pragma unroll
+      for (uint32_t i = 0; i < kItems; ++i) {
+        add(x[i], base);
+        if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    // those above the token's logit; as large, and before it
+    const uint32_t e0 = head + step * kVecs * 64 * kPer, e1 = e0 + kVecs * 64 * kPer;
+    if (((uint32_t)token >= e1 || (uint32_t)token < e0) && !last) {
+      const float from = (uint32_t)token < e0 ? beyond : mine;
+#pragma unroll
+      for (uint32_t i = 0; i < kItems; ++i) above += (uint32_t)__popcll(__ballot(x[i] >= from));
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < kItems; ++i)
+        above += (uint32_t)__popcll(__ballot(
+            v0 + i / kPer * 64 < vecs &&
+            (x[i] > mine || (x[i] == mine && head + (v0 + i / kPer * 64) * kPer + i % kPer < (uint32_t)token))));
+    }
+    if constexpr (TOP) {
+      // two lanes' 32 elements at a time
+      while (hot) {
+        if (n > kList - 64) cut();
+        const uint32_t l0 = (uint32_t)__builtin_ctzll(hot);
+        hot &= hot - 1;
+        const uint32_t l1 = hot ? (uint32_t)__builtin_ctzll(hot) : l0;
+        const bool in = lane < kItems || l1 != l0;
+        hot &= hot - 1;
+        const uint32_t i = lane % kItems, at = (i / kPer) * 64 + (lane < kItems ? l0 : l1);
+        float y;
+        if constexpr (TYPE == ARGUS_FP32) y = reinterpret_cast<const any_f32*>(&s_step[wave][at])[i % kPer];
+        else y = of_word<TYPE>(reinterpret_cast<const any_u16*>(&s_step[wave][at])[i % kPer], 0);
+        const uint32_t tok = head + (step * kVecs * 64 + at) * kPer + i % kPer;
+        const uint64_t key = key_of(y, tok);
+        const bool there = step * kVecs * 64 + at < vecs;
+        append(in && there && y >= least_value && key > least && y > -INFINITY, key);
       }
     }
   };
@@ -249,68 +316,72 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
     const bool in = lane < kPer ? j < head : lane < 2 * kPer && j < a.V;
     const float x = in ? element<TYPE>(base, j) : -INFINITY;
     if (x > -INFINITY) my.top = x;
-    if (in) add(x);
-    my.above += in && (x > mine || (x == mine && j < (uint32_t)token));
+    if (in) add(x, my.top == -INFINITY ? 0.0f : my.top);
+    above += (uint32_t)__popcll(__ballot(in && (x > mine || (x == mine && j < (uint32_t)token))));
     if constexpr (TOP) append(x > -INFINITY, key_of(x, j));
   }
-  u32x4 w0[kVecs], w1[kVecs];
   uint32_t step = part * a.steps + wave;
-  if (step < end) {
-    load(step, w0);
-    for (; step + kWaves < end; step += 2 * kWaves) {
-      load(step + kWaves, w1);
-      look(step, w0);
-      load(step + 2 * kWaves < end ? step + 2 * kWaves : step, w0);
-      look(step + kWaves, w1);
+  if (step < end) load(step);
+  if constexpr (TOP) {
+    float top = my.top;
+    if (step < end) {
+      const bool last = (step + 1) * kVecs * 64 > vecs;
+#pragma unroll
+      for (uint32_t i = 0; i < kItems; ++i) {
+        const float x = of_word<TYPE>(w[i / kPer][(i % kPer) * kBytes / 4], i % (4 / kBytes));
+        top = !last || step * kVecs * 64 + lane + i / kPer * 64 < vecs ? fmaxf(top, x) : top;
+      }
     }
-    if (step < end) look(step, w0);
+    s_tops[tid] = top;
+    __syncthreads();
+    raise();
   }
-#pragma unroll 1
-  for (int d = 1; d < 64; d <<= 1)
-    join(my, Sums{__shfl_xor(my.top, d), __shfl_xor(my.s, d), __shfl_xor(my.t, d), (uint32_t)__shfl_xor((int)my.above, d)});
-  if constexpr (TOP) cut();
-  if (lane == 0) {
-    s_sums[wave] = my;
-    s_n[wave] = n;
-  }
+  for (; step < end; step += kWaves) look(step);
+  join_lanes(my);
+  if (lane == 0) s_sums[wave] = Sums{my.top, my.s, my.t, above};
   __syncthreads();
-  Sums sum = s_sums[0];
-#pragma unroll 1
-  for (int w = 1; w < kWaves; ++w) join(sum, s_sums[w]);
-  if (a.parts == 1) {
-    const Row r = row_of(sum);
-    if (tid == 0) put_row(a, row, r, sum.above, token, mine);
-    if constexpr (TOP) {
-      // a wave's candidates are in order: those of the others that are above one of them
-      uint32_t total = 0;
-      for (int w = 0; w < kWaves; ++w) total += s_n[w];
-      if (lane < n) {
-        const uint64_t key = list[lane];
-        uint32_t above = lane;
-        for (int w = 0; w < kWaves; ++w) {
-          if (w == (int)wave) continue;
-          for (uint32_t i = 0; i < s_n[w]; ++i) above += s_list[w][i] > key;
-        }
-        if (above < a.K) put_top(a, row, r, above, key);
-      }
-      for (uint32_t i = total + tid; i < a.K; i += kThreads) put_top(a, row, r, i, 0);
+  Sums sum = lane < kWaves ? s_sums[lane] : Sums{-INFINITY, 0.0f, 0.0f, 0u};
+  join_lanes(sum);
+  const Row r = row_of(sum);
+  if (tid == 0) {
+    if (a.parts == 1) put_row(a, row, r, sum.above, token, mine);
+    else a.sums[blockIdx.x] = sum;
+  }
+  if constexpr (TOP) {
+    // what the whole block's bound leaves, 64 of a wave at most; a candidate's place is the number of those above it
+    raise();
+    uint32_t kept = 0;
+    for (uint32_t i = 0; i < n; i += 64) {
+      const uint64_t key = i + lane < n ? list[i + lane] : 0;
+      const bool keep = key && key >= least;  // (the k-th of a list that was cut is its least)
+      const uint64_t take = __ballot(keep);
+      __builtin_amdgcn_wave_barrier();
+      if (keep) list[kept + (uint32_t)__popcll(take & lanemask_lt())] = key;
+      kept += (uint32_t)__popcll(take);
     }
-  } else {
-    if (tid == 0) a.sums[blockIdx.x] = sum;
-    if constexpr (TOP) {
-      uint64_t* to = a.cands + (uint64_t)blockIdx.x * a.K;
-      uint32_t total = 0;
-      for (int w = 0; w < kWaves; ++w) total += s_n[w];
-      if (lane < n) {
-        const uint64_t key = list[lane];
-        uint32_t above = lane;
-        for (int w = 0; w < kWaves; ++w) {
-          if (w == (int)wave) continue;
-          for (uint32_t i = 0; i < s_n[w]; ++i) above += s_list[w][i] > key;
-        }
-        if (above < a.K) to[above] = key;
+    n = kept;
+    if (n > 64) cut();
+    if (lane == 0) s_n[wave] = n;
+    __syncthreads();
+    uint32_t total = 0;
+    for (int w = 0; w < kWaves; ++w) total += s_n[w];
+    uint64_t* to = a.cands + (uint64_t)blockIdx.x * a.K;
+    if (lane < n) {
+      const uint64_t key = list[lane];
+      uint32_t place = 0;
+      for (int w = 0; w < kWaves; ++w) {
+        const uint32_t many = s_n[w];
+#pragma unroll 8
+        for (uint32_t i = 0; i < many; ++i) place += s_list[w][i] > key;
       }
-      for (uint32_t i = total + tid; i < a.K; i += kThreads) to[i] = 0;
+      if (place < a.K) {
+        if (a.parts == 1) put_top(a, row, r, place, key);
+        else to[place] = key;
+      }
+    }
+    for (uint32_t i = total + tid; i < a.K; i += kThreads) {
+      if (a.parts == 1) put_top(a, row, r, i, 0);
+      else to[i] = 0;
     }
   }
   mk.end(ARGUS_REGION_SCORE_ROWS);
@@ -327,9 +398,7 @@ __global__ __launch_bounds__(kThreads) void k_score_join(ScoreArgs a) {
   for (uint32_t i = tid; i < total; i += kThreads) s_cand[i] = a.cands[(uint64_t)row * total + i];
   Sums sum{-INFINITY, 0.0f, 0.0f, 0u};
   for (uint32_t i = lane; i < a.parts; i += 64) join(sum, a.sums[(uint64_t)row * a.parts + i]);
-#pragma unroll 1
-  for (int d = 1; d < 64; d <<= 1)
-    join(sum, Sums{__shfl_xor(sum.top, d), __shfl_xor(sum.s, d), __shfl_xor(sum.t, d), (uint32_t)__shfl_xor((int)sum.above, d)});
+  join_lanes(sum);
   const Row r = row_of(sum);
   if (tid == 0) {
     const int32_t token = a.tokens[row];
