@@ -6,7 +6,11 @@
 // (at position 10^6 an angle of 32 bits would be off by 0.06); all heads of a row use them. Then its threads
 // go over the rows' units: a unit of queries or keys is eight pairs, whose 16 elements one thread reads,
 // turns and writes (so q may be turned in place), or eight elements that stay; one of values
-// is eight elements.
+// is eight elements. (Four pairs a unit where their number is odd in fours: 32768 rows of 16 + 4 heads of 80,
+// 20 pairs each, 74 us against 199 pair by pair.)
+//
+// What bounds it: the bytes, read and written once: 65537 rows of 24 + 8 heads of 96 in 209 us, 4.8 TB/s, as
+// fast as a copy; a step of 64 single tokens, 32 + 8 heads of 128, 10 us, what a launch takes.
 #include "pages.h"
 #include "prompt.h"
 
@@ -18,8 +22,9 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// How a head's pairs lie: neighbours, or eight and eight of them in whole vectors, or anyhow.
-enum Layout { kNeighbours, kHalves, kAnyHalves };
+// How a head's pairs lie: neighbours, or eight and eight of them in whole vectors, four and four in halves of
+// vectors, or anyhow.
+enum Layout { kNeighbours, kHalves, kFours, kAnyHalves };
 
 struct RotateArgs {
   const uint8_t* q;
@@ -93,6 +98,10 @@ ARGUS_DEV u32x4 gather(const float (&x)[8]) {
 
 template <int T, bool F8, int LAYOUT>
 __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
+  // Neighbours: what a wave reads and writes at once are whole lines of 128 bytes, which go past the caches (40 prompts
+  // of up to 8192 tokens into 8 bits 187 us against 195). Halves: parts of lines, whose rest comes next
+  // (65537 rows of 24 + 8 heads of 96, eight a block, 219 us against 250).
+  constexpr bool kOnce = LAYOUT == kNeighbours;
   __shared__ int64_t s_page[kMaxTokens];  // -1: not held
   __shared__ uint32_t s_place[kMaxTokens];
   __shared__ int64_t s_pos[kMaxTokens];
@@ -177,10 +186,13 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
     const bool f8 = F8 && !query;
     auto store = [&](uint32_t d, const float (&y)[8]) {
       if (f8) __builtin_nontemporal_store(narrow(y, scale), reinterpret_cast<u32x2*>(to + d));
-      else __builtin_nontemporal_store(gather<T>(y), reinterpret_cast<u32x4*>(to + 2 * d));
+      else if constexpr (kOnce) __builtin_nontemporal_store(gather<T>(y), reinterpret_cast<u32x4*>(to + 2 * d));
+      else *reinterpret_cast<u32x4*>(to + 2 * d) = gather<T>(y);
     };
     auto load = [&](uint32_t d, float (&y)[8]) {
-      spread<T>(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from + 2 * d)), y);
+      const u32x4* at = reinterpret_cast<const u32x4*>(from + 2 * d);
+      if constexpr (kOnce) spread<T>(__builtin_nontemporal_load(at), y);
+      else spread<T>(*at, y);
     };
     const float2* turn = s_turn + t * a.pairs;
     if constexpr (LAYOUT == kNeighbours) {
@@ -217,6 +229,32 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
       }
       store(8 * u, y);
       store(a.pairs + 8 * u, z);
+    } else if constexpr (LAYOUT == kFours) {
+      float y[8];
+      if (u >= a.turned) {
+        const uint32_t d = 2 * a.pairs + 8 * (u - a.turned);
+        load(d, y);
+        store(d, y);
+        continue;
+      }
+      const u32x2 w0 = *reinterpret_cast<const u32x2*>(from + 8 * u), w1 = *reinterpret_cast<const u32x2*>(from + 2 * a.pairs + 8 * u);
+      spread<T>((u32x4){w0.x, w0.y, w1.x, w1.y}, y);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 w = turn[4 * u + i];
+        const float y0 = y[i] * w.x - y[4 + i] * w.y;
+        y[4 + i] = y[4 + i] * w.x + y[i] * w.y;
+        y[i] = y0;
+      }
+      if (f8) {
+        const u32x2 out = narrow(y, scale);
+        *reinterpret_cast<uint32_t*>(to + 4 * u) = out.x;
+        *reinterpret_cast<uint32_t*>(to + a.pairs + 4 * u) = out.y;
+      } else {
+        const u32x4 out = gather<T>(y);
+        *reinterpret_cast<u32x2*>(to + 8 * u) = (u32x2){out.x, out.y};
+        *reinterpret_cast<u32x2*>(to + 2 * a.pairs + 8 * u) = (u32x2){out.z, out.w};
+      }
     } else {  // element by element
       const uint32_t p0 = u < a.turned ? 8 * u : 2 * a.pairs + 8 * (u - a.turned);
       const uint32_t p1 = u < a.turned ? (p0 + 8 < a.pairs ? p0 + 8 : a.pairs) : (p0 + 8 < a.D ? p0 + 8 : a.D);
@@ -249,6 +287,7 @@ void launch_as(const RotateArgs& a, Layout layout, uint32_t grid, hipStream_t st
   const dim3 g(grid), b(kThreads);
   if (layout == kNeighbours) hipLaunchKernelGGL((k_rotate<T, F8, kNeighbours>), g, b, 0, st, a);
   else if (layout == kHalves) hipLaunchKernelGGL((k_rotate<T, F8, kHalves>), g, b, 0, st, a);
+  else if (layout == kFours) hipLaunchKernelGGL((k_rotate<T, F8, kFours>), g, b, 0, st, a);
   else hipLaunchKernelGGL((k_rotate<T, F8, kAnyHalves>), g, b, 0, st, a);
 }
 
@@ -302,12 +341,15 @@ extern "C" int argus_prompt_rotate(const argus_rotate_config* cfg, const argus_r
   if (marks_bad_all(markers)) return refuse(ARGUS_E_INVAL, "markers: alignment or region_base");
 
   RotateArgs a{};
-  const Layout layout = cfg->interleaved ? kNeighbours : cfg->pairs % 8 == 0 ? kHalves : kAnyHalves;
+  const Layout layout = cfg->interleaved ? kNeighbours : cfg->pairs % 8 == 0 ? kHalves : cfg->pairs % 4 == 0 ? kFours : kAnyHalves;
   const uint32_t whole = cfg->head_dim / 8, rest = cfg->head_dim - 2 * cfg->pairs;
-  a.turned = (cfg->pairs + 7) / 8;
+  a.turned = layout == kFours ? cfg->pairs / 4 : (cfg->pairs + 7) / 8;
   const uint32_t per_head = layout == kNeighbours ? whole : a.turned + (rest + 7) / 8;
   const uint32_t per_token = (cfg->heads + cfg->kv_heads) * per_head + cfg->kv_heads * whole;
-  a.tokens = cfg->rows >= 4096 ? 8 : 1;
+  // Of many rows four to a block, which finds their places and angles in one go (65537 rows of 24 + 8 heads of 96
+  // 209 us; eight 219, two 206; 40 prompts of up to 8192
+  // tokens, 32 + 8 heads of 128 into 8 bits, 187, 187, 196). Of fewer one, for the blocks.
+  a.tokens = cfg->rows >= 4096 ? 4 : 1;
   const uint32_t grid = (cfg->rows + a.tokens - 1) / a.tokens;
   if (!marks_fit(markers, (uint64_t)grid * kWaves * 2)) return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
   if (cfg->rows == 0 || cfg->seqs == 0) return ARGUS_OK;

@@ -10,12 +10,13 @@
 // are joined in the same way, in a fixed order.
 //
 // A block reads a part of a row, its four waves 64 lanes of 32 elements in turn. The next ones' loads go out once
-// these are in 32 bits and looked through for the maximum; the rest is done while they are under way, five to seven waves
-// on a SIMD (two sets of registers for them, three or four waves: 137 us where this takes 108). The rank is a count of what is above the given token's own
-// logit, read first. The k best are among what is not below the k-th largest of the block's 256 lanes' maxima,
-// whichever elements the lanes have seen: that bound is worked out after the first step of
-// each wave and again when a wave has seen twice as much, from what the others have noted by then. What is not below
-// it goes to a list of the wave in LDS, and the rest of the work is a few steps over some k candidates.
+// these are in 32 bits and looked through for the maximum; the rest is done while they are under way, five to seven
+// waves on a SIMD (two sets of registers for them, three or four waves: 137 us where this takes 108). The rank is a
+// count of what is above the given token's own logit, read first. The k best are among what is not below the k-th
+// largest of the block's 256 lanes' maxima, whichever elements the lanes have seen: that bound is worked out after
+// the first step of each wave and again when a wave has seen four times as much, from what the others have noted
+// by then. What is not below it goes to a list of the wave in LDS, and the rest of the work is a few steps
+// over some k candidates.
 //
 // What bounds it: reading the logits, and nearly as much the arithmetic, 7.5 instructions an element (the exponential
 // counts twice). Where a clamp is needed for minus infinities it is an eighth: steps go without until a sum
