@@ -4,11 +4,13 @@ A small transformer with random weights answers a few prompts with beam search.
 Every step is made of this library's operators: page tables move on with the
 beams that were selected (step_pages), the new token's keys and values go into
 their pages (append_tokens), attention reads them (attend_pages), and the next
-beams are selected (select_beams).  The operators write marker records of their
+beams are selected (select_beams).  With --chunk the prompts are taken so many tokens
+at a time (attend_chunks) and scored first (score_tokens); with --rotary queries and keys
+have rotary positions (rotate_tokens).  The operators write marker records of their
 own regions; region attribution of those records says how long each took, on which
 waves.
 
-    python examples/decode_loop.py [--steps 32] [--groups 8] [--beams 4] [--marked 8]
+    python examples/decode_loop.py [--steps 32] [--groups 8] [--beams 4] [--marked 8] [--chunk 64] [--rotary]
 """
 from __future__ import annotations
 
@@ -20,16 +22,19 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 import torch  # noqa: E402
 
-from paper_2609_12299_amd import (NUM_REGIONS, REGION_NAMES, MarkerBuffer, RegionAttribution,  # noqa: E402
-                                  append_tokens, attend_pages, compact_pages, select_beams, step_pages)
+from paper_2609_12299_amd import (ALL_REGION_NAMES, NUM_ALL_REGIONS, MarkerBuffer, RegionAttribution,  # noqa: E402
+                                  append_tokens, attend_chunks, attend_pages, compact_pages, rotary_frequencies,
+                                  rotate_tokens, score_tokens, select_beams, step_pages)
 
 
 class Model:
-    """Random weights: `layers` of attention with grouped heads and a residual, tied embeddings."""
+    """Random weights: `layers` of attention with grouped heads and a residual, tied embeddings; with
+    `rotary` the positions are rotary, else there are none."""
 
-    def __init__(self, layers=4, vocab=4099, heads=8, kv_heads=2, head_dim=64, seed=0, device="cuda"):
+    def __init__(self, layers=4, vocab=4099, heads=8, kv_heads=2, head_dim=64, seed=0, device="cuda", rotary=False):
         gen = torch.Generator(device=device).manual_seed(seed)
         self.layers, self.vocab, self.heads, self.kv_heads, self.head_dim = layers, vocab, heads, kv_heads, head_dim
+        self.frequencies = rotary_frequencies(head_dim, device=device) if rotary else None
         width = heads * head_dim
 
         def weight(*shape):
@@ -71,10 +76,35 @@ class Decoder:
             qkv = (x @ m.qkv[layer]).view(x.shape[0], -1, m.head_dim)
             q, k, v = qkv.split([m.heads, m.kv_heads, m.kv_heads], 1)
             k_cache, v_cache = self.caches[0][layer], self.caches[1][layer]
-            append_tokens(k, v, k_cache, v_cache, self.table, starts, markers=markers)
+            q = self.place(q, k, v, k_cache, v_cache, starts, None, markers)
             a = attend_pages(q, k_cache, v_cache, self.table, self.lens, markers=markers)["out"]
             x = x + a.view(x.shape[0], -1) @ m.out[layer]
         return x @ m.logits
+
+    def place(self, q, k, v, k_cache, v_cache, starts, offsets, markers):
+        """New keys and values into their pages; the queries, turned where positions are rotary."""
+        m = self.m
+        if m.frequencies is None:
+            append_tokens(k, v, k_cache, v_cache, self.table, starts, offsets, markers=markers)
+            return q
+        return rotate_tokens(q, k, v, k_cache, v_cache, self.table, starts, m.frequencies, offsets, markers=markers)["out"]
+
+    def take(self, tokens, markers=None):
+        """The logits [sequences, n, vocab] of n more tokens of every sequence, in one pass."""
+        m, (S, n) = self.m, tokens.shape
+        moved = step_pages(self.table, self.lens, self.parents, self.one * n, self.ps, caches=self.caches, markers=markers)
+        starts = moved["lens"] - n
+        self.table, self.lens, self.refs = moved["table"], moved["lens"], moved["refs"]
+        offsets = torch.arange(0, S * n + 1, n, dtype=torch.int32, device=tokens.device)
+        x = m.embed[tokens.reshape(-1).long()]
+        for layer in range(m.layers):
+            qkv = (x @ m.qkv[layer]).view(x.shape[0], -1, m.head_dim)
+            q, k, v = qkv.split([m.heads, m.kv_heads, m.kv_heads], 1)
+            k_cache, v_cache = self.caches[0][layer], self.caches[1][layer]
+            q = self.place(q, k, v, k_cache, v_cache, starts, offsets, markers)
+            a = attend_chunks(q, k_cache, v_cache, self.table, self.lens, offsets, markers=markers)["out"]
+            x = x + a.view(x.shape[0], -1) @ m.out[layer]
+        return (x @ m.logits).view(S, n, -1)
 
     def stay(self):
         self.parents = torch.arange(len(self.lens), dtype=torch.int32, device=self.lens.device)
@@ -94,17 +124,34 @@ class Decoder:
         return moved["counters"]
 
 
+def read(model: Model, prompts, chunk: int, top=0, markers=None, page_size=16):
+    """What the model makes of prompts [groups, length], taken `chunk` tokens at a time: log probabilities, entropies
+    and ranks [groups, length - 1] of their tokens behind the first, and the `top` alternatives to each."""
+    G, L = prompts.shape
+    d = Decoder(model, G, 1, page_size, -(-L // page_size))
+    parts = []
+    for i in range(0, L - 1, chunk):
+        d.stay()
+        n = min(chunk, L - 1 - i)
+        logits = d.take(prompts[:, i:i + n], markers)
+        chosen = prompts[:, i + 1:i + n + 1].reshape(-1).int()
+        got = score_tokens(logits.view(G * n, -1), chosen, top=top, markers=markers)
+        parts.append({name: x.view(G, n, *x.shape[1:]) for name, x in got.items()})
+    return {name: torch.cat([p[name] for p in parts], 1) for name in parts[0]} if parts else {}
+
+
 def search(model: Model, prompts, beams: int, steps: int, eos: int = -1, markers=None, marked: int = 0,
-           page_size=16):
+           page_size=16, chunk=0):
     """Beam search from prompts [groups, length], the last `marked` steps with markers; returns (tokens
-    [groups, beams, length + steps], scores [groups, beams], finished, decoder)."""
+    [groups, beams, length + steps], scores [groups, beams], finished, decoder).  The prompts are taken token by
+    token, or `chunk` at a time."""
     G, L = prompts.shape
     columns = -(-(L + steps) // page_size)
     d = Decoder(model, G, beams, page_size, columns)
     rows = prompts.repeat_interleave(beams, 0)
-    for i in range(L):
+    for i in range(0, L, chunk or 1):
         d.stay()
-        logits = d.forward(rows[:, i])
+        logits = d.take(rows[:, i:i + chunk])[:, -1].contiguous() if chunk else d.forward(rows[:, i])
     history = rows.clone()
     for i in range(steps):
         mk = markers if i >= steps - marked else None
@@ -126,15 +173,23 @@ def main():
     ap.add_argument("--beams", type=int, default=4)
     ap.add_argument("--prompt", type=int, default=100)
     ap.add_argument("--marked", type=int, default=8, help="steps at the end that write markers")
+    ap.add_argument("--chunk", type=int, default=0, help="tokens of a prompt taken at a time (0: one, and no scores of them)")
+    ap.add_argument("--rotary", action="store_true", help="rotary positions")
     args = ap.parse_args()
-    model = Model()
+    model = Model(rotary=args.rotary)
     gen = torch.Generator(device="cuda").manual_seed(1)
     prompts = torch.randint(3, model.vocab, (args.groups, args.prompt), generator=gen, device="cuda")
     markers = MarkerBuffer(1 << 22)
-    tokens, scores, finished, d = search(model, prompts, args.beams, args.steps, eos=2, markers=markers, marked=args.marked)
+    if args.chunk:
+        seen = read(model, prompts, args.chunk, markers=markers)
+        if seen:
+            print(f"prompts of {args.prompt} tokens, {args.chunk} at a time: {seen['logprobs'].mean().item():.3f} nats a token, "
+                  f"entropy {seen['entropy'].mean().item():.3f}, median rank {int(seen['ranks'].median())}")
+    tokens, scores, finished, d = search(model, prompts, args.beams, args.steps, eos=2, markers=markers, marked=args.marked,
+                                         chunk=args.chunk)
     live, moved = d.compact(markers).tolist()[:2]
     records = markers.records()
-    report = RegionAttribution(NUM_REGIONS, max_records=len(records), instances=False, instance_excl=False)
+    report = RegionAttribution(NUM_ALL_REGIONS, max_records=len(records), instances=False, instance_excl=False)
     stats = report.run(records)
     torch.cuda.synchronize()
     rows = stats["region_stats"].cpu().numpy()
@@ -144,7 +199,7 @@ def main():
     print(f"{live} pages in use, {moved} moved to the front; {len(records)} marker records, "
           f"{int(counters[10])} mismatched, {int(counters[11])} unclosed, {int(counters[12])} orphans")
     print(f"{'region':16s} {'instances':>10s} {'mean us':>10s} {'least us':>10s} {'most us':>10s}")
-    for r, name in enumerate(REGION_NAMES):
+    for r, name in enumerate(ALL_REGION_NAMES):
         n = int(rows[r][0])
         if n:
             print(f"{name:16s} {n:10d} {int(rows[r][1]) / n / 100:10.2f} {int(rows[r][3]) / 100:10.2f} {int(rows[r][4]) / 100:10.2f}")
