@@ -20,10 +20,11 @@
 //
 // What bounds it: reading the logits, and nearly as much the arithmetic, 7.5 instructions an element (the exponential
 // counts twice). Where a clamp is needed for minus infinities it is an eighth: steps go without until a sum
-// becomes NaN, and ranks are counted by the scalar unit. 2048 rows of 128003 in bf16 with 20 alternatives take 108 us,
-// 4.8 TB/s (a list of its own bound for each wave, a rank in each lane and a clamp of two instructions 143); 500 rows of
-// 65537 in 32 bits, some of it minus infinity, 26 us, 5.0 TB/s; one row of 32000, 5 alternatives, 14 us, two
-// launches.
+// becomes NaN, and ranks are counted by the scalar unit. 2048 rows of 128003 in bf16 with 20 alternatives take 106 us,
+// 4.9 TB/s (a list of its own bound for each wave, a rank in each lane and a clamp of two instructions 143); 500 rows of
+// 65537 in 32 bits, some of it minus infinity, 23.7 us, 5.5 TB/s; one row of 32000, 5 alternatives, 10.8 us, most
+// of it the host's. Of a kernel that short a step is all: its loads go out first, and what few elements need (the token's
+// own vector, the row's end) is done with the others' instructions.
 #include "prompt.h"
 #include "rows.h"
 
@@ -35,6 +36,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint32_t kItems = 32;       // elements of a lane per step
 constexpr uint32_t kStep = kItems * 64;
 constexpr uint32_t kList = 192;       // candidates of a wave
+constexpr uint32_t kManyWaves = 16;   // of a block that reads a row by itself
 constexpr uint32_t kMaxTop = 64;
 constexpr uint32_t kCands = 512;      // of the parts of a row, ranked by counting
 
@@ -118,14 +120,15 @@ ARGUS_DEV float element(const uint8_t* base, uint32_t i) {
   else return of_word<TYPE>(*reinterpret_cast<const uint16_t*>(base + (uint64_t)i * 2), 0);
 }
 
-template <int TYPE, bool TOP>
-__global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
+// W waves.
+template <int TYPE, bool TOP, int W>
+__global__ __launch_bounds__(64 * W) void k_score_rows(ScoreArgs a) {
   constexpr uint32_t kBytes = TYPE == ARGUS_FP32 ? 4 : 2, kPer = 16 / kBytes, kVecs = kItems / kPer;
-  __shared__ uint64_t s_list[TOP ? kWaves : 1][TOP ? kList : 1];
-  __shared__ u32x4 s_step[TOP ? kWaves : 1][TOP ? kVecs * 64 : 1];
-  __shared__ float s_tops[TOP ? kThreads : 1];  // the lanes' maxima
-  __shared__ Sums s_sums[kWaves];
-  __shared__ uint32_t s_n[kWaves];
+  __shared__ uint64_t s_list[TOP ? W : 1][TOP ? kList : 1];
+  __shared__ u32x4 s_step[TOP ? W : 1][TOP ? kVecs * 64 : 1];
+  __shared__ float s_tops[TOP ? 64 * W : 1];  // the lanes' maxima
+  __shared__ Sums s_sums[W];
+  __shared__ uint32_t s_n[W];
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_SCORE_ROWS);
   const uint32_t tid = threadIdx.x, lane = tid & 63u;
@@ -133,10 +136,6 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
   const uint32_t row = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
   const uint8_t* base = a.logits + (int64_t)row * a.row_stride;
   const int32_t token = a.tokens[row];
-  const bool known = (uint32_t)token < a.V;
-  const float mine = known ? element<TYPE>(base, (uint32_t)token) : INFINITY;
-  // the least number above it (what is as large and comes behind the token is not above)
-  const float beyond = value_of(order_of(mine) + 1);
   // Vectors lie on 16 bytes: `head` elements come before the first of `vecs`
   // vectors, less than a vector behind the last.
   uint32_t head = (uint32_t)(0 - (uintptr_t)base & 15u) / kBytes;
@@ -158,6 +157,14 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
         w[v] = __builtin_nontemporal_load(&body[v0 + lane + v * 64 < vecs ? v0 + lane + v * 64 : vecs - 1]);
     }
   };
+  uint32_t step = part * a.steps + wave;
+  if (step < end) load(step);
+  const bool known = (uint32_t)token < a.V;
+  const float mine = known ? element<TYPE>(base, (uint32_t)token) : INFINITY;
+  // the least number above it (what is as large and comes behind the token is not above)
+  const float beyond = value_of(order_of(mine) + 1);
+  // the vector that has the token; none: -1 or vecs
+  const int32_t its = token < (int32_t)head ? -1 : (uint32_t)token >= tail ? (int32_t)vecs : (int32_t)((token - head) / kPer);
   Sums my{-INFINITY, 0.0f, 0.0f, 0u};
   uint32_t above = 0;  // of the wave's elements
   auto add = [&](float x, float base) {  // (a NaN of x goes on in s, a d of -inf has no part)
@@ -210,15 +217,21 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
   // The k-th largest of the lanes' maxima, for 16-bit logits in its upper 16 bits: the largest number that k of them
   // are not below. What other waves note meanwhile may count or not.
   auto raise = [&]() {
-    uint32_t its[kWaves], v = 0;
+    // (of 16 waves: of the maxima of four lanes each)
+    uint32_t its[4], v = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-      its[w] = order_of(__hip_atomic_load(&s_tops[w * 64 + lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
+    for (int i = 0; i < 4; ++i) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = i; w < W; w += 4)
+        top = fmaxf(top, __hip_atomic_load(&s_tops[w * 64 + lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
+      its[i] = order_of(top);
+    }
 #pragma unroll 1
     for (uint32_t bit = 1u << 31; bit >= (kBytes == 4 ? 1u : 1u << 16); bit >>= 1) {
       uint32_t many = 0;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) many += (uint32_t)__popcll(__ballot(its[w] >= (v | bit)));
+      for (int i = 0; i < 4; ++i) many += (uint32_t)__popcll(__ballot(its[i] >= (v | bit)));
       v = many >= a.K ? v | bit : v;
     }
     const uint64_t bound = join64(0u, v);  // below every key of this value
@@ -257,7 +270,7 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
         __builtin_amdgcn_wave_barrier();
       }
     }
-    if (step + kWaves < end) load(step + kWaves);
+    if (step + W < end) load(step + W);
     float base = my.top == -INFINITY ? 0.0f : my.top;
     const float s0 = my.s, t0 = my.t;
     if (!holes) {
@@ -279,18 +292,19 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
         if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
       }
     }
-    // those above the token's logit; as large, and before it
-    const uint32_t e0 = head + step * kVecs * 64 * kPer, e1 = e0 + kVecs * 64 * kPer;
-    if (((uint32_t)token >= e1 || (uint32_t)token < e0) && !last) {
-      const float from = (uint32_t)token < e0 ? beyond : mine;
+    // those above the token's logit, up to the end of its vector also those as large
+    const uint32_t first = step * kVecs * 64;
+    if (((int32_t)first > its || (int32_t)(first + kVecs * 64) <= its) && !last) {
+      const float from = (int32_t)first > its ? beyond : mine;
 #pragma unroll
       for (uint32_t i = 0; i < kItems; ++i) above += (uint32_t)__popcll(__ballot(x[i] >= from));
     } else {
 #pragma unroll
-      for (uint32_t i = 0; i < kItems; ++i)
-        above += (uint32_t)__popcll(__ballot(
-            v0 + i / kPer * 64 < vecs &&
-            (x[i] > mine || (x[i] == mine && head + (v0 + i / kPer * 64) * kPer + i % kPer < (uint32_t)token))));
+      for (uint32_t v = 0; v < kVecs; ++v) {
+        const float from = v0 + v * 64 >= vecs ? NAN : (int32_t)(v0 + v * 64) > its ? beyond : mine;
+#pragma unroll
+        for (uint32_t i = v * kPer; i < (v + 1) * kPer; ++i) above += (uint32_t)__popcll(__ballot(x[i] >= from));
+      }
     }
     if constexpr (TOP) {
       // two lanes' 32 elements at a time
@@ -319,10 +333,13 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
     if (x > -INFINITY) my.top = x;
     if (in) add(x, my.top == -INFINITY ? 0.0f : my.top);
     above += (uint32_t)__popcll(__ballot(in && (x > mine || (x == mine && j < (uint32_t)token))));
+    // what is counted below of the token's own vector, and is as large but not before it
+    if (its >= 0 && its < (int32_t)vecs) {
+      const uint32_t k = head + (uint32_t)its * kPer + lane;
+      above -= (uint32_t)__popcll(__ballot(lane < kPer && k >= (uint32_t)token && element<TYPE>(base, lane < kPer ? k : head) == mine));
+    }
     if constexpr (TOP) append(x > -INFINITY, key_of(x, j));
   }
-  uint32_t step = part * a.steps + wave;
-  if (step < end) load(step);
   if constexpr (TOP) {
     float top = my.top;
     if (step < end) {
@@ -337,11 +354,11 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
     __syncthreads();
     raise();
   }
-  for (; step < end; step += kWaves) look(step);
+  for (; step < end; step += W) look(step);
   join_lanes(my);
   if (lane == 0) s_sums[wave] = Sums{my.top, my.s, my.t, above};
   __syncthreads();
-  Sums sum = lane < kWaves ? s_sums[lane] : Sums{-INFINITY, 0.0f, 0.0f, 0u};
+  Sums sum = lane < W ? s_sums[lane] : Sums{-INFINITY, 0.0f, 0.0f, 0u};
   join_lanes(sum);
   const Row r = row_of(sum);
   if (tid == 0) {
@@ -350,7 +367,7 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
   }
   if constexpr (TOP) {
     // what the whole block's bound leaves, 64 of a wave at most; a candidate's place is the number of those above it
-    raise();
+    if (seen > 1) raise();
     uint32_t kept = 0;
     for (uint32_t i = 0; i < n; i += 64) {
       const uint64_t key = i + lane < n ? list[i + lane] : 0;
@@ -365,12 +382,12 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
     if (lane == 0) s_n[wave] = n;
     __syncthreads();
     uint32_t total = 0;
-    for (int w = 0; w < kWaves; ++w) total += s_n[w];
+    for (int w = 0; w < W; ++w) total += s_n[w];
     uint64_t* to = a.cands + (uint64_t)blockIdx.x * a.K;
     if (lane < n) {
       const uint64_t key = list[lane];
       uint32_t place = 0;
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < W; ++w) {
         const uint32_t many = s_n[w];
 #pragma unroll 8
         for (uint32_t i = 0; i < many; ++i) place += s_list[w][i] > key;
@@ -380,7 +397,7 @@ __global__ __launch_bounds__(kThreads) void k_score_rows(ScoreArgs a) {
         else to[place] = key;
       }
     }
-    for (uint32_t i = total + tid; i < a.K; i += kThreads) {
+    for (uint32_t i = total + tid; i < a.K; i += 64 * W) {
       if (a.parts == 1) put_top(a, row, r, i, 0);
       else to[i] = 0;
     }
@@ -422,17 +439,28 @@ __global__ __launch_bounds__(kThreads) void k_score_join(ScoreArgs a) {
 }
 
 template <int TYPE>
-void launch_score(const ScoreArgs& a, uint32_t grid, hipStream_t st) {
-  if (a.K) hipLaunchKernelGGL((k_score_rows<TYPE, true>), dim3(grid), dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((k_score_rows<TYPE, false>), dim3(grid), dim3(kThreads), 0, st, a);
+void launch_score(const ScoreArgs& a, uint32_t grid, uint32_t waves, hipStream_t st) {
+  const dim3 g(grid), b(64 * waves);
+  if (waves == kManyWaves) {
+    if (a.K) hipLaunchKernelGGL((k_score_rows<TYPE, true, kManyWaves>), g, b, 0, st, a);
+    else hipLaunchKernelGGL((k_score_rows<TYPE, false, kManyWaves>), g, b, 0, st, a);
+  } else {
+    if (a.K) hipLaunchKernelGGL((k_score_rows<TYPE, true, kWaves>), g, b, 0, st, a);
+    else hipLaunchKernelGGL((k_score_rows<TYPE, false, kWaves>), g, b, 0, st, a);
+  }
 }
 
 struct Plan {
-  uint32_t parts, steps, grid;
+  uint32_t parts, steps, grid, waves;
   size_t cands_at, bytes;
 };
 
 constexpr uint32_t kRowBlocks = 768;
+// Rows of which each compute unit has one at most: a block of 16 waves reads one by itself, and nothing is joined, where
+// its waves have one step each (one row of 32000, 5 alternatives, 10.8 us against 13.5 in parts), or there are so many
+// rows that parts of them would not fill the card better (256 of 128003, 20 alternatives, 26.0 us against 30.9; 100 of
+// 128003 23.3 against 19.6). Beyond that, parts or rows of four waves (300 of 32000 17.8 us, with 16 waves 23.0).
+constexpr uint32_t kFewRows = 256, kFewSteps = 4;
 
 int make_plan(const argus_score_config* c, Plan* p) {
   if (!c) return refuse(ARGUS_E_INVAL, "no configuration");
@@ -443,6 +471,10 @@ int make_plan(const argus_score_config* c, Plan* p) {
   if (c->rows > (1u << 22)) return refuse(ARGUS_E_CAPACITY, "rows %u", c->rows);
   const uint32_t steps = (c->vocab + kStep - 1) / kStep;
   uint32_t parts = c->rows ? kRowBlocks / c->rows : 1;
+  p->waves = steps > kWaves && c->rows <= kFewRows &&
+                     (steps <= kManyWaves || (c->rows > kFewRows / 2 && steps <= kFewSteps * kManyWaves))
+                 ? kManyWaves : kWaves;
+  if (p->waves == kManyWaves) parts = 1;
   uint32_t most = (steps + kWaves - 1) / kWaves;
   if (c->top && kCands / c->top < most) most = kCands / c->top;
   parts = parts < most ? parts : most;
@@ -487,7 +519,7 @@ extern "C" int argus_prompt_score(const argus_score_config* cfg, const argus_sco
   if (p.bytes && !aligned_to(d_workspace, 256)) return refuse(ARGUS_E_ALIGN, "the workspace lies on 256 bytes");
   if (workspace_bytes < p.bytes) return refuse(ARGUS_E_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
   const uint32_t joins = p.parts > 1 ? cfg->rows : 0;
-  if (!marks_fit(markers, ((uint64_t)p.grid + joins) * kWaves * 2))
+  if (!marks_fit(markers, ((uint64_t)p.grid * p.waves + joins * kWaves) * 2))
     return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
   if (cfg->rows == 0) return ARGUS_OK;
   if ((rc = device_ok()) != ARGUS_OK) return rc;
@@ -499,10 +531,10 @@ extern "C" int argus_prompt_score(const argus_score_config* cfg, const argus_sco
   a.cands = (uint64_t*)((char*)d_workspace + p.cands_at);
   a.V = cfg->vocab, a.K = cfg->top, a.parts = p.parts, a.steps = p.steps, a.rows = cfg->rows;
   hipStream_t st = (hipStream_t)stream_v;
-  a.marks = take_marks(markers, p.grid, 2);
-  if (cfg->type == ARGUS_BF16) launch_score<ARGUS_BF16>(a, p.grid, st);
-  else if (cfg->type == ARGUS_FP16) launch_score<ARGUS_FP16>(a, p.grid, st);
-  else launch_score<ARGUS_FP32>(a, p.grid, st);
+  a.marks = take_marks(markers, p.grid * (p.waves / kWaves), 2);
+  if (cfg->type == ARGUS_BF16) launch_score<ARGUS_BF16>(a, p.grid, p.waves, st);
+  else if (cfg->type == ARGUS_FP16) launch_score<ARGUS_FP16>(a, p.grid, p.waves, st);
+  else launch_score<ARGUS_FP32>(a, p.grid, p.waves, st);
   if (joins) {
     a.marks = take_marks(markers, joins, 2);
     if (cfg->type == ARGUS_BF16) hipLaunchKernelGGL(k_score_join<ARGUS_BF16>, dim3(joins), dim3(kThreads), 0, st, a);

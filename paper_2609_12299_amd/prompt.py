@@ -175,7 +175,8 @@ def attend_chunks(q, k_cache, v_cache, table, lens, offsets, scale: float | None
     S, P = table.shape
     if not (0 <= window < 2 ** 30 and 0 <= sinks < 2 ** 30):
         _bad(f"window {window}, sinks {sinks}")
-    cfg = _pack(_CHUNK_CONFIG, ABI_VERSION, qt, ct, S, T, H, heads // H if heads else 1, D, ps, N, P, window, sinks,
+    # (no heads: nothing to read or write)
+    cfg = _pack(_CHUNK_CONFIG, ABI_VERSION, qt, ct, S, T if heads else 0, H, heads // H or 1, D, ps, N, P, window, sinks,
                 D ** -0.5 if scale is None else scale)
     given = out is not None
     if not given:

@@ -152,7 +152,7 @@ def test_markers():
     short = attend.build("fp16", sizes=[(30, 100)], D=64, G=4, ps=16)
     long = attend.build("bf16", sizes=[(6000, 300)], H=4, D=128, G=4, ps=64, junk=False)
     r = rotate.build()
-    x, t = score.build("bf16", 3, 40001)
+    x, t = score.build("bf16", 3, 300001)
     y, u = score.build("fp32", 900, 701)
 
     def all_of_them(markers):
@@ -269,6 +269,20 @@ def test_gradients_are_refused_and_writes_are_seen():
     before = out._version
     fw.attend_chunks(**a, out=out)
     assert out._version > before
+
+
+def test_no_heads():
+    from paper_2609_12299_amd import attend_chunks, rotate_tokens
+    log("[gpu] no heads")
+    a, r = inputs("chunks"), inputs("rotate")
+    room = torch.full((4096,), 7.0, dtype=torch.bfloat16, device="cuda")
+    none = room.as_strided((len(a["q"]), 0, 64), (0, 64, 1))
+    got = attend_chunks(**{**a, "q": none}, lse=True, out=none)
+    assert got["out"].shape == none.shape and got["lse"].shape == (len(a["q"]), 0)
+    want = r["k_cache"].clone(), r["v_cache"].clone()
+    rotate_tokens(**{**r, "k_cache": want[0], "v_cache": want[1]})
+    assert rotate_tokens(**{**r, "q": r["q"][:, :0]})["out"].shape == (len(r["q"]), 0, 64)
+    assert torch.equal(r["k_cache"], want[0]) and torch.equal(r["v_cache"], want[1]) and (room == 7).all()
 
 
 def test_example_runs():

@@ -57,6 +57,18 @@ def test_alignments(kind, shift):
     check(x[:, shift:], (t - shift).clamp(min=0), 7)
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_few_and_many_rows(kind):
+    """Rows that a block reads by itself, in one step of its waves or in some, and rows in parts."""
+    check(*build(kind, 140, 33001), 6)
+    check(*build(kind, 2, 32768), 64)
+    check(*build(kind, 257, 9001), 3)
+    x, t = build(kind, 130, 33003)
+    check((x[:, 1:] * 0.4).round(), t.clamp(max=33001), 20, "few values")
+    x, t = build(kind, 4, 140001)
+    check((x[:, 1:] * 0.4).round(), t.clamp(max=139999), 20, "few values")
+
+
 def test_equal_logits():
     """The lower token comes first, in ranks and alternatives; -0 and 0 are equal."""
     for kind in TYPES:
