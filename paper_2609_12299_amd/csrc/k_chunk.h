@@ -213,12 +213,14 @@ constexpr uint32_t kFrac = T == 0 ? 7 : 10;  // bits of a fraction
 template <int T>
 constexpr uint32_t kFracs = ((1u << kFrac<T>) - 1) * 0x10001u;
 
-// O, maxima and sums of steps [t0, t1) of a row tile for one head.
-template <int T, bool F8, int DP, int W>
+// O, maxima and sums of steps [t0, t1) of a row tile for one head. Rows of LDS have room for DP elements, of which DC
+// are multiplied (at head size 96, of 128, a quarter of the products less: a batch of single tokens and chunks 153 us
+// against 166, 4 prompts of up to 6000 tokens 467 against 519).
+template <int T, bool F8, int DP, int DC, int W>
 ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint32_t t0, uint32_t t1, lds_byte* lds,
-                           f32x16 (&acc)[DP / 32], float& m, float& l) {
+                           f32x16 (&acc)[DC / 32], float& m, float& l) {
   constexpr int KT = kStepTokens<DP>, HT = KT / 32;      // halves of a step
-  constexpr int KF = DP / 16, DB = DP / 32;              // fragments of a key row, 32-wide parts of O
+  constexpr int KF = DC / 16, DB = DC / 32;              // fragments of a key row, 32-wide parts of O
   constexpr uint32_t kRuns = KT / 8;                     // of eight tokens, in a step
   constexpr int RUNS = kRuns / W;                        // that a wave loads
   constexpr int NB = kBuffers<F8, DP, W>, PD = NB - 1;   // buffers; steps that loads are ahead
@@ -629,9 +631,9 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
   }
 }
 
-template <int T, bool F8, int DP, int W, bool PIECES>
+template <int T, bool F8, int DP, int DC, int W, bool PIECES>
 __global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : DP == 128 ? 2 : 3) void k_chunk(ChunkArgs a) {
-  constexpr int DB = DP / 32, KT = kStepTokens<DP>, TR = 32 * W;
+  constexpr int DB = DC / 32, KT = kStepTokens<DP>, TR = 32 * W;
   using Hf = Half<T>;
   __shared__ __align__(1024) uint8_t s_raw[2 * kBuffers<F8, DP, W> * KT * DP * 2 + 512 * W];
   lds_byte* lds = (lds_byte*)s_raw;
@@ -694,7 +696,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : DP == 128 ? 2 : 3
     const uint32_t first = slot_of(a, lo);
     if (first <= x && reach_of(a, lo, x - first, &g)) {
       g = scalar(g);
-      chunk_steps<T, F8, DP, W>(a, g, h, 0, g.steps, lds, acc, m, l);
+      chunk_steps<T, F8, DP, DC, W>(a, g, h, 0, g.steps, lds, acc, m, l);
       put(a, g, h, acc, m, l, true, 0);
     }
   } else {
@@ -703,7 +705,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : DP == 128 ? 2 : 3
       const uint4 piece = a.pieces[q];
       if (reach_of(a, scalar(piece.x), scalar(piece.y), &g)) {
         g = scalar(g);
-        chunk_steps<T, F8, DP, W>(a, g, h, scalar(piece.z), scalar(piece.w), lds, acc, m, l);
+        chunk_steps<T, F8, DP, DC, W>(a, g, h, scalar(piece.z), scalar(piece.w), lds, acc, m, l);
         const ChunkArgs e = fresh_args();
         put(e, g, h, acc, m, l, q >= (uint32_t)e.head[3], (uint64_t)q * e.H + h);
       }
@@ -712,18 +714,25 @@ __global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : DP == 128 ? 2 : 3
   mk.end(ARGUS_REGION_CHUNK);
 }
 
-template <int T, bool F8, int DP, int W>
+template <int T, bool F8, int DP, int DC, int W>
 void launch_chunk_as(const ChunkArgs& a, uint32_t grid, hipStream_t st) {
-  if (a.blocks) hipLaunchKernelGGL((k_chunk<T, F8, DP, W, true>), dim3(grid), dim3(64 * W), 0, st, a);
-  else hipLaunchKernelGGL((k_chunk<T, F8, DP, W, false>), dim3(grid), dim3(64 * W), 0, st, a);
+  if (a.blocks) hipLaunchKernelGGL((k_chunk<T, F8, DP, DC, W, true>), dim3(grid), dim3(64 * W), 0, st, a);
+  else hipLaunchKernelGGL((k_chunk<T, F8, DP, DC, W, false>), dim3(grid), dim3(64 * W), 0, st, a);
 }
 
 template <int T, bool F8>
 void launch_chunk_type(const ChunkArgs& a, uint32_t grid, hipStream_t st) {
-  if (a.D <= 64) launch_chunk_as<T, F8, 64, 4>(a, grid, st);
-  else if (a.D > 128) launch_chunk_as<T, F8, 256, 4>(a, grid, st);
-  else if (a.tile_shift == 8) launch_chunk_as<T, F8, 128, 8>(a, grid, st);
-  else launch_chunk_as<T, F8, 128, 4>(a, grid, st);
+  if (a.D <= 64) {
+    launch_chunk_as<T, F8, 64, 64, 4>(a, grid, st);
+  } else if (a.D > 128) {
+    launch_chunk_as<T, F8, 256, 256, 4>(a, grid, st);
+  } else if (a.D <= 96) {
+    if (a.tile_shift == 8) launch_chunk_as<T, F8, 128, 96, 8>(a, grid, st);
+    else launch_chunk_as<T, F8, 128, 96, 4>(a, grid, st);
+  } else {
+    if (a.tile_shift == 8) launch_chunk_as<T, F8, 128, 128, 8>(a, grid, st);
+    else launch_chunk_as<T, F8, 128, 128, 4>(a, grid, st);
+  }
 }
 
 // One source file each, so that they compile side by side.

@@ -306,3 +306,18 @@ def test_long_sequences(kind, D, G, sizes):
     a = build(kind, D=D, G=G, ps=64, sizes=sizes)
     check(a, what=kind, **kw)
     check(a, what=kind, window=5000, sinks=70, **kw)
+
+
+@pytest.mark.parametrize("kind,D,kw", [("bf16", 128, {}), ("fp8", 96, {}), ("fp16", 80, dict(window=300, sinks=5)), ("bf16", 120, dict(window=1000))])
+def test_many_row_tiles(kind, D, kw):
+    """Long chunks of many heads: more waves share what is read."""
+    a = build(kind, D=D, G=1, H=128, ps=16, sizes=[(1100, 150)])
+    if kind == "fp8":
+        kw = dict(kw, k_scale=torch.rand(128, device="cuda") + 0.5, v_scale=torch.rand(128, device="cuda") + 0.5)
+    check(a, what=kind, **kw)
+
+
+def test_batches_of_many_lengths():
+    """More row tiles than two rounds of blocks, of all lengths: some cut, the others in classes."""
+    check(build("bf16", D=64, G=2, H=8, ps=16, sizes=[(1 + 37 * i % 90, 61 * i % 700) for i in range(150)] + [(3, 9000), (70, 4000)]))
+    check(build("fp16", D=96, G=1, H=4, ps=32, sizes=[(1, 97 * i % 3000) for i in range(260)]), window=700, sinks=2)
