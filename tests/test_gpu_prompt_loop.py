@@ -154,6 +154,7 @@ def test_markers():
     r = rotate.build()
     x, t = score.build("bf16", 3, 300001)
     y, u = score.build("fp32", 900, 701)
+    z, w = score.build("fp16", 3, 20000)
 
     def all_of_them(markers):
         caches = r["k_cache"].clone(), r["v_cache"].clone()
@@ -163,6 +164,7 @@ def test_markers():
         for b in (a, short, long):
             out += attend_chunks(**b, lse=True, markers=markers).values()
         out += score_tokens(x, t, 5, markers=markers).values()
+        out += score_tokens(z, w, 2, markers=markers).values()
         return out + list(score_tokens(y, u, markers=markers).values())
 
     plain = all_of_them(None)
