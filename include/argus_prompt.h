@@ -30,7 +30,9 @@ extern "C" {
 #endif
 
 /* Regions of these operators' markers, behind those of argus_decode.h; a call
- * needs region_base + ARGUS_NUM_ALL_REGIONS <= 65536. */
+ * needs region_base + ARGUS_NUM_ALL_REGIONS <= 65536.  A block has four waves and
+ * so four contexts; eight where a row tile of attend is 256 rows; sixteen in
+ * attend's plan, and in score where a block reads a row by itself. */
 enum {
   ARGUS_REGION_CHUNK_PLAN = 14, /* attend: the batch shared out */
   ARGUS_REGION_CHUNK = 15,      /*   a wave's part of it */

@@ -192,6 +192,31 @@ def test_markers():
     assert small.used == m.used - 3 and torch.equal(small.buffer, before)
 
 
+def test_contexts_of_a_block():
+    from paper_2609_12299_amd import ALL_REGION_NAMES, MarkerBuffer, attend_chunks, score_tokens
+    log("[gpu] contexts of a block")
+    m = MarkerBuffer(1 << 18, ctx_base=40)
+
+    def contexts(region):
+        torch.cuda.synchronize()
+        words = m.records().cpu().numpy().view(np.uint32).reshape(-1, 4)
+        return set(words[words[:, 3] & 0xFFFF == ALL_REGION_NAMES.index(region), 2].tolist())
+    score_tokens(*score.build("bf16", 3, 20000), markers=m)
+    assert m.used == 3 * 16 * 2 and contexts("score.rows") == set(range(40, 88))
+    m.clear()
+    score_tokens(*score.build("bf16", 3, 2000), markers=m)
+    assert m.used == 3 * 4 * 2 and contexts("score.rows") == set(range(40, 52))
+    m.clear()
+    attend_chunks(**attend.build(sizes=[(10, 20)], H=2, G=3), markers=m)  # a row tile, a place for one more, two heads
+    assert contexts("chunk") == set(range(40, 40 + m.used // 2)) and m.used == 2 * 4 * 2
+    m.clear()
+    attend_chunks(**attend.build(sizes=[(10, 3000)], H=2, G=3, junk=False), markers=m)
+    assert contexts("chunk.plan") == set(range(40, 56)) and min(contexts("chunk")) == 40  # (each launch from ctx_base on)
+    m.clear()
+    attend_chunks(**attend.build(sizes=[(1100, 0)], H=128, G=1, D=128, ps=16, junk=False), markers=m)
+    assert m.used == (1100 // 256 + 1) * 128 * 8 * 2
+
+
 def inputs(op):
     if op == "chunks":
         return attend.build("bf16", junk=False)
