@@ -180,7 +180,7 @@ def attend_chunks(q, k_cache, v_cache, table, lens, offsets, scale: float | None
                 D ** -0.5 if scale is None else scale)
     given = out is not None
     if not given:
-        out = q.new_empty((T, heads, D))
+        out = q.new_empty(T, heads, D)
     elif not (out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.is_contiguous()):
         _bad("out: like q, dense")
     elif out.requires_grad:
@@ -188,7 +188,7 @@ def attend_chunks(q, k_cache, v_cache, table, lens, offsets, scale: float | None
     res = dict(out=out)
     l_ptr = 0
     if lse:
-        res["lse"] = t.empty((T, heads), dtype=t.float32, device=dev)
+        res["lse"] = q.new_empty(T, heads, dtype=t.float32)
         l_ptr = res["lse"].data_ptr()
     io = _pack(_CHUNK_IO, q.data_ptr(), qs[0], qs[1], *k, *v, tab, tab_stride, _ints(lens, (S,), "lens", dev),
                _ints(offsets, (S + 1,), "offsets", dev), _scales(k_scale, H, "k_scale", dev),
@@ -254,7 +254,7 @@ def rotate_tokens(q, new_k, new_v, k_cache, v_cache, table, starts, frequencies,
             _differentiable("q")
         heads = q.shape[1]
         if not given:
-            out = q.new_empty((T, heads, D))
+            out = q.new_empty(T, heads, D)
         os_ = _rows(out, "out", dev)
         if not (out.shape == q.shape and out.dtype == q.dtype):
             _bad("out: like q")
@@ -323,11 +323,11 @@ def score_tokens(logits, tokens, top: int = 0, markers=None, stream=None) -> dic
         _bad(f"top {top} (0..{MAX_TOP})")
     cfg = _pack(_SCORE_CONFIG, ABI_VERSION, lt, R, V, top, 0)
     chosen = _ints(tokens, (R,), "tokens", dev)
-    logprobs = t.empty(R, dtype=t.float32, device=dev)
+    logprobs = logits.new_empty(R, dtype=t.float32)
     out = dict(logprobs=logprobs, entropy=logprobs.new_empty(R), ranks=tokens.new_empty(R))
     best = (0, 0)
     if top:
-        out["top_logprobs"], out["top_tokens"] = logprobs.new_empty((R, top)), tokens.new_empty((R, top))
+        out["top_logprobs"], out["top_tokens"] = logprobs.new_empty(R, top), tokens.new_empty(R, top)
         best = (out["top_logprobs"].data_ptr(), out["top_tokens"].data_ptr())
     io = _pack(_SCORE_IO, logits.data_ptr(), ls[0], chosen, logprobs.data_ptr(), out["entropy"].data_ptr(),
                out["ranks"].data_ptr(), *best)
