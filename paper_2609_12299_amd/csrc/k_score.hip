@@ -20,11 +20,12 @@
 //
 // What bounds it: reading the logits, and nearly as much the arithmetic, 7.5 instructions an element (the exponential
 // counts twice). Where a clamp is needed for minus infinities it is an eighth: steps go without until a sum
-// becomes NaN, and ranks are counted by the scalar unit. 2048 rows of 128003 in bf16 with 20 alternatives take 106 us,
-// 4.9 TB/s (a list of its own bound for each wave, a rank in each lane and a clamp of two instructions 143); 500 rows of
-// 65537 in 32 bits, some of it minus infinity, 23.7 us, 5.5 TB/s; one row of 32000, 5 alternatives, 10.8 us, most
-// of it the host's. Of a kernel that short a step is all: its loads go out first, and what few elements need (the token's
-// own vector, the row's end) is done with the others' instructions.
+// becomes NaN, and ranks are counted by the scalar unit. 2048 rows of 128003 in bf16 with 20 alternatives take 103 us,
+// 5.1 TB/s (a list of its own bound for each wave, a rank in each lane and a clamp of two instructions 143); 500 rows of
+// 65537 in 32 bits, some of it minus infinity, 23.5 us, 5.6 TB/s; one row of 32000, 5 alternatives, 10.0 us, the
+// host's and the kernel's time alike. Of a kernel that short a step is all: its loads go out first, and what few elements need (the token's
+// own vector, the row's end) is done with the others' instructions, and
+// lanes are joined without LDS (10.7 us with shuffles through it).
 #include "prompt.h"
 #include "rows.h"
 
@@ -78,15 +79,23 @@ ARGUS_DEV void join(Sums& a, Sums b) {
   move(b, to);
   a.s += b.s, a.t += b.t, a.above += b.above;
 }
-// A wave's, in all lanes.
+// A wave's, in all lanes: rows of 16 lanes without LDS, then the four of them.
+ARGUS_DEV float lanes_sum(float v) {
+  auto with = [&](uint32_t o) { v += __builtin_bit_cast(float, o); };
+  with(dpp32<kDppQuad1032>(__builtin_bit_cast(uint32_t, v)));
+  with(dpp32<kDppQuad2301>(__builtin_bit_cast(uint32_t, v)));
+  with(dpp32<kDppHalfMirror>(__builtin_bit_cast(uint32_t, v)));
+  with(dpp32<kDppMirror>(__builtin_bit_cast(uint32_t, v)));
+  auto row = [&](int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); };
+  return (row(0) + row(16)) + (row(32) + row(48));
+}
 ARGUS_DEV void join_lanes(Sums& a) {
-  float to = a.top;
-  for (int d = 1; d < 64; d <<= 1) to = fmaxf(to, __shfl_xor(to, d));
-  move(a, to);
-  for (int d = 1; d < 64; d <<= 1) {
-    a.s += __shfl_xor(a.s, d), a.t += __shfl_xor(a.t, d);
-    a.above += (uint32_t)__shfl_xor((int)a.above, d);
-  }
+  move(a, wave_max(a.top));
+  a.s = lanes_sum(a.s);
+  a.t = lanes_sum(a.t);
+  const uint32_t n = row_sum32(a.above);
+  auto row = [&](int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)n, lane); };
+  a.above = (row(0) + row(16)) + (row(32) + row(48));
 }
 
 // A row's numbers, once its sums are known. `lane`: of those that write its alternatives.
@@ -457,7 +466,7 @@ struct Plan {
 
 constexpr uint32_t kRowBlocks = 768;
 // Rows of which each compute unit has one at most: a block of 16 waves reads one by itself, and nothing is joined, where
-// its waves have one step each (one row of 32000, 5 alternatives, 10.8 us against 13.5 in parts), or there are so many
+// its waves have one step each (one row of 32000, 5 alternatives, 10.0 us against 13.5 in parts), or there are so many
 // rows that parts of them would not fill the card better (256 of 128003, 20 alternatives, 26.0 us against 30.9; 100 of
 // 128003 23.3 against 19.6). Beyond that, parts or rows of four waves (300 of 32000 17.8 us, with 16 waves 23.0).
 constexpr uint32_t kFewRows = 256, kFewSteps = 4;
