@@ -23,9 +23,9 @@
 // becomes NaN, and ranks are counted by the scalar unit. 2048 rows of 128003 in bf16 with 20 alternatives take 103 us,
 // 5.1 TB/s (a list of its own bound for each wave, a rank in each lane and a clamp of two instructions 143); 500 rows of
 // 65537 in 32 bits, some of it minus infinity, 23.5 us, 5.6 TB/s; one row of 32000, 5 alternatives, 10.0 us, the
-// host's and the kernel's time alike. Of a kernel that short a step is all: its loads go out first, and what few elements need (the token's
-// own vector, the row's end) is done with the others' instructions, and
-// lanes are joined without LDS (10.7 us with shuffles through it).
+// host's and the kernel's time alike. Of a kernel that short a step is all: its loads go out first, what few elements
+// need (the token's own vector, the row's end) is done with the others' instructions, and lanes are joined without
+// LDS (10.7 us with shuffles through it).
 #include "prompt.h"
 #include "rows.h"
 
@@ -186,31 +186,26 @@ __global__ __launch_bounds__(64 * W) void k_score_rows(ScoreArgs a) {
   uint32_t n = 0;
   uint64_t least = 0;
   float least_value = -INFINITY;
-  auto rank = [&](auto keys) {
-    constexpr uint32_t C = keys();
+  auto cut = [&]() {  // to its first, in order
+    constexpr uint32_t C = kList / 64;
     uint64_t key[C];
-    uint32_t above[C];
+    uint32_t place[C];
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (uint32_t c = 0; c < C; ++c) {
       key[c] = lane + 64 * c < n ? list[lane + 64 * c] : 0;
-      above[c] = 0;
+      place[c] = 0;
     }
-#pragma unroll 8
+#pragma unroll 4
     for (uint32_t i = 0; i < n; ++i) {
       const uint64_t o = list[i];
 #pragma unroll
-      for (uint32_t c = 0; c < C; ++c) above[c] += o > key[c];
+      for (uint32_t c = 0; c < C; ++c) place[c] += o > key[c];
     }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (uint32_t c = 0; c < C; ++c)
-      if (lane + 64 * c < n && above[c] < a.K) list[above[c]] = key[c];
-  };
-  auto cut = [&]() {
-    __builtin_amdgcn_wave_barrier();
-    if (n <= 64) rank([]() constexpr { return 1u; });
-    else if (n <= 128) rank([]() constexpr { return 2u; });
-    else rank([]() constexpr { return kList / 64; });
+      if (lane + 64 * c < n && place[c] < a.K) list[place[c]] = key[c];
     __builtin_amdgcn_wave_barrier();
     n = n < a.K ? n : a.K;
     if (n == a.K) {
