@@ -98,7 +98,7 @@ ARGUS_DEV void join_lanes(Sums& a) {
   a.above = (row(0) + row(16)) + (row(32) + row(48));
 }
 
-// A row's numbers, once its sums are known. `lane`: of those that write its alternatives.
+// A row's numbers, once its sums are known.
 struct Row {
   float top, log, entropy;
   bool fine;
