@@ -254,12 +254,13 @@ def rotate_tokens(q, new_k, new_v, k_cache, v_cache, table, starts, frequencies,
             _differentiable("q")
         heads = q.shape[1]
         if not given:
-            out = q.new_empty(T, heads, D)
-        os_ = _rows(out, "out", dev)
-        if not (out.shape == q.shape and out.dtype == q.dtype):
-            _bad("out: like q")
-        if out.requires_grad:
-            _differentiable("out")
+            out, os_ = q.new_empty(T, heads, D), (heads * D, D)
+        else:
+            os_ = _rows(out, "out", dev)
+            if not (out.shape == q.shape and out.dtype == q.dtype):
+                _bad("out: like q")
+            if out.requires_grad:
+                _differentiable("out")
         q_part, o_part = (q.data_ptr(), qs[0], qs[1]), (out.data_ptr(), os_[0], os_[1])
     elif given:
         _bad("out without q")
