@@ -16,9 +16,10 @@
  *
  * Rows are tokens of several sequences one after the other: sequence s has the
  * rows offsets[s] <= r < offsets[s + 1].  Offsets never fall, and lie in
- * [0, rows] (one that does not is taken as the nearer end, one below its
- * predecessor as a sequence without rows).  Rows of no sequence are left out:
- * nothing of theirs is read, and what the outputs hold there stays.
+ * [0, rows] (one that does not is taken as the nearer end; where they fall,
+ * which sequence a row counts to is not defined, but only rows of the call are
+ * read and written).  Rows of no sequence are left out: nothing of theirs is
+ * read, and what the outputs hold there stays.
  */
 #ifndef ARGUS_PROMPT_H
 #define ARGUS_PROMPT_H
@@ -96,9 +97,9 @@ int argus_prompt_attend(const argus_chunk_config* cfg, const argus_chunk_io* io,
                         size_t workspace_bytes, argus_markers* markers, void* stream);
 
 /* ----------------------------------------------------------------- rotate */
-/* Row r of sequence s is the token of position p = starts[s] + r - offsets[s]
- * (without offsets there is one row per sequence).  Of the first 2 * pairs
- * elements of a head, elements (x, y) of pair i become
+/* Row r of sequence s is the token of position p = starts[s] + r - offsets[s],
+ * its offset taken as above (without offsets there is one row per sequence).
+ * Of the first 2 * pairs elements of a head, elements (x, y) of pair i become
  *
  *   (amplitude (x cos a - y sin a), amplitude (y cos a + x sin a)), a = p * frequencies[i],
  *

@@ -125,7 +125,9 @@ __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
       }
       in = lo < a.S && a.offsets[0] <= row;
       s = in ? lo : 0;
-      pos = in ? (int64_t)a.starts[s] + row - a.offsets[s] : 0;
+      // (an offset outside [0, rows] is the nearer end: the comparisons come to the same without a look at that)
+      const int32_t first = a.offsets[s];
+      pos = in ? (int64_t)a.starts[s] + row - (first < 0 ? 0 : first) : 0;
     } else {
       pos = a.starts[s];
     }
