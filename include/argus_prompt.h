@@ -57,8 +57,16 @@ enum {
  * j > p - window or j < sinks, of the key/value head h / group.  A row that
  * sees nothing (one of a position below 0 too, or only scores of minus
  * infinity) answers zeros and an lse of minus infinity.  What a row does not
- * see has no part in it, NaN and infinities among that.  Lengths as in
- * argus_decode_attend, whose answer this is where n is 1. */
+ * see has no part in it, NaN and infinities among that.  An infinite v_j that it
+ * sees makes its element infinite however small w_j is, and NaN beside one of
+ * the other sign.
+ *
+ * Scores, weights, their sums and the answer are held in 32 bits.  The weights
+ * that multiply values are rounded once to q's type (in fp16 those below 2^-21
+ * of the largest to multiples of 2^-31 of it, or finer), the sums are of the
+ * unrounded ones.  So where n is 1 this is the answer of argus_decode_attend,
+ * which keeps more of the weights, to within half a step of the values in q's
+ * type.  Lengths as there. */
 typedef struct argus_chunk_config {
   uint32_t abi_version;  /* ARGUS_ATTR_ABI_VERSION */
   uint32_t q_type;       /* ARGUS_BF16 or ARGUS_FP16: of q and out */

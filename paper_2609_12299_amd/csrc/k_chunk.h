@@ -187,19 +187,22 @@ ARGUS_DEV void to_lds_word(const uint8_t* base, uint32_t at, uint32_t to) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(at), "s"(base), "s"(to) : "memory");
 }
 
-// The order of N matrix instructions that take a fragment each, of R reads from LDS: the reads are
-// A fragments ahead.
+// N matrix instructions that take a fragment each, read from LDS some ahead: barriers that only vector, scalar and
+// exponential instructions may pass keep the reads from coming later. (Groups for the compiler's scheduler in their place
+// were given up by it in some kernels, in others after any change, and reads came one ahead: one prompt of 2048 tokens
+// 59.9 us against 53.8 so, head size 256 474 against 409. Barriers that nothing passes: 1330 us in 8 bits against 1310.)
 constexpr int kFragsAhead = 4;
-template <int N, int R, int A>
-ARGUS_DEV void ahead() {
-  constexpr int kMatrix = 0x8, kRead = 0x100;
-  __builtin_amdgcn_sched_group_barrier(kRead, R * A, 0);
+constexpr int kVector = 0x2, kScalar = 0x4, kExponential = 0x400;  // that a barrier lets pass
+template <int N, class Read, class Take>
+ARGUS_DEV void fragments(Read read, Take take) {
 #pragma unroll
-  for (int i = 0; i < N - A; ++i) {
-    __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(kRead, R, 0);
+  for (int i = 0; i < kFragsAhead; ++i) read(i);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_barrier(kVector | kScalar | kExponential);
+    take(i);
+    if (i + kFragsAhead < N) read(i + kFragsAhead);
   }
-  __builtin_amdgcn_sched_group_barrier(kMatrix, A, 0);
 }
 
 // Bits of 16-bit numbers whose exponent is all ones: infinities and NaN.
@@ -417,16 +420,13 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
   const Range mine_all = all_seen(p_least, p_most);
   const Range block_all = all_seen(g.pos0 + (int32_t)divide(g.r0, a.by_group), g.pos0 + (int32_t)divide(g.r0 + g.rows - 1, a.by_group));
   constexpr uint32_t kHeld = (1u << kRuns) - 1;
-  f32x16 sc[HT];    // scores
-  u32x4 p[2 * HT];  // weights as the second product takes them
+  f32x16 sc[HT];  // scores, then weights
   auto score = [&](int buffer) {
 #pragma unroll
     for (int th = 0; th < HT; ++th) sc[th] = (f32x16)(0.0f);
-#pragma unroll
-    for (int f = 0; f < KF; ++f)
-#pragma unroll
-      for (int th = 0; th < HT; ++th) sc[th] = mfma32<T>(k_part(buffer, th, f), qf[f], sc[th]);
-    ahead<KF * HT, 1, kFragsAhead>();
+    u32x4 k[KF * HT];
+    auto read = [&](int i) { k[i] = k_part(buffer, i % HT, i / HT); };
+    fragments<KF * HT>(read, [&](int i) { sc[i % HT] = mfma32<T>(k[i], qf[i / HT], sc[i % HT]); });
   };
   auto weigh = [&](uint32_t tok, uint32_t held, bool whole) {
     if (__builtin_expect(!whole, 0)) {
@@ -464,34 +464,42 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
       base = mn == -INFINITY ? 0.0f : fmaf(mn, kLog2e, -Hf::kRaise);
       far = far || __any(fabsf(mn) > kFar && mn != -INFINITY);
     }
-    float sum[4];
 #pragma unroll
     for (int th = 0; th < HT; ++th) {
-      float w[16];
       if (__builtin_expect(!far, 1)) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(sc[th][i], kd2, -base));
+        for (int i = 0; i < 16; ++i) sc[th][i] = __builtin_amdgcn_exp2f(fmaf(sc[th][i], kd2, -base));
       } else {
         const float ms = m == -INFINITY ? 0.0f : m;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const float x = sc[th][i], y = x == -INFINITY ? x : x * kd;
-          w[i] = __builtin_amdgcn_exp2f(fmaf(y - ms, kLog2e, Hf::kRaise));
+          sc[th][i] = __builtin_amdgcn_exp2f(fmaf(y - ms, kLog2e, Hf::kRaise));
         }
       }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sum[i % 4] = th == 0 && i < 4 ? w[i] : sum[i % 4] + w[i];
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) p[2 * th + i / 8][i / 2 % 4] = Hf::pack(w[i], w[i + 1]);
     }
-    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
   };
+  // The weights' sums, and their rounding for the next products, beside the matrix instructions.
   auto apply = [&](int buffer) {
+    u32x4 v[2 * HT * DB], p[2 * HT];
+    float sum[4];
+    auto round = [&](int f) {
 #pragma unroll
-    for (int f = 0; f < 2 * HT; ++f)
+      for (int j = 0; j < 4; ++j) p[f][j] = Hf::pack(sc[f / 2][f % 2 * 8 + 2 * j], sc[f / 2][f % 2 * 8 + 2 * j + 1]);
+    };
+    round(0);
+    fragments<2 * HT * DB>([&](int i) { v[i] = v_part(buffer, i % DB, i / DB); },
+                           [&](int i) {
+                             const int f = i / DB, d = i % DB;
+                             acc[d] = mfma32<T>(v[i], p[f], acc[d]);
+                             if (d == 0 && f + 1 < 2 * HT) round(f + 1);
 #pragma unroll
-      for (int d = 0; d < DB; ++d) acc[d] = mfma32<T>(v_part(buffer, d, f), p[f], acc[d]);
-    ahead<2 * HT * DB, 2, kFragsAhead>();
+                             for (int e = 8 * d / DB; e < 8 * (d + 1) / DB; ++e) {
+                               const float w = sc[f / 2][f % 2 * 8 + e];
+                               sum[e % 4] = f == 0 && e < 4 ? w : sum[e % 4] + w;
+                             }
+                           });
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
   };
 
   // Of a step that some of the block's rows do not see, the values that are not finite (0 times infinity
@@ -631,6 +639,92 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
   }
 }
 
+// Which of a lane's elements (16 in a row from 32 d + 16 hk on, for each d) have values above, and which below all finite ones
+// among the tokens of steps [t0, t1) that its row sees (NaN: both). For a wave whose rows came to NaN in elements `odd`: no
+// further than until these are known to be. (A prompt of 16384 tokens all of which see a NaN 4.8 ms, without one 4.5.)
+template <int T, int DP, int DC>
+ARGUS_DEV void odd_values(const ChunkArgs& a, const Reach& g, uint32_t h, uint32_t t0, uint32_t t1, const uint32_t (&odd)[DC / 32],
+                          uint32_t (&plus)[DC / 32], uint32_t (&minus)[DC / 32]) {
+  constexpr int DB = DC / 32, KT = kStepTokens<DP>;
+  const uint32_t tid = fresh_thread(), lane = tid & 63u, c = lane & 31u, hk = lane >> 5, mine = 32 * (tid >> 6) + c;
+  const int32_t* tab = a.table + (int64_t)g.s * a.table_stride;
+  const uint8_t* vb = a.v + (int64_t)h * a.v_head;
+  const int32_t p0 = g.pos0 + (int32_t)divide(g.r0, a.by_group), p1 = g.pos0 + (int32_t)divide(g.r0 + g.rows - 1, a.by_group);
+  const int32_t pos = g.pos0 + (int32_t)divide(g.r0 + (mine < g.rows ? mine : 0), a.by_group), end = mine < g.rows ? pos + 1 : 0;
+  const int32_t low = a.window ? pos + 1 - (int32_t)a.window : 0, sinks = (int32_t)a.sinks;
+  auto add = [&](u32x4 x, uint32_t& up, uint32_t& down) {  // of eight values
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t bad = not_finite<T>(x[w]) >> 15, sign = x[w] >> 15 & 0x10001u;
+      const uint32_t nan = bad & ((x[w] & kFracs<T>) + kFracs<T>) >> kFrac<T>, u = nan | (bad & ~sign), v = nan | (bad & sign);
+      up |= ((u | u >> 15) & 3u) << (2 * w), down |= ((v | v >> 15) & 3u) << (2 * w);
+    }
+  };
+  auto value = [&](uint32_t at) {  // token `at`'s values; NULL: its page is not held
+    const int32_t page = at < g.len ? tab[at >> a.shift] : -1;
+    const uint8_t* r = vb + (int64_t)page * a.v_page + (uint64_t)(at & ((1u << a.shift) - 1)) * a.v_tok;
+    return (uint32_t)page < a.num_pages ? r : nullptr;
+  };
+  uint32_t up = 0, down = 0;  // of steps that all of the block's rows see: eight elements of a lane, some tokens
+  const uint32_t chunk = lane % (DP / 8);
+  uint32_t open = 0;  // of the chunk's elements, those that are NaN in a row
+#pragma unroll
+  for (int d = 0; d < DB; ++d) {
+    plus[d] = minus[d] = 0;
+    uint32_t x = odd[d];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) x |= __shfl_xor(x, o);
+    x = __shfl(x, chunk / 2 % 2 * 32);
+    if (chunk / 4 == (uint32_t)d) open = x >> (8 * (chunk % 2)) & 255u;
+  }
+  auto lanes_of_a_chunk = [&](uint32_t x) {
+#pragma unroll
+    for (int o = DP / 8; o < 64; o <<= 1) x |= __shfl_xor(x, o);
+    return x;
+  };
+#pragma unroll 1
+  for (uint32_t t = t0; t < t1; ++t) {
+    const int32_t first = (int32_t)((t < g.sink_steps ? t : t - g.sink_steps + g.first) * KT), last = first + KT - 1;
+    if (last <= p0 && (!a.window || first > p1 - (int32_t)a.window || last < sinks)) {
+      const uint32_t at = first + lane / (DP / 8);
+      constexpr int kDeep = 4, kOf = 512 / DP;  // tokens at a time
+#pragma unroll 1
+      for (int j = 0; j < KT; j += kDeep * kOf) {
+        const uint8_t* r[kDeep];
+        u32x4 x[kDeep];
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) r[i] = value(at + j + i * kOf);
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) x[i] = r[i] && 8 * chunk < a.D ? *reinterpret_cast<const u32x4*>(r[i] + 16 * chunk) : (u32x4)(0u);
+#pragma unroll
+        for (int i = 0; i < kDeep; ++i) add(x[i], up, down);
+      }
+      if (__all((open & ~lanes_of_a_chunk(up & down)) == 0)) break;
+    } else {
+#pragma unroll 1
+      for (int32_t at = first; at <= last; ++at) {
+        const uint8_t* r = value((uint32_t)at);
+        if (r && at < end && (at >= low || at < sinks))
+#pragma unroll
+          for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              if (32 * d + 16 * hk + 8 * e < a.D) {
+                uint32_t u = 0, v = 0;
+                add(*reinterpret_cast<const u32x4*>(r + 2 * (32 * d + 16 * hk + 8 * e)), u, v);
+                plus[d] |= u << (8 * e), minus[d] |= v << (8 * e);
+              }
+      }
+    }
+  }
+  up = lanes_of_a_chunk(up), down = lanes_of_a_chunk(down);
+#pragma unroll
+  for (int d = 0; d < DB; ++d) {
+    const uint32_t from = 4 * d + 2 * hk;
+    plus[d] |= __shfl(up, from) | __shfl(up, from + 1) << 8, minus[d] |= __shfl(down, from) | __shfl(down, from + 1) << 8;
+  }
+}
+
 template <int T, bool F8, int DP, int DC, int W, bool PIECES>
 __global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : DP == 128 ? 2 : 3) void k_chunk(ChunkArgs a) {
   constexpr int DB = DC / 32, KT = kStepTokens<DP>, TR = 32 * W;
@@ -639,41 +733,78 @@ __global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : DP == 128 ? 2 : 3
   lds_byte* lds = (lds_byte*)s_raw;
   WaveMarks mk(a.marks);
   mk.begin(ARGUS_REGION_CHUNK);
-  // O of the rows, or (slot: not done) a piece of it
+  // O of the rows, or (slot: not done) a piece of it, of steps t0 to t1
   auto put = [&](const ChunkArgs& a, const Reach& g, uint32_t h, const f32x16 (&acc)[DB], float m, float l, bool done,
-                 uint64_t slot) {
+                 uint64_t slot, uint32_t t0, uint32_t t1) {
     const uint32_t tid = fresh_thread(), c = tid & 31u, hk = tid >> 5 & 1u;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const float vs = a.v_scale ? a.v_scale[h] : 1.0f;
     const uint32_t mine = 32 * wave + c;
-    if (mine >= g.rows) return;
-    const uint32_t r = g.r0 + mine, tok = divide(r, a.by_group);
+    const bool in = mine < g.rows;
+    const uint32_t r = g.r0 + (in ? mine : 0), tok = divide(r, a.by_group);
     const uint64_t row = (uint64_t)(g.row0 + tok) * a.H * a.G + h * a.G + (r - tok * a.G);
     const float inv = l == 0.0f ? 0.0f : vs / l;
+    uint16_t* const out = a.out + row * a.D;
+    float* const part = a.part_o + (slot * TR + mine) * DP;
+    uint32_t nan = 0;
+    if (in) {
 #pragma unroll
-    for (int d = 0; d < DB; ++d) {
-      const uint32_t e = 32 * d + 16 * hk;
-      if (done) {
+      for (int d = 0; d < DB; ++d) {
+        const uint32_t e = 32 * d + 16 * hk;
+        if (done) {
 #pragma unroll
-        for (int i = 0; i < 16; i += 8)
-          if (e + i < a.D) {
-            u32x4 x;
+          for (int i = 0; i < 16; i += 8)
+            if (e + i < a.D) {
+              u32x4 x;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) x[w] = Hf::pack(acc[d][i + 2 * w] * inv, acc[d][i + 2 * w + 1] * inv);
-            *reinterpret_cast<u32x4*>(a.out + row * a.D + e + i) = x;
-          }
-      } else {
+              for (int w = 0; w < 4; ++w) x[w] = Hf::pack(acc[d][i + 2 * w] * inv, acc[d][i + 2 * w + 1] * inv);
+              if (l == 0.0f) x = (u32x4)(0u);  // (whatever the values are)
+              *reinterpret_cast<u32x4*>(out + e + i) = x;
+            }
+        } else {
 #pragma unroll
-        for (int i = 0; i < 16; i += 4)
-          *reinterpret_cast<f32x4*>(a.part_o + (slot * TR + mine) * DP + e + i) =
-              (f32x4){acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
+          for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<f32x4*>(part + e + i) = (f32x4){acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
+        }
+        if constexpr (!F8)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) nan |= acc[d][i] == acc[d][i] ? 0u : 1u;
+      }
+      if (hk == 0) {
+        if (!done)
+          *reinterpret_cast<f32x2*>(a.part_ml + (slot * TR + mine) * 2) = (f32x2){m, l};
+        else if (a.lse)
+          a.lse[row] = l == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m - Hf::kRaise * kLn2) + logf(l);
       }
     }
-    if (hk == 0) {
-      if (!done)
-        *reinterpret_cast<f32x2*>(a.part_ml + (slot * TR + mine) * 2) = (f32x2){m, l};
-      else if (a.lse)
-        a.lse[row] = l == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m - Hf::kRaise * kLn2) + logf(l);
+    if constexpr (!F8) {  // (e4m3 has no infinities)
+      // An infinite value that all rows of a step see is NaN times a weight that is none in 16 bits, and NaN once a maximum
+      // lies so far above its own that what came before is none. So where an element is NaN, and not by
+      // its row's scores, it is what the values that the row sees make of it: infinite, or NaN.
+      if (__builtin_expect(__any(nan && l == l && !(done && l == 0.0f)), 0)) {
+        uint32_t odd[DB], plus[DB], minus[DB];
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          odd[d] = 0;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) odd[d] |= in && l == l && acc[d][i] != acc[d][i] ? 1u << i : 0u;
+        }
+        odd_values<T, DP, DC>(fresh_args(), g, h, t0, t1, odd, plus, minus);
+        if (in && l == l && !(done && l == 0.0f)) {
+#pragma unroll 1
+          for (uint32_t i = 0; i < 16 * DB; ++i) {
+            uint32_t u = 0, v = 0;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+              if (i / 16 == (uint32_t)d) u = plus[d] >> (i % 16) & 1u, v = minus[d] >> (i % 16) & 1u;
+            const float x = u && v ? NAN : u ? INFINITY : -INFINITY;
+            const uint32_t e = 32 * (i / 16) + 16 * hk + i % 16;
+            if (!(u | v)) continue;
+            if (done) out[e] = (uint16_t)Hf::pack(x * inv, 0.0f);
+            else part[e] = x;
+          }
+        }
+      }
     }
   };
 
@@ -697,7 +828,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : DP == 128 ? 2 : 3
     if (first <= x && reach_of(a, lo, x - first, &g)) {
       g = scalar(g);
       chunk_steps<T, F8, DP, DC, W>(a, g, h, 0, g.steps, lds, acc, m, l);
-      put(a, g, h, acc, m, l, true, 0);
+      put(a, g, h, acc, m, l, true, 0, 0, g.steps);
     }
   } else {
     const uint32_t q = blockIdx.x / a.H;
@@ -707,7 +838,7 @@ __global__ __launch_bounds__(64 * W, DP == 256 || W == 8 ? 1 : DP == 128 ? 2 : 3
         g = scalar(g);
         chunk_steps<T, F8, DP, DC, W>(a, g, h, scalar(piece.z), scalar(piece.w), lds, acc, m, l);
         const ChunkArgs e = fresh_args();
-        put(e, g, h, acc, m, l, q >= (uint32_t)e.head[3], (uint64_t)q * e.H + h);
+        put(e, g, h, acc, m, l, q >= (uint32_t)e.head[3], (uint64_t)q * e.H + h, scalar(e.pieces[q].z), scalar(e.pieces[q].w));
       }
     }
   }

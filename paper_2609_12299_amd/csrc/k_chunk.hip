@@ -222,11 +222,23 @@ __global__ __launch_bounds__(kThreads) void k_chunk_join(ChunkArgs a) {
         }
         m = top;
       }
+      // (NaN, and not by the scores: a piece's infinite sum may have met a weight that is none in 32 bits)
+      if (__builtin_expect(l == l && !(o.x == o.x && o.y == o.y && o.z == o.z && o.w == o.w), 0)) {
+        f32x4 sum = (f32x4)(0.0f);  // of what is not finite
+        for (uint32_t i = 0; i < n; ++i) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + (((uint64_t)(join.z + i) * a.H + h) * TR + mine) * DP + d);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[e] += fabsf(v[e]) < INFINITY ? 0.0f : v[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = o[e] == o[e] ? o[e] : sum[e];
+      }
       const uint32_t r = g.r0 + mine, tok = divide(r, a.by_group);
       const uint64_t row = (uint64_t)(g.row0 + tok) * a.H * a.G + h * a.G + (r - tok * a.G);
       const float inv = l == 0.0f ? 0.0f : (a.v_scale ? a.v_scale[h] : 1.0f) / l;
       if (d < a.D)
-        *reinterpret_cast<u32x2*>(a.out + row * a.D + d) = (u32x2){Hf::pack(o.x * inv, o.y * inv), Hf::pack(o.z * inv, o.w * inv)};
+        *reinterpret_cast<u32x2*>(a.out + row * a.D + d) =
+            l == 0.0f ? (u32x2)(0u) : (u32x2){Hf::pack(o.x * inv, o.y * inv), Hf::pack(o.z * inv, o.w * inv)};
       if (d == 0 && a.lse)
         a.lse[row] = l == 0.0f ? -INFINITY : (m == -INFINITY ? 0.0f : m - Hf::kRaise * kLn2) + logf(l);
     }
