@@ -8,7 +8,7 @@ not made to wait for the current one, nor the current one for it: the order of t
 work is the caller's, and what a call returns is valid once its stream has come that
 far.  Every step of the computation runs in the HIP kernels of libargus_attr.so; there
 is no fallback.  The operators have no backward pass: a tensor that requires gradients
-is refused unless gradients are off (torch.no_grad).
+is refused unless gradients are off (torch.no_grad), and one with a forward-mode tangent.
 """
 from __future__ import annotations
 
@@ -176,7 +176,7 @@ def argus_decode_select(cfg, io, d_workspace, workspace_bytes, markers, stream) 
 
 _torch = None
 _types = {}
-_raw_stream = _device = _written = None
+_raw_stream = _device = _written = _forward = None
 _lib_attend = _lib_attend_bytes = _lib_append = _lib_step = _lib_compact = _lib_select = _lib_select_bytes = None
 
 # The structures of the header, field by field (native alignment).
@@ -189,7 +189,7 @@ _SELECT_CONFIG, _SELECT_IO = struct.Struct("6IiI"), struct.Struct("Q2q 6Q")
 
 
 def _t():
-    global _torch, _raw_stream, _device, _written, _lib_attend, _lib_attend_bytes, _lib_append, _lib_step, _lib_compact
+    global _torch, _raw_stream, _device, _written, _forward, _lib_attend, _lib_attend_bytes, _lib_append, _lib_step, _lib_compact
     global _lib_select, _lib_select_bytes
     if _torch is None:
         import torch
@@ -201,6 +201,7 @@ def _t():
         _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         # (of tensors that a call writes in place, so that autograd sees it where it has kept them)
         _written = getattr(torch._C, "_increment_version", torch.autograd.graph.increment_version)
+        _forward = torch.autograd.forward_ad  # (its level is below 0 outside of forward-mode derivatives)
         lib = _library()
 
         def of(name, *types):
@@ -239,6 +240,13 @@ def _differentiable(name: str) -> None:
         _bad(f"{name} requires gradients, and there is no backward pass: detach it, or call under torch.no_grad()")
 
 
+def _no_tangents(**tensors) -> None:
+    """Within forward-mode derivatives: tensors with a tangent are refused, whose part in the results would be lost."""
+    for name, x in tensors.items():
+        if x is not None and _forward.unpack_dual(x).tangent is not None:
+            _bad(f"{name} has a forward-mode tangent, and there is no derivative: unpack it first")
+
+
 def _type(x, allowed, name: str) -> int:
     got = _types.get(x.dtype)
     if got not in allowed:
@@ -267,6 +275,8 @@ def _scales(x, heads: int, name: str, dev):
         _bad(f"{name}: float32 [{heads}], dense, on {dev}")
     if x.requires_grad:
         _differentiable(name)
+    if _forward._current_level >= 0:
+        _no_tangents(**{name: x})
     return x.data_ptr()
 
 
@@ -287,6 +297,8 @@ def _planes(caches, num_pages: int, dev, out) -> None:
             _bad(f"caches[{i}]: [layers, {num_pages} pages, ...] on {dev}")
         if c.requires_grad:
             _differentiable(f"caches[{i}]")
+        if _forward._current_level >= 0:
+            _no_tangents(**{f"caches[{i}]": c})
         # a page is one run of memory, in whatever order its dimensions lie
         run = 1
         for step, n in sorted(zip(st[2:], shape[2:])):
@@ -420,6 +432,8 @@ def attend_pages(q, k_cache, v_cache, table, lens, scale: float | None = None, w
     ct = _type(k_cache, (qt, FP8), "k_cache")
     if q.requires_grad or k_cache.requires_grad or v_cache.requires_grad:
         _differentiable("q, k_cache or v_cache")
+    if _forward._current_level >= 0:
+        _no_tangents(q=q, k_cache=k_cache, v_cache=v_cache, out=out)
     k, v = _view(k_cache, "k_cache", dev), _view(v_cache, "v_cache", dev)
     N, H, ps, kd = k_cache.shape
     if not (v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype and kd == D):
@@ -480,6 +494,8 @@ def append_tokens(new_k, new_v, k_cache, v_cache, table, starts, offsets=None, k
     st = _type(new_k, (BF16, FP16), "new_k")
     if new_k.requires_grad or new_v.requires_grad or k_cache.requires_grad or v_cache.requires_grad:
         _differentiable("new_k, new_v, k_cache or v_cache")
+    if _forward._current_level >= 0:
+        _no_tangents(new_k=new_k, new_v=new_v, k_cache=k_cache, v_cache=v_cache)
     ct = _type(k_cache, (st, FP8), "k_cache")
     if not (v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype):
         _bad("k_cache and v_cache differ")
@@ -588,6 +604,8 @@ def select_beams(logits, scores, k: int, finished=None, eos: int = -1, markers=N
         _bad(f"scores: float32 {(G, W)}, dense, on {dev}")
     if logits.requires_grad or scores.requires_grad:
         _differentiable("logits or scores")
+    if _forward._current_level >= 0:
+        _no_tangents(logits=logits, scores=scores)
     done = 0
     if finished is not None:
         if not (finished.dtype in (t.bool, t.uint8) and finished.shape == (G, W) and finished.device == dev

@@ -3,8 +3,8 @@ decode step and over the same paged cache.
 
 The functions named ``argus_prompt_*`` are one-to-one wrappers (argument marshalling only).
 The others take torch CUDA tensors, as those of ``decode`` do: the same checks, streams, errors and
-markers, no fallback, and no backward pass (a tensor that requires gradients is refused unless
-gradients are off).
+markers, no fallback, and no derivatives (a tensor that requires gradients is refused unless
+gradients are off, and one with a forward-mode tangent).
 """
 from __future__ import annotations
 
@@ -15,7 +15,7 @@ import struct
 from . import decode
 from .attr import ABI_VERSION
 from .decode import (BF16, FP8, FP16, FP32, NUM_REGIONS, REGION_NAMES, _bad, _buffer, _differentiable, _done, _elsewhere,
-                     _ints, _marks, _on, _pack, _scales, _table, _type, _view, _workspace, argus_markers, argus_page_view)
+                     _ints, _marks, _no_tangents, _on, _pack, _scales, _table, _type, _view, _workspace, argus_markers, argus_page_view)
 
 PROMPT_REGION_NAMES = ["chunk.plan", "chunk", "chunk.join", "rotate", "score.rows", "score.join"]
 ALL_REGION_NAMES = REGION_NAMES + PROMPT_REGION_NAMES
@@ -165,6 +165,8 @@ def attend_chunks(q, k_cache, v_cache, table, lens, offsets, scale: float | None
     ct = _type(k_cache, (qt, FP8), "k_cache")
     if q.requires_grad or k_cache.requires_grad or v_cache.requires_grad:
         _differentiable("q, k_cache or v_cache")
+    if decode._forward._current_level >= 0:
+        _no_tangents(q=q, k_cache=k_cache, v_cache=v_cache, out=out)
     k, v = _view(k_cache, "k_cache", dev), _view(v_cache, "v_cache", dev)
     N, H, ps, kd = k_cache.shape
     if not (v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype and kd == D):
@@ -246,6 +248,8 @@ def rotate_tokens(q, new_k, new_v, k_cache, v_cache, table, starts, frequencies,
         _bad(f"frequencies: float64 [pairs], dense, on {dev}")
     if frequencies.requires_grad:
         _differentiable("frequencies")
+    if decode._forward._current_level >= 0:
+        _no_tangents(q=q, new_k=new_k, new_v=new_v, k_cache=k_cache, v_cache=v_cache, frequencies=frequencies, out=out)
     q_part = o_part = (0, 0, 0)
     given = out is not None
     if q is not None:
@@ -320,6 +324,8 @@ def score_tokens(logits, tokens, top: int = 0, markers=None, stream=None) -> dic
     R, V = logits.shape
     if logits.requires_grad:
         _differentiable("logits")
+    if decode._forward._current_level >= 0:
+        _no_tangents(logits=logits)
     if not 0 <= top <= MAX_TOP:
         _bad(f"top {top} (0..{MAX_TOP})")
     cfg = _pack(_SCORE_CONFIG, ABI_VERSION, lt, R, V, top, 0)
