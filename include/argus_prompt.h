@@ -72,7 +72,7 @@ typedef struct argus_chunk_config {
   uint32_t q_type;       /* ARGUS_BF16 or ARGUS_FP16: of q and out */
   uint32_t cache_type;   /* q_type, or ARGUS_FP8 */
   uint32_t seqs;         /* 0..2^20 */
-  uint32_t rows;         /* rows * group below 2^30 */
+  uint32_t rows;         /* rows * group below 2^30; (rows * group / 128 + seqs) * kv_heads up to 2^24 - 4096 */
   uint32_t kv_heads;     /* 1..1024 */
   uint32_t group;        /* query heads per key/value head, 1..256 */
   uint32_t head_dim;     /* a multiple of 8 (of 16 beyond 128 or with ARGUS_FP8), 8..256 */

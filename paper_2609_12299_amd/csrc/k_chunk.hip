@@ -305,20 +305,25 @@ int make_plan(const argus_chunk_config* c, Plan* p) {
   p->tile_shift = c->head_dim > 64 && c->head_dim <= 128 && rows >= (uint64_t)kManyRows * c->seqs &&
                           rows / 256 * c->kv_heads >= kManyTiles
                       ? 8 : 7;
-  p->slots = c->seqs ? ((c->rows * c->group) >> p->tile_shift) + c->seqs : 0;
-  const uint64_t tiles = (uint64_t)p->slots * c->kv_heads;
   const uint32_t kt = c->head_dim > 128 ? 32 : 64, dp = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
-  // steps of a row tile, as far as the table (or the window) allows
-  uint64_t steps = ((uint64_t)c->columns * c->page_size + kt - 1) / kt;
-  if (c->window) {
-    const uint64_t w = (c->window + (1u << p->tile_shift) / c->group + 2 * kt) / kt + 1 + (c->sinks + kt - 1) / kt;
-    steps = w < steps ? w : steps;
-  }
-  p->blocks = tiles && c->rows && (steps > kWholeSteps || tiles > kMaxBlocks) ? blocks_at_once(p->tile_shift, c->head_dim) : 0;
   // At most two pieces for each block that runs at once are of items that were cut, and so few more than
   // the items are all pieces.
-  const uint64_t most = p->slots + 2 * p->blocks / c->kv_heads + 1, grid = p->blocks ? most * c->kv_heads : tiles;
-  if (grid > kMaxBlocks) return refuse(ARGUS_E_CAPACITY, "rows x heads");
+  uint64_t most, grid;
+  for (;; p->tile_shift = 7) {
+    p->slots = c->seqs ? ((c->rows * c->group) >> p->tile_shift) + c->seqs : 0;
+    const uint64_t tiles = (uint64_t)p->slots * c->kv_heads;
+    // steps of a row tile, as far as the table (or the window) allows
+    uint64_t steps = ((uint64_t)c->columns * c->page_size + kt - 1) / kt;
+    if (c->window) {
+      const uint64_t w = (c->window + (1u << p->tile_shift) / c->group + 2 * kt) / kt + 1 + (c->sinks + kt - 1) / kt;
+      steps = w < steps ? w : steps;
+    }
+    p->blocks = tiles && c->rows && steps > kWholeSteps ? blocks_at_once(p->tile_shift, c->head_dim) : 0;
+    most = p->slots + 2 * p->blocks / c->kv_heads + 1, grid = p->blocks ? most * c->kv_heads : tiles;
+    // (blocks of eight waves have twice the threads, and a launch has less than 2^32)
+    if (grid <= (p->tile_shift == 8 ? kMaxBlocks / 2 : kMaxBlocks)) break;
+    if (p->tile_shift == 7) return refuse(ARGUS_E_CAPACITY, "rows %u x group %u, seqs %u, kv_heads %u", c->rows, c->group, c->seqs, c->kv_heads);
+  }
   p->grid = (uint32_t)grid;
   const uint32_t cut = p->slots < p->blocks / c->kv_heads ? p->slots : p->blocks / c->kv_heads;
   p->joins = p->blocks ? cut * c->kv_heads : 0;
