@@ -46,7 +46,7 @@ struct RotateArgs {
   Marks marks;
 };
 
-constexpr uint32_t kMaxTokens = 16, kMaxPairs = 128;
+constexpr uint32_t kMaxTokens = 4, kMaxPairs = 128;
 
 template <int T>
 ARGUS_DEV float of_half(uint16_t x) {
@@ -351,7 +351,7 @@ extern "C" int argus_prompt_rotate(const argus_rotate_config* cfg, const argus_r
   // Of many rows four to a block, which finds their places and angles in one go (65537 rows of 24 + 8 heads of 96
   // 209 us; eight 219, two 206; 40 prompts of up to 8192
   // tokens, 32 + 8 heads of 128 into 8 bits, 187, 187, 196). Of fewer one, for the blocks.
-  a.tokens = cfg->rows >= 4096 ? 4 : 1;
+  a.tokens = cfg->rows >= 4096 ? kMaxTokens : 1;
   const uint32_t grid = (cfg->rows + a.tokens - 1) / a.tokens;
   if (!marks_fit(markers, (uint64_t)grid * kWaves * 2)) return refuse(ARGUS_E_CAPACITY, "the marker records do not fit");
   if (cfg->rows == 0 || cfg->seqs == 0) return ARGUS_OK;
