@@ -83,6 +83,27 @@ def test_no_score_at_all():
         assert (got["out"] == 0).all() and torch.isneginf(got["lse"]).all()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "fp8"])
+@pytest.mark.parametrize("D,H,G,columns", SHAPES)
+def test_rows_without_a_score(kind, D, H, G, columns):
+    """Queries of minus infinity beside others, over values that are not finite: zeros for them alone."""
+    from paper_2609_12299_amd import attend_chunks
+    log(f"[gpu] rows without a score {kind} {D} {columns}")
+    a = ladder(kind, D, H, G, [(60, 300), (40, 0)], lambda j: 8.0, columns)
+    none = torch.arange(100, device="cuda") % 3 == 1
+    a["q"][none, :, 0] = -INF
+    for j in (5, 200, 350):
+        put(a, 0, j, 0, 3, NAN)
+        put(a, 0, j + 1, 0, 4, NAN if kind == "fp8" else INF)
+    got = attend_chunks(**a, scale=1.0, lse=True)
+    assert (got["out"][none] == 0).all() and torch.isneginf(got["lse"][none]).all()
+    rest = got["out"][~none].float()
+    mine = torch.arange(100, device="cuda")[~none] < 60
+    assert torch.isnan(rest[mine][:, :G, 3]).all() and (~torch.isfinite(rest[mine][:, :G, 4])).all()
+    rest[:, :G, 3:5] = 0
+    assert torch.isfinite(rest).all() and torch.isfinite(got["lse"][~none]).all()
+
+
 @pytest.mark.parametrize("kind,D", [("bf16", 128), ("fp16", 96), ("bf16", 80)])
 def test_many_row_tiles(kind, D):
     """The same with eight waves to a block, planned and not."""
