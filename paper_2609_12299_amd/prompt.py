@@ -243,6 +243,8 @@ def rotate_tokens(q, new_k, new_v, k_cache, v_cache, table, starts, frequencies,
                                  amplitude, k_scale, v_scale, out, markers)
     st = _type(some, (BF16, FP16), "q" if q is not None else "new_k")
     T, _, D = some.shape if some.dim() == 3 else _bad("q, new_k, new_v: [rows, heads, head_dim]")
+    if starts.dim() != 1:
+        _bad("starts: int32 [seqs]")
     S, heads, H, ps, N, P, ct = starts.shape[0], 0, 0, 0, 0, 0, st
     if not (frequencies.dtype == t.float64 and frequencies.dim() == 1 and frequencies.device == dev and frequencies.is_contiguous()):
         _bad(f"frequencies: float64 [pairs], dense, on {dev}")

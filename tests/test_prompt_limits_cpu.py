@@ -1,4 +1,4 @@
-"""Joint limits of the operators of a prompt's pass: what the header names is taken, what a launch cannot hold is refused, before any HIP
+"""Limits of the operators of a prompt's pass: what the header names is taken, what a launch cannot hold is refused, before any HIP
 call."""
 from __future__ import annotations
 
@@ -43,3 +43,15 @@ def test_more_than_a_launch_holds_is_refused(pr, rows, group, seqs, kv_heads, co
         kw = dict(rows=rows, group=group, seqs=seqs, kv_heads=kv_heads, head_dim=head_dim, columns=columns)
         assert attend(pr, **kw) == -4
         assert pr.argus_prompt_attend_workspace_bytes(config(pr, **kw)) == (1 << 64) - 1
+
+
+def test_starts_have_one_dimension(monkeypatch):
+    import torch
+
+    from paper_2609_12299_amd import ArgusError, prompt, rotate_tokens
+    prompt._t()
+    monkeypatch.setattr(prompt, "_elsewhere", lambda stream, dev: False)
+    q, f = torch.zeros(3, 4, 64, dtype=torch.bfloat16), torch.ones(32, dtype=torch.float64)
+    for starts in (torch.zeros((), dtype=torch.int32), torch.zeros(1, 1, dtype=torch.int32)):
+        with pytest.raises(ArgusError, match="starts"):
+            rotate_tokens(q, None, None, None, None, None, starts, f, torch.tensor([0, 3]).int())
