@@ -12,18 +12,20 @@
 // other 16, and what the first product leaves in its registers is what the second takes:
 // which token stands at which place of a contraction is free. Keys and values go through
 // LDS, read once for the block; queries and O stay in registers. Weights are rounded once, to the 16 bits that
-// the second product takes (to the nearest; in fp16 times 2^7, so that small ones keep their bits), their sums are
-// of the unrounded ones in 32 bits: a row's answer is off by half a step of a value at most.
+// the second product takes (to the nearest; in fp16 times 2^7, so that small ones keep their bits: those below 2^-32 of
+// the largest have none left, and count in the sums alone), their sums are
+// of the unrounded ones in 32 bits: a row's answer is off by half a step of a value at most, in all by 1.2 to 1.4 times
+// what the answer's own rounding is. (As two 16-bit numbers they would take half as many matrix instructions again.)
 //
-// What bounds it. Long chunks: the matrix cores. One sequence of 16384 tokens, 8 x 8 heads of 128 in bf16
-// (4.4 TFLOP), takes 3.93 to 4.1 ms, 1070 to 1120 TFLOP/s; a library product of 8192^3 reaches 1220 to 1270 on this
-// card, whose clock falls to 2.0 GHz under either. The instructions of the two products alone go at 1380;
-// between them stand the exponentials and maxima of 64 tokens a row, which two waves of a SIMD overlap
-// little: half-blocks that take turns at them, and other priorities, measured the same. What gave time: eight
-// waves a block instead of four (4.5 to 4.05 ms), fragments that are read from LDS four matrix instructions
-// ahead (1 ahead 4.20, 4 3.94, 12 3.95), loads three steps ahead, straight into LDS.
+// What bounds it. Long chunks: the matrix cores and the exponentials, one after the other. One sequence of 16384 tokens,
+// 8 x 8 heads of 128 in bf16 (4.4 TFLOP), takes 3.8 to 4.1 ms, 1070 to 1150 TFLOP/s; a library product of 8192^3 reaches 1220
+// to 1270 on this card, at 2.0 to 2.1 GHz both. By the counters the matrix cores are busy 0.52 of the time and the vector units 0.46:
+// the two waves of a SIMD, which the block's barrier lets go together, hide next to nothing of each
+// other; half-blocks that take turns, and other priorities, measured the same. What gave time: eight
+// waves a block instead of four (4.25 to 3.97 ms), fragments that are read from LDS four matrix instructions
+// ahead (1 ahead 4.08, 4 3.97, 8 3.98), loads three steps ahead, straight into LDS.
 // Few tokens over long contexts: the cache's bytes. 4 sequences of 131000 tokens with 6 new ones each read
-// 2.1 GB in 341 us (6.3 TB/s, a plain read reaches 6.7). Prompts of a few hundred tokens: the steps of the longest row
+// 2.1 GB in 340 us (6.3 TB/s, a plain read reaches 6.7). Prompts of a few hundred tokens: the steps of the longest row
 // tile, one after the other.
 #pragma once
 
@@ -217,8 +219,8 @@ template <int T>
 constexpr uint32_t kFracs = ((1u << kFrac<T>) - 1) * 0x10001u;
 
 // O, maxima and sums of steps [t0, t1) of a row tile for one head. Rows of LDS have room for DP elements, of which DC
-// are multiplied (at head size 96, of 128, a quarter of the products less: a batch of single tokens and chunks 153 us
-// against 166, 4 prompts of up to 6000 tokens 467 against 519).
+// are multiplied (at head size 96, of 128, a quarter of the products less: a batch of single tokens and chunks 139 us
+// against 150, 4 prompts of up to 6000 tokens 469 against 523).
 template <int T, bool F8, int DP, int DC, int W>
 ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint32_t t0, uint32_t t1, lds_byte* lds,
                            f32x16 (&acc)[DC / 32], float& m, float& l) {
@@ -319,7 +321,7 @@ ARGUS_DEV void chunk_steps(const ChunkArgs& a, const Reach& g, uint32_t h, uint3
   // Step s's keys (side 0) and values on their way, into LDS or (8 bits) registers. What lies behind
   // the sequence's end or in no page is 0; where nothing does, without a look at that.
   // (Four waves: few rows of a sequence, which read most of it once, past the caches. 4 sequences of 131000
-  // tokens with 6 new ones each 341 us against 384, 64 of up to 30000 with one 301 against 329, and batches in which
+  // tokens with 6 new ones each 340 us against 382, 64 of up to 30000 with one 278 against 306, and batches in which
   // row tiles share what they read the same.)
   auto load = [&](uint32_t s, int buffer, auto all_of) {
     constexpr bool all = all_of(), once = W == 4;

@@ -15,8 +15,8 @@ namespace {
 // tried, none but those whose pieces are as few, and the shortest way is taken: rounds times (length + what
 // a piece costs), and what joining costs, all in steps; or nothing is cut. Where there are more items than two
 // rounds of blocks take, those of more than 2 U / C steps are cut. What is not cut comes in eight classes of length, the
-// longest first, each in the order of its slots (a batch of single tokens and chunks whose last blocks ended at
-// step 75 ends at 69: 137.5 us against 150.6; 64 single tokens behind up to 30000 283 against 301).
+// longest first, each in the order of its slots (a batch of single tokens and chunks 139 us against 171, 64 single tokens
+// behind up to 30000 278 against 295, chunks over 8 bits 1295 against 1377).
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
 constexpr uint32_t kPlanItems = 4096, kPlanSplit = 1024;
 constexpr uint32_t kLeastPiece = 4, kItemCost = 2, kPieceCost = 8, kJoinCost = 8, kClasses = 8;
@@ -261,20 +261,21 @@ void launch_chunk_join(const ChunkArgs& a, dim3 g, hipStream_t st) {
 }
 
 // Eight waves a block, that read the cache once for 256 rows, or four. Eight where sequences have so many
-// rows on the average, and there are so many tiles of them (4 prompts in chunks over 8 bits 1350 us against 1463 with
-// four, one of 16384 tokens 4.12 ms against 4.46; 16 prompts of up to 2000 tokens, 8 x 4 heads, 103 us against
-// 107), else four (proposals over 131000 tokens 342 us against 390 with eight, a batch of single tokens and
-// chunks 168 against 172, one prompt of 512 tokens 20.4 against 22.9, of 2048, 8 x 4 heads, 59.5 against 62.2; the
-// other way round is one of 512 over 8192 in the cache, 190 against 177: what is in the cache is not known
-// here), and at head size 64, whose blocks of four run three at a time on a compute unit (4 prompts of up to
-// 4000 tokens 158 us against 186 with eight).
+// rows on the average, and there are so many tiles of them (16 prompts in chunks over 8 bits 1295 us against 1415 with
+// four, one of 16384 tokens 3.97 ms against 4.25, four of up to 6000 at head size 96 469 us against 498; 16 prompts of up to
+// 2000 tokens, 8 x 4 heads, 100.2 against 101.4, at head size 80 89 against 86), else four (proposals over 131000 tokens 340 us
+// against 388 with eight, 64 single tokens 278 against 526, a batch of single tokens and chunks 139 against 150,
+// one prompt of 512 tokens 18.6 against 22.8, of 2048, 8 x 4 heads, 54.3 against 60.7, of 512 behind 8192 in the cache 182
+// both), and at head size 64, whose blocks of four run three at a time on a compute unit (4 prompts of up to
+// 4000 tokens 159 us against 193 with eight).
 constexpr uint32_t kManyRows = 1024, kManyTiles = 512;
 // Blocks that run at once.
 uint32_t blocks_at_once(uint32_t tile_shift, uint32_t head_dim) {
   return 256u * (head_dim > 128 || tile_shift == 8 ? 1 : head_dim > 64 ? 2 : 3);
 }
 // Row tiles of at most so many steps are not cut, and are found by their blocks: no plan and no joining (a
-// prompt of 2048 tokens 69.6 us against 74.4).
+// prompt of 2048 tokens 54.3 us against 65.5, 16 of up to 2000 100 against 111). A table of more steps means both, and a workspace of
+// 52 to 68 MB, whatever the lengths are, which are on the GPU: one prompt of 45 tokens 16.9 us where it is 9.7.
 constexpr uint32_t kWholeSteps = 32;
 constexpr uint32_t kJoinBlocks = 8;  // of an item, for its rows
 

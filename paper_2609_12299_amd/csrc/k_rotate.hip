@@ -7,10 +7,10 @@
 // go over the rows' units: a unit of queries or keys is eight pairs, whose 16 elements one thread reads,
 // turns and writes (so q may be turned in place), or eight elements that stay; one of values
 // is eight elements. (Four pairs a unit where their number is odd in fours: 32768 rows of 16 + 4 heads of 80,
-// 20 pairs each, 74 us against 199 pair by pair.)
+// 20 pairs each, 72 us against 201 pair by pair.)
 //
 // What bounds it: the bytes, read and written once: 65537 rows of 24 + 8 heads of 96 in 209 us, 4.8 TB/s, as
-// fast as a copy; a step of 64 single tokens, 32 + 8 heads of 128, 10 us, what a launch takes.
+// fast as a copy; a step of 64 single tokens, 32 + 8 heads of 128, 4.1 us, of a call's 10, which are the host's.
 #include "pages.h"
 #include "prompt.h"
 
@@ -99,8 +99,8 @@ ARGUS_DEV u32x4 gather(const float (&x)[8]) {
 template <int T, bool F8, int LAYOUT>
 __global__ __launch_bounds__(kThreads) void k_rotate(RotateArgs a) {
   // Neighbours: what a wave reads and writes at once are whole lines of 128 bytes, which go past the caches (40 prompts
-  // of up to 8192 tokens into 8 bits 187 us against 195). Halves: parts of lines, whose rest comes next
-  // (65537 rows of 24 + 8 heads of 96, eight a block, 219 us against 250).
+  // of up to 8192 tokens into 8 bits 186 us against 195). Halves: parts of lines, whose rest comes next
+  // (65537 rows of 24 + 8 heads of 96 209 us against 226).
   constexpr bool kOnce = LAYOUT == kNeighbours;
   __shared__ int64_t s_page[kMaxTokens];  // -1: not held
   __shared__ uint32_t s_place[kMaxTokens];

@@ -10,8 +10,8 @@
 // are joined in the same way, in a fixed order.
 //
 // A block reads a part of a row, its four waves 64 lanes of 32 elements in turn. The next ones' loads go out once
-// these are in 32 bits and looked through for the maximum; the rest is done while they are under way, five to seven
-// waves on a SIMD (two sets of registers for them, three or four waves: 137 us where this takes 108). The rank is a
+// these are in 32 bits and looked through for the maximum; the rest is done while they are under way, four to six
+// waves on a SIMD (two sets of registers for them, three or four waves: 137 us where this took 108). The rank is a
 // count of what is above the given token's own logit, read first. The k best are among what is not below the k-th
 // largest of the block's 256 lanes' maxima, whichever elements the lanes have seen: that bound is worked out after
 // the first step of each wave and again when a wave has seen four times as much, from what the others have noted
@@ -461,9 +461,10 @@ struct Plan {
 
 constexpr uint32_t kRowBlocks = 768;
 // Rows of which each compute unit has one at most: a block of 16 waves reads one by itself, and nothing is joined, where
-// its waves have one step each (one row of 32000, 5 alternatives, 10.0 us against 13.5 in parts), or there are so many
-// rows that parts of them would not fill the card better (256 of 128003, 20 alternatives, 26.0 us against 30.9; 100 of
-// 128003 23.3 against 19.6). Beyond that, parts or rows of four waves (300 of 32000 17.8 us, with 16 waves 23.0).
+// its waves have one step each (one row of 32000, 5 alternatives, 10.0 us against 14.0 in parts; one of 128003 20.9 against 13.7), or there are so many
+// rows that parts of them would not fill the card better (256 of 128003, 20 alternatives, 25.1 us against 30.3; 100 of
+// 128003 24.4 against 24.3, with 5 alternatives 22.4 against 19.1). Beyond that, parts or rows of four waves (300 of 32000, 20
+// alternatives, 19.6 us, with 16 waves 24.5; 512 19.3 against 25.1).
 constexpr uint32_t kFewRows = 256, kFewSteps = 4;
 
 int make_plan(const argus_score_config* c, Plan* p) {
