@@ -147,8 +147,8 @@ def attend_chunks(q, k_cache, v_cache, table, lens, offsets, scale: float | None
     """Attention of chunks of new tokens over a paged cache that holds them already.
 
     q: [rows, heads, head_dim] bf16 or fp16, contiguous rows (a view of a fused projection's
-    result does); sequence s has the rows offsets[s] to offsets[s + 1] (int32 [seqs + 1], within
-    the rows, never falling), the queries of its last positions; lens: int32 [seqs], its tokens, the new ones
+    result does); sequence s has the rows offsets[s] to offsets[s + 1] (int32 [seqs + 1], never
+    falling; one outside the rows is taken as the nearer end), the queries of its last positions; lens: int32 [seqs], its tokens, the new ones
     included.  A row sees the tokens up to its own; with a window the last `window` of these and
     the first `sinks`.  Caches, table and scales as in attend_pages.  Returns out (like q,
     dense) and, if asked, lse (float32 [rows, heads]); a row that sees nothing answers zeros and
@@ -226,7 +226,7 @@ def rotate_tokens(q, new_k, new_v, k_cache, v_cache, table, starts, frequencies,
 
     q: [rows, heads, head_dim], new_k, new_v: [rows, kv_heads, head_dim], bf16 or fp16,
     contiguous rows; caches, table, starts, offsets and scales as in append_tokens: row r of sequence s has
-    position starts[s] + r - offsets[s].  frequencies: float64 [pairs], radians per token; the first 2 * pairs
+    position starts[s] + r - offsets[s], an offset outside the rows taken as the nearer end.  frequencies: float64 [pairs], radians per token; the first 2 * pairs
     elements of a head turn, pair i of elements i and i + pairs, or (interleaved) 2 i and 2 i + 1; `amplitude`
     multiplies them.  q may be None (keys and values alone), or new_k, new_v, k_cache, v_cache and
     table (queries alone).  Returns out (like q; q itself may be given), without q nothing.  Rows of no sequence
